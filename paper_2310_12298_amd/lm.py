@@ -1,0 +1,388 @@
+"""Operators of a language model's training step beside the Jorge step: layer norm, embedding,
+and AdamW with the global gradient norm.
+
+ctypes binding of include/jorge_lm.h. layer_norm() and embedding() are
+differentiable; the *_forward and *_backward functions are the two passes by themselves; AdamW
+steps a list of tensors. torch owns the memory (outputs and workspaces are torch tensors of the
+current stream) and names the current HIP stream. Tensors are fp32 or bfloat16 CUDA tensors of the
+current device; the last dimension has to be dense, rows may have a stride. There is no CPU
+fallback: a missing library raises.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import numpy as np
+import torch
+
+from .jorge import JORGE_OK, JorgeError, _current_stream, load_library
+
+_P, _I32, _I64, _F64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_double
+BLOCK = 256                                   # elements of an 8-bit moment that share a scale
+DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+class AdamWTensor(ctypes.Structure):
+    # Addresses as numbers, so that a numpy view of an array of these can set them by the column.
+    _fields_ = [("param", ctypes.c_uint64), ("grad", ctypes.c_uint64), ("numel", _I64), ("block", _I64),
+                ("dtype", _I32), ("reserved", _I32)]
+
+
+class AdamWMoments(ctypes.Structure):
+    _fields_ = [("exp_avg", _P), ("exp_avg_sq", _P), ("exp_avg_scale", _P), ("exp_avg_sq_scale", _P),
+                ("blocks", _I64), ("bits", _I32), ("seed", ctypes.c_uint32)]
+
+
+_PT, _PM = ctypes.POINTER(AdamWTensor), ctypes.POINTER(AdamWMoments)
+# name -> (restype, argtypes); mirrors include/jorge_lm.h
+_SIGNATURES = {
+    "jorge_lm_last_error": (ctypes.c_char_p, []),
+    "jorge_layernorm_forward": (_I32, [_P, _I64, _I32, _P, _P, _I32, _P, _I64, _P, _P, _I64, _I64, _F64, _P]),
+    "jorge_layernorm_workspace": (_I32, [_I64, _I64, ctypes.POINTER(_I64)]),
+    "jorge_layernorm_backward": (_I32, [_P, _I64, _P, _I64, _I32, _P, _P, _P, _I32, _P, _I64, _P, _P, _I64, _I64, _P,
+                                        _I64, _P]),
+    "jorge_embedding_forward": (_I32, [_P, _I64, _P, _I64, _I32, _I64, _I64, _F64, _P, _I64, _P]),
+    "jorge_embedding_workspace": (_I32, [_I64, _I64, _I64, ctypes.POINTER(_I64)]),
+    "jorge_embedding_backward": (_I32, [_P, _I64, _P, _I64, _I32, _I64, _I64, _F64, _I64, _P, _I64, _P, _I64, _P]),
+    "jorge_gradient_norm_workspace": (_I32, [_PT, _I32, ctypes.POINTER(_I64)]),
+    "jorge_gradient_norm": (_I32, [_PT, _I32, _F64, _P, _P, _I64, _P]),
+    "jorge_adamw_step": (_I32, [_PT, _I32, _PM, _I64, _F64, _F64, _F64, _F64, _F64, _P, _P]),
+    "jorge_adamw_read": (_I32, [_PM, _I32, _I64, _I64, _P, _I32, _P]),
+    "jorge_adamw_write": (_I32, [_PM, _I32, _I64, _I64, _P, _P]),
+}
+
+_BOUND = None
+
+
+def load_operators() -> ctypes.CDLL:
+    """The library with the entry points of include/jorge_lm.h bound; raises if it is not built."""
+    global _BOUND
+    lib = load_library()
+    if _BOUND is not lib:
+        for name, (res, args) in _SIGNATURES.items():
+            fn = getattr(lib, name)
+            fn.restype = res
+            fn.argtypes = args
+        _BOUND = lib
+    return lib
+
+
+def _check(lib, status):
+    if status != JORGE_OK:
+        raise JorgeError(status, f"{lib.jorge_status_string(status).decode()} ({lib.jorge_lm_last_error().decode()})")
+
+
+def _cuda(t, what, dtypes=None):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{what}: a CUDA tensor is needed")
+    if t.dtype not in (DTYPES if dtypes is None else dtypes):
+        raise ValueError(f"{what}: unsupported type {t.dtype}")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{what}: on device {t.get_device()}, not the current one")
+    return t
+
+
+def _matrix(t, what):
+    """A matrix with dense rows that holds t's values, without a copy where t's layout allows it."""
+    _cuda(t, what)
+    if t.dim() == 0:
+        raise ValueError(f"{what}: at least one dimension is needed")
+    m = t if t.dim() == 2 else t.reshape(-1, t.shape[-1]) if t.numel() else t.reshape(
+        t.shape[:-1].numel(), t.shape[-1])
+    if (m.shape[1] > 1 and m.stride(1) != 1) or (m.shape[0] > 1 and m.stride(0) < m.shape[1]):
+        m = m.contiguous()
+    return m
+
+
+def _ld(m):
+    """Row stride of a matrix; that of a single row does not matter."""
+    return m.stride(0) if m.shape[0] > 1 else m.shape[1]
+
+
+def _vector(t, n, what):
+    _cuda(t, what)
+    if tuple(t.shape) != (n,):
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, not {(n,)}")
+    return t.contiguous()
+
+
+def _int64s(t, what):
+    if not isinstance(t, torch.Tensor) or t.dtype.is_floating_point or t.dtype.is_complex or t.dtype == torch.bool:
+        raise ValueError(f"{what}: a tensor of whole numbers is needed")
+    return _cuda(t.long().contiguous(), what, (torch.int64,))
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _workspace(n):
+    return torch.empty(n, dtype=torch.uint8, device="cuda") if n else None
+
+
+# ---------------------------------------------------------------- layer norm
+def layer_norm_forward(x, weight=None, bias=None, eps=1e-5):
+    """(y, mean, rstd) of layer norm over the last dimension; y has x's shape and type, mean and
+    rstd are fp32, one per row. weight, bias: fp32 or bfloat16 vectors (one type), or None."""
+    lib = load_operators()
+    m = _matrix(x, "x")
+    rows, cols = m.shape
+    params = [_vector(p, cols, n) for p, n in ((weight, "weight"), (bias, "bias")) if p is not None]
+    if len({p.dtype for p in params}) > 1:
+        raise ValueError("weight and bias must have one type")
+    w = params[0] if weight is not None else None
+    b = params[-1] if bias is not None else None
+    y = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    stats = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+    _check(lib, lib.jorge_layernorm_forward(m.data_ptr(), _ld(m), DTYPES[x.dtype], _ptr(w), _ptr(b),
+                                            DTYPES[params[0].dtype] if params else 0, y.data_ptr(), cols,
+                                            stats[0].data_ptr(), stats[1].data_ptr(), rows, cols, float(eps),
+                                            _current_stream()))
+    return y.view(x.shape), stats[0], stats[1]
+
+
+def layer_norm_backward(dy, x, mean, rstd, weight=None, affine=True):
+    """(dx, dweight, dbias) from the gradient of y and what layer_norm_forward returned. dweight and
+    dbias have weight's type (fp32 without one); affine=False leaves them out (None)."""
+    lib = load_operators()
+    m, d = _matrix(x, "x"), _matrix(dy, "dy")
+    rows, cols = m.shape
+    if tuple(dy.shape) != tuple(x.shape) or dy.dtype != x.dtype:
+        raise ValueError("dy must have x's shape and type")
+    for s, what in ((mean, "mean"), (rstd, "rstd")):
+        if _cuda(s, what, (torch.float32,)).shape != (rows,) or not s.is_contiguous():
+            raise ValueError(f"{what}: as layer_norm_forward returned it")
+    w = None if weight is None else _vector(weight, cols, "weight")
+    ptype = torch.float32 if w is None else w.dtype
+    dx = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    sums = torch.empty((2, cols), dtype=ptype, device=x.device) if affine else None
+    ws, n = None, _I64(0)
+    if affine:
+        _check(lib, lib.jorge_layernorm_workspace(rows, cols, ctypes.byref(n)))
+        ws = _workspace(n.value)
+    _check(lib, lib.jorge_layernorm_backward(d.data_ptr(), _ld(d), m.data_ptr(), _ld(m), DTYPES[x.dtype],
+                                             mean.data_ptr(), rstd.data_ptr(), _ptr(w), DTYPES[ptype], dx.data_ptr(),
+                                             cols, sums[0].data_ptr() if affine else None,
+                                             sums[1].data_ptr() if affine else None, rows, cols, _ptr(ws), n.value,
+                                             _current_stream()))
+    return dx.view(x.shape), sums[0] if affine else None, sums[1] if affine else None
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        y, mean, rstd = layer_norm_forward(x, weight, bias, eps)
+        ctx.save_for_backward(x, mean, rstd, weight, bias)
+        return y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, mean, rstd, weight, bias = ctx.saved_tensors
+        need_w, need_b = ctx.needs_input_grad[1], ctx.needs_input_grad[2]
+        dx, dw, db = layer_norm_backward(dy, x, mean, rstd, weight, affine=need_w or need_b)
+        return dx, dw if need_w else None, db.to(bias.dtype) if need_b else None, None
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5):
+    """Differentiable layer norm over the last dimension (see layer_norm_forward)."""
+    return _LayerNorm.apply(x, weight, bias, eps)
+
+
+# ---------------------------------------------------------------- embedding
+def embedding_forward(tokens, table, scale=1.0):
+    """scale * table[tokens], of table's type. A token outside the table gives a row of zeros."""
+    lib = load_operators()
+    t, tok = _matrix(table, "table"), _int64s(tokens, "tokens")
+    if table.dim() != 2:
+        raise ValueError("table: a matrix is needed")
+    vocab, cols = t.shape
+    out = torch.empty((tok.numel(), cols), dtype=t.dtype, device=t.device)
+    _check(lib, lib.jorge_embedding_forward(tok.data_ptr(), tok.numel(), t.data_ptr(), _ld(t), DTYPES[t.dtype], vocab,
+                                            cols, float(scale), out.data_ptr(), cols, _current_stream()))
+    return out.view(*tokens.shape, cols)
+
+
+def embedding_backward(dout, tokens, vocab, scale=1.0, padding=None):
+    """The gradient of embedding_forward's table (vocab rows, dout's type). padding: a token whose row gets none."""
+    lib = load_operators()
+    d, tok = _matrix(dout, "dout"), _int64s(tokens, "tokens")
+    if tuple(dout.shape[:-1]) != tuple(tokens.shape):
+        raise ValueError(f"dout: shape {tuple(dout.shape)} for tokens of shape {tuple(tokens.shape)}")
+    if padding is not None and not 0 <= int(padding) < int(vocab):
+        raise ValueError("padding must be a row of the table")
+    count, cols = d.shape
+    n = _I64(0)
+    _check(lib, lib.jorge_embedding_workspace(count, int(vocab), cols, ctypes.byref(n)))
+    out = torch.empty((int(vocab), cols), dtype=d.dtype, device=d.device)
+    ws = _workspace(n.value)
+    _check(lib, lib.jorge_embedding_backward(d.data_ptr(), _ld(d), tok.data_ptr(), count, DTYPES[d.dtype], int(vocab),
+                                             cols, float(scale), -1 if padding is None else int(padding),
+                                             out.data_ptr(), cols, _ptr(ws), n.value, _current_stream()))
+    return out
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, tokens, table, scale, padding):
+        ctx.save_for_backward(tokens)
+        ctx.more = (table.shape[0], scale, padding)
+        return embedding_forward(tokens, table, scale)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        (tokens,), (vocab, scale, padding) = ctx.saved_tensors, ctx.more
+        return None, embedding_backward(dout, tokens, vocab, scale, padding), None, None
+
+
+def embedding(tokens, table, scale=1.0, padding=None):
+    """Differentiable scale * table[tokens]; the gradient of table is dense (see embedding_backward)."""
+    return _Embedding.apply(tokens, table, scale, padding)
+
+
+# ---------------------------------------------------------------- AdamW
+class AdamW:
+    """AdamW steps of a list of dense fp32 or bfloat16 CUDA tensors, all in one launch (per 112 of them).
+
+    bits: 32, or 8 for moments of a byte per element with a scale per block of 256, rounded by random
+    bits made from seed, the step and the element's place (include/jorge_lm.h has the format). moments:
+    existing flat buffers to take over instead of zeros, as `moments` of another AdamW over tensors of
+    the same sizes. t: the number of steps taken. norm: after a step with max_norm, the gradients' global
+    norm before clipping (a device tensor).
+    """
+
+    def __init__(self, params, bits=32, seed=0, moments=None):
+        self.lib = load_operators()
+        self.params = list(params)
+        self.bits, self.seed, self.t, self.norm = int(bits), int(seed), 0, None
+        if self.bits not in (8, 32):
+            raise ValueError("bits must be 8 or 32")
+        if not 0 <= self.seed < 1 << 32:
+            raise ValueError("seed must be in [0, 2^32)")
+        for i, p in enumerate(self.params):
+            if not _dense(_cuda(p, f"parameter {i}")):
+                raise ValueError(f"parameter {i}: a dense tensor is needed")
+        self._numel = [p.numel() for p in self.params]
+        self.blocks = np.cumsum([0] + [-(-n // BLOCK) for n in self._numel])
+        self._tensors = (AdamWTensor * max(1, len(self.params)))()
+        self._table = np.frombuffer(self._tensors, dtype=np.dtype(AdamWTensor))[:len(self.params)]
+        self._table["numel"] = self._numel
+        self._table["block"] = self.blocks[:-1]
+        self._table["dtype"] = [DTYPES[p.dtype] for p in self.params]
+        total = int(self.blocks[-1])
+        kind = torch.float32 if self.bits == 32 else torch.uint8
+        want = {"exp_avg": (kind, total * BLOCK), "exp_avg_sq": (kind, total * BLOCK)}
+        if self.bits == 8:
+            want.update(exp_avg_scale=(torch.uint8, total), exp_avg_sq_scale=(torch.uint8, total))
+        if moments is None:
+            moments = {k: torch.zeros(n, dtype=d, device="cuda") for k, (d, n) in want.items()}
+        for k, (d, n) in want.items():
+            m = moments.get(k)
+            if m is None or _cuda(m, k, (d,)).shape != (n,) or not m.is_contiguous():
+                raise ValueError(f"{k}: a dense tensor of {n} elements of {d} is needed")
+        self.moments = {k: moments[k] for k in want}
+        self._moments = AdamWMoments(*(_ptr(self.moments.get(k)) for k in (
+            "exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale")), total, self.bits, self.seed)
+
+    def _gradients(self, grads):
+        """Puts the gradients' pointers into the table; a parameter without one (None) takes no part."""
+        if len(grads) != len(self.params):
+            raise ValueError(f"grads: expected {len(self.params)} tensors, got {len(grads)}")
+        keep, ptrs, numel = [], [], self._numel
+        for i, (g, p) in enumerate(zip(grads, self.params)):
+            if g is None:
+                if numel is self._numel:
+                    numel = list(numel)
+                numel[i] = 0
+                ptrs.append(0)
+                continue
+            if g.dtype is not p.dtype or g.shape != p.shape or g.device != p.device:
+                raise ValueError("grads: each must have its parameter's shape, type and device")
+            if g.stride() != p.stride():
+                g = torch.empty_strided(p.shape, p.stride(), dtype=p.dtype, device=p.device).copy_(g)
+                keep.append(g)
+            ptrs.append(g.data_ptr())
+        self._table["grad"] = ptrs
+        self._table["numel"] = numel
+        return keep
+
+    def step(self, grads=None, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, max_norm=0.0, clip=None):
+        """One step from the gradients (default: each parameter's .grad; None entries are left as they
+        are). max_norm > 0 scales all gradients to that global norm if theirs is larger; clip: the factor
+        itself, one fp32 number on the device (of another gradient_norm call)."""
+        keep = self._gradients([p.grad for p in self.params] if grads is None else grads)
+        self._table["param"] = [p.data_ptr() for p in self.params]
+        if max_norm and clip is not None:
+            raise ValueError("max_norm or clip, not both")
+        if max_norm:
+            out = self._norm(max_norm)
+            self.norm, clip = out[0], out[1:]
+        elif clip is not None and (_cuda(clip, "clip", (torch.float32,)).numel() != 1):
+            raise ValueError("clip: one number is needed")
+        _check(self.lib, self.lib.jorge_adamw_step(self._tensors, len(self.params), ctypes.byref(self._moments),
+                                                   self.t + 1, float(lr), float(beta1), float(beta2), float(eps),
+                                                   float(weight_decay), _ptr(clip), _current_stream()))
+        self.t += 1
+        del keep
+
+    def _norm(self, max_norm):
+        n = _I64(0)
+        _check(self.lib, self.lib.jorge_gradient_norm_workspace(self._tensors, len(self.params), ctypes.byref(n)))
+        ws, out = _workspace(n.value), torch.empty(2, dtype=torch.float32, device="cuda")
+        _check(self.lib, self.lib.jorge_gradient_norm(self._tensors, len(self.params), float(max_norm), out.data_ptr(),
+                                                      _ptr(ws), n.value, _current_stream()))
+        return out
+
+    def gradient_norm(self, grads=None, max_norm=0.0):
+        """[norm, clip factor] of the gradients on the device, without a step."""
+        keep = self._gradients([p.grad for p in self.params] if grads is None else grads)
+        out = self._norm(max_norm)
+        del keep
+        return out
+
+    def moment_values(self, dtype=torch.float32):
+        """The two moments' values as flat tensors of dtype, in the layout of `moments` (parameter i starts
+        at blocks[i] * 256)."""
+        if self.bits == 32:
+            return self.moments["exp_avg"].to(dtype), self.moments["exp_avg_sq"].to(dtype)
+        total, out = int(self.blocks[-1]), []
+        for second in (0, 1):
+            v = torch.empty(total * BLOCK, dtype=dtype, device="cuda")
+            _check(self.lib, self.lib.jorge_adamw_read(ctypes.byref(self._moments), second, 0, total, v.data_ptr(),
+                                                       DTYPES[dtype], _current_stream()))
+            out.append(v)
+        return out[0], out[1]
+
+    def set_moment_values(self, exp_avg, exp_avg_sq):
+        """Takes the moments' values from flat fp32 tensors in the layout of moment_values (8 bits: rounded to nearest)."""
+        for second, (k, v) in enumerate((("exp_avg", exp_avg), ("exp_avg_sq", exp_avg_sq))):
+            v = _cuda(v, k, (torch.float32,)).contiguous()
+            if v.shape != self.moments[k].shape:
+                raise ValueError(f"{k}: {self.moments[k].numel()} values are needed")
+            if self.bits == 32:
+                self.moments[k].copy_(v)
+            else:
+                _check(self.lib, self.lib.jorge_adamw_write(ctypes.byref(self._moments), second, 0,
+                                                            int(self.blocks[-1]), v.data_ptr(), _current_stream()))
+
+    def state_dict(self):
+        return {"t": self.t, "bits": self.bits, "seed": self.seed, **{k: v.cpu() for k, v in self.moments.items()}}
+
+    def load_state_dict(self, sd):
+        if sd["bits"] != self.bits or any(sd[k].shape != v.shape for k, v in self.moments.items()):
+            raise ValueError("the state is of another set of tensors or of other bits")
+        for k, v in self.moments.items():
+            v.copy_(sd[k])
+        self.t, self.seed = int(sd["t"]), int(sd["seed"])
+        self._moments.seed = self.seed
+
+
+def _dense(t):
+    """Whether t's elements fill one span of memory without overlap, in whatever order of dimensions."""
+    expect = 1
+    for n, s in sorted(((n, s) for n, s in zip(t.shape, t.stride()) if n > 1), key=lambda x: x[1]):
+        if s != expect:
+            return False
+        expect *= n
+    return True
