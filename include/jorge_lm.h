@@ -1,7 +1,7 @@
 /*
  * jorge_lm.h - C ABI of the operators of a language model's training step that
  * stand beside the Jorge step (jorge.h) in libjorge.so: layer norm, embedding
- * lookup, and AdamW with the global
+ * lookup, softmax cross entropy over a vocabulary, and AdamW with the global
  * gradient norm for the parameters that Jorge does not precondition (gains,
  * biases, tables wider than JORGE_MAX_DIM). Each has its forward and backward
  * pass where it has one.
@@ -102,6 +102,54 @@ jorge_status jorge_embedding_backward(const void* dout, int64_t lddo, const int6
                                       int32_t dtype, int64_t vocab, int64_t cols, double scale, int64_t padding,
                                       void* dtable, int64_t lddt, void* workspace, int64_t workspace_bytes,
                                       void* hip_stream);
+
+/* ---------------------------------------------------------------- cross entropy
+ * Of logits z = hidden weight^T (tokens x vocab), which are formed piece by piece and never kept:
+ *   lse_i = log sum_v exp(z_iv),
+ *   loss_i = lse_i - (1 - e) z_i,target_i - (e / vocab) sum_v z_iv,  e the label smoothing.
+ * A target outside [0, vocab), or equal to ignore_index, is no target: loss_i = 0, and the row
+ * takes no part in the sums and gradients (its lse_i is written). */
+
+/* Largest tokens, vocab and cols. */
+#define JORGE_LOSS_MAX_TOKENS (1 << 22)
+#define JORGE_LOSS_MAX_VOCAB  (1 << 22)
+#define JORGE_LOSS_MAX_COLS   32768
+
+/* What grad of the backward pass is the gradient of. */
+#define JORGE_LOSS_ROWS 0 /* of every loss_i: tokens floats        */
+#define JORGE_LOSS_SUM  1 /* of total[0], the sum: one float       */
+#define JORGE_LOSS_MEAN 2 /* of total[2], the mean: one float      */
+
+typedef struct jorge_loss_shape {
+    int64_t tokens, cols, vocab; /* >= 1 (tokens may be 0)                            */
+    int64_t ldh, ldw;            /* row strides of hidden (and dhidden), of weight (and dweight) */
+    int32_t dtype;               /* of hidden, weight and their gradients             */
+    int32_t reserved;            /* 0 */
+    int64_t ignore_index;
+    double  label_smoothing;     /* e, in [0, 1]                                      */
+} jorge_loss_shape;
+
+/* Bytes of workspace of the forward (backward = 0) or backward pass (host pointers). */
+jorge_status jorge_cross_entropy_workspace(const jorge_loss_shape* shape, int32_t backward, int64_t* bytes);
+
+/* shape: host. hidden: tokens x cols, weight: vocab x cols, targets: tokens of int64. loss, lse: tokens
+ * floats each. total: three floats: the sum of the losses, the number of rows with a target, and the mean
+ * over them (0 without any). */
+jorge_status jorge_cross_entropy_forward(const jorge_loss_shape* shape, const void* hidden, const void* weight,
+                                         const int64_t* targets, float* loss, float* lse, float* total,
+                                         void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* lse, total: as the forward pass wrote them. kind: JORGE_LOSS_*; grad: see there. With g_i the gradient of
+ * loss_i (0 without a target) and p = exp(z - lse):
+ *   dz_iv = g_i (p_iv - (1 - e) [v = target_i] - e / vocab),
+ *   dhidden = dz weight,  dweight = dz^T hidden.
+ * dhidden, dweight: written whole; either may be NULL. bfloat16 inputs: dz (without g where that is one
+ * number) is rounded to bfloat16 for the two products, whose sums are fp32. fp32 inputs: every product is
+ * formed from three-term bfloat16 splits as the Jorge step's are (jorge.h), dz included. */
+jorge_status jorge_cross_entropy_backward(const jorge_loss_shape* shape, const float* grad, int32_t kind,
+                                          const void* hidden, const void* weight, const int64_t* targets,
+                                          const float* lse, const float* total, void* dhidden, void* dweight,
+                                          void* workspace, int64_t workspace_bytes, void* hip_stream);
 
 /* ---------------------------------------------------------------- AdamW
  * Step t of every element p of every tensor, with g its gradient times the clip factor:

@@ -1,0 +1,773 @@
+// Softmax cross entropy of logits z = hidden weight^T over a vocabulary, forward and backward, for gfx950.
+//
+// Bound by the matrix products: 2 tokens vocab cols flops forward, and backward as many again for the
+// logits, which are not kept, and twice that for the two gradients. All of them run on the bfloat16
+// matrix instructions (lm_loss_gemm.hpp).
+//
+// Forward: a workgroup forms a tile of logits and leaves, for each of its tokens, the maximum of its
+// words' logits, the sum of their exponentials relative to it and (label smoothing) their sum; a second
+// kernel joins the tiles' statistics of a token in a fixed order.
+//
+// Backward, a piece of the vocabulary at a time:
+//   dz = p - (target distribution), from a tile of logits formed again, rounded to bfloat16 and written
+//   both ways round, so that both products below have K-contiguous operands;
+//   dhidden += dz weight      (K: the piece's words; the sum over the pieces in fp32)
+//   dweight  = dz^T hidden    (K: the tokens; whole, as a piece holds all tokens)
+// A piece is as large as keeps dz within a fixed number of elements, so the memory does not grow with
+// the vocabulary. Transposed copies of weight's piece and of hidden cost a hundredth of the time of the
+// products that they feed.
+//
+// fp32 operands are split into three bfloat16 terms that sum to them exactly (in bfloat16's range), and a
+// product is the six products of terms down to 2^-16 of the whole: the same K loop, six times as long.
+// dz is split alike. This is the scheme of the Jorge step's products; there the terms are formed while a
+// slab is staged, here once before the product, because every operand enters many tiles.
+#include "lm_common.hpp"
+#include "lm_loss_gemm.hpp"
+
+#include <math.h>
+
+#include <algorithm>
+
+namespace jorge_lm {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr int kTerms = 3;      // of a split fp32 operand
+constexpr int kSegments = 6;   // products of terms
+constexpr int kPadK = 64;      // K of every product is a multiple of two stages
+
+// ---------------------------------------------------------------- operands
+// dst[t][r][c] = term t of src[r][c], 0 past the row's end (c < ldd, a multiple of 8).
+template <typename T, int TERMS>
+__global__ __launch_bounds__(256) void pack_kernel(const T* __restrict__ src, int64_t lds, int64_t rows, int cols,
+                                                   bf16* __restrict__ dst, int ldd, int64_t plane) {
+    const int64_t r = blockIdx.x;
+    for (int c = (blockIdx.y * 256 + threadIdx.x) * 8; c < ldd; c += gridDim.y * 2048) {
+        float f[8];
+        const T* const p = src + r * lds + c;
+        const int left = cols - c;
+        typedef T V __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+        if (left >= 8) {
+            const V v = *reinterpret_cast<const V*>(p);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = (float)v[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = e < left ? (float)p[e] : 0.0f;
+        }
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t) {
+            bf16x8 o;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                o[e] = (bf16)f[e];
+                f[e] -= (float)o[e];
+            }
+            *reinterpret_cast<bf16x8*>(dst + t * plane + r * ldd + c) = o;
+        }
+    }
+}
+
+// dst[t][c][r] = term t of src[r][c] for c < cols, r < ldd (a multiple of 64), 0 for r >= rows and for the rows
+// that `targets` (if given) has no target for: what such a row holds must not reach a sum that it has no part in.
+template <typename T, int TERMS>
+__global__ __launch_bounds__(256) void transpose_kernel(const T* __restrict__ src, int64_t lds, int64_t rows, int cols,
+                                                        bf16* __restrict__ dst, int64_t ldd, int64_t plane,
+                                                        const int64_t* __restrict__ targets, int64_t vocab,
+                                                        int64_t ignore) {
+    __shared__ float tile[64][65];
+    const int64_t r0 = (int64_t)blockIdx.x * 64;
+    const int c0 = blockIdx.y * 64, x = threadIdx.x & 63, y = threadIdx.x >> 6;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        const int64_t r = r0 + y + 4 * k;
+        float v = 0.0f;
+        if (r < rows && c0 + x < cols) {
+            bool live = true;
+            if (targets) {
+                const int64_t t = targets[r];
+                live = t >= 0 && t < vocab && t != ignore;
+            }
+            if (live) v = (float)src[r * lds + c0 + x];
+        }
+        tile[y + 4 * k][x] = v;
+    }
+    __syncthreads();
+    // Eight rows of src per lane: 16 bytes of a row of dst.
+    const int part = threadIdx.x & 7;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int c = (threadIdx.x >> 3) + 32 * k;
+        if (c0 + c >= cols) continue;
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = tile[part * 8 + e][c];
+#pragma unroll
+        for (int t = 0; t < TERMS; ++t) {
+            bf16x8 o;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                o[e] = (bf16)f[e];
+                f[e] -= (float)o[e];
+            }
+            *reinterpret_cast<bf16x8*>(dst + t * plane + (int64_t)(c0 + c) * ldd + r0 + part * 8) = o;
+        }
+    }
+}
+
+// ---------------------------------------------------------------- tiles
+// The tile of workgroup g of a grid of ta x tb tiles. Workgroup g runs on XCD g mod 8; each XCD takes a
+// contiguous share of an order in which 32 neighbours span 8 tiles of b and 4 of a: what its CUs work on at a time
+// shares operands in its L2.
+struct Place {
+    int a, b;
+};
+__device__ __forceinline__ Place place_of(int g, int ta, int tb) {
+    const int total = ta * tb, q = total / 8, r = total % 8, x = g % 8;
+    const int id = x * q + min(x, r) + g / 8;
+    const int band = id / (8 * ta), nb = min(8, tb - band * 8), in = id - band * 8 * ta;
+    return {in / nb, band * 8 + in % nb};
+}
+
+struct Product {
+    Operand A, B;
+    int per;         // stages of one segment
+    int split;       // operands in three terms: kSegments segments
+    int ta, tb;
+};
+
+struct LossRows {
+    const int64_t* targets;
+    int64_t tokens, vocab, ignore;
+    __device__ __forceinline__ int64_t target(int64_t i) const {
+        if (i >= tokens) return -1;
+        const int64_t t = targets[i];
+        return t >= 0 && t < vocab && t != ignore ? t : -1;
+    }
+};
+
+// Of a lane's 4 WA words: how many of them exist where `left` do from its first one on; and which of them word
+// `target` is, -1 if none.
+template <int WA>
+__device__ __forceinline__ int lane_left(int64_t left) {
+    return left < 0 ? 0 : left < 4 * WA ? (int)left : 4 * WA;
+}
+template <int WA>
+__device__ __forceinline__ int lane_word(int64_t target, int64_t first) {
+    const int64_t k = target - first;
+    return target >= 0 && k >= 0 && k < 4 * WA ? (int)k : -1;
+}
+
+__device__ __forceinline__ float across_groups_max(float v) {
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float across_groups_sum(float v) {
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+// Statistics of one part (the 16 WA words of a wave) of the logits: planes [parts][tokens].
+struct Stats {
+    float *top, *sum, *all;  // all: the plain sum of logits, if wanted
+    float* at_target;        // [tokens]
+};
+
+// A: words from word0 on; B: tokens.
+template <int WA, int WB>
+__global__ __launch_bounds__(256, 1) void loss_forward_kernel(Product p, LossRows rows, Stats out, int64_t word0) {
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    using T = Tile<WA, WB>;
+    const Place at = place_of(blockIdx.x, p.ta, p.tb);
+    T t;
+    t.multiply(p.A, p.B, (int64_t)at.a * T::kA, (int64_t)at.b * T::kB, 0, p.per * (p.split ? kSegments : 1), p.per, p.split, lds);
+    const int64_t a0 = (int64_t)at.a * T::kA + T::lane_a(), b0 = (int64_t)at.b * T::kB + T::lane_b();
+    const int left = lane_left<WA>(p.A.rows - a0);  // words of this lane that exist
+    const int64_t part = (word0 + (int64_t)at.a * T::kA) / (16 * WA) + (threadIdx.x >> 7);
+    float top[WB], sum[WB], all[WB];
+#pragma unroll
+    for (int j = 0; j < WB; ++j) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < WA; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (4 * i + r >= left) t.acc[i][j][r] = -INFINITY;
+                m = fmaxf(m, t.acc[i][j][r]);
+            }
+        m = across_groups_max(m);
+        // With nothing above minus infinity the sum is 0, not NaN.
+        const float base = m == -INFINITY ? 0.0f : m;
+        float s = 0.0f, u = 0.0f;
+#pragma unroll
+        for (int i = 0; i < WA; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s += __builtin_amdgcn_exp2f((t.acc[i][j][r] - base) * kLog2e);
+        if (out.all)
+#pragma unroll
+            for (int i = 0; i < WA; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) u += 4 * i + r < left ? t.acc[i][j][r] : 0.0f;
+        top[j] = m;
+        sum[j] = across_groups_sum(s);
+        all[j] = out.all ? across_groups_sum(u) : 0.0f;
+        // The target's logit, by the one lane that has it.
+        const int here = lane_word<WA>(rows.target(b0 + j), word0 + a0);
+        const bool hit = here >= 0 && here < left;
+        if (__ballot(hit)) {
+            float z = 0.0f;
+#pragma unroll
+            for (int i = 0; i < WA; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) z = here == 4 * i + r ? t.acc[i][j][r] : z;
+            if (hit) out.at_target[b0 + j] = z;
+        }
+    }
+    if ((threadIdx.x & 63) < 16) {
+#pragma unroll
+        for (int j = 0; j < WB; ++j)
+            if (b0 + j < p.B.rows) {
+                out.top[part * rows.tokens + b0 + j] = top[j];
+                out.sum[part * rows.tokens + b0 + j] = sum[j];
+                if (out.all) out.all[part * rows.tokens + b0 + j] = all[j];
+            }
+    }
+}
+
+// Joins the parts' statistics of 64 tokens: 16 waves take every 16th part, ascending, and are joined in order.
+constexpr int kJoinWaves = 16;
+__global__ __launch_bounds__(kJoinWaves * 64) void loss_join_kernel(Stats in, int64_t parts, LossRows rows, float smoothing,
+                                                                    float* __restrict__ loss, float* __restrict__ lse) {
+    __shared__ float lt[kJoinWaves][64], ls[kJoinWaves][64], la[kJoinWaves][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t i = (int64_t)blockIdx.x * 64 + lane, at = i < rows.tokens ? i : rows.tokens - 1;
+    float top = -INFINITY, sum = 0.0f, all = 0.0f;
+    const auto add = [&](float m, float s) {
+        const float n = fmaxf(top, m);
+        // A NaN anywhere stays: fmaxf passes it by, but its sum is NaN.
+        const float base = n == -INFINITY ? 0.0f : n;
+        sum = sum * __builtin_amdgcn_exp2f((top - base) * kLog2e) + s * __builtin_amdgcn_exp2f((m - base) * kLog2e);
+        top = n;
+    };
+    for (int64_t k = wave; k < parts; k += kJoinWaves) {
+        add(in.top[k * rows.tokens + at], in.sum[k * rows.tokens + at]);
+        if (in.all) all += in.all[k * rows.tokens + at];
+    }
+    lt[wave][lane] = top;
+    ls[wave][lane] = sum;
+    la[wave][lane] = all;
+    __syncthreads();
+    if (wave || i >= rows.tokens) return;
+    for (int w = 1; w < kJoinWaves; ++w) {
+        add(lt[w][lane], ls[w][lane]);
+        all += la[w][lane];
+    }
+    const float l = top + logf(sum);
+    lse[i] = l;
+    float v = 0.0f;
+    if (rows.target(i) >= 0) {
+        v = l - (1.0f - smoothing) * in.at_target[i];
+        if (in.all) v -= smoothing * (all / (float)rows.vocab);
+    }
+    loss[i] = v;
+}
+
+// total = [sum of the losses, rows with a target, mean], by one workgroup, in fp64.
+__global__ __launch_bounds__(1024) void loss_total_kernel(const float* __restrict__ loss, LossRows rows,
+                                                          float* __restrict__ total) {
+    __shared__ double rs[16], rc[16];
+    double s = 0.0, c = 0.0;
+    for (int64_t i = threadIdx.x; i < rows.tokens; i += 1024)
+        if (rows.target(i) >= 0) {
+            s += loss[i];
+            c += 1.0;
+        }
+    s = wave_sum(s);
+    c = wave_sum(c);
+    if ((threadIdx.x & 63) == 0) {
+        rs[threadIdx.x >> 6] = s;
+        rc[threadIdx.x >> 6] = c;
+    }
+    __syncthreads();
+    if (threadIdx.x) return;
+    s = c = 0.0;
+    for (int w = 0; w < 16; ++w) {
+        s += rs[w];
+        c += rc[w];
+    }
+    total[0] = (float)s;
+    total[1] = (float)c;
+    total[2] = c > 0.0 ? (float)(s / c) : 0.0f;
+}
+
+// ---------------------------------------------------------------- backward
+struct DzOut {
+    bf16 *dz, *dzt;            // [terms][tokens][ldz], [terms][words][ldt]
+    int64_t ldz, ldt, plane_z, plane_t;
+};
+
+// dz of a piece: words word0 .. word0 + A.rows; padding up to ldz words and ldt tokens is written as 0.
+template <int WA, int WB, int TERMS>
+__global__ __launch_bounds__(256, 1) void loss_dz_kernel(Product p, LossRows rows, const float* __restrict__ lse,
+                                                         const float* __restrict__ row_grad, float smoothing, int64_t word0,
+                                                         DzOut out) {
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    using T = Tile<WA, WB>;
+    const Place at = place_of(blockIdx.x, p.ta, p.tb);
+    T t;
+    t.multiply(p.A, p.B, (int64_t)at.a * T::kA, (int64_t)at.b * T::kB, 0, p.per * (p.split ? kSegments : 1), p.per, p.split, lds);
+    const int64_t a0 = (int64_t)at.a * T::kA + T::lane_a(), b0 = (int64_t)at.b * T::kB + T::lane_b();
+    const int left = lane_left<WA>(p.A.rows - a0);
+    const float even = smoothing / (float)rows.vocab;
+#pragma unroll
+    for (int j = 0; j < WB; ++j) {
+        const int64_t target = rows.target(b0 + j);
+        const bool live = target >= 0;
+        const int here = lane_word<WA>(target, word0 + a0);
+        const float l = live ? lse[b0 + j] : 0.0f, g = live && row_grad ? row_grad[b0 + j] : 1.0f;
+        const float hit = 1.0f - smoothing;
+#pragma unroll
+        for (int i = 0; i < WA; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float v = __builtin_amdgcn_exp2f((t.acc[i][j][r] - l) * kLog2e) - even;
+                if (here == 4 * i + r) v -= hit;
+                // Selected, not multiplied by 0: what stands in a row without a target may be anything.
+                t.acc[i][j][r] = live && 4 * i + r < left ? g * v : 0.0f;
+            }
+    }
+#pragma unroll
+    for (int term = 0; term < TERMS; ++term) {
+        bf16* const dz = out.dz + term * out.plane_z;
+        bf16* const dzt = out.dzt + term * out.plane_t;
+#pragma unroll
+        for (int j = 0; j < WB; ++j)
+            if (b0 + j < rows.tokens)
+#pragma unroll
+                for (int i = 0; i < WA; i += 2) {
+                    bf16x8 o;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o[e] = (bf16)t.acc[i + e / 4][j][e & 3];
+                    if (a0 + 4 * i < out.ldz) *reinterpret_cast<bf16x8*>(dz + (b0 + j) * out.ldz + a0 + 4 * i) = o;
+                }
+        if (b0 < out.ldt)
+#pragma unroll
+            for (int i = 0; i < WA; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (4 * i + r < left) {
+                        typedef __bf16 V __attribute__((ext_vector_type(WB)));
+                        V o;
+#pragma unroll
+                        for (int j = 0; j < WB; ++j) o[j] = (bf16)t.acc[i][j][r];
+                        *reinterpret_cast<V*>(dzt + (a0 + 4 * i + r) * out.ldt + b0) = o;
+                    }
+        if constexpr (TERMS > 1)
+#pragma unroll
+            for (int j = 0; j < WB; ++j)
+#pragma unroll
+                for (int i = 0; i < WA; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) t.acc[i][j][r] -= (float)(bf16)t.acc[i][j][r];
+    }
+}
+
+// What a gradient is multiplied by after its product: grad[0] (or 1), over the number of rows with a target for a mean.
+struct Scale {
+    const float *grad, *count;
+    __device__ __forceinline__ float value() const {
+        return (grad ? *grad : 1.0f) / (count ? fmaxf(*count, 1.0f) : 1.0f);
+    }
+};
+
+// C[b][a] over one of gridDim.y ranges of K, to out (whole: one range) or to the range's slice of fp32 sums
+// [ranges][B.rows][lda], added to it where `add`.
+template <int WA, int WB, typename O>
+__global__ __launch_bounds__(256, 1) void loss_grad_kernel(Product p, O* __restrict__ out, int64_t ldo, float* __restrict__ slices,
+                                                           int64_t lda, int add, Scale scale) {
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    using T = Tile<WA, WB>;
+    const Place at = place_of(blockIdx.x, p.ta, p.tb);
+    const int pairs = p.per * (p.split ? kSegments : 1) / 2;
+    const int s0 = (int)((int64_t)pairs * blockIdx.y / gridDim.y) * 2, s1 = (int)((int64_t)pairs * (blockIdx.y + 1) / gridDim.y) * 2;
+    T t;
+    t.multiply(p.A, p.B, (int64_t)at.a * T::kA, (int64_t)at.b * T::kB, s0, s1, p.per, p.split, lds);
+    const int64_t a0 = (int64_t)at.a * T::kA + T::lane_a(), b0 = (int64_t)at.b * T::kB + T::lane_b();
+    const int left = lane_left<WA>(p.A.rows - a0);
+    if (slices) {
+        float* const to = slices + (int64_t)blockIdx.y * p.B.rows * lda;
+#pragma unroll
+        for (int j = 0; j < WB; ++j)
+            if (b0 + j < p.B.rows) {
+                f32x4* const q = reinterpret_cast<f32x4*>(to + (b0 + j) * lda + a0);
+                // Past the last column up to lda there is room for a whole piece.
+                if (add)
+#pragma unroll
+                    for (int i = 0; i < WA; ++i)
+                        if (4 * i < left) t.acc[i][j] += q[i];
+#pragma unroll
+                for (int i = 0; i < WA; ++i)
+                    if (4 * i < left) q[i] = t.acc[i][j];
+            }
+        return;
+    }
+    const float f = scale.value();
+    constexpr int N = Wide<O>::N;
+#pragma unroll
+    for (int j = 0; j < WB; ++j)
+        if (b0 + j < p.B.rows)
+#pragma unroll
+            for (int i = 0; i < WA; i += N / 4) {
+                float v[N];
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[e] = t.acc[i + e / 4][j][e & 3] * f;
+                if (4 * i < left) store_wide(out + (b0 + j) * ldo + a0 + 4 * i, left - 4 * i, v);
+            }
+}
+
+// out[r][c] = scale times the sum of the slices, in order.
+template <typename O>
+__global__ __launch_bounds__(256) void loss_slices_kernel(const float* __restrict__ slices, int n, int64_t rows, int cols,
+                                                          int64_t lda, O* __restrict__ out, int64_t ldo, Scale scale) {
+    const int64_t r = blockIdx.x;
+    const float f = scale.value();
+    for (int c = (blockIdx.y * 256 + threadIdx.x) * 4; c < cols; c += gridDim.y * 1024) {
+        const float* p = slices + r * lda + c;
+        f32x4 s = *reinterpret_cast<const f32x4*>(p);
+        for (int k = 1; k < n; ++k) s += *reinterpret_cast<const f32x4*>(p + k * rows * lda);
+        O* const o = out + r * ldo + c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c + e < cols) o[e] = (O)(s[e] * f);
+    }
+}
+
+// ---------------------------------------------------------------- host
+constexpr int kCus = 256;
+
+// Which tile a product of `a` x `b` takes, and over how many ranges of K it is cut.
+struct Shape {
+    bool large;   // 256 x 256, else 128 x 128
+    int ranges;
+};
+// Large tiles run a product at twice the small ones' rate, where there are enough of them for the CUs.
+Shape shape_of(int64_t a, int64_t b, int64_t stages, bool may_cut) {
+    const int64_t big = ceil_div(a, 256) * ceil_div(b, 256), small = ceil_div(a, 128) * ceil_div(b, 128);
+    if (big >= kCus / 2 || !may_cut) {
+        if (big >= kCus / 2) return {true, 1};
+        return {false, 1};
+    }
+    // Cut along K until the tiles fill the CUs; a range keeps at least 16 stages.
+    const auto cut = [&](int64_t tiles, int64_t want) {
+        const int64_t most = stages / 16;
+        return std::max<int64_t>(1, std::min(want / tiles, most));
+    };
+    const int64_t rb = cut(big, kCus);
+    if (big * rb >= kCus / 2) return {true, (int)rb};
+    return {false, (int)cut(small, 2 * kCus)};
+}
+
+struct Plan {
+    int terms, segments;
+    int64_t kd, kn, piece;       // padded cols, padded tokens, words of a piece
+    bool direct_x, direct_w;     // hidden and weight serve as operands as they are
+    Shape logits, dh, dw;
+};
+
+bool direct(const jorge_loss_shape& s, const void* p, int64_t ld) {
+    return s.dtype == JORGE_BF16 && s.cols % kPadK == 0 && ld % 8 == 0 && aligned(p, 16);
+}
+
+// Elements of one layout of dz: what bounds the backward pass's workspace.
+constexpr int64_t kPieceElements = 1 << 26;
+// Tiles of one launch: its threads have to stay below 2^32.
+constexpr int64_t kMostTiles = 1 << 23;
+
+Plan plan_of(const jorge_loss_shape& s, bool backward, bool direct_x, bool direct_w) {
+    Plan p{};
+    p.terms = s.dtype == JORGE_F32 ? kTerms : 1;
+    p.segments = s.dtype == JORGE_F32 ? kSegments : 1;
+    p.kd = round_up(s.cols, kPadK);
+    p.kn = round_up(s.tokens, kPadK);
+    p.direct_x = direct_x;
+    p.direct_w = direct_w;
+    // Pieces of equal size; without copies of weight the forward pass needs none.
+    int64_t most = kPieceElements / (s.dtype == JORGE_F32 ? 2 : 1) / std::max<int64_t>(1, backward ? p.kn : p.kd);
+    if (!backward && direct_w) most = s.vocab;
+    most = std::min(most, kMostTiles / ceil_div(std::max<int64_t>(1, s.tokens), 128) * 128);
+    most = std::max<int64_t>(512, most / 256 * 256);
+    p.piece = round_up(ceil_div(s.vocab, ceil_div(s.vocab, most)), 256);
+    const int64_t words = std::min(p.piece, s.vocab), seg = p.segments;
+    p.logits = shape_of(words, s.tokens, seg * p.kd / kStageK, false);
+    p.dh = shape_of(s.cols, s.tokens, seg * round_up(words, kPadK) / kStageK, true);
+    p.dw = shape_of(s.cols, words, seg * p.kn / kStageK, true);
+    return p;
+}
+
+struct Work {
+    bf16 *x, *w;                          // K-contiguous copies: hidden, a piece of weight
+    bf16 *xt, *wt;                        // transposed copies
+    bf16 *dz, *dzt;
+    float *top, *sum, *all, *at_target;   // forward
+    float *dh, *dw;                       // slices
+    int64_t bytes;
+};
+Work carve(void* base, const jorge_loss_shape& s, const Plan& p, bool backward) {
+    Carve c{(char*)base};
+    Work w{};
+    const int64_t words = std::min(p.piece, s.vocab), ld = round_up(s.cols, 4);
+    if (!p.direct_x) w.x = c.take<bf16>(p.terms * s.tokens * p.kd);
+    if (!p.direct_w) w.w = c.take<bf16>(p.terms * words * p.kd);
+    if (!backward) {
+        const int64_t parts = ceil_div(s.vocab, p.logits.large ? 128 : 64) + 3;
+        w.top = c.take<float>(parts * s.tokens);
+        w.sum = c.take<float>(parts * s.tokens);
+        if (s.label_smoothing > 0.0) w.all = c.take<float>(parts * s.tokens);
+        w.at_target = c.take<float>(s.tokens);
+    } else {
+        const int64_t ldz = round_up(words, kPadK);
+        w.xt = c.take<bf16>(p.terms * s.cols * p.kn);
+        w.wt = c.take<bf16>(p.terms * s.cols * ldz);
+        w.dz = c.take<bf16>(p.terms * s.tokens * ldz);
+        w.dzt = c.take<bf16>(p.terms * words * p.kn);
+        if (p.dh.ranges > 1 || s.vocab > p.piece) w.dh = c.take<float>(p.dh.ranges * s.tokens * ld);
+        if (p.dw.ranges > 1) w.dw = c.take<float>(p.dw.ranges * words * ld);
+    }
+    w.bytes = c.used;
+    return w;
+}
+// Whether hidden and weight serve as they are depends on their addresses: room for copies is asked for where
+// their type and strides alone do not rule it out.
+int64_t workspace_bytes_of(const jorge_loss_shape& s, bool backward) {
+    int64_t most = 0;
+    for (int k = 0; k < 4; ++k) most = std::max(most, carve(nullptr, s, plan_of(s, backward, k & 1, k & 2), backward).bytes);
+    return most;
+}
+
+template <typename F>
+void with_tile(bool large, F&& f) {
+    if (large) f(std::integral_constant<int, 8>());
+    else f(std::integral_constant<int, 4>());
+}
+Product product_of(const Shape& sh, const Operand& A, const Operand& B, int64_t k, bool split) {
+    const int64_t t = sh.large ? 256 : 128;
+    return {A, B, (int)(k / kStageK), split ? 1 : 0, (int)ceil_div(A.rows, t), (int)ceil_div(B.rows, t)};
+}
+// Lets a kernel use the LDS of its ring (more than the default limit).
+template <typename K>
+jorge_status allow_lds(K* kernel, int bytes) {
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) {
+        (void)hipGetLastError();
+        return refuse(JORGE_ERR_HIP, "cross entropy: no LDS for a tile");
+    }
+    return JORGE_OK;
+}
+
+template <typename T>
+void pack(const void* src, int64_t ld, int64_t rows, int64_t cols, bf16* dst, int64_t kd, hipStream_t s) {
+    if (rows == 0) return;
+    pack_kernel<T, sizeof(T) == 4 ? kTerms : 1><<<dim3((unsigned)rows, (unsigned)ceil_div(kd, 2048)), dim3(256), 0, s>>>(
+        (const T*)src, ld, rows, (int)cols, dst, (int)kd, rows * kd);
+}
+template <typename T>
+void transpose(const void* src, int64_t ld, int64_t rows, int64_t cols, bf16* dst, int64_t ldd, const LossRows* targets,
+               hipStream_t s) {
+    transpose_kernel<T, sizeof(T) == 4 ? kTerms : 1><<<dim3((unsigned)(ldd / 64), (unsigned)ceil_div(cols, 64)), dim3(256), 0, s>>>(
+        (const T*)src, ld, rows, (int)cols, dst, ldd, cols * ldd, targets ? targets->targets : nullptr,
+        targets ? targets->vocab : 0, targets ? targets->ignore : 0);
+}
+
+// hidden, and words [v0, v0 + n) of weight, as operands.
+template <typename T>
+Operand operand_x(const jorge_loss_shape& s, const Plan& p, const Work& w, const void* hidden) {
+    if (p.direct_x) return {(const bf16*)hidden, s.ldh, 0, s.tokens};
+    return {w.x, p.kd, s.tokens * p.kd, s.tokens};
+}
+template <typename T>
+Operand operand_w(const jorge_loss_shape& s, const Plan& p, const Work& w, const void* weight, int64_t v0, int64_t n, hipStream_t st) {
+    const T* const from = (const T*)weight + v0 * s.ldw;
+    if (p.direct_w) return {(const bf16*)from, s.ldw, 0, n};
+    pack<T>(from, s.ldw, n, s.cols, w.w, p.kd, st);
+    return {w.w, p.kd, n * p.kd, n};
+}
+
+template <typename T>
+jorge_status forward(const jorge_loss_shape& s, const Plan& p, const Work& w, const void* hidden, const void* weight,
+                     const LossRows& rows, float* loss, float* lse, float* total, hipStream_t st) {
+    if (!p.direct_x) pack<T>(hidden, s.ldh, s.tokens, s.cols, w.x, p.kd, st);
+    const Operand x = operand_x<T>(s, p, w, hidden);
+    const Stats stats{w.top, w.sum, w.all, w.at_target};
+    jorge_status err = JORGE_OK;
+    for (int64_t v0 = 0; v0 < s.vocab; v0 += p.piece) {
+        const int64_t n = std::min(p.piece, s.vocab - v0);
+        const Product pr = product_of(p.logits, operand_w<T>(s, p, w, weight, v0, n, st), x, p.kd, p.terms > 1);
+        with_tile(p.logits.large, [&](auto W) {
+            constexpr int WA = decltype(W)::value;
+            const auto k = loss_forward_kernel<WA, WA>;
+            if ((err = allow_lds(k, Tile<WA, WA>::kBytes)) != JORGE_OK) return;
+            k<<<dim3(pr.ta * pr.tb), dim3(256), Tile<WA, WA>::kBytes, st>>>(pr, rows, stats, v0);
+        });
+        if (err != JORGE_OK) return err;
+    }
+    // Words of a part: every piece but the last is a whole number of parts, and the last one's tile
+    // may have parts past its end, whose statistics are those of nothing.
+    const int64_t per = p.logits.large ? 128 : 64, last = (ceil_div(s.vocab, p.piece) - 1) * p.piece;
+    const int64_t parts = last / per + ceil_div(s.vocab - last, 2 * per) * 2;
+    loss_join_kernel<<<dim3((unsigned)ceil_div(s.tokens, 64)), dim3(kJoinWaves * 64), 0, st>>>(
+        stats, parts, rows, (float)s.label_smoothing, loss, lse);
+    loss_total_kernel<<<dim3(1), dim3(1024), 0, st>>>(loss, rows, total);
+    return launched("cross entropy");
+}
+
+// One gradient: out = scale * A-by-B, in slices where K is cut or the sum goes on (first, last: of the sum's pieces).
+template <typename T>
+jorge_status gradient(const Shape& sh, const Product& pr, T* out, int64_t ldo, int64_t cols, float* slices, bool first, bool last,
+                      const Scale& scale, hipStream_t st) {
+    jorge_status err = JORGE_OK;
+    const int64_t lda = round_up(cols, 4);
+    with_tile(sh.large, [&](auto W) {
+        constexpr int WA = decltype(W)::value;
+        const auto k = loss_grad_kernel<WA, WA, T>;
+        if ((err = allow_lds(k, Tile<WA, WA>::kBytes)) != JORGE_OK) return;
+        // The first piece of a sum is the longest and has at least 16 stages for each range; a short last one adds to
+        // fewer slices.
+        const int ranges = std::min(sh.ranges, pr.per * (pr.split ? kSegments : 1) / 2);
+        k<<<dim3(pr.ta * pr.tb, ranges), dim3(256), Tile<WA, WA>::kBytes, st>>>(pr, out, ldo, slices, lda, first ? 0 : 1, scale);
+    });
+    if (err != JORGE_OK) return err;
+    if (slices && last)
+        loss_slices_kernel<T><<<dim3((unsigned)pr.B.rows, (unsigned)ceil_div(cols, 1024)), dim3(256), 0, st>>>(
+            slices, sh.ranges, pr.B.rows, (int)cols, lda, out, ldo, scale);
+    return JORGE_OK;
+}
+
+template <typename T>
+jorge_status backward(const jorge_loss_shape& s, const Plan& p, const Work& w, const float* grad, int32_t kind, const void* hidden,
+                      const void* weight, const LossRows& rows, const float* lse, const float* total, void* dhidden,
+                      void* dweight, hipStream_t st) {
+    const bool split = p.terms > 1;
+    const Scale scale{kind == JORGE_LOSS_ROWS ? nullptr : grad, kind == JORGE_LOSS_MEAN ? total + 1 : nullptr};
+    const float* const row_grad = kind == JORGE_LOSS_ROWS ? grad : nullptr;
+    if (!p.direct_x) pack<T>(hidden, s.ldh, s.tokens, s.cols, w.x, p.kd, st);
+    if (dweight) transpose<T>(hidden, s.ldh, s.tokens, s.cols, w.xt, p.kn, &rows, st);
+    const Operand x = operand_x<T>(s, p, w, hidden);
+    const Operand xt{w.xt, p.kn, s.cols * p.kn, s.cols};
+    jorge_status err = JORGE_OK;
+    for (int64_t v0 = 0; v0 < s.vocab; v0 += p.piece) {
+        const int64_t n = std::min(p.piece, s.vocab - v0), ldz = round_up(n, kPadK);
+        const Product pr = product_of(p.logits, operand_w<T>(s, p, w, weight, v0, n, st), x, p.kd, split);
+        const DzOut dz{w.dz, w.dzt, ldz, p.kn, s.tokens * ldz, n * p.kn};
+        with_tile(p.logits.large, [&](auto W) {
+            constexpr int WA = decltype(W)::value;
+            const auto k = loss_dz_kernel<WA, WA, sizeof(T) == 4 ? kTerms : 1>;
+            if ((err = allow_lds(k, Tile<WA, WA>::kBytes)) != JORGE_OK) return;
+            k<<<dim3(pr.ta * pr.tb), dim3(256), Tile<WA, WA>::kBytes, st>>>(pr, rows, lse, row_grad, (float)s.label_smoothing, v0, dz);
+        });
+        if (err != JORGE_OK) return err;
+        if (dhidden) {
+            transpose<T>((const T*)weight + v0 * s.ldw, s.ldw, n, s.cols, w.wt, ldz, nullptr, st);
+            const Product g = product_of(p.dh, {w.wt, ldz, s.cols * ldz, s.cols}, {w.dz, ldz, dz.plane_z, s.tokens}, ldz, split);
+            if ((err = gradient(p.dh, g, (T*)dhidden, s.ldh, s.cols, w.dh, v0 == 0, v0 + n == s.vocab, scale, st)) != JORGE_OK) return err;
+        }
+        if (dweight) {
+            const Product g = product_of(p.dw, xt, {w.dzt, p.kn, dz.plane_t, n}, p.kn, split);
+            if ((err = gradient(p.dw, g, (T*)dweight + v0 * s.ldw, s.ldw, s.cols, w.dw, true, true, scale, st)) != JORGE_OK) return err;
+        }
+    }
+    return launched("cross entropy");
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void zero_rows_kernel(T* p, int64_t ld, int64_t cols) {
+    for (int64_t c = threadIdx.x; c < cols; c += 256) p[blockIdx.x * ld + c] = (T)0.0f;
+}
+
+jorge_status check(const jorge_loss_shape* s) {
+    if (!s) return bad("cross entropy: a shape is needed");
+    if (!known_dtype(s->dtype)) return bad("cross entropy: unknown element type");
+    if (s->tokens < 0 || s->cols < 1 || s->vocab < 1) return bad("cross entropy: tokens >= 0, cols >= 1 and vocab >= 1 are needed");
+    if (s->tokens > JORGE_LOSS_MAX_TOKENS) return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: tokens above JORGE_LOSS_MAX_TOKENS");
+    if (s->vocab > JORGE_LOSS_MAX_VOCAB) return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: vocab above JORGE_LOSS_MAX_VOCAB");
+    if (s->cols > JORGE_LOSS_MAX_COLS) return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: cols above JORGE_LOSS_MAX_COLS");
+    if (s->ldh < s->cols || s->ldw < s->cols) return bad("cross entropy: a row stride is below cols");
+    if (s->ldh > (int64_t)1 << 22 || s->ldw > (int64_t)1 << 22) return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: a row stride above 2^22");
+    if (!(s->label_smoothing >= 0.0 && s->label_smoothing <= 1.0)) return bad("cross entropy: label_smoothing must be in [0, 1]");
+    return JORGE_OK;
+}
+
+}  // namespace
+}  // namespace jorge_lm
+
+using namespace jorge_lm;
+
+extern "C" {
+
+jorge_status jorge_cross_entropy_workspace(const jorge_loss_shape* shape, int32_t backward, int64_t* bytes) {
+    if (!bytes) return bad("cross entropy: bytes is needed");
+    const jorge_status st = check(shape);
+    if (st != JORGE_OK) return st;
+    *bytes = shape->tokens ? workspace_bytes_of(*shape, backward != 0) : 0;
+    return JORGE_OK;
+}
+
+jorge_status jorge_cross_entropy_forward(const jorge_loss_shape* shape, const void* hidden, const void* weight,
+                                         const int64_t* targets, float* loss, float* lse, float* total, void* workspace,
+                                         int64_t workspace_bytes, void* hip_stream) {
+    jorge_status st = check(shape);
+    if (st != JORGE_OK) return st;
+    const jorge_loss_shape& s = *shape;
+    const int64_t e = dtype_bytes(s.dtype);
+    if (!total || !aligned(total, 4)) return bad("cross entropy: total is needed");
+    if (s.tokens > 0) {
+        if (!hidden || !weight || !targets || !loss || !lse) return bad("cross entropy: hidden, weight, targets, loss and lse are needed");
+        if (!aligned(hidden, e) || !aligned(weight, e) || !aligned(targets, 8) || !aligned(loss, 4) || !aligned(lse, 4))
+            return bad("cross entropy: a pointer is not aligned to its element");
+        if (!workspace || !aligned(workspace, kAlign)) return bad("cross entropy: a workspace aligned to 256 bytes is needed");
+        if (workspace_bytes < workspace_bytes_of(s, false)) return bad("cross entropy: the workspace is too small");
+    }
+    const LossRows rows{targets, s.tokens, s.vocab, s.ignore_index};
+    const hipStream_t q = reinterpret_cast<hipStream_t>(hip_stream);
+    if (s.tokens == 0) {
+        loss_total_kernel<<<dim3(1), dim3(1024), 0, q>>>(loss, rows, total);
+        return launched("cross entropy");
+    }
+    const Plan p = plan_of(s, false, direct(s, hidden, s.ldh), direct(s, weight, s.ldw));
+    const Work w = carve(workspace, s, p, false);
+    if (s.dtype == JORGE_F32) return forward<float>(s, p, w, hidden, weight, rows, loss, lse, total, q);
+    return forward<bf16>(s, p, w, hidden, weight, rows, loss, lse, total, q);
+}
+
+jorge_status jorge_cross_entropy_backward(const jorge_loss_shape* shape, const float* grad, int32_t kind, const void* hidden,
+                                          const void* weight, const int64_t* targets, const float* lse, const float* total,
+                                          void* dhidden, void* dweight, void* workspace, int64_t workspace_bytes,
+                                          void* hip_stream) {
+    jorge_status st = check(shape);
+    if (st != JORGE_OK) return st;
+    const jorge_loss_shape& s = *shape;
+    const int64_t e = dtype_bytes(s.dtype);
+    if (kind != JORGE_LOSS_ROWS && kind != JORGE_LOSS_SUM && kind != JORGE_LOSS_MEAN) return bad("cross entropy: unknown kind of gradient");
+    if (!aligned(dhidden, e) || !aligned(dweight, e)) return bad("cross entropy: a pointer is not aligned to its element");
+    const hipStream_t q = reinterpret_cast<hipStream_t>(hip_stream);
+    if (s.tokens == 0) {
+        if (dweight) {
+            if (s.dtype == JORGE_F32) zero_rows_kernel<float><<<dim3((unsigned)s.vocab), dim3(256), 0, q>>>((float*)dweight, s.ldw, s.cols);
+            else zero_rows_kernel<bf16><<<dim3((unsigned)s.vocab), dim3(256), 0, q>>>((bf16*)dweight, s.ldw, s.cols);
+        }
+        return launched("cross entropy");
+    }
+    if (!grad || !hidden || !weight || !targets || !lse || !total)
+        return bad("cross entropy: grad, hidden, weight, targets, lse and total are needed");
+    if (!aligned(grad, 4) || !aligned(hidden, e) || !aligned(weight, e) || !aligned(targets, 8) || !aligned(lse, 4) || !aligned(total, 4))
+        return bad("cross entropy: a pointer is not aligned to its element");
+    if (!workspace || !aligned(workspace, kAlign)) return bad("cross entropy: a workspace aligned to 256 bytes is needed");
+    if (workspace_bytes < workspace_bytes_of(s, true)) return bad("cross entropy: the workspace is too small");
+    if (!dhidden && !dweight) return JORGE_OK;
+    const Plan p = plan_of(s, true, direct(s, hidden, s.ldh), direct(s, weight, s.ldw));
+    const Work w = carve(workspace, s, p, true);
+    const LossRows rows{targets, s.tokens, s.vocab, s.ignore_index};
+    if (s.dtype == JORGE_F32)
+        return backward<float>(s, p, w, grad, kind, hidden, weight, rows, lse, total, dhidden, dweight, q);
+    return backward<bf16>(s, p, w, grad, kind, hidden, weight, rows, lse, total, dhidden, dweight, q);
+}
+
+}  // extern "C"

@@ -1,7 +1,7 @@
 """Operators of a language model's training step beside the Jorge step: layer norm, embedding,
-and AdamW with the global gradient norm.
+cross entropy over a vocabulary, and AdamW with the global gradient norm.
 
-ctypes binding of include/jorge_lm.h. layer_norm() and embedding() are
+ctypes binding of include/jorge_lm.h. layer_norm(), embedding() and linear_cross_entropy() are
 differentiable; the *_forward and *_backward functions are the two passes by themselves; AdamW
 steps a list of tensors. torch owns the memory (outputs and workspaces are torch tensors of the
 current stream) and names the current HIP stream. Tensors are fp32 or bfloat16 CUDA tensors of the
@@ -20,6 +20,12 @@ from .jorge import JORGE_OK, JorgeError, _current_stream, load_library
 _P, _I32, _I64, _F64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_double
 BLOCK = 256                                   # elements of an 8-bit moment that share a scale
 DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+REDUCTIONS = {"none": 0, "sum": 1, "mean": 2}
+
+
+class LossShape(ctypes.Structure):
+    _fields_ = [("tokens", _I64), ("cols", _I64), ("vocab", _I64), ("ldh", _I64), ("ldw", _I64), ("dtype", _I32),
+                ("reserved", _I32), ("ignore_index", _I64), ("label_smoothing", _F64)]
 
 
 class AdamWTensor(ctypes.Structure):
@@ -33,7 +39,7 @@ class AdamWMoments(ctypes.Structure):
                 ("blocks", _I64), ("bits", _I32), ("seed", ctypes.c_uint32)]
 
 
-_PT, _PM = ctypes.POINTER(AdamWTensor), ctypes.POINTER(AdamWMoments)
+_PT, _PM, _PS = ctypes.POINTER(AdamWTensor), ctypes.POINTER(AdamWMoments), ctypes.POINTER(LossShape)
 # name -> (restype, argtypes); mirrors include/jorge_lm.h
 _SIGNATURES = {
     "jorge_lm_last_error": (ctypes.c_char_p, []),
@@ -44,6 +50,9 @@ _SIGNATURES = {
     "jorge_embedding_forward": (_I32, [_P, _I64, _P, _I64, _I32, _I64, _I64, _F64, _P, _I64, _P]),
     "jorge_embedding_workspace": (_I32, [_I64, _I64, _I64, ctypes.POINTER(_I64)]),
     "jorge_embedding_backward": (_I32, [_P, _I64, _P, _I64, _I32, _I64, _I64, _F64, _I64, _P, _I64, _P, _I64, _P]),
+    "jorge_cross_entropy_workspace": (_I32, [_PS, _I32, ctypes.POINTER(_I64)]),
+    "jorge_cross_entropy_forward": (_I32, [_PS, _P, _P, _P, _P, _P, _P, _P, _I64, _P]),
+    "jorge_cross_entropy_backward": (_I32, [_PS, _P, _I32, _P, _P, _P, _P, _P, _P, _P, _P, _I64, _P]),
     "jorge_gradient_norm_workspace": (_I32, [_PT, _I32, ctypes.POINTER(_I64)]),
     "jorge_gradient_norm": (_I32, [_PT, _I32, _F64, _P, _P, _I64, _P]),
     "jorge_adamw_step": (_I32, [_PT, _I32, _PM, _I64, _F64, _F64, _F64, _F64, _F64, _P, _P]),
@@ -239,6 +248,88 @@ class _Embedding(torch.autograd.Function):
 def embedding(tokens, table, scale=1.0, padding=None):
     """Differentiable scale * table[tokens]; the gradient of table is dense (see embedding_backward)."""
     return _Embedding.apply(tokens, table, scale, padding)
+
+
+# ---------------------------------------------------------------- cross entropy
+def _loss_args(hidden, weight, targets, ignore_index, label_smoothing):
+    h, w, t = _matrix(hidden, "hidden"), _matrix(weight, "weight"), _int64s(targets, "targets")
+    if weight.dim() != 2 or h.shape[1] != w.shape[1]:
+        raise ValueError("weight: a matrix with a row of hidden's width per word is needed")
+    if h.dtype != w.dtype:
+        raise ValueError("hidden and weight must have one type")
+    if tuple(targets.shape) != tuple(hidden.shape[:-1]):
+        raise ValueError(f"targets: shape {tuple(targets.shape)} for hidden of shape {tuple(hidden.shape)}")
+    shape = LossShape(h.shape[0], h.shape[1], w.shape[0], _ld(h), _ld(w), DTYPES[h.dtype], 0, int(ignore_index),
+                      float(label_smoothing))
+    return h, w, t, shape
+
+
+def cross_entropy_forward(hidden, weight, targets, ignore_index=-100, label_smoothing=0.0):
+    """(loss, lse, total) of the cross entropy of the logits hidden @ weight.T, which are not kept:
+    loss and lse (log sum exp) one per row in fp32, total = [sum of the losses, rows with a target,
+    mean over those (0 without any)]. Targets outside [0, vocab), or equal to ignore_index, are none."""
+    lib = load_operators()
+    h, w, t, shape = _loss_args(hidden, weight, targets, ignore_index, label_smoothing)
+    n = _I64(0)
+    _check(lib, lib.jorge_cross_entropy_workspace(ctypes.byref(shape), 0, ctypes.byref(n)))
+    ws = _workspace(n.value)
+    loss, lse = (torch.empty(h.shape[0], dtype=torch.float32, device=h.device) for _ in range(2))
+    total = torch.empty(3, dtype=torch.float32, device=h.device)
+    _check(lib, lib.jorge_cross_entropy_forward(ctypes.byref(shape), h.data_ptr(), w.data_ptr(), t.data_ptr(),
+                                                loss.data_ptr(), lse.data_ptr(), total.data_ptr(), _ptr(ws), n.value,
+                                                _current_stream()))
+    return loss.view(targets.shape), lse.view(targets.shape), total
+
+
+def cross_entropy_backward(grad, hidden, weight, targets, lse, total, reduction="mean", ignore_index=-100,
+                           label_smoothing=0.0, need_hidden=True, need_weight=True):
+    """(dhidden, dweight) from lse and total of cross_entropy_forward. grad: the gradient of every row's
+    loss (reduction "none"), or of their sum or mean (one number, on the device)."""
+    lib = load_operators()
+    h, w, t, shape = _loss_args(hidden, weight, targets, ignore_index, label_smoothing)
+    kind = REDUCTIONS[reduction]
+    g = _cuda(grad, "grad").float().contiguous()
+    if g.numel() != (h.shape[0] if kind == 0 else 1):
+        raise ValueError("grad: one number per row for reduction 'none', one in all otherwise")
+    for s, k, what in ((lse, h.shape[0], "lse"), (total, 3, "total")):
+        if _cuda(s, what, (torch.float32,)).numel() != k or not s.is_contiguous():
+            raise ValueError(f"{what}: as cross_entropy_forward returned it")
+    n = _I64(0)
+    _check(lib, lib.jorge_cross_entropy_workspace(ctypes.byref(shape), 1, ctypes.byref(n)))
+    ws = _workspace(n.value)
+    # In the inputs' own row strides, as the call writes them.
+    dh = torch.empty((h.shape[0], shape.ldh), dtype=h.dtype, device=h.device) if need_hidden else None
+    dw = torch.empty((w.shape[0], shape.ldw), dtype=w.dtype, device=w.device) if need_weight else None
+    _check(lib, lib.jorge_cross_entropy_backward(ctypes.byref(shape), g.data_ptr(), kind, h.data_ptr(), w.data_ptr(),
+                                                 t.data_ptr(), lse.data_ptr(), total.data_ptr(), _ptr(dh), _ptr(dw),
+                                                 _ptr(ws), n.value, _current_stream()))
+    if need_hidden:
+        dh = dh[:, :h.shape[1]].reshape(hidden.shape)
+    return dh, dw[:, :w.shape[1]] if need_weight else None
+
+
+class _CrossEntropy(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, hidden, weight, targets, ignore_index, label_smoothing, reduction):
+        loss, lse, total = cross_entropy_forward(hidden, weight, targets, ignore_index, label_smoothing)
+        ctx.save_for_backward(hidden, weight, targets, lse, total)
+        ctx.more = (reduction, ignore_index, label_smoothing)
+        return loss if reduction == "none" else total[0 if reduction == "sum" else 2].clone()
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        dh, dw = cross_entropy_backward(grad, *ctx.saved_tensors, *ctx.more, need_hidden=ctx.needs_input_grad[0],
+                                        need_weight=ctx.needs_input_grad[1])
+        return dh, dw, None, None, None, None
+
+
+def linear_cross_entropy(hidden, weight, targets, ignore_index=-100, label_smoothing=0.0, reduction="mean"):
+    """Differentiable cross entropy of hidden @ weight.T without the logits (see cross_entropy_forward).
+    reduction: "mean" over the rows with a target, "sum" or "none"."""
+    if reduction not in REDUCTIONS:
+        raise ValueError(f"reduction: {reduction!r} is none of {sorted(REDUCTIONS)}")
+    return _CrossEntropy.apply(hidden, weight, targets, ignore_index, label_smoothing, reduction)
 
 
 # ---------------------------------------------------------------- AdamW

@@ -85,6 +85,44 @@ def test_embedding_refusals(lib):
         refused(lib, backward(**kw), INVALID, why)
 
 
+def test_cross_entropy_refusals(lib):
+    def shape(tokens=4, cols=8, vocab=5, ldh=8, ldw=8, dtype=1, ignore=-100, smoothing=0.0):
+        return lm.LossShape(tokens, cols, vocab, ldh, ldw, dtype, 0, ignore, smoothing)
+
+    def forward(h=A, w=A, t=A, loss=A, total=A, ws=A, size=1 << 30, **kw):
+        return lib.jorge_cross_entropy_forward(ctypes.byref(shape(**kw)), P(h), P(w), P(t), P(loss), P(A), P(total), P(ws),
+                                               size, None)
+    for kw, why in ((dict(tokens=-1), "tokens"), (dict(cols=0), "cols"), (dict(vocab=0), "vocab"), (dict(dtype=4), "type"),
+                    (dict(ldh=7), "stride"), (dict(ldw=7), "stride"), (dict(smoothing=1.01), "smoothing"),
+                    (dict(smoothing=float("nan")), "smoothing"), (dict(h=None), "needed"), (dict(t=A + 4), "aligned"),
+                    (dict(w=A + 1), "aligned"), (dict(total=None), "total"), (dict(ws=A + 8), "workspace"),
+                    (dict(size=64), "too small")):
+        refused(lib, forward(**kw), INVALID, why)
+    for kw, why in ((dict(tokens=(1 << 22) + 1), "TOKENS"), (dict(vocab=(1 << 22) + 1), "VOCAB"),
+                    (dict(cols=32769, ldh=32769, ldw=32769), "COLS"), (dict(ldw=(1 << 22) + 1), "stride")):
+        refused(lib, forward(**kw), UNSUPPORTED, why)
+
+    def backward(kind=0, grad=A, lse=A, dh=A, ws=A, size=1 << 30, **kw):
+        return lib.jorge_cross_entropy_backward(ctypes.byref(shape(**kw)), P(grad), kind, P(A), P(A), P(A), P(lse), P(A),
+                                                P(dh), P(A), P(ws), size, None)
+    for kw, why in ((dict(kind=3), "kind"), (dict(kind=-1), "kind"), (dict(grad=None), "needed"), (dict(lse=None), "needed"),
+                    (dict(dh=A + 1), "aligned"), (dict(ws=None), "workspace"), (dict(size=64), "too small")):
+        refused(lib, backward(**kw), INVALID, why)
+    n = I64()
+    assert lib.jorge_cross_entropy_workspace(None, 0, ctypes.byref(n)) == INVALID
+    sizes = {}
+    for tokens in (0, 1, 63, 8192, 1 << 22):
+        for vocab in (1, 50001, 1 << 22):
+            for dtype in (0, 1):
+                for back in (0, 1):
+                    s = shape(tokens=tokens, vocab=vocab, cols=2048, ldh=2048, ldw=2048, dtype=dtype)
+                    assert lib.jorge_cross_entropy_workspace(ctypes.byref(s), back, ctypes.byref(n)) == 0
+                    assert n.value % 256 == 0 and (n.value > 0) == (tokens > 0)
+                    sizes[tokens, vocab, dtype, back] = n.value
+    # The logits are not kept: a large vocabulary takes no more than a piece of it does.
+    assert sizes[8192, 1 << 22, 1, 1] < 1.2 * sizes[8192, 50001, 1, 1] < 8192 * 50001 * 4
+
+
 def test_adamw_refusals(lib):
     def step(numels=(300, 10), blocks=(0, 2), held=3, bits=32, dtype=0, t=1, ptr=A, scale=A, m=A, **kw):
         ts = (lm.AdamWTensor * len(numels))(*[lm.AdamWTensor(ptr, A, n, b, dtype, 0) for n, b in zip(numels, blocks)])
