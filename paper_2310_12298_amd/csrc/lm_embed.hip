@@ -6,11 +6,12 @@
 // dtable is written. Bound by HBM too: dout read once, dtable written once. Float atomics
 // would make the sum's order, and so its last bits, a matter of timing, and serialise on
 // the tokens that make up most of a text. So the tokens are sorted:
-//   1. tiles of 16384 tokens, each by one workgroup in LDS: a stable radix sort, so equal
-//      tokens keep their order of position;
-//   2. where there are several tiles, runs of up to eight tiles are merged per launch: an
+//   1. tiles of 4096 tokens, each by one workgroup in LDS: a stable radix sort, so equal
+//      tokens keep their order of position. (One tile of 16384 takes 37 us, bound by the one
+//      CU's LDS.);
+//   2. where there are several tiles, up to 16 sorted runs are merged per launch: an
 //      element's place is its place in its own run plus, in each of the others, the number
-//      of elements before it, by binary search;
+//      of elements before it, by binary searches that go on side by side;
 //   3. the sorted list is cut into chunks of equal length, whatever the tokens: a wave sums
 //      the runs of equal tokens of one chunk, in order, eight rows in flight. A run within
 //      the chunk is a finished row of dtable. The first and the last run of a chunk may
@@ -19,6 +20,8 @@
 //   4. the runs that cross chunks: their chunks' sums are added by a workgroup per run.
 // A token that half of all positions hold is thus spread over as many waves as any others.
 #include "lm_common.hpp"
+
+#include <utility>
 
 namespace jorge_lm {
 namespace {
@@ -58,7 +61,7 @@ struct Entry {
 
 constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / 64;
-constexpr int kSortItems = 16;
+constexpr int kSortItems = 4;
 constexpr int kSortTile = kSortThreads * kSortItems;
 constexpr int kDigitBits = 8;
 constexpr int kDigits = 1 << kDigitBits;
@@ -156,20 +159,47 @@ __device__ __forceinline__ int64_t before(const Entry* __restrict__ a, int64_t n
     return low;
 }
 
-constexpr int kMergeRuns = 8;
-// Merges groups of up to kMergeRuns sorted runs of length `run` (the last may be shorter).
-__global__ __launch_bounds__(256) void merge_kernel(const Entry* __restrict__ in, int64_t count, int64_t run,
+constexpr int kMergeRuns = 16;
+// Merges groups of up to RUNS sorted runs of length `run` (the last may be shorter). steps: halvings until a run's
+// length is 0.
+template <int RUNS>
+__global__ __launch_bounds__(256) void merge_kernel(const Entry* __restrict__ in, int count, int run, int steps,
                                                     Entry* __restrict__ out) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int i = blockIdx.x * 256 + threadIdx.x;
     if (i >= count) return;
     const Entry e = in[i];
-    const int64_t mine = i / run, g = mine / kMergeRuns * kMergeRuns;
-    int64_t at = g * run + i - mine * run;
+    const int mine = i / run, g = mine / RUNS * RUNS;
+    int low[RUNS], high[RUNS];
 #pragma unroll
-    for (int r = 0; r < kMergeRuns; ++r) {
-        const int64_t b = g + r, s = b * run;
-        if (b == mine || s >= count) continue;
-        at += before(in + s, count - s < run ? count - s : run, e.key, b < mine);
+    for (int r = 0; r < RUNS; ++r) {
+        const int s = (g + r) * run;
+        low[r] = s < count ? s : count - 1;
+        high[r] = s >= count ? low[r] : count - s < run ? count : s + run;
+        if (g + r == mine) low[r] = high[r] = i;  // its place among its own run is known
+    }
+    for (int k = 0; k < steps; ++k) {
+        uint32_t key[RUNS];
+#pragma unroll
+        for (int r = 0; r < RUNS; ++r) {
+            const int mid = (low[r] + high[r]) >> 1;
+            key[r] = in[mid < count ? mid : count - 1].key;
+        }
+#pragma unroll
+        for (int r = 0; r < RUNS; ++r) {
+            // Equal tokens of an earlier run come first.
+            const int mid = (low[r] + high[r]) >> 1;
+            const bool first = g + r < mine ? key[r] <= e.key : key[r] < e.key;
+            if (low[r] < high[r]) {
+                if (first) low[r] = mid + 1;
+                else high[r] = mid;
+            }
+        }
+    }
+    int at = g * run;
+#pragma unroll
+    for (int r = 0; r < RUNS; ++r) {
+        const int s = (g + r) * run;
+        if (s < count) at += low[r] - s;
     }
     out[at] = e;
 }
@@ -284,8 +314,16 @@ __global__ __launch_bounds__(kJoinWaves * 64) void embed_join_kernel(SumArgs a, 
     if (key >= a.vocab || a.sorted[s1 - 1].key != key) return;
     const bool first_run = a.sorted[s0].key == key;  // the run fills the whole chunk
     if (first_run && s0 > 0 && a.sorted[s0 - 1].key == key) return;  // it started before
-    const int64_t end = s1 + before(a.sorted + s1, a.count - s1, key, true);
-    const int64_t last = (end - 1) / a.chunk;
+    // The run's last chunk: the first whose end it does not cross. 64 chunks' ends are looked at at a time.
+    int64_t last = part + 1;
+    for (;; last += 64) {
+        const int64_t next = (last + (threadIdx.x & 63) + 1) * a.chunk;
+        const uint64_t on = __ballot(next < a.count && a.sorted[next < a.count ? next : 0].key == key);
+        if (~on) {
+            last += __ffsll((unsigned long long)~on) - 1;
+            break;
+        }
+    }
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (blockIdx.y * 64 + lane) * 4;
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
     if (c < a.cols) {
@@ -376,15 +414,17 @@ jorge_status backward(const void* dout, int64_t lddo, const int64_t* tokens, int
         // A single short tile leaves out the elements that it does not have.
         if (count <= kSortThreads)
             sort_tiles_kernel<1><<<tiles, threads, 0, s>>>(tokens, count, vocab, padding, bits, w.a);
-        else if (count <= 4 * kSortThreads)
-            sort_tiles_kernel<4><<<tiles, threads, 0, s>>>(tokens, count, vocab, padding, bits, w.a);
         else
             sort_tiles_kernel<kSortItems><<<tiles, threads, 0, s>>>(tokens, count, vocab, padding, bits, w.a);
         for (int64_t run = kSortTile; run < count; run *= kMergeRuns) {
-            merge_kernel<<<dim3((unsigned)ceil_div(count, 256)), dim3(256), 0, s>>>(w.a, count, run, w.b);
-            Entry* const t = w.a;
-            w.a = w.b;
-            w.b = t;
+            const dim3 grid((unsigned)ceil_div(count, 256));
+            int steps = 1;
+            while (run >> steps) ++steps;
+            if (ceil_div(count, run) <= 4)
+                merge_kernel<4><<<grid, dim3(256), 0, s>>>(w.a, (int)count, (int)run, steps, w.b);
+            else
+                merge_kernel<kMergeRuns><<<grid, dim3(256), 0, s>>>(w.a, (int)count, (int)run, steps, w.b);
+            std::swap(w.a, w.b);
         }
     }
     SumArgs a{};

@@ -33,85 +33,87 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr int kTerms = 3;      // of a split fp32 operand
-constexpr int kSegments = 6;   // products of terms
 constexpr int kPadK = 64;      // K of every product is a multiple of two stages
 
 // ---------------------------------------------------------------- operands
-// dst[t][r][c] = term t of src[r][c], 0 past the row's end (c < ldd, a multiple of 8).
-template <typename T, int TERMS>
-__global__ __launch_bounds__(256) void pack_kernel(const T* __restrict__ src, int64_t lds, int64_t rows, int cols,
-                                                   bf16* __restrict__ dst, int ldd, int64_t plane) {
-    const int64_t r = blockIdx.x;
-    for (int c = (blockIdx.y * 256 + threadIdx.x) * 8; c < ldd; c += gridDim.y * 2048) {
-        float f[8];
-        const T* const p = src + r * lds + c;
-        const int left = cols - c;
-        typedef T V __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-        if (left >= 8) {
-            const V v = *reinterpret_cast<const V*>(p);
+// Copies of a matrix that the products read: `flat`, its rows padded with zeros to ldf (a multiple of 64), and `turned`,
+// its transpose, padded to ldt (a multiple of 64) with zeros, which also stand in for the rows that `targets` (if
+// given) has no target for: what such a row holds must not reach a sum that it has no part in. Either may be null;
+// term t of the elements goes to plane t.
+struct Copies {
+    const void* src;
+    int64_t ld, rows;
+    int cols, tiles_c;       // 64 x 64 tiles along the columns
+    bf16 *flat, *turned;
+    int64_t ldf, plane_f, ldt, plane_t;
+    const int64_t* targets;
+    int64_t vocab, ignore;
+    int64_t tiles;           // of the whole job
+};
+struct CopyJobs {
+    Copies job[2];
+};
+
+template <int TERMS>
+__device__ __forceinline__ void store_terms(bf16* dst, int64_t plane, float (&f)[8]) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = (float)v[e];
-        } else {
+    for (int t = 0; t < TERMS; ++t) {
+        bf16x8 o;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = e < left ? (float)p[e] : 0.0f;
+        for (int e = 0; e < 8; ++e) {
+            o[e] = (bf16)f[e];
+            f[e] -= (float)o[e];
         }
-#pragma unroll
-        for (int t = 0; t < TERMS; ++t) {
-            bf16x8 o;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                o[e] = (bf16)f[e];
-                f[e] -= (float)o[e];
-            }
-            *reinterpret_cast<bf16x8*>(dst + t * plane + r * ldd + c) = o;
-        }
+        *reinterpret_cast<bf16x8*>(dst + t * plane) = o;
     }
 }
 
-// dst[t][c][r] = term t of src[r][c] for c < cols, r < ldd (a multiple of 64), 0 for r >= rows and for the rows
-// that `targets` (if given) has no target for: what such a row holds must not reach a sum that it has no part in.
+// One workgroup per 64 x 64 tile: read once, eight elements of a row per lane, and written both ways.
 template <typename T, int TERMS>
-__global__ __launch_bounds__(256) void transpose_kernel(const T* __restrict__ src, int64_t lds, int64_t rows, int cols,
-                                                        bf16* __restrict__ dst, int64_t ldd, int64_t plane,
-                                                        const int64_t* __restrict__ targets, int64_t vocab,
-                                                        int64_t ignore) {
-    __shared__ float tile[64][65];
-    const int64_t r0 = (int64_t)blockIdx.x * 64;
-    const int c0 = blockIdx.y * 64, x = threadIdx.x & 63, y = threadIdx.x >> 6;
+__global__ __launch_bounds__(256) void copies_kernel(CopyJobs jobs) {
+    __shared__ T tile[64][64 + 4 / sizeof(T)];  // the odd row length spreads a column over the banks
+    const bool second = blockIdx.x >= jobs.job[0].tiles;
+    const Copies& j = jobs.job[second];
+    const int64_t g = blockIdx.x - (second ? jobs.job[0].tiles : 0);
+    const int64_t r0 = g / j.tiles_c * 64;
+    const int c0 = (int)(g % j.tiles_c) * 64, part = (threadIdx.x & 7) * 8;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        const int64_t r = r0 + y + 4 * k;
-        float v = 0.0f;
-        if (r < rows && c0 + x < cols) {
-            bool live = true;
-            if (targets) {
-                const int64_t t = targets[r];
-                live = t >= 0 && t < vocab && t != ignore;
+    for (int k = 0; k < 2; ++k) {
+        const int y = (threadIdx.x >> 3) + 32 * k, c = c0 + part, left = j.cols - c;
+        const int64_t r = r0 + y;
+        float f[8] = {};
+        bool live = r < j.rows;
+        if (live) {
+            typedef T V __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+            const T* const p = (const T*)j.src + r * j.ld + c;
+            if (left >= 8) {
+                const V v = *reinterpret_cast<const V*>(p);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = (float)v[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] = e < left ? (float)p[e] : 0.0f;
             }
-            if (live) v = (float)src[r * lds + c0 + x];
+            if (j.targets) {
+                const int64_t t = j.targets[r];
+                live = t >= 0 && t < j.vocab && t != j.ignore;
+            }
         }
-        tile[y + 4 * k][x] = v;
+        if (j.turned)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) tile[y][part + e] = live ? (T)f[e] : (T)0.0f;
+        if (j.flat && r < j.rows) store_terms<TERMS>(j.flat + r * j.ldf + c, j.plane_f, f);
     }
+    if (!j.turned) return;
     __syncthreads();
-    // Eight rows of src per lane: 16 bytes of a row of dst.
-    const int part = threadIdx.x & 7;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const int c = (threadIdx.x >> 3) + 32 * k;
-        if (c0 + c >= cols) continue;
+        if (c0 + c >= j.cols || r0 + part >= j.ldt) continue;
         float f[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = tile[part * 8 + e][c];
-#pragma unroll
-        for (int t = 0; t < TERMS; ++t) {
-            bf16x8 o;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                o[e] = (bf16)f[e];
-                f[e] -= (float)o[e];
-            }
-            *reinterpret_cast<bf16x8*>(dst + t * plane + (int64_t)(c0 + c) * ldd + r0 + part * 8) = o;
-        }
+        for (int e = 0; e < 8; ++e) f[e] = (float)tile[part + e][c];
+        store_terms<TERMS>(j.turned + (int64_t)(c0 + c) * j.ldt + r0 + part, j.plane_t, f);
     }
 }
 
@@ -132,7 +134,6 @@ __device__ __forceinline__ Place place_of(int g, int ta, int tb) {
 struct Product {
     Operand A, B;
     int per;         // stages of one segment
-    int split;       // operands in three terms: kSegments segments
     int ta, tb;
 };
 
@@ -174,13 +175,13 @@ struct Stats {
 };
 
 // A: words from word0 on; B: tokens.
-template <int WA, int WB>
+template <int WA, int WB, int RING, bool SPLIT>
 __global__ __launch_bounds__(256, 1) void loss_forward_kernel(Product p, LossRows rows, Stats out, int64_t word0) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
-    using T = Tile<WA, WB>;
+    using T = Tile<WA, WB, RING, SPLIT>;
     const Place at = place_of(blockIdx.x, p.ta, p.tb);
     T t;
-    t.multiply(p.A, p.B, (int64_t)at.a * T::kA, (int64_t)at.b * T::kB, 0, p.per * (p.split ? kSegments : 1), p.per, p.split, lds);
+    t.multiply(p.A, p.B, (int64_t)at.a * T::kA, (int64_t)at.b * T::kB, 0, p.per * (SPLIT ? kSegments : 1), p.per, lds);
     const int64_t a0 = (int64_t)at.a * T::kA + T::lane_a(), b0 = (int64_t)at.b * T::kB + T::lane_b();
     const int left = lane_left<WA>(p.A.rows - a0);  // words of this lane that exist
     const int64_t part = (word0 + (int64_t)at.a * T::kA) / (16 * WA) + (threadIdx.x >> 7);
@@ -307,15 +308,15 @@ struct DzOut {
 };
 
 // dz of a piece: words word0 .. word0 + A.rows; padding up to ldz words and ldt tokens is written as 0.
-template <int WA, int WB, int TERMS>
+template <int WA, int WB, int RING, bool SPLIT>
 __global__ __launch_bounds__(256, 1) void loss_dz_kernel(Product p, LossRows rows, const float* __restrict__ lse,
                                                          const float* __restrict__ row_grad, float smoothing, int64_t word0,
                                                          DzOut out) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
-    using T = Tile<WA, WB>;
+    using T = Tile<WA, WB, RING, SPLIT>;
     const Place at = place_of(blockIdx.x, p.ta, p.tb);
     T t;
-    t.multiply(p.A, p.B, (int64_t)at.a * T::kA, (int64_t)at.b * T::kB, 0, p.per * (p.split ? kSegments : 1), p.per, p.split, lds);
+    t.multiply(p.A, p.B, (int64_t)at.a * T::kA, (int64_t)at.b * T::kB, 0, p.per * (SPLIT ? kSegments : 1), p.per, lds);
     const int64_t a0 = (int64_t)at.a * T::kA + T::lane_a(), b0 = (int64_t)at.b * T::kB + T::lane_b();
     const int left = lane_left<WA>(p.A.rows - a0);
     const float even = smoothing / (float)rows.vocab;
@@ -337,7 +338,7 @@ __global__ __launch_bounds__(256, 1) void loss_dz_kernel(Product p, LossRows row
             }
     }
 #pragma unroll
-    for (int term = 0; term < TERMS; ++term) {
+    for (int term = 0; term < (SPLIT ? kTerms : 1); ++term) {
         bf16* const dz = out.dz + term * out.plane_z;
         bf16* const dzt = out.dzt + term * out.plane_t;
 #pragma unroll
@@ -362,7 +363,7 @@ __global__ __launch_bounds__(256, 1) void loss_dz_kernel(Product p, LossRows row
                         for (int j = 0; j < WB; ++j) o[j] = (bf16)t.acc[i][j][r];
                         *reinterpret_cast<V*>(dzt + (a0 + 4 * i + r) * out.ldt + b0) = o;
                     }
-        if constexpr (TERMS > 1)
+        if constexpr (SPLIT)
 #pragma unroll
             for (int j = 0; j < WB; ++j)
 #pragma unroll
@@ -382,16 +383,16 @@ struct Scale {
 
 // C[b][a] over one of gridDim.y ranges of K, to out (whole: one range) or to the range's slice of fp32 sums
 // [ranges][B.rows][lda], added to it where `add`.
-template <int WA, int WB, typename O>
+template <int WA, int WB, int RING, bool SPLIT, typename O>
 __global__ __launch_bounds__(256, 1) void loss_grad_kernel(Product p, O* __restrict__ out, int64_t ldo, float* __restrict__ slices,
                                                            int64_t lda, int add, Scale scale) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
-    using T = Tile<WA, WB>;
+    using T = Tile<WA, WB, RING, SPLIT>;
     const Place at = place_of(blockIdx.x, p.ta, p.tb);
-    const int pairs = p.per * (p.split ? kSegments : 1) / 2;
+    const int pairs = p.per * (SPLIT ? kSegments : 1) / 2;
     const int s0 = (int)((int64_t)pairs * blockIdx.y / gridDim.y) * 2, s1 = (int)((int64_t)pairs * (blockIdx.y + 1) / gridDim.y) * 2;
     T t;
-    t.multiply(p.A, p.B, (int64_t)at.a * T::kA, (int64_t)at.b * T::kB, s0, s1, p.per, p.split, lds);
+    t.multiply(p.A, p.B, (int64_t)at.a * T::kA, (int64_t)at.b * T::kB, s0, s1, p.per, lds);
     const int64_t a0 = (int64_t)at.a * T::kA + T::lane_a(), b0 = (int64_t)at.b * T::kB + T::lane_b();
     const int left = lane_left<WA>(p.A.rows - a0);
     if (slices) {
@@ -433,8 +434,15 @@ __global__ __launch_bounds__(256) void loss_slices_kernel(const float* __restric
     const float f = scale.value();
     for (int c = (blockIdx.y * 256 + threadIdx.x) * 4; c < cols; c += gridDim.y * 1024) {
         const float* p = slices + r * lda + c;
-        f32x4 s = *reinterpret_cast<const f32x4*>(p);
-        for (int k = 1; k < n; ++k) s += *reinterpret_cast<const f32x4*>(p + k * rows * lda);
+        f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+        int k = 0;
+        for (; k + 8 <= n; k += 8) {
+            f32x4 v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = *reinterpret_cast<const f32x4*>(p + (k + u) * rows * lda);
+            s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        }
+        for (; k < n; ++k) s += *reinterpret_cast<const f32x4*>(p + k * rows * lda);
         O* const o = out + r * ldo + c;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -447,24 +455,28 @@ constexpr int kCus = 256;
 
 // Which tile a product of `a` x `b` takes, and over how many ranges of K it is cut.
 struct Shape {
-    bool large;   // 256 x 256, else 128 x 128
+    int blocks;   // 8, 4 or 2: tiles of 256 x 256, 128 x 128 or 64 x 64
     int ranges;
+    bool deep;    // a tile has its CU to itself: a ring of eight stages, else of four
 };
-// Large tiles run a product at twice the small ones' rate, where there are enough of them for the CUs.
+// Large tiles run a product at twice the small ones' rate (8192 x 8192 x 2048: 354 us against 474, 4096 x 4096 x 8192:
+// 238 against 395), where there are enough of them for the CUs. A stage of a 64 x 64 tile takes a third of the time
+// of a 128 x 128 one's, which the LDS bounds: they serve where those would leave CUs idle.
 Shape shape_of(int64_t a, int64_t b, int64_t stages, bool may_cut) {
     const int64_t big = ceil_div(a, 256) * ceil_div(b, 256), small = ceil_div(a, 128) * ceil_div(b, 128);
-    if (big >= kCus / 2 || !may_cut) {
-        if (big >= kCus / 2) return {true, 1};
-        return {false, 1};
-    }
+    if (big >= kCus / 2) return {8, 1, false};
+    if (!may_cut) return small > kCus / 2 ? Shape{4, 1, small <= kCus} : Shape{2, 1, true};
     // Cut along K until the tiles fill the CUs; a range keeps at least 16 stages.
     const auto cut = [&](int64_t tiles, int64_t want) {
         const int64_t most = stages / 16;
         return std::max<int64_t>(1, std::min(want / tiles, most));
     };
     const int64_t rb = cut(big, kCus);
-    if (big * rb >= kCus / 2) return {true, (int)rb};
-    return {false, (int)cut(small, 2 * kCus)};
+    if (big * rb >= kCus / 2) return {8, (int)rb, false};
+    const int64_t rs = cut(small, kCus);
+    if (small * rs > kCus / 2) return {4, (int)rs, small * rs <= kCus};
+    const int64_t least = ceil_div(a, 64) * ceil_div(b, 64);
+    return {2, (int)cut(least, kCus), true};
 }
 
 struct Plan {
@@ -483,6 +495,28 @@ constexpr int64_t kPieceElements = 1 << 26;
 // Tiles of one launch: its threads have to stay below 2^32.
 constexpr int64_t kMostTiles = 1 << 23;
 
+// Words of a piece, a multiple of 256 up to `most`: where the tiles are large, those that leave the CUs idle least in the
+// last round of a launch's tiles, over the whole vocabulary. A round of dz costs cols (and its exponentials, about 400
+// elements of K), one of dweight tokens; a piece's other launches about a thousand.
+int64_t piece_of(const jorge_loss_shape& s, int64_t most, bool backward) {
+    const int64_t even = round_up(ceil_div(s.vocab, ceil_div(s.vocab, most)), 256);
+    const int64_t tokens = ceil_div(s.tokens, 256), cols = ceil_div(s.cols, 256);
+    if (!backward || even >= s.vocab || tokens * ceil_div(even, 256) < kCus) return even;
+    const auto cost = [&](int64_t n) {
+        const int64_t w = ceil_div(n, 256);
+        return ceil_div(tokens * w, kCus) * (s.cols + 400) + ceil_div(cols * w, kCus) * s.tokens + 1000;
+    };
+    int64_t best = even, least = INT64_MAX;
+    for (int64_t n = most; n >= std::max<int64_t>(512, most / 2); n -= 256) {
+        const int64_t last = s.vocab % n, c = s.vocab / n * cost(n) + (last ? cost(last) : 0);
+        if (c < least) {
+            least = c;
+            best = n;
+        }
+    }
+    return best;
+}
+
 Plan plan_of(const jorge_loss_shape& s, bool backward, bool direct_x, bool direct_w) {
     Plan p{};
     p.terms = s.dtype == JORGE_F32 ? kTerms : 1;
@@ -491,12 +525,11 @@ Plan plan_of(const jorge_loss_shape& s, bool backward, bool direct_x, bool direc
     p.kn = round_up(s.tokens, kPadK);
     p.direct_x = direct_x;
     p.direct_w = direct_w;
-    // Pieces of equal size; without copies of weight the forward pass needs none.
+    // Without copies of weight the forward pass needs no pieces.
     int64_t most = kPieceElements / (s.dtype == JORGE_F32 ? 2 : 1) / std::max<int64_t>(1, backward ? p.kn : p.kd);
     if (!backward && direct_w) most = s.vocab;
     most = std::min(most, kMostTiles / ceil_div(std::max<int64_t>(1, s.tokens), 128) * 128);
-    most = std::max<int64_t>(512, most / 256 * 256);
-    p.piece = round_up(ceil_div(s.vocab, ceil_div(s.vocab, most)), 256);
+    p.piece = piece_of(s, std::max<int64_t>(512, round_up(most, 256) - (most < s.vocab && most % 256 ? 256 : 0)), backward);
     const int64_t words = std::min(p.piece, s.vocab), seg = p.segments;
     p.logits = shape_of(words, s.tokens, seg * p.kd / kStageK, false);
     p.dh = shape_of(s.cols, s.tokens, seg * round_up(words, kPadK) / kStageK, true);
@@ -519,7 +552,7 @@ Work carve(void* base, const jorge_loss_shape& s, const Plan& p, bool backward) 
     if (!p.direct_x) w.x = c.take<bf16>(p.terms * s.tokens * p.kd);
     if (!p.direct_w) w.w = c.take<bf16>(p.terms * words * p.kd);
     if (!backward) {
-        const int64_t parts = ceil_div(s.vocab, p.logits.large ? 128 : 64) + 3;
+        const int64_t parts = ceil_div(s.vocab, 16 * p.logits.blocks) + 1;
         w.top = c.take<float>(parts * s.tokens);
         w.sum = c.take<float>(parts * s.tokens);
         if (s.label_smoothing > 0.0) w.all = c.take<float>(parts * s.tokens);
@@ -545,13 +578,15 @@ int64_t workspace_bytes_of(const jorge_loss_shape& s, bool backward) {
 }
 
 template <typename F>
-void with_tile(bool large, F&& f) {
-    if (large) f(std::integral_constant<int, 8>());
-    else f(std::integral_constant<int, 4>());
+void with_tile(const Shape& s, F&& f) {
+    if (s.blocks == 8) f(std::integral_constant<int, 8>(), std::integral_constant<int, 4>());
+    else if (s.blocks == 2) f(std::integral_constant<int, 2>(), std::integral_constant<int, 8>());
+    else if (s.deep) f(std::integral_constant<int, 4>(), std::integral_constant<int, 8>());
+    else f(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
 }
-Product product_of(const Shape& sh, const Operand& A, const Operand& B, int64_t k, bool split) {
-    const int64_t t = sh.large ? 256 : 128;
-    return {A, B, (int)(k / kStageK), split ? 1 : 0, (int)ceil_div(A.rows, t), (int)ceil_div(B.rows, t)};
+Product product_of(const Shape& sh, const Operand& A, const Operand& B, int64_t k) {
+    const int64_t t = 32 * sh.blocks;
+    return {A, B, (int)(k / kStageK), (int)ceil_div(A.rows, t), (int)ceil_div(B.rows, t)};
 }
 // Lets a kernel use the LDS of its ring (more than the default limit).
 template <typename K>
@@ -563,55 +598,69 @@ jorge_status allow_lds(K* kernel, int bytes) {
     return JORGE_OK;
 }
 
-template <typename T>
-void pack(const void* src, int64_t ld, int64_t rows, int64_t cols, bf16* dst, int64_t kd, hipStream_t s) {
-    if (rows == 0) return;
-    pack_kernel<T, sizeof(T) == 4 ? kTerms : 1><<<dim3((unsigned)rows, (unsigned)ceil_div(kd, 2048)), dim3(256), 0, s>>>(
-        (const T*)src, ld, rows, (int)cols, dst, (int)kd, rows * kd);
+// The copies of a matrix of rows x cols; flat and turned may be null, padded is the transpose's row length.
+Copies copies_of(const void* src, int64_t ld, int64_t rows, int64_t cols, bf16* flat, int64_t kd, bf16* turned,
+                 int64_t padded, const LossRows* targets) {
+    Copies c{};
+    if (!flat && !turned) return c;
+    c.src = src;
+    c.ld = ld;
+    c.rows = rows;
+    c.cols = (int)cols;
+    c.tiles_c = (int)(kd / 64);
+    c.flat = flat;
+    c.turned = turned;
+    c.ldf = kd;
+    c.plane_f = rows * kd;
+    c.ldt = padded;
+    c.plane_t = cols * padded;
+    if (targets) {
+        c.targets = targets->targets;
+        c.vocab = targets->vocab;
+        c.ignore = targets->ignore;
+    }
+    c.tiles = ceil_div(rows, 64) * c.tiles_c;
+    return c;
 }
 template <typename T>
-void transpose(const void* src, int64_t ld, int64_t rows, int64_t cols, bf16* dst, int64_t ldd, const LossRows* targets,
-               hipStream_t s) {
-    transpose_kernel<T, sizeof(T) == 4 ? kTerms : 1><<<dim3((unsigned)(ldd / 64), (unsigned)ceil_div(cols, 64)), dim3(256), 0, s>>>(
-        (const T*)src, ld, rows, (int)cols, dst, ldd, cols * ldd, targets ? targets->targets : nullptr,
-        targets ? targets->vocab : 0, targets ? targets->ignore : 0);
+void copy(const Copies& a, const Copies& b, hipStream_t s) {
+    if (a.tiles + b.tiles == 0) return;
+    copies_kernel<T, sizeof(T) == 4 ? kTerms : 1><<<dim3((unsigned)(a.tiles + b.tiles)), dim3(256), 0, s>>>({{a, b}});
 }
 
-// hidden, and words [v0, v0 + n) of weight, as operands.
-template <typename T>
+// hidden, and a piece of n words of weight from `from` on, as operands.
 Operand operand_x(const jorge_loss_shape& s, const Plan& p, const Work& w, const void* hidden) {
     if (p.direct_x) return {(const bf16*)hidden, s.ldh, 0, s.tokens};
     return {w.x, p.kd, s.tokens * p.kd, s.tokens};
 }
-template <typename T>
-Operand operand_w(const jorge_loss_shape& s, const Plan& p, const Work& w, const void* weight, int64_t v0, int64_t n, hipStream_t st) {
-    const T* const from = (const T*)weight + v0 * s.ldw;
+Operand operand_w(const jorge_loss_shape& s, const Plan& p, const Work& w, const void* from, int64_t n) {
     if (p.direct_w) return {(const bf16*)from, s.ldw, 0, n};
-    pack<T>(from, s.ldw, n, s.cols, w.w, p.kd, st);
     return {w.w, p.kd, n * p.kd, n};
 }
 
 template <typename T>
 jorge_status forward(const jorge_loss_shape& s, const Plan& p, const Work& w, const void* hidden, const void* weight,
                      const LossRows& rows, float* loss, float* lse, float* total, hipStream_t st) {
-    if (!p.direct_x) pack<T>(hidden, s.ldh, s.tokens, s.cols, w.x, p.kd, st);
-    const Operand x = operand_x<T>(s, p, w, hidden);
+    const Operand x = operand_x(s, p, w, hidden);
     const Stats stats{w.top, w.sum, w.all, w.at_target};
     jorge_status err = JORGE_OK;
     for (int64_t v0 = 0; v0 < s.vocab; v0 += p.piece) {
         const int64_t n = std::min(p.piece, s.vocab - v0);
-        const Product pr = product_of(p.logits, operand_w<T>(s, p, w, weight, v0, n, st), x, p.kd, p.terms > 1);
-        with_tile(p.logits.large, [&](auto W) {
-            constexpr int WA = decltype(W)::value;
-            const auto k = loss_forward_kernel<WA, WA>;
-            if ((err = allow_lds(k, Tile<WA, WA>::kBytes)) != JORGE_OK) return;
-            k<<<dim3(pr.ta * pr.tb), dim3(256), Tile<WA, WA>::kBytes, st>>>(pr, rows, stats, v0);
+        const T* const from = (const T*)weight + v0 * s.ldw;
+        copy<T>(v0 ? Copies{} : copies_of(hidden, s.ldh, s.tokens, s.cols, w.x, p.kd, nullptr, 0, nullptr),
+                copies_of(from, s.ldw, n, s.cols, w.w, p.kd, nullptr, 0, nullptr), st);
+        const Product pr = product_of(p.logits, operand_w(s, p, w, from, n), x, p.kd);
+        with_tile(p.logits, [&](auto W, auto R) {
+            constexpr int WA = decltype(W)::value, RING = decltype(R)::value;
+            const auto k = loss_forward_kernel<WA, WA, RING, sizeof(T) == 4>;
+            if ((err = allow_lds(k, Tile<WA, WA, RING, sizeof(T) == 4>::kBytes)) != JORGE_OK) return;
+            k<<<dim3(pr.ta * pr.tb), dim3(256), Tile<WA, WA, RING, sizeof(T) == 4>::kBytes, st>>>(pr, rows, stats, v0);
         });
         if (err != JORGE_OK) return err;
     }
     // Words of a part: every piece but the last is a whole number of parts, and the last one's tile
     // may have parts past its end, whose statistics are those of nothing.
-    const int64_t per = p.logits.large ? 128 : 64, last = (ceil_div(s.vocab, p.piece) - 1) * p.piece;
+    const int64_t per = 16 * p.logits.blocks, last = (ceil_div(s.vocab, p.piece) - 1) * p.piece;
     const int64_t parts = last / per + ceil_div(s.vocab - last, 2 * per) * 2;
     loss_join_kernel<<<dim3((unsigned)ceil_div(s.tokens, 64)), dim3(kJoinWaves * 64), 0, st>>>(
         stats, parts, rows, (float)s.label_smoothing, loss, lse);
@@ -625,14 +674,14 @@ jorge_status gradient(const Shape& sh, const Product& pr, T* out, int64_t ldo, i
                       const Scale& scale, hipStream_t st) {
     jorge_status err = JORGE_OK;
     const int64_t lda = round_up(cols, 4);
-    with_tile(sh.large, [&](auto W) {
-        constexpr int WA = decltype(W)::value;
-        const auto k = loss_grad_kernel<WA, WA, T>;
-        if ((err = allow_lds(k, Tile<WA, WA>::kBytes)) != JORGE_OK) return;
+    with_tile(sh, [&](auto W, auto R) {
+        constexpr int WA = decltype(W)::value, RING = decltype(R)::value;
+        const auto k = loss_grad_kernel<WA, WA, RING, sizeof(T) == 4, T>;
+        if ((err = allow_lds(k, Tile<WA, WA, RING, sizeof(T) == 4>::kBytes)) != JORGE_OK) return;
         // The first piece of a sum is the longest and has at least 16 stages for each range; a short last one adds to
         // fewer slices.
-        const int ranges = std::min(sh.ranges, pr.per * (pr.split ? kSegments : 1) / 2);
-        k<<<dim3(pr.ta * pr.tb, ranges), dim3(256), Tile<WA, WA>::kBytes, st>>>(pr, out, ldo, slices, lda, first ? 0 : 1, scale);
+        const int ranges = std::min(sh.ranges, pr.per * (sizeof(T) == 4 ? kSegments : 1) / 2);
+        k<<<dim3(pr.ta * pr.tb, ranges), dim3(256), Tile<WA, WA, RING, sizeof(T) == 4>::kBytes, st>>>(pr, out, ldo, slices, lda, first ? 0 : 1, scale);
     });
     if (err != JORGE_OK) return err;
     if (slices && last)
@@ -645,32 +694,31 @@ template <typename T>
 jorge_status backward(const jorge_loss_shape& s, const Plan& p, const Work& w, const float* grad, int32_t kind, const void* hidden,
                       const void* weight, const LossRows& rows, const float* lse, const float* total, void* dhidden,
                       void* dweight, hipStream_t st) {
-    const bool split = p.terms > 1;
     const Scale scale{kind == JORGE_LOSS_ROWS ? nullptr : grad, kind == JORGE_LOSS_MEAN ? total + 1 : nullptr};
     const float* const row_grad = kind == JORGE_LOSS_ROWS ? grad : nullptr;
-    if (!p.direct_x) pack<T>(hidden, s.ldh, s.tokens, s.cols, w.x, p.kd, st);
-    if (dweight) transpose<T>(hidden, s.ldh, s.tokens, s.cols, w.xt, p.kn, &rows, st);
-    const Operand x = operand_x<T>(s, p, w, hidden);
+    const Operand x = operand_x(s, p, w, hidden);
     const Operand xt{w.xt, p.kn, s.cols * p.kn, s.cols};
     jorge_status err = JORGE_OK;
     for (int64_t v0 = 0; v0 < s.vocab; v0 += p.piece) {
         const int64_t n = std::min(p.piece, s.vocab - v0), ldz = round_up(n, kPadK);
-        const Product pr = product_of(p.logits, operand_w<T>(s, p, w, weight, v0, n, st), x, p.kd, split);
+        const T* const from = (const T*)weight + v0 * s.ldw;
+        copy<T>(v0 ? Copies{} : copies_of(hidden, s.ldh, s.tokens, s.cols, w.x, p.kd, dweight ? w.xt : nullptr, p.kn, &rows),
+                copies_of(from, s.ldw, n, s.cols, w.w, p.kd, dhidden ? w.wt : nullptr, ldz, nullptr), st);
+        const Product pr = product_of(p.logits, operand_w(s, p, w, from, n), x, p.kd);
         const DzOut dz{w.dz, w.dzt, ldz, p.kn, s.tokens * ldz, n * p.kn};
-        with_tile(p.logits.large, [&](auto W) {
-            constexpr int WA = decltype(W)::value;
-            const auto k = loss_dz_kernel<WA, WA, sizeof(T) == 4 ? kTerms : 1>;
-            if ((err = allow_lds(k, Tile<WA, WA>::kBytes)) != JORGE_OK) return;
-            k<<<dim3(pr.ta * pr.tb), dim3(256), Tile<WA, WA>::kBytes, st>>>(pr, rows, lse, row_grad, (float)s.label_smoothing, v0, dz);
+        with_tile(p.logits, [&](auto W, auto R) {
+            constexpr int WA = decltype(W)::value, RING = decltype(R)::value;
+            const auto k = loss_dz_kernel<WA, WA, RING, sizeof(T) == 4>;
+            if ((err = allow_lds(k, Tile<WA, WA, RING, sizeof(T) == 4>::kBytes)) != JORGE_OK) return;
+            k<<<dim3(pr.ta * pr.tb), dim3(256), Tile<WA, WA, RING, sizeof(T) == 4>::kBytes, st>>>(pr, rows, lse, row_grad, (float)s.label_smoothing, v0, dz);
         });
         if (err != JORGE_OK) return err;
         if (dhidden) {
-            transpose<T>((const T*)weight + v0 * s.ldw, s.ldw, n, s.cols, w.wt, ldz, nullptr, st);
-            const Product g = product_of(p.dh, {w.wt, ldz, s.cols * ldz, s.cols}, {w.dz, ldz, dz.plane_z, s.tokens}, ldz, split);
+            const Product g = product_of(p.dh, {w.wt, ldz, s.cols * ldz, s.cols}, {w.dz, ldz, dz.plane_z, s.tokens}, ldz);
             if ((err = gradient(p.dh, g, (T*)dhidden, s.ldh, s.cols, w.dh, v0 == 0, v0 + n == s.vocab, scale, st)) != JORGE_OK) return err;
         }
         if (dweight) {
-            const Product g = product_of(p.dw, xt, {w.dzt, p.kn, dz.plane_t, n}, p.kn, split);
+            const Product g = product_of(p.dw, xt, {w.dzt, p.kn, dz.plane_t, n}, p.kn);
             if ((err = gradient(p.dw, g, (T*)dweight + v0 * s.ldw, s.ldw, s.cols, w.dw, true, true, scale, st)) != JORGE_OK) return err;
         }
     }
@@ -689,6 +737,7 @@ jorge_status check(const jorge_loss_shape* s) {
     if (s->tokens > JORGE_LOSS_MAX_TOKENS) return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: tokens above JORGE_LOSS_MAX_TOKENS");
     if (s->vocab > JORGE_LOSS_MAX_VOCAB) return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: vocab above JORGE_LOSS_MAX_VOCAB");
     if (s->cols > JORGE_LOSS_MAX_COLS) return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: cols above JORGE_LOSS_MAX_COLS");
+    if (ceil_div(s->tokens, 64) * ceil_div(s->cols, 64) > 1 << 23) return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: tokens * cols above 2^35");
     if (s->ldh < s->cols || s->ldw < s->cols) return bad("cross entropy: a row stride is below cols");
     if (s->ldh > (int64_t)1 << 22 || s->ldw > (int64_t)1 << 22) return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: a row stride above 2^22");
     if (!(s->label_smoothing >= 0.0 && s->label_smoothing <= 1.0)) return bad("cross entropy: label_smoothing must be in [0, 1]");

@@ -8,8 +8,8 @@
 // takes 16 KB from LDS per 64 MFMAs, the least per flop that the registers allow: LDS would bound
 // waves of 128 x 64 (two per SIMD) at 9/8 of the MFMAs' time, these at 3/4.
 //
-// K goes by stages of 32 through a ring of kRing buffers in LDS. Each stage is written by
-// direct-to-LDS loads, started kRing - 1 stages ahead; nothing passes through registers. A wave
+// K goes by stages of 32 through a ring of RING buffers in LDS. Each stage is written by
+// direct-to-LDS loads, started RING - 1 stages ahead; nothing passes through registers. A wave
 // reads the next stage's fragments while the MFMAs of the current one run.
 //
 // Which row of the tile goes where. An MFMA leaves lane l with rows 4 (l / 16) + r (r = 0 .. 3) and
@@ -30,7 +30,6 @@
 namespace jorge_lm {
 
 constexpr int kStageK = 32;
-constexpr int kRing = 4;
 
 // One operand of a product: `rows` rows of K elements at a stride of ld elements. Rows past the end are
 // not read: the last one is, in their place. `plane`: elements between the terms of a split operand.
@@ -42,16 +41,18 @@ struct Operand {
 
 // The order in which the terms of split operands are multiplied: the six products down to 2^-16 of the
 // whole, smallest first (term t of A with term u of B).
+constexpr int kSegments = 6;
 __device__ __forceinline__ int term_a(int seg) { return (0x001012 >> (4 * seg)) & 3; }
 __device__ __forceinline__ int term_b(int seg) { return (0x010210 >> (4 * seg)) & 3; }
 
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) const void global_void;
 
-__device__ __forceinline__ int swizzle(int rho) { return ((rho >> 1) & 3) ^ ((rho >> 3) & 1); }
+__device__ __forceinline__ int swizzle(int rho) { return -(rho >> 2) & 3; }
 
-template <int WA, int WB>
+template <int WA, int WB, int RING, bool SPLIT>
 struct Tile {
+    static constexpr int kRing = RING;
     static constexpr int kA = 32 * WA, kB = 32 * WB;
     static constexpr int kStageBytes = (kA + kB) * kStageK * 2;
     static constexpr int kBytes = kRing * kStageBytes;
@@ -73,7 +74,7 @@ struct Tile {
     // Stages [s0, s1) of the product of rows a0 .. of A and b0 .. of B; each segment (pair of terms) has
     // `per` stages. s0, s1 and per are even, s1 > s0. lds: kBytes.
     __device__ __forceinline__ void multiply(const Operand& A, const Operand& B, int64_t a0, int64_t b0, int s0, int s1,
-                                             int per, bool split, char* lds) {
+                                             int per, char* lds) {
         const int lane = threadIdx.x & 63;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         // Where this lane's loads start: block n of the operand (n = wave * kLoads + v), row rho of it.
@@ -96,45 +97,44 @@ struct Tile {
         const unsigned lenA = (unsigned)(limA * A.ld + per * kStageK) * 2u, lenB = (unsigned)(limB * B.ld + per * kStageK) * 2u;
         const bf16* const baseA = A.p + a0 * A.ld;
         const bf16* const baseB = B.p + b0 * B.ld;
+        // The loads of one stage after the other. What it takes to go on to the next stage is spread over the MFMAs
+        // of a step (the scalar unit runs beside them, but not beside a wait).
         struct Loader {
-            const bf16 *baseA, *baseB;
-            int64_t planeA, planeB;  // 0 where the operands are not split
             const unsigned *offA, *offB;
-            char* lds;
+            int64_t planeA, planeB;
+            const bf16 *pa, *pb;     // of the stage's terms
             unsigned lenA, lenB;
-            int wave, per, seg, in, left, k;
-            __amdgpu_buffer_rsrc_t ra, rb;
-            char* to;
-            __device__ __forceinline__ void begin(int slot) {
-                ra = resource(baseA + term_a(seg) * planeA, lenA);
-                rb = resource(baseB + term_b(seg) * planeB, lenB);
-                to = lds + slot * kStageBytes;
-                k = in * (kStageK * 2);
-            }
+            int per, seg, in, left, k, wave;
+            char *lds, *to;
             __device__ __forceinline__ void one(int v) {
                 if (v < kLoadsA)
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void*)(to + (wave * kLoadsA + v) * 1024), 16, offA[v], k, 0, 0);
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(resource(pa, lenA), (lds_void*)(to + v * 1024), 16, offA[v], k, 0, 0);
                 else
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void*)(to + (2 * WA + wave * kLoadsB + v - kLoadsA) * 1024), 16,
-                                                             offB[v - kLoadsA], k, 0, 0);
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(resource(pb, lenB), (lds_void*)(to + (2 * WA - wave * (kLoadsA - kLoadsB) + v - kLoadsA) * 1024),
+                                                             16, offB[v - kLoadsA], k, 0, 0);
             }
+            __device__ __forceinline__ void slot(int n) { to = lds + n * kStageBytes + wave * kLoadsA * 1024; }
             // Where no stage is left the last one is loaded again and not used: every wave always has the same
-            // number of loads in flight. Selects, so that the loop's body stays one block.
-            __device__ __forceinline__ void end() {
+            // number of loads in flight. Arithmetic, so that the loop's body stays one block.
+            __device__ __forceinline__ void next() {
                 --left;
-                const int on = left > 0 ? 1 : 0, wrap = in + on == per ? 1 : 0;
-                in = wrap ? 0 : in + on;
-                seg += wrap;
-            }
-            __device__ __forceinline__ void all(int slot) {
-                begin(slot);
-#pragma unroll
-                for (int v = 0; v < kLoads; ++v) one(v);
-                end();
+                const int on = left > 0 ? 1 : 0;
+                if constexpr (SPLIT) {
+                    const int wrap = in + on == per ? 1 : 0;
+                    pa += (int64_t)((term_a(seg + 1) - term_a(seg)) * wrap) * planeA;
+                    pb += (int64_t)((term_b(seg + 1) - term_b(seg)) * wrap) * planeB;
+                    in = (in + on) * (1 - wrap);
+                    seg += wrap;
+                    k = in * (kStageK * 2);
+                } else {
+                    k += on * (kStageK * 2);
+                }
             }
         };
-        const int seg0 = split ? s0 / per : 0;
-        Loader load{baseA, baseB, split ? A.plane : 0, split ? B.plane : 0, offA, offB, lds, lenA, lenB, wave, per, seg0, s0 - seg0 * per, s1 - s0, 0};
+        const int seg0 = SPLIT ? s0 / per : 0, in0 = s0 - seg0 * per;
+        Loader load{offA, offB, A.plane, B.plane, baseA + (SPLIT ? term_a(seg0) * A.plane : 0),
+                    baseB + (SPLIT ? term_b(seg0) * B.plane : 0), lenA, lenB, per, seg0, in0, s1 - s0,
+                    in0 * (kStageK * 2), wave, lds, lds};
         const int frag = (lane & 15) * 64 + (((lane >> 4) ^ swizzle(lane & 15)) * 16);
         const int fragA = frag + (wave >> 1) * WA * 1024, fragB = frag + (2 * WA + (wave & 1) * WB) * 1024;
         bf16x8 fa[2][WA], fb[2][WB];
@@ -149,7 +149,12 @@ struct Tile {
 #pragma unroll
             for (int j = 0; j < WB; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int r = 0; r < kRing - 1; ++r) load.all(r);
+        for (int r = 0; r < kRing - 1; ++r) {
+            load.slot(r);
+#pragma unroll
+            for (int v = 0; v < kLoads; ++v) load.one(v);
+            load.next();
+        }
         wait_loads<(kRing - 2) * kLoads>();
         __builtin_amdgcn_s_barrier();
 #pragma unroll
@@ -160,10 +165,10 @@ struct Tile {
             // new loads write was read by all before their last barrier but one.
             wait_loads<(kRing - 3) * kLoads>();
             __builtin_amdgcn_s_barrier();
-            const int ahead = (slot + 1) & (kRing - 1);
-            load.begin((slot + kRing - 1) & (kRing - 1));
+            const int ahead = slot + 1 == kRing ? 0 : slot + 1;
+            load.slot(slot == 0 ? kRing - 1 : slot - 1);
             // In this order: the fragment reads by twos in the first half, so that the next step need not wait for
-            // them, the loads in the second.
+            // them, a load in every second group, and after the last load the way to the next stage.
             constexpr int G = WA + WB, PER = WA * WB / G;
 #pragma unroll
             for (int g = 0; g < G; ++g) {
@@ -171,28 +176,24 @@ struct Tile {
                 if (g < G / 2) {
                     read(ahead, set ^ 1, 2 * g);
                     read(ahead, set ^ 1, 2 * g + 1);
-                } else {
-                    load.one(g - G / 2);
                 }
+                if (g % 2 == 0) load.one(g / 2);
+                if (g == G - 1) load.next();
 #pragma unroll
                 for (int m = g * PER; m < (g + 1) * PER; ++m) mfma(acc[m / WB][m % WB], fa[set][m / WB], fb[set][m % WB]);
             }
             __builtin_amdgcn_sched_barrier(0);
-            load.end();
             slot = ahead;
         };
         for (int s = s0; s < s1; s += 2) {
             step(0);
             step(1);
+            // After the last MFMA of all, the wait states that reading its result takes. They stand inside the loop,
+            // ahead of any place where the compiler, which does not see MFMAs in the asm, may copy an accumulator.
+            asm volatile("s_cmp_lt_i32 %0, %1\n\ts_cbranch_scc1 1f\n\ts_nop 15\n\ts_nop 15\n1:" ::"s"(s + 2), "s"(s1) : "scc");
         }
         wait_loads<0>();
         __builtin_amdgcn_s_barrier();  // the ring is free for the epilogue
-        // The last MFMAs have written their results (the compiler does not see them in the asm).
-        asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
-#pragma unroll
-        for (int i = 0; i < WA; ++i)
-#pragma unroll
-            for (int j = 0; j < WB; ++j) asm volatile("" : "+a"(acc[i][j]));
     }
 
     // In place, in accumulator registers: left to the compiler the 64 accumulators wander between the two halves
