@@ -332,11 +332,15 @@ __global__ __launch_bounds__(kJoinWaves * 64) void embed_join_kernel(SumArgs a, 
         const int64_t stride = 2 * (int64_t)a.ldp;
         if (wave == 0) sum = *reinterpret_cast<const f32x4*>(p + part * stride + (first_run ? 0 : a.ldp));
         int64_t k = part + 1 + wave;
-        for (; k + 7 * kJoinWaves <= last; k += 8 * kJoinWaves) {
-            f32x4 v[8];
+        for (; k + 15 * kJoinWaves <= last; k += 16 * kJoinWaves) {
+            f32x4 v[16];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = *reinterpret_cast<const f32x4*>(p + (k + u * kJoinWaves) * stride);
-            sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+            for (int u = 0; u < 16; ++u) v[u] = *reinterpret_cast<const f32x4*>(p + (k + u * kJoinWaves) * stride);
+#pragma unroll
+            for (int half = 8; half > 0; half >>= 1)
+#pragma unroll
+                for (int u = 0; u < half; ++u) v[u] += v[u + half];
+            sum += v[0];
         }
         for (; k <= last; k += kJoinWaves) sum += *reinterpret_cast<const f32x4*>(p + k * stride);
     }

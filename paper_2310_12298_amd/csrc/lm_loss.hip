@@ -459,24 +459,29 @@ struct Shape {
     int ranges;
     bool deep;    // a tile has its CU to itself: a ring of eight stages, else of four
 };
-// Large tiles run a product at twice the small ones' rate (8192 x 8192 x 2048: 354 us against 474, 4096 x 4096 x 8192:
-// 238 against 395), where there are enough of them for the CUs. A stage of a 64 x 64 tile takes a third of the time
-// of a 128 x 128 one's, which the LDS bounds: they serve where those would leave CUs idle.
+// The tile and the number of ranges that a model of the launch puts first: rounds of workgroups over the CUs, each the
+// stages of its range and a fixed part (the ring's first loads, the epilogue), and adding the ranges' sums up. A stage
+// takes 0.88, 0.36 and 0.15 us (tiles of 256, 128 and 64, all CUs busy; per flop the large one is 1.6 and 2.7 times as
+// fast: 4096 x 4096 x 8192 takes 238 us in large tiles and 395 in middle ones), the fixed part 12, 6 and 4 us. The small
+// ones win where the large ones leave CUs idle or are mostly padding: 64 tokens, 8192 words of 512 in fp32 30 -> 17 us
+// for the logits.
 Shape shape_of(int64_t a, int64_t b, int64_t stages, bool may_cut) {
-    const int64_t big = ceil_div(a, 256) * ceil_div(b, 256), small = ceil_div(a, 128) * ceil_div(b, 128);
-    if (big >= kCus / 2) return {8, 1, false};
-    if (!may_cut) return small > kCus / 2 ? Shape{4, 1, small <= kCus} : Shape{2, 1, true};
-    // Cut along K until the tiles fill the CUs; a range keeps at least 16 stages.
-    const auto cut = [&](int64_t tiles, int64_t want) {
-        const int64_t most = stages / 16;
-        return std::max<int64_t>(1, std::min(want / tiles, most));
-    };
-    const int64_t rb = cut(big, kCus);
-    if (big * rb >= kCus / 2) return {8, (int)rb, false};
-    const int64_t rs = cut(small, kCus);
-    if (small * rs > kCus / 2) return {4, (int)rs, small * rs <= kCus};
-    const int64_t least = ceil_div(a, 64) * ceil_div(b, 64);
-    return {2, (int)cut(least, kCus), true};
+    constexpr double kStage[3] = {0.88, 0.36, 0.15}, kFixed[3] = {12.0, 6.0, 4.0};
+    Shape best{};
+    double least = 1e300;
+    for (int t = 0; t < 3; ++t) {
+        const int64_t blocks = 8 >> t, tiles = ceil_div(a, 32 * blocks) * ceil_div(b, 32 * blocks);
+        // A range keeps at least eight stages.
+        for (int64_t r = 1; r == 1 || (may_cut && r <= stages / 8 && tiles * r <= 2 * kCus); r *= 2) {
+            double us = (double)ceil_div(tiles * r, kCus) * ((double)ceil_div(stages, r) * kStage[t] + kFixed[t]);
+            if (r > 1) us += 4.0 + (double)(r * a * b) * 8.0 / 4.5e6;
+            if (us < least) {
+                least = us;
+                best = {(int)blocks, (int)r, tiles * r <= kCus};
+            }
+        }
+    }
+    return best;
 }
 
 struct Plan {
@@ -678,8 +683,8 @@ jorge_status gradient(const Shape& sh, const Product& pr, T* out, int64_t ldo, i
         constexpr int WA = decltype(W)::value, RING = decltype(R)::value;
         const auto k = loss_grad_kernel<WA, WA, RING, sizeof(T) == 4, T>;
         if ((err = allow_lds(k, Tile<WA, WA, RING, sizeof(T) == 4>::kBytes)) != JORGE_OK) return;
-        // The first piece of a sum is the longest and has at least 16 stages for each range; a short last one adds to
-        // fewer slices.
+        // The first piece of a sum is the longest and has at least eight stages for each range; a short last one may
+        // add to fewer slices.
         const int ranges = std::min(sh.ranges, pr.per * (sizeof(T) == 4 ? kSegments : 1) / 2);
         k<<<dim3(pr.ta * pr.tb, ranges), dim3(256), Tile<WA, WA, RING, sizeof(T) == 4>::kBytes, st>>>(pr, out, ldo, slices, lda, first ? 0 : 1, scale);
     });

@@ -81,10 +81,10 @@ def _check(lib, status):
         raise JorgeError(status, f"{lib.jorge_status_string(status).decode()} ({lib.jorge_lm_last_error().decode()})")
 
 
-def _cuda(t, what, dtypes=None):
+def _cuda(t, what, dtypes=DTYPES):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{what}: a CUDA tensor is needed")
-    if t.dtype not in (DTYPES if dtypes is None else dtypes):
+    if t.dtype not in dtypes:
         raise ValueError(f"{what}: unsupported type {t.dtype}")
     if t.get_device() != torch.cuda.current_device():
         raise ValueError(f"{what}: on device {t.get_device()}, not the current one")
@@ -94,10 +94,15 @@ def _cuda(t, what, dtypes=None):
 def _matrix(t, what):
     """A matrix with dense rows that holds t's values, without a copy where t's layout allows it."""
     _cuda(t, what)
-    if t.dim() == 0:
+    dims = t.dim()
+    if dims == 2:
+        if t.is_contiguous():
+            return t
+        m = t
+    elif dims == 0:
         raise ValueError(f"{what}: at least one dimension is needed")
-    m = t if t.dim() == 2 else t.reshape(-1, t.shape[-1]) if t.numel() else t.reshape(
-        t.shape[:-1].numel(), t.shape[-1])
+    else:
+        m = t.reshape(t.shape[:-1].numel(), t.shape[-1])
     if (m.shape[1] > 1 and m.stride(1) != 1) or (m.shape[0] > 1 and m.stride(0) < m.shape[1]):
         m = m.contiguous()
     return m
@@ -141,13 +146,13 @@ def layer_norm_forward(x, weight=None, bias=None, eps=1e-5):
         raise ValueError("weight and bias must have one type")
     w = params[0] if weight is not None else None
     b = params[-1] if bias is not None else None
-    y = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-    stats = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind(0)
     _check(lib, lib.jorge_layernorm_forward(m.data_ptr(), _ld(m), DTYPES[x.dtype], _ptr(w), _ptr(b),
                                             DTYPES[params[0].dtype] if params else 0, y.data_ptr(), cols,
-                                            stats[0].data_ptr(), stats[1].data_ptr(), rows, cols, float(eps),
+                                            mean.data_ptr(), rstd.data_ptr(), rows, cols, float(eps),
                                             _current_stream()))
-    return y.view(x.shape), stats[0], stats[1]
+    return y, mean, rstd
 
 
 def layer_norm_backward(dy, x, mean, rstd, weight=None, affine=True):
@@ -163,18 +168,17 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, affine=True):
             raise ValueError(f"{what}: as layer_norm_forward returned it")
     w = None if weight is None else _vector(weight, cols, "weight")
     ptype = torch.float32 if w is None else w.dtype
-    dx = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-    sums = torch.empty((2, cols), dtype=ptype, device=x.device) if affine else None
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    dw, db = torch.empty((2, cols), dtype=ptype, device=x.device).unbind(0) if affine else (None, None)
     ws, n = None, _I64(0)
     if affine:
         _check(lib, lib.jorge_layernorm_workspace(rows, cols, ctypes.byref(n)))
         ws = _workspace(n.value)
     _check(lib, lib.jorge_layernorm_backward(d.data_ptr(), _ld(d), m.data_ptr(), _ld(m), DTYPES[x.dtype],
                                              mean.data_ptr(), rstd.data_ptr(), _ptr(w), DTYPES[ptype], dx.data_ptr(),
-                                             cols, sums[0].data_ptr() if affine else None,
-                                             sums[1].data_ptr() if affine else None, rows, cols, _ptr(ws), n.value,
+                                             cols, _ptr(dw), _ptr(db), rows, cols, _ptr(ws), n.value,
                                              _current_stream()))
-    return dx.view(x.shape), sums[0] if affine else None, sums[1] if affine else None
+    return dx, dw, db
 
 
 class _LayerNorm(torch.autograd.Function):
@@ -355,6 +359,7 @@ class AdamW:
             if not _dense(_cuda(p, f"parameter {i}")):
                 raise ValueError(f"parameter {i}: a dense tensor is needed")
         self._numel = [p.numel() for p in self.params]
+        self._layout = [(p.dtype, p.shape, p.stride(), p.get_device()) for p in self.params]
         self.blocks = np.cumsum([0] + [-(-n // BLOCK) for n in self._numel])
         self._tensors = (AdamWTensor * max(1, len(self.params)))()
         self._table = np.frombuffer(self._tensors, dtype=np.dtype(AdamWTensor))[:len(self.params)]
@@ -381,17 +386,17 @@ class AdamW:
         if len(grads) != len(self.params):
             raise ValueError(f"grads: expected {len(self.params)} tensors, got {len(grads)}")
         keep, ptrs, numel = [], [], self._numel
-        for i, (g, p) in enumerate(zip(grads, self.params)):
+        for i, (g, (dtype, shape, stride, device)) in enumerate(zip(grads, self._layout)):
             if g is None:
                 if numel is self._numel:
                     numel = list(numel)
                 numel[i] = 0
                 ptrs.append(0)
                 continue
-            if g.dtype is not p.dtype or g.shape != p.shape or g.device != p.device:
+            if g.dtype is not dtype or g.shape != shape or g.get_device() != device:
                 raise ValueError("grads: each must have its parameter's shape, type and device")
-            if g.stride() != p.stride():
-                g = torch.empty_strided(p.shape, p.stride(), dtype=p.dtype, device=p.device).copy_(g)
+            if g.stride() != stride:
+                g = torch.empty_strided(shape, stride, dtype=dtype, device=g.device).copy_(g)
                 keep.append(g)
             ptrs.append(g.data_ptr())
         self._table["grad"] = ptrs
@@ -403,6 +408,9 @@ class AdamW:
         are). max_norm > 0 scales all gradients to that global norm if theirs is larger; clip: the factor
         itself, one fp32 number on the device (of another gradient_norm call)."""
         keep = self._gradients([p.grad for p in self.params] if grads is None else grads)
+        for p, (dtype, shape, stride, device) in zip(self.params, self._layout):
+            if p.dtype is not dtype or p.get_device() != device or p.shape != shape or p.stride() != stride:
+                raise ValueError("a parameter's type, device, shape or layout has changed since it was handed over")
         self._table["param"] = [p.data_ptr() for p in self.params]
         if max_norm and clip is not None:
             raise ValueError("max_norm or clip, not both")
