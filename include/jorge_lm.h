@@ -111,7 +111,7 @@ jorge_status jorge_embedding_backward(const void* dout, int64_t lddo, const int6
  * takes no part in the sums and gradients (its lse_i is written). */
 
 /* Largest tokens, vocab and cols. */
-#define JORGE_LOSS_MAX_TOKENS (1 << 22)
+#define JORGE_LOSS_MAX_TOKENS (1 << 21)
 #define JORGE_LOSS_MAX_VOCAB  (1 << 22)
 #define JORGE_LOSS_MAX_COLS   32768
 

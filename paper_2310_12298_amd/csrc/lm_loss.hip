@@ -32,20 +32,19 @@ namespace jorge_lm {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896341f;
-constexpr int kTerms = 3;      // of a split fp32 operand
 constexpr int kPadK = 64;      // K of every product is a multiple of two stages
 
 // ---------------------------------------------------------------- operands
 // Copies of a matrix that the products read: `flat`, its rows padded with zeros to ldf (a multiple of 64), and `turned`,
 // its transpose, padded to ldt (a multiple of 64) with zeros, which also stand in for the rows that `targets` (if
 // given) has no target for: what such a row holds must not reach a sum that it has no part in. Either may be null;
-// term t of the elements goes to plane t.
+// the terms of a row follow one another.
 struct Copies {
     const void* src;
     int64_t ld, rows;
     int cols, tiles_c;       // 64 x 64 tiles along the columns
     bf16 *flat, *turned;
-    int64_t ldf, plane_f, ldt, plane_t;
+    int64_t padded_f, padded_t;  // of one term of a row
     const int64_t* targets;
     int64_t vocab, ignore;
     int64_t tiles;           // of the whole job
@@ -102,18 +101,18 @@ __global__ __launch_bounds__(256) void copies_kernel(CopyJobs jobs) {
         if (j.turned)
 #pragma unroll
             for (int e = 0; e < 8; ++e) tile[y][part + e] = live ? (T)f[e] : (T)0.0f;
-        if (j.flat && r < j.rows) store_terms<TERMS>(j.flat + r * j.ldf + c, j.plane_f, f);
+        if (j.flat && r < j.rows) store_terms<TERMS>(j.flat + r * TERMS * j.padded_f + c, j.padded_f, f);
     }
     if (!j.turned) return;
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const int c = (threadIdx.x >> 3) + 32 * k;
-        if (c0 + c >= j.cols || r0 + part >= j.ldt) continue;
+        if (c0 + c >= j.cols) continue;
         float f[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] = (float)tile[part + e][c];
-        store_terms<TERMS>(j.turned + (int64_t)(c0 + c) * j.ldt + r0 + part, j.plane_t, f);
+        store_terms<TERMS>(j.turned + (int64_t)(c0 + c) * TERMS * j.padded_t + r0 + part, j.padded_t, f);
     }
 }
 
@@ -303,11 +302,11 @@ __global__ __launch_bounds__(1024) void loss_total_kernel(const float* __restric
 
 // ---------------------------------------------------------------- backward
 struct DzOut {
-    bf16 *dz, *dzt;            // [terms][tokens][ldz], [terms][words][ldt]
-    int64_t ldz, ldt, plane_z, plane_t;
+    bf16 *dz, *dzt;            // [tokens][terms][words], [words][terms][tokens]
+    int64_t words, tokens;     // padded to multiples of 64
 };
 
-// dz of a piece: words word0 .. word0 + A.rows; padding up to ldz words and ldt tokens is written as 0.
+// dz of a piece: words word0 .. word0 + A.rows; the padding of both copies is written as 0.
 template <int WA, int WB, int RING, bool SPLIT>
 __global__ __launch_bounds__(256, 1) void loss_dz_kernel(Product p, LossRows rows, const float* __restrict__ lse,
                                                          const float* __restrict__ row_grad, float smoothing, int64_t word0,
@@ -339,8 +338,9 @@ __global__ __launch_bounds__(256, 1) void loss_dz_kernel(Product p, LossRows row
     }
 #pragma unroll
     for (int term = 0; term < (SPLIT ? kTerms : 1); ++term) {
-        bf16* const dz = out.dz + term * out.plane_z;
-        bf16* const dzt = out.dzt + term * out.plane_t;
+        constexpr int terms = SPLIT ? kTerms : 1;
+        bf16* const dz = out.dz + term * out.words + a0;
+        bf16* const dzt = out.dzt + term * out.tokens + b0;
 #pragma unroll
         for (int j = 0; j < WB; ++j)
             if (b0 + j < rows.tokens)
@@ -349,9 +349,10 @@ __global__ __launch_bounds__(256, 1) void loss_dz_kernel(Product p, LossRows row
                     bf16x8 o;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) o[e] = (bf16)t.acc[i + e / 4][j][e & 3];
-                    if (a0 + 4 * i < out.ldz) *reinterpret_cast<bf16x8*>(dz + (b0 + j) * out.ldz + a0 + 4 * i) = o;
+                    if (a0 + 4 * i < out.words)
+                        *reinterpret_cast<bf16x8*>(dz + (b0 + j) * terms * out.words + 4 * i) = o;
                 }
-        if (b0 < out.ldt)
+        if (b0 < out.tokens)
 #pragma unroll
             for (int i = 0; i < WA; ++i)
 #pragma unroll
@@ -361,7 +362,7 @@ __global__ __launch_bounds__(256, 1) void loss_dz_kernel(Product p, LossRows row
                         V o;
 #pragma unroll
                         for (int j = 0; j < WB; ++j) o[j] = (bf16)t.acc[i][j][r];
-                        *reinterpret_cast<V*>(dzt + (a0 + 4 * i + r) * out.ldt + b0) = o;
+                        *reinterpret_cast<V*>(dzt + (a0 + 4 * i + r) * terms * out.tokens) = o;
                     }
         if constexpr (SPLIT)
 #pragma unroll
@@ -615,10 +616,8 @@ Copies copies_of(const void* src, int64_t ld, int64_t rows, int64_t cols, bf16* 
     c.tiles_c = (int)(kd / 64);
     c.flat = flat;
     c.turned = turned;
-    c.ldf = kd;
-    c.plane_f = rows * kd;
-    c.ldt = padded;
-    c.plane_t = cols * padded;
+    c.padded_f = kd;
+    c.padded_t = padded;
     if (targets) {
         c.targets = targets->targets;
         c.vocab = targets->vocab;
@@ -636,11 +635,11 @@ void copy(const Copies& a, const Copies& b, hipStream_t s) {
 // hidden, and a piece of n words of weight from `from` on, as operands.
 Operand operand_x(const jorge_loss_shape& s, const Plan& p, const Work& w, const void* hidden) {
     if (p.direct_x) return {(const bf16*)hidden, s.ldh, 0, s.tokens};
-    return {w.x, p.kd, s.tokens * p.kd, s.tokens};
+    return {w.x, p.terms * p.kd, p.kd, s.tokens};
 }
 Operand operand_w(const jorge_loss_shape& s, const Plan& p, const Work& w, const void* from, int64_t n) {
     if (p.direct_w) return {(const bf16*)from, s.ldw, 0, n};
-    return {w.w, p.kd, n * p.kd, n};
+    return {w.w, p.terms * p.kd, p.kd, n};
 }
 
 template <typename T>
@@ -702,7 +701,7 @@ jorge_status backward(const jorge_loss_shape& s, const Plan& p, const Work& w, c
     const Scale scale{kind == JORGE_LOSS_ROWS ? nullptr : grad, kind == JORGE_LOSS_MEAN ? total + 1 : nullptr};
     const float* const row_grad = kind == JORGE_LOSS_ROWS ? grad : nullptr;
     const Operand x = operand_x(s, p, w, hidden);
-    const Operand xt{w.xt, p.kn, s.cols * p.kn, s.cols};
+    const Operand xt{w.xt, p.terms * p.kn, p.kn, s.cols};
     jorge_status err = JORGE_OK;
     for (int64_t v0 = 0; v0 < s.vocab; v0 += p.piece) {
         const int64_t n = std::min(p.piece, s.vocab - v0), ldz = round_up(n, kPadK);
@@ -710,7 +709,7 @@ jorge_status backward(const jorge_loss_shape& s, const Plan& p, const Work& w, c
         copy<T>(v0 ? Copies{} : copies_of(hidden, s.ldh, s.tokens, s.cols, w.x, p.kd, dweight ? w.xt : nullptr, p.kn, &rows),
                 copies_of(from, s.ldw, n, s.cols, w.w, p.kd, dhidden ? w.wt : nullptr, ldz, nullptr), st);
         const Product pr = product_of(p.logits, operand_w(s, p, w, from, n), x, p.kd);
-        const DzOut dz{w.dz, w.dzt, ldz, p.kn, s.tokens * ldz, n * p.kn};
+        const DzOut dz{w.dz, w.dzt, ldz, p.kn};
         with_tile(p.logits, [&](auto W, auto R) {
             constexpr int WA = decltype(W)::value, RING = decltype(R)::value;
             const auto k = loss_dz_kernel<WA, WA, RING, sizeof(T) == 4>;
@@ -719,11 +718,11 @@ jorge_status backward(const jorge_loss_shape& s, const Plan& p, const Work& w, c
         });
         if (err != JORGE_OK) return err;
         if (dhidden) {
-            const Product g = product_of(p.dh, {w.wt, ldz, s.cols * ldz, s.cols}, {w.dz, ldz, dz.plane_z, s.tokens}, ldz);
+            const Product g = product_of(p.dh, {w.wt, p.terms * ldz, ldz, s.cols}, {w.dz, p.terms * ldz, ldz, s.tokens}, ldz);
             if ((err = gradient(p.dh, g, (T*)dhidden, s.ldh, s.cols, w.dh, v0 == 0, v0 + n == s.vocab, scale, st)) != JORGE_OK) return err;
         }
         if (dweight) {
-            const Product g = product_of(p.dw, xt, {w.dzt, p.kn, dz.plane_t, n}, p.kn);
+            const Product g = product_of(p.dw, xt, {w.dzt, p.terms * p.kn, p.kn, n}, p.kn);
             if ((err = gradient(p.dw, g, (T*)dweight + v0 * s.ldw, s.ldw, s.cols, w.dw, true, true, scale, st)) != JORGE_OK) return err;
         }
     }

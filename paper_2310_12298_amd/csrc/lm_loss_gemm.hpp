@@ -32,7 +32,7 @@ namespace jorge_lm {
 constexpr int kStageK = 32;
 
 // One operand of a product: `rows` rows of K elements at a stride of ld elements. Rows past the end are
-// not read: the last one is, in their place. `plane`: elements between the terms of a split operand.
+// not read: the last one is, in their place. `plane`: elements between a row's terms, of a split operand.
 struct Operand {
     const bf16* p;
     int64_t ld, plane;
@@ -41,7 +41,7 @@ struct Operand {
 
 // The order in which the terms of split operands are multiplied: the six products down to 2^-16 of the
 // whole, smallest first (term t of A with term u of B).
-constexpr int kSegments = 6;
+constexpr int kTerms = 3, kSegments = 6;
 __device__ __forceinline__ int term_a(int seg) { return (0x001012 >> (4 * seg)) & 3; }
 __device__ __forceinline__ int term_b(int seg) { return (0x010210 >> (4 * seg)) & 3; }
 
@@ -94,47 +94,48 @@ struct Tile {
             offB[v] = (unsigned)(row < limB ? row : limB) * (unsigned)B.ld * 2u + chunk * 16u;
         }
         // Bytes from the tile's first row to the end of its last one: what a load may reach.
-        const unsigned lenA = (unsigned)(limA * A.ld + per * kStageK) * 2u, lenB = (unsigned)(limB * B.ld + per * kStageK) * 2u;
-        const bf16* const baseA = A.p + a0 * A.ld;
-        const bf16* const baseB = B.p + b0 * B.ld;
+        const unsigned K = (unsigned)(per * kStageK), terms = SPLIT ? kTerms - 1 : 0;
+        const unsigned lenA = ((unsigned)limA * (unsigned)A.ld + terms * (unsigned)A.plane + K) * 2u;
+        const unsigned lenB = ((unsigned)limB * (unsigned)B.ld + terms * (unsigned)B.plane + K) * 2u;
         // The loads of one stage after the other. What it takes to go on to the next stage is spread over the MFMAs
         // of a step (the scalar unit runs beside them, but not beside a wait).
         struct Loader {
             const unsigned *offA, *offB;
-            int64_t planeA, planeB;
-            const bf16 *pa, *pb;     // of the stage's terms
-            unsigned lenA, lenB;
-            int per, seg, in, left, k, wave;
+            __amdgpu_buffer_rsrc_t ra, rb;
+            int planeA, planeB;      // bytes
+            int per, seg, in, left, kA, kB, wave;  // in: bytes into the segment
             char *lds, *to;
             __device__ __forceinline__ void one(int v) {
                 if (v < kLoadsA)
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(resource(pa, lenA), (lds_void*)(to + v * 1024), 16, offA[v], k, 0, 0);
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void*)(to + v * 1024), 16, offA[v], kA, 0, 0);
                 else
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(resource(pb, lenB), (lds_void*)(to + (2 * WA - wave * (kLoadsA - kLoadsB) + v - kLoadsA) * 1024),
-                                                             16, offB[v - kLoadsA], k, 0, 0);
+                    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                        rb, (lds_void*)(to + (2 * WA - wave * (kLoadsA - kLoadsB) + v - kLoadsA) * 1024), 16,
+                        offB[v - kLoadsA], kB, 0, 0);
             }
             __device__ __forceinline__ void slot(int n) { to = lds + n * kStageBytes + wave * kLoadsA * 1024; }
             // Where no stage is left the last one is loaded again and not used: every wave always has the same
             // number of loads in flight. Arithmetic, so that the loop's body stays one block.
             __device__ __forceinline__ void next() {
                 --left;
-                const int on = left > 0 ? 1 : 0;
+                const int on = left > 0 ? kStageK * 2 : 0;
                 if constexpr (SPLIT) {
-                    const int wrap = in + on == per ? 1 : 0;
-                    pa += (int64_t)((term_a(seg + 1) - term_a(seg)) * wrap) * planeA;
-                    pb += (int64_t)((term_b(seg + 1) - term_b(seg)) * wrap) * planeB;
-                    in = (in + on) * (1 - wrap);
-                    seg += wrap;
-                    k = in * (kStageK * 2);
+                    // Uniform, which the compiler does not see by itself.
+                    const int k = __builtin_amdgcn_readfirstlane(in + on), wrap = k == per * (kStageK * 2) ? 1 : 0;
+                    in = k - wrap * k;
+                    seg = __builtin_amdgcn_readfirstlane(seg + wrap);
+                    kA = term_a(seg) * planeA + in;
+                    kB = term_b(seg) * planeB + in;
                 } else {
-                    k += on * (kStageK * 2);
+                    kA += on;
+                    kB = kA;
                 }
             }
         };
-        const int seg0 = SPLIT ? s0 / per : 0, in0 = s0 - seg0 * per;
-        Loader load{offA, offB, A.plane, B.plane, baseA + (SPLIT ? term_a(seg0) * A.plane : 0),
-                    baseB + (SPLIT ? term_b(seg0) * B.plane : 0), lenA, lenB, per, seg0, in0, s1 - s0,
-                    in0 * (kStageK * 2), wave, lds, lds};
+        const int seg0 = SPLIT ? s0 / per : 0, in0 = (s0 - seg0 * per) * (kStageK * 2), pA = SPLIT ? (int)A.plane * 2 : 0,
+                  pB = SPLIT ? (int)B.plane * 2 : 0;
+        Loader load{offA, offB, resource(A.p + a0 * A.ld, lenA), resource(B.p + b0 * B.ld, lenB), pA, pB, per, seg0, in0, s1 - s0,
+                    term_a(seg0) * pA + in0, term_b(seg0) * pB + in0, wave, lds, lds};
         const int frag = (lane & 15) * 64 + (((lane >> 4) ^ swizzle(lane & 15)) * 16);
         const int fragA = frag + (wave >> 1) * WA * 1024, fragB = frag + (2 * WA + (wave & 1) * WB) * 1024;
         bf16x8 fa[2][WA], fb[2][WB];
