@@ -51,8 +51,7 @@ struct RowSum {
 // time); ITEMS 16-byte pieces per lane.
 template <typename T, typename P, int WAVES, int ITEMS>
 __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void norm_forward_kernel(
-    const T* __restrict__ x, int64_t ldx, const P* __restrict__ weight, const P* __restrict__ bias, T* __restrict__ y,
-    int64_t ldy, float* __restrict__ mean_out, float* __restrict__ rstd_out, int64_t rows, int cols, float eps) {
+    const T* x, int64_t ldx, const P* __restrict__ weight, const P* __restrict__ bias, T* y, int64_t ldy, float* __restrict__ mean_out, float* __restrict__ rstd_out, int64_t rows, int cols, float eps) {
     constexpr int N = Wide<T>::N, TEAMS = WAVES > 4 ? 1 : 4 / WAVES, LANES = WAVES * 64;
     __shared__ float red[TEAMS * 4 * WAVES];
     const int team = threadIdx.x / LANES, lane = threadIdx.x % LANES;
@@ -111,8 +110,8 @@ __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void norm_forward_ker
 // partial: [gridDim.x][2][cols] sums of dy xhat and of dy (SUMS).
 template <typename T, typename P, int WAVES, int ITEMS, bool SUMS>
 __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void norm_backward_kernel(
-    const T* __restrict__ dy, int64_t lddy, const T* __restrict__ x, int64_t ldx, const float* __restrict__ mean,
-    const float* __restrict__ rstd, const P* __restrict__ weight, T* __restrict__ dx, int64_t lddx,
+    const T* dy, int64_t lddy, const T* __restrict__ x, int64_t ldx, const float* __restrict__ mean,
+    const float* __restrict__ rstd, const P* __restrict__ weight, T* dx, int64_t lddx,
     float* __restrict__ partial, int64_t rows, int cols) {
     constexpr int N = Wide<T>::N, TEAMS = WAVES > 4 ? 1 : 4 / WAVES, LANES = WAVES * 64;
     static_assert(WAVES == 1 || TEAMS == 1, "a barrier is for a whole workgroup");

@@ -337,6 +337,25 @@ def linear_cross_entropy(hidden, weight, targets, ignore_index=-100, label_smoot
 
 
 # ---------------------------------------------------------------- AdamW
+def _gradient_norm(lib, tensors, count, max_norm):
+    n = _I64(0)
+    _check(lib, lib.jorge_gradient_norm_workspace(tensors, count, ctypes.byref(n)))
+    ws, out = _workspace(n.value), torch.empty(2, dtype=torch.float32, device="cuda")
+    _check(lib, lib.jorge_gradient_norm(tensors, count, float(max_norm), out.data_ptr(), _ptr(ws), n.value,
+                                        _current_stream()))
+    return out
+
+
+def gradient_norm(grads, max_norm=0.0):
+    """[norm, factor] on the device: the root of the sum of all gradients' squares, and what scales them
+    to max_norm where that is positive and below it (else 1). grads: fp32 or bfloat16, None entries are left out."""
+    grads = [_cuda(g, "gradient") for g in grads if g is not None]
+    grads = [g if _dense(g) else g.contiguous() for g in grads]
+    tensors = (AdamWTensor * max(1, len(grads)))(*[AdamWTensor(0, g.data_ptr(), g.numel(), 0, DTYPES[g.dtype], 0)
+                                                   for g in grads])
+    return _gradient_norm(load_operators(), tensors, len(grads), max_norm)
+
+
 class AdamW:
     """AdamW steps of a list of dense fp32 or bfloat16 CUDA tensors, all in one launch (per 112 of them).
 
@@ -415,7 +434,7 @@ class AdamW:
         if max_norm and clip is not None:
             raise ValueError("max_norm or clip, not both")
         if max_norm:
-            out = self._norm(max_norm)
+            out = _gradient_norm(self.lib, self._tensors, len(self.params), max_norm)
             self.norm, clip = out[0], out[1:]
         elif clip is not None and (_cuda(clip, "clip", (torch.float32,)).numel() != 1):
             raise ValueError("clip: one number is needed")
@@ -425,18 +444,10 @@ class AdamW:
         self.t += 1
         del keep
 
-    def _norm(self, max_norm):
-        n = _I64(0)
-        _check(self.lib, self.lib.jorge_gradient_norm_workspace(self._tensors, len(self.params), ctypes.byref(n)))
-        ws, out = _workspace(n.value), torch.empty(2, dtype=torch.float32, device="cuda")
-        _check(self.lib, self.lib.jorge_gradient_norm(self._tensors, len(self.params), float(max_norm), out.data_ptr(),
-                                                      _ptr(ws), n.value, _current_stream()))
-        return out
-
     def gradient_norm(self, grads=None, max_norm=0.0):
-        """[norm, clip factor] of the gradients on the device, without a step."""
+        """[norm, clip factor] of the gradients on the device, without a step (see gradient_norm)."""
         keep = self._gradients([p.grad for p in self.params] if grads is None else grads)
-        out = self._norm(max_norm)
+        out = _gradient_norm(self.lib, self._tensors, len(self.params), max_norm)
         del keep
         return out
 

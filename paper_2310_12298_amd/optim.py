@@ -1,4 +1,4 @@
-"""torch.optim front end of the Jorge library, with the paper's single-shot tuning.
+"""torch.optim front ends of the library: Jorge, with the paper's single-shot tuning, and AdamW.
 
 JorgeOptimizer hands the parameters of two or more dimensions of each
 parameter group to one Jorge context (the C ABI of include/jorge.h): an N-d
@@ -184,3 +184,61 @@ class JorgeOptimizer(torch.optim.Optimizer):
                 for k, v in tensors.items():
                     g["ctx"].set_state(l, k, v)
             g["ctx"].t = rec["t"]
+
+
+class AdamWOptimizer(torch.optim.Optimizer):
+    """torch.optim-style AdamW: one grouped library step per parameter group (see lm.AdamW).
+
+    Hyperparameters (per group): lr, betas, eps, weight_decay (decoupled, lr-scaled). max_norm > 0 clips
+    the gradients of all groups together by their global norm, which `norm` then holds on the device.
+    bits: 32, or 8 for moments of one byte per element; seed: of their random rounding. The moments of a
+    group live in its handle's flat buffers. A parameter without a gradient is left as it is.
+    """
+
+    def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
+                 max_norm: float = 0.0, bits: int = 32, seed: int = 0):
+        self.max_norm, self.norm = float(max_norm), None
+        self._bits, self._seed = int(bits), int(seed)
+        self._handles = []   # one lm.AdamW per parameter group
+        super().__init__(params, dict(lr=lr, betas=tuple(betas), eps=eps, weight_decay=weight_decay))
+
+    def add_param_group(self, param_group):
+        super().add_param_group(param_group)
+        from .lm import AdamW
+        try:
+            self._handles.append(AdamW(self.param_groups[-1]["params"], bits=self._bits,
+                                       seed=(self._seed + len(self._handles)) % (1 << 32)))
+        except Exception:
+            self.param_groups.pop()
+            raise
+
+    @torch.no_grad()
+    def step(self, closure=None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        clip = None
+        if self.max_norm:
+            from .lm import gradient_norm
+            out = gradient_norm([p.grad for h in self._handles for p in h.params], self.max_norm)
+            self.norm, clip = out[0], out[1:]
+        for group, h in zip(self.param_groups, self._handles):
+            b1, b2 = group["betas"]
+            h.step(lr=group["lr"], beta1=b1, beta2=b2, eps=group["eps"], weight_decay=group["weight_decay"], clip=clip)
+        return loss
+
+    def state_dict(self):
+        """The torch state plus each group's moments and step counter (host copies)."""
+        sd = super().state_dict()
+        sd["adamw"] = [h.state_dict() for h in self._handles]
+        return sd
+
+    def load_state_dict(self, state_dict):
+        sd = dict(state_dict)
+        held = sd.pop("adamw")
+        if len(held) != len(self._handles):
+            raise ValueError("the state is of another number of parameter groups")
+        super().load_state_dict(sd)
+        for h, rec in zip(self._handles, held):
+            h.load_state_dict(rec)

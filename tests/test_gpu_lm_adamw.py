@@ -259,6 +259,64 @@ def test_state_round_trip_resumes_bitwise(bits):
         assert torch.equal(x, y)
 
 
+def test_optimizer_groups_clip_together_and_resume():
+    from paper_2310_12298_amd.optim import AdamWOptimizer
+
+    def make():
+        torch.manual_seed(0)
+        return torch.nn.Sequential(torch.nn.Linear(40, 30), torch.nn.LayerNorm(30), torch.nn.Linear(30, 7)).cuda()
+
+    def groups(m):
+        vec = [p for p in m.parameters() if p.dim() < 2]
+        return [{"params": [p for p in m.parameters() if p.dim() >= 2]}, {"params": vec, "weight_decay": 0.0, "lr": 2e-3}]
+
+    def backward(m, t):
+        g = torch.Generator(device="cuda").manual_seed(t)
+        for p in m.parameters():
+            p.grad = torch.randn(p.shape, generator=g, device="cuda")
+
+    a, b = make(), make()
+    opt = AdamWOptimizer(groups(a), lr=1e-3, max_norm=1.0, bits=8, seed=5)
+    ref = torch.optim.AdamW(groups(b), lr=1e-3, weight_decay=0.01, foreach=True)
+    for t in range(1, 3):
+        backward(a, t)
+        backward(b, t)
+        opt.step()
+        norm = torch.nn.utils.clip_grad_norm_(b.parameters(), 1.0)
+        assert abs(opt.norm - norm) <= 1e-5 * norm
+        if t == 1:                                            # moments that have not been rounded yet
+            ref.step()
+            for x, y in zip(a.parameters(), b.parameters()):
+                assert torch.allclose(x, y, rtol=1e-5, atol=1e-6)
+    buf = io.BytesIO()
+    torch.save(opt.state_dict(), buf)
+    buf.seek(0)
+    c = make()
+    c.load_state_dict(a.state_dict())
+    twin = AdamWOptimizer(groups(c), lr=1e-3, max_norm=1.0, bits=8)
+    twin.load_state_dict(torch.load(buf, weights_only=True))
+    for m, o in ((a, opt), (c, twin)):
+        backward(m, 9)
+        o.step()
+    for x, y in zip(a.parameters(), c.parameters()):
+        assert torch.equal(x, y)
+    with pytest.raises(ValueError):
+        AdamWOptimizer([torch.zeros(3)])
+
+
+def test_a_parameter_that_moved_is_refused():
+    p = torch.nn.Parameter(tensors([64], F32)[0].view(8, 8))
+    opt = lm.AdamW([p])
+    p.grad = torch.ones_like(p)
+    opt.step()
+    p.data = p.data.t()                                       # the moments are in the old order
+    with pytest.raises(ValueError, match="has changed"):
+        opt.step([torch.ones_like(p)])
+    p.data = p.data.cpu()
+    with pytest.raises(ValueError):
+        opt.step([None])
+
+
 def test_refusals():
     p = tensors([10, 20], F32)
     opt = lm.AdamW(p)
