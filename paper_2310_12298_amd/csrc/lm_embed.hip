@@ -211,9 +211,12 @@ constexpr int kZeroRows = 64;
 struct SumArgs {
     const Entry* sorted;
     int64_t count, vocab, lddo, lddt;
-    float* partial;  // [chunks][2][ldp]: sums of a chunk's first run and of its last, where they cross its ends
+    float* partial;  // [2][chunks][ldp]: sums of a chunk's first run and of its last, where they cross its ends
     int64_t chunks;
-    int cols, chunk, slabs, ldp;  // ldp: cols rounded up to 4
+    int cols, chunk, slabs;
+    // cols rounded up to 64, and 64 more: a long run's rows, 2 KB apart for 512 columns, would all lie in the same few
+    // channels of the L2.
+    int ldp;
     float scale;
 };
 
@@ -261,7 +264,7 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(SumArgs a, const T* __r
                 for (int e = 0; e < N; ++e) o[e] = acc[e] * a.scale;
                 store_wide(dtable + (int64_t)key * a.lddt + c, left, o);
             } else {
-                float* const p = a.partial + (part * 2 + (begin == s0 ? 0 : 1)) * a.ldp + c;
+                float* const p = a.partial + (part + (begin == s0 ? 0 : a.chunks)) * a.ldp + c;
 #pragma unroll
                 for (int e = 0; e < N; ++e)
                     if (e < left) p[e] = acc[e];
@@ -301,59 +304,105 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(SumArgs a, const T* __r
     flush(s1);
 }
 
-// One workgroup per (chunk, slab of 256 floats): where a run starts in this chunk and goes on past its end, adds the
-// sums that its chunks left, eight waves taking every eighth chunk.
+// Adds the sums that the chunks of one run left, where a run starts in a chunk and goes on past its end. A workgroup
+// looks at the ends of kJoinWaves neighbouring chunks, a wave at each, for a slab of 4 LANES columns: LANES lanes take a
+// chunk's sums, a wave 64 / LANES chunks at a time. A wave adds a short run's sums by itself; a long run is shared by all
+// waves of the workgroup. Slabs of 64 columns serve narrow tables, where a long run would have too few CUs to itself (one
+// gets some 50 GB/s): 1024 chunks of 512 columns take 17 us, in slabs of 256 columns 27. Wide tables have enough slabs of
+// 256, and four times as many workgroups would cost more: 16384 tokens, 2048 columns 7 us against 13.
 constexpr int kJoinWaves = 8;
-template <typename T>
-__global__ __launch_bounds__(kJoinWaves * 64) void embed_join_kernel(SumArgs a, T* __restrict__ dtable) {
-    __shared__ f32x4 lds[kJoinWaves][64];
-    const int64_t part = blockIdx.x;
-    const int64_t s0 = part * a.chunk, s1 = s0 + a.chunk;
-    if (s1 >= a.count) return;
-    const uint32_t key = a.sorted[s1].key;
-    if (key >= a.vocab || a.sorted[s1 - 1].key != key) return;
-    const bool first_run = a.sorted[s0].key == key;  // the run fills the whole chunk
-    if (first_run && s0 > 0 && a.sorted[s0 - 1].key == key) return;  // it started before
-    // The run's last chunk: the first whose end it does not cross. 64 chunks' ends are looked at at a time.
-    int64_t last = part + 1;
-    for (;; last += 64) {
-        const int64_t next = (last + (threadIdx.x & 63) + 1) * a.chunk;
-        const uint64_t on = __ballot(next < a.count && a.sorted[next < a.count ? next : 0].key == key);
-        if (~on) {
-            last += __ffsll((unsigned long long)~on) - 1;
-            break;
-        }
-    }
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (blockIdx.y * 64 + lane) * 4;
+constexpr int kJoinAlone = 16;  // chunks after the first that a wave adds alone
+
+__device__ __forceinline__ f32x4 add_up(const float* p, int64_t stride, int64_t k, int64_t last, int step) {
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (c < a.cols) {
-        // The run is the last of this chunk and the first of each later one.
-        const float* const p = a.partial + c;
-        const int64_t stride = 2 * (int64_t)a.ldp;
-        if (wave == 0) sum = *reinterpret_cast<const f32x4*>(p + part * stride + (first_run ? 0 : a.ldp));
-        int64_t k = part + 1 + wave;
-        for (; k + 15 * kJoinWaves <= last; k += 16 * kJoinWaves) {
-            f32x4 v[16];
+    for (; k + 15 * step <= last; k += 16 * step) {
+        f32x4 v[16];
 #pragma unroll
-            for (int u = 0; u < 16; ++u) v[u] = *reinterpret_cast<const f32x4*>(p + (k + u * kJoinWaves) * stride);
+        for (int u = 0; u < 16; ++u) v[u] = *reinterpret_cast<const f32x4*>(p + (k + u * step) * stride);
 #pragma unroll
-            for (int half = 8; half > 0; half >>= 1)
+        for (int half = 8; half > 0; half >>= 1)
 #pragma unroll
-                for (int u = 0; u < half; ++u) v[u] += v[u + half];
-            sum += v[0];
-        }
-        for (; k <= last; k += kJoinWaves) sum += *reinterpret_cast<const f32x4*>(p + k * stride);
+            for (int u = 0; u < half; ++u) v[u] += v[u + half];
+        sum += v[0];
     }
-    lds[wave][lane] = sum;
-    __syncthreads();
-    if (wave == 0 && c < a.cols) {
-        f32x4 t = lds[0][lane];
-#pragma unroll
-        for (int w = 1; w < kJoinWaves; ++w) t += lds[w][lane];
+    for (; k <= last; k += step) sum += *reinterpret_cast<const f32x4*>(p + k * stride);
+    return sum;
+}
+
+template <typename T, int LANES>
+__global__ __launch_bounds__(kJoinWaves * 64) void embed_join_kernel(SumArgs a, T* __restrict__ dtable) {
+    __shared__ f32x4 lds[kJoinWaves][LANES];
+    constexpr int ROWS = 64 / LANES;
+    __shared__ int64_t run_part[kJoinWaves], run_last[kJoinWaves];  // long runs
+    __shared__ uint32_t run_key[kJoinWaves];
+    __shared__ int64_t run_first[kJoinWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane / LANES, c = (blockIdx.y * LANES + lane % LANES) * 4;
+    const int64_t stride = a.ldp, tails = a.chunks * stride;
+    const auto write = [&](uint32_t key, const f32x4& t) {
         T* const out = dtable + (int64_t)key * a.lddt + c;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
             if (c + e < a.cols) out[e] = (T)(t[e] * a.scale);
+    };
+    const int64_t part = (int64_t)blockIdx.x * kJoinWaves + wave, s0 = part * a.chunk, s1 = s0 + a.chunk;
+    bool run = s1 < a.count;
+    uint32_t key = 0;
+    bool fills = false;  // the run takes the whole chunk
+    if (run) {
+        key = a.sorted[s1].key;
+        fills = a.sorted[s0].key == key;
+        run = key < a.vocab && a.sorted[s1 - 1].key == key && !(fills && s0 > 0 && a.sorted[s0 - 1].key == key);
+    }
+    // The run's last chunk: the first whose end it does not cross. 64 ends are looked at at a time: every end, every
+    // 64th, then every one again.
+    int64_t last = part + 1;
+    if (run)
+        for (int step = 1;; step = 65 - step) {
+            const int64_t next = (last + (int64_t)lane * step + step) * a.chunk;
+            const uint64_t on = __ballot(next < a.count && a.sorted[next < a.count ? next : 0].key == key);
+            const int crossed = ~on ? __ffsll((unsigned long long)~on) - 1 : 64;
+            last += (int64_t)crossed * step;
+            if (step == 1 && crossed < 64) break;
+        }
+    const bool alone = last - part <= kJoinAlone;
+    if (lane == 0) {
+        run_part[wave] = run && !alone ? part : -1;
+        run_last[wave] = last;
+        run_key[wave] = key;
+        run_first[wave] = fills ? 0 : tails;
+    }
+    // The run is the last of its first chunk (its only one, if it fills it) and the first of each later one.
+    // Columns past the last one, as far as a row of sums reaches, are added up and not written.
+    const float* const p = a.partial + (c < a.ldp ? c : 0);
+    const auto over_rows = [&](f32x4 v) {  // of a wave
+#pragma unroll
+        for (int off = LANES; off < 64; off <<= 1)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += __shfl_xor(v[e], off);
+        return v;
+    };
+    if (run && alone) {
+        f32x4 sum = add_up(p, stride, part + 1 + sub, last, ROWS);
+        if (sub == 0) sum += *reinterpret_cast<const f32x4*>(p + part * stride + (fills ? 0 : tails));
+        sum = over_rows(sum);
+        if (sub == 0) write(key, sum);
+    }
+    __syncthreads();
+    for (int w = 0; w < kJoinWaves; ++w) {
+        const int64_t q = run_part[w];
+        if (q < 0) continue;  // the same for all waves
+        f32x4 sum = add_up(p, stride, q + 1 + ROWS * wave + sub, run_last[w], ROWS * kJoinWaves);
+        if (wave == 0 && sub == 0) sum += *reinterpret_cast<const f32x4*>(p + q * stride + run_first[w]);
+        sum = over_rows(sum);
+        __syncthreads();
+        if (sub == 0) lds[wave][lane] = sum;
+        __syncthreads();
+        if (wave == 0 && sub == 0) {
+            f32x4 t = lds[0][lane];
+#pragma unroll
+            for (int u = 1; u < kJoinWaves; ++u) t += lds[u][lane];
+            write(run_key[w], t);
+        }
     }
 }
 
@@ -364,6 +413,8 @@ int chunk_of(int64_t count) {
     while (ceil_div(count, c) > 4096 && c < 4096) c *= 2;
     return c;
 }
+
+int64_t partial_row(int64_t cols) { return round_up(cols, 64) + 64; }
 
 struct Work {
     Entry *a, *b;
@@ -376,7 +427,7 @@ Work carve(void* base, int64_t count, int64_t cols) {
     w.a = c.take<Entry>(count);
     w.b = count > kSortTile ? c.take<Entry>(count) : nullptr;
     const int64_t chunks = ceil_div(count, chunk_of(count));
-    w.partial = chunks > 1 ? c.take<float>(chunks * 2 * round_up(cols, 4)) : nullptr;
+    w.partial = chunks > 1 ? c.take<float>(chunks * 2 * partial_row(cols)) : nullptr;
     w.bytes = c.used;
     return w;
 }
@@ -441,7 +492,7 @@ jorge_status backward(const void* dout, int64_t lddo, const int64_t* tokens, int
     a.chunk = chunk_of(count);
     a.chunks = ceil_div(count, a.chunk);
     a.cols = (int)cols;
-    a.ldp = (int)round_up(cols, 4);
+    a.ldp = (int)partial_row(cols);
     a.slabs = (int)ceil_div(cols, 64 * Wide<T>::N);
     a.scale = (float)scale;
     const int64_t sum_groups = ceil_div(a.chunks * a.slabs, 4);
@@ -449,9 +500,13 @@ jorge_status backward(const void* dout, int64_t lddo, const int64_t* tokens, int
     if (sum_groups + zero_groups > kMaxGroups) return refuse(JORGE_ERR_UNSUPPORTED, "embedding: vocab * cols is too large");
     embed_sums_kernel<T><<<dim3((unsigned)(sum_groups + zero_groups)), dim3(256), 0, s>>>(a, (const T*)dout, (T*)dtable,
                                                                                          sum_groups);
-    if (a.chunks > 1)
-        embed_join_kernel<T><<<dim3((unsigned)(a.chunks - 1), (unsigned)ceil_div(cols, 256)), dim3(kJoinWaves * 64), 0, s>>>(
-            a, (T*)dtable);
+    if (a.chunks > 1) {
+        const unsigned groups = (unsigned)ceil_div(a.chunks - 1, kJoinWaves);
+        if (cols <= 1024)
+            embed_join_kernel<T, 16><<<dim3(groups, (unsigned)ceil_div(cols, 64)), dim3(kJoinWaves * 64), 0, s>>>(a, (T*)dtable);
+        else
+            embed_join_kernel<T, 64><<<dim3(groups, (unsigned)ceil_div(cols, 256)), dim3(kJoinWaves * 64), 0, s>>>(a, (T*)dtable);
+    }
     return launched("embedding");
 }
 

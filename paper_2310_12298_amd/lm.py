@@ -15,7 +15,7 @@ import ctypes
 import numpy as np
 import torch
 
-from .jorge import JORGE_OK, JorgeError, _current_stream, load_library
+from .jorge import JORGE_OK, JorgeError, load_library
 
 _P, _I32, _I64, _F64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_double
 BLOCK = 256                                   # elements of an 8-bit moment that share a scale
@@ -76,6 +76,11 @@ def load_operators() -> ctypes.CDLL:
     return lib
 
 
+def _stream(t=None):
+    """The current HIP stream of t's device as a number (torch's own shortcut: a Stream object takes 3 us to make)."""
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if t is None else t.get_device())
+
+
 def _check(lib, status):
     if status != JORGE_OK:
         raise JorgeError(status, f"{lib.jorge_status_string(status).decode()} ({lib.jorge_lm_last_error().decode()})")
@@ -121,6 +126,8 @@ def _vector(t, n, what):
 
 
 def _int64s(t, what):
+    if isinstance(t, torch.Tensor) and t.dtype is torch.int64 and t.is_contiguous():
+        return _cuda(t, what, (torch.int64,))
     if not isinstance(t, torch.Tensor) or t.dtype.is_floating_point or t.dtype.is_complex or t.dtype == torch.bool:
         raise ValueError(f"{what}: a tensor of whole numbers is needed")
     return _cuda(t.long().contiguous(), what, (torch.int64,))
@@ -147,11 +154,12 @@ def layer_norm_forward(x, weight=None, bias=None, eps=1e-5):
     w = params[0] if weight is not None else None
     b = params[-1] if bias is not None else None
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind(0)
+    mean = torch.empty(rows, dtype=torch.float32, device=x.device)
+    rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
     _check(lib, lib.jorge_layernorm_forward(m.data_ptr(), _ld(m), DTYPES[x.dtype], _ptr(w), _ptr(b),
                                             DTYPES[params[0].dtype] if params else 0, y.data_ptr(), cols,
                                             mean.data_ptr(), rstd.data_ptr(), rows, cols, float(eps),
-                                            _current_stream()))
+                                            _stream(x)))
     return y, mean, rstd
 
 
@@ -169,15 +177,17 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, affine=True):
     w = None if weight is None else _vector(weight, cols, "weight")
     ptype = torch.float32 if w is None else w.dtype
     dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    dw, db = torch.empty((2, cols), dtype=ptype, device=x.device).unbind(0) if affine else (None, None)
-    ws, n = None, _I64(0)
+    dw = db = ws = None
+    n = _I64(0)
     if affine:
+        dw = torch.empty(cols, dtype=ptype, device=x.device)
+        db = torch.empty(cols, dtype=ptype, device=x.device)
         _check(lib, lib.jorge_layernorm_workspace(rows, cols, ctypes.byref(n)))
         ws = _workspace(n.value)
     _check(lib, lib.jorge_layernorm_backward(d.data_ptr(), _ld(d), m.data_ptr(), _ld(m), DTYPES[x.dtype],
                                              mean.data_ptr(), rstd.data_ptr(), _ptr(w), DTYPES[ptype], dx.data_ptr(),
                                              cols, _ptr(dw), _ptr(db), rows, cols, _ptr(ws), n.value,
-                                             _current_stream()))
+                                             _stream(x)))
     return dx, dw, db
 
 
@@ -210,10 +220,10 @@ def embedding_forward(tokens, table, scale=1.0):
     if table.dim() != 2:
         raise ValueError("table: a matrix is needed")
     vocab, cols = t.shape
-    out = torch.empty((tok.numel(), cols), dtype=t.dtype, device=t.device)
+    out = torch.empty(tokens.shape + (cols,), dtype=t.dtype, device=t.device)
     _check(lib, lib.jorge_embedding_forward(tok.data_ptr(), tok.numel(), t.data_ptr(), _ld(t), DTYPES[t.dtype], vocab,
-                                            cols, float(scale), out.data_ptr(), cols, _current_stream()))
-    return out.view(*tokens.shape, cols)
+                                            cols, float(scale), out.data_ptr(), cols, _stream(t)))
+    return out
 
 
 def embedding_backward(dout, tokens, vocab, scale=1.0, padding=None):
@@ -231,7 +241,7 @@ def embedding_backward(dout, tokens, vocab, scale=1.0, padding=None):
     ws = _workspace(n.value)
     _check(lib, lib.jorge_embedding_backward(d.data_ptr(), _ld(d), tok.data_ptr(), count, DTYPES[d.dtype], int(vocab),
                                              cols, float(scale), -1 if padding is None else int(padding),
-                                             out.data_ptr(), cols, _ptr(ws), n.value, _current_stream()))
+                                             out.data_ptr(), cols, _ptr(ws), n.value, _stream(d)))
     return out
 
 
@@ -277,12 +287,13 @@ def cross_entropy_forward(hidden, weight, targets, ignore_index=-100, label_smoo
     n = _I64(0)
     _check(lib, lib.jorge_cross_entropy_workspace(ctypes.byref(shape), 0, ctypes.byref(n)))
     ws = _workspace(n.value)
-    loss, lse = (torch.empty(h.shape[0], dtype=torch.float32, device=h.device) for _ in range(2))
+    loss = torch.empty(targets.shape, dtype=torch.float32, device=h.device)
+    lse = torch.empty(targets.shape, dtype=torch.float32, device=h.device)
     total = torch.empty(3, dtype=torch.float32, device=h.device)
     _check(lib, lib.jorge_cross_entropy_forward(ctypes.byref(shape), h.data_ptr(), w.data_ptr(), t.data_ptr(),
                                                 loss.data_ptr(), lse.data_ptr(), total.data_ptr(), _ptr(ws), n.value,
-                                                _current_stream()))
-    return loss.view(targets.shape), lse.view(targets.shape), total
+                                                _stream(h)))
+    return loss, lse, total
 
 
 def cross_entropy_backward(grad, hidden, weight, targets, lse, total, reduction="mean", ignore_index=-100,
@@ -306,7 +317,7 @@ def cross_entropy_backward(grad, hidden, weight, targets, lse, total, reduction=
     dw = torch.empty((w.shape[0], shape.ldw), dtype=w.dtype, device=w.device) if need_weight else None
     _check(lib, lib.jorge_cross_entropy_backward(ctypes.byref(shape), g.data_ptr(), kind, h.data_ptr(), w.data_ptr(),
                                                  t.data_ptr(), lse.data_ptr(), total.data_ptr(), _ptr(dh), _ptr(dw),
-                                                 _ptr(ws), n.value, _current_stream()))
+                                                 _ptr(ws), n.value, _stream(h)))
     if need_hidden:
         dh = dh[:, :h.shape[1]].reshape(hidden.shape)
     return dh, dw[:, :w.shape[1]] if need_weight else None
@@ -342,7 +353,7 @@ def _gradient_norm(lib, tensors, count, max_norm):
     _check(lib, lib.jorge_gradient_norm_workspace(tensors, count, ctypes.byref(n)))
     ws, out = _workspace(n.value), torch.empty(2, dtype=torch.float32, device="cuda")
     _check(lib, lib.jorge_gradient_norm(tensors, count, float(max_norm), out.data_ptr(), _ptr(ws), n.value,
-                                        _current_stream()))
+                                        _stream()))
     return out
 
 
@@ -440,7 +451,7 @@ class AdamW:
             raise ValueError("clip: one number is needed")
         _check(self.lib, self.lib.jorge_adamw_step(self._tensors, len(self.params), ctypes.byref(self._moments),
                                                    self.t + 1, float(lr), float(beta1), float(beta2), float(eps),
-                                                   float(weight_decay), _ptr(clip), _current_stream()))
+                                                   float(weight_decay), _ptr(clip), _stream()))
         self.t += 1
         del keep
 
@@ -460,7 +471,7 @@ class AdamW:
         for second in (0, 1):
             v = torch.empty(total * BLOCK, dtype=dtype, device="cuda")
             _check(self.lib, self.lib.jorge_adamw_read(ctypes.byref(self._moments), second, 0, total, v.data_ptr(),
-                                                       DTYPES[dtype], _current_stream()))
+                                                       DTYPES[dtype], _stream()))
             out.append(v)
         return out[0], out[1]
 
@@ -474,7 +485,7 @@ class AdamW:
                 self.moments[k].copy_(v)
             else:
                 _check(self.lib, self.lib.jorge_adamw_write(ctypes.byref(self._moments), second, 0,
-                                                            int(self.blocks[-1]), v.data_ptr(), _current_stream()))
+                                                            int(self.blocks[-1]), v.data_ptr(), _stream()))
 
     def state_dict(self):
         return {"t": self.t, "bits": self.bits, "seed": self.seed, **{k: v.cpu() for k, v in self.moments.items()}}
