@@ -1,0 +1,146 @@
+"""How programs use the operators: in captured graphs, on several streams, on tensors past 2^31 elements."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from lm_check import U32, within  # noqa: E402
+from paper_2310_12298_amd import lm  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+def everything(x, w, b, dy, table, tok, head, tgt, params, grads, opt):
+    """One pass of every operator on fixed tensors; the optimizer steps from zeroed moments."""
+    for m in opt.moments.values():
+        m.zero_()
+    y, mean, rstd = lm.layer_norm_forward(x, w, b)
+    out = [y, *lm.layer_norm_backward(dy, x, mean, rstd, w)]
+    out += [lm.embedding_forward(tok, table, 2.0), lm.embedding_backward(dy, tok, table.shape[0], 2.0)]
+    loss, lse, total = lm.cross_entropy_forward(y, head, tgt)
+    out += [loss, total, *lm.cross_entropy_backward(total[1:2], y, head, tgt, lse, total)]
+    opt.t = 0
+    opt.step(grads, max_norm=0.5)
+    return out + [opt.norm] + [p.clone() for p in params]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_captured_into_a_graph(dtype):
+    g = torch.Generator(device="cuda").manual_seed(0)
+
+    def rand(*shape, d=dtype):
+        return torch.randn(shape, generator=g, device="cuda").to(d)
+    n, d, v = 300, 192, 900
+    x, dy, table, head = rand(n, d), rand(n, d), rand(v, d), rand(v, d)
+    w, b = rand(d, d=torch.float32), rand(d, d=torch.float32)
+    tok, tgt = (torch.randint(0, v, (n,), generator=g, device="cuda") for _ in range(2))
+    params, grads = [rand(1000), rand(77, 5)], [rand(1000), rand(77, 5)]
+    opt = lm.AdamW(params, bits=8, seed=1)
+    start = [p.clone() for p in params]
+    args = (x, w, b, dy, table, tok, head, tgt, params, grads, opt)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        everything(*args)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = everything(*args)
+    for round_ in range(4):                                  # other inputs, eager work and waits between the replays
+        for t in (x, dy, head, *grads):
+            t.copy_(rand(*t.shape))
+        tok.copy_(torch.randint(0, v, (n,), generator=g, device="cuda"))
+        tgt.copy_(torch.randint(-1, v, (n,), generator=g, device="cuda"))
+        for p, s in zip(params, start):
+            p.copy_(s)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in captured]
+        for p, s in zip(params, start):
+            p.copy_(s)
+        for i, (a, c) in enumerate(zip(got, everything(*args))):
+            assert torch.equal(a, c), (round_, i)
+
+
+def test_two_streams_at_once():
+    g = torch.Generator(device="cuda").manual_seed(1)
+    tok = [torch.randint(0, 5000, (20000,), generator=g, device="cuda") for _ in range(2)]
+    dout = [torch.randn(20000, 64, generator=g, device="cuda") for _ in range(2)]
+    h = [torch.randn(500, 128, generator=g, device="cuda") for _ in range(2)]
+    w = torch.randn(3000, 128, generator=g, device="cuda")
+    tgt = torch.randint(0, 3000, (500,), generator=g, device="cuda")
+
+    def work(i):
+        e = lm.embedding_backward(dout[i], tok[i], 5000)
+        loss, lse, total = lm.cross_entropy_forward(h[i], w, tgt)
+        return [e, loss, *lm.cross_entropy_backward(total[1:2], h[i], w, tgt, lse, total)]
+    want = [work(0), work(1)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [None, None]
+    for _ in range(3):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i] = work(i)
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_layer_norm_past_two_to_the_31_elements():
+    rows, cols = 140000, 16384
+    x = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda")
+    part = torch.randn(1000, cols, device="cuda").bfloat16()
+    for r in range(0, rows, 1000):
+        x[r:r + 1000] = part
+    y, mean, rstd = lm.layer_norm_forward(x)
+    few, m0, r0 = lm.layer_norm_forward(part)
+    assert all(torch.equal(y[r:r + 1000], few) for r in (0, 131000, 139000))
+    assert torch.equal(mean.view(-1, 1000), m0.expand(140, 1000))
+    dx = lm.layer_norm_backward(y, x, mean, rstd, affine=False)[0]
+    assert torch.equal(dx[139000:], lm.layer_norm_backward(few, part, m0, r0, affine=False)[0])
+    x[-1] = 1.0                                              # a constant row
+    assert torch.count_nonzero(lm.layer_norm_forward(x[-1:])[0]) == 0
+
+
+def test_embedding_past_two_to_the_31_elements():
+    vocab, cols = 140000, 16384
+    table = torch.zeros(vocab, cols, dtype=torch.bfloat16, device="cuda")
+    tok = torch.tensor([0, 139999, 131072, 139999, 135001], device="cuda")
+    rows = torch.randn(5, cols, device="cuda").bfloat16()
+    table[tok] = rows
+    out = lm.embedding_forward(tok, table)
+    assert torch.equal(out, table[tok])
+    dtable = lm.embedding_backward(rows, tok, vocab)
+    assert torch.equal(dtable[131072], rows[2]) and torch.equal(dtable[135001], rows[4])
+    within(dtable[139999], rows[1].double() + rows[3].double(), rows[1].double().abs() + rows[3].double().abs(), 1, "row")
+    dtable[tok] = 0
+    assert not bool(dtable.view(torch.int32).any())
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_adamw_past_two_to_the_31_elements(bits):
+    n = (1 << 31) + 70000
+    p, g = torch.zeros(n, dtype=torch.bfloat16, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g[-60000:] = 1.0
+    opt = lm.AdamW([p], bits=bits)
+    opt.step([g], lr=0.5, weight_decay=0.0, max_norm=1.0)
+    assert abs(opt.norm.item() - 60000 ** 0.5) <= 300 * U32 * 60000 ** 0.5
+    assert bool((p[-60000:] == -0.5).all())                  # the first step is lr, but for eps
+    assert not bool(p[:-60000].view(torch.int32).any())
+
+
+def test_cross_entropy_with_gradients_past_two_to_the_31_elements():
+    n, d, v = 3, 4096, 530000
+    w = torch.zeros(v, d, dtype=torch.bfloat16, device="cuda")
+    h = torch.randn(n, d, device="cuda").bfloat16()
+    w[-1] = h[0] / 64
+    tgt = torch.tensor([v - 1, 0, 5], device="cuda")
+    loss, lse, total = lm.cross_entropy_forward(h, w, tgt)
+    z = h.double() @ w[-1].double()
+    want = torch.logaddexp(z, torch.log(torch.tensor(float(v - 1), dtype=torch.float64)).cuda().expand(n))
+    assert torch.allclose(lse.double(), want, rtol=1e-5)
+    dh, dw = lm.cross_entropy_backward(torch.ones((), device="cuda"), h, w, tgt, lse, total, reduction="sum")
+    p = torch.exp(z - want)
+    ref = (p[0] - 1) * h[0].double() + p[1] * h[1].double() + p[2] * h[2].double()
+    assert (dw[-1].double() - ref).norm() <= 0.02 * ref.norm()
+    assert (dw[5].double() + h[2].double()).norm() <= 0.02 * h[2].double().norm()
