@@ -132,7 +132,7 @@ __device__ __forceinline__ Place place_of(int g, int ta, int tb) {
 
 struct Product {
     Operand A, B;
-    int per;         // stages of one segment
+    int stages;      // of 32 k
     int ta, tb;
 };
 
@@ -180,7 +180,7 @@ __global__ __launch_bounds__(256, 1) void loss_forward_kernel(Product p, LossRow
     using T = Tile<WA, WB, RING, SPLIT>;
     const Place at = place_of(blockIdx.x, p.ta, p.tb);
     T t;
-    t.multiply(p.A, p.B, (int64_t)at.a * T::kA, (int64_t)at.b * T::kB, 0, p.per * (SPLIT ? kSegments : 1), p.per, lds);
+    t.multiply(p.A, p.B, (int64_t)at.a * T::kA, (int64_t)at.b * T::kB, 0, p.stages, p.stages, lds);
     const int64_t a0 = (int64_t)at.a * T::kA + T::lane_a(), b0 = (int64_t)at.b * T::kB + T::lane_b();
     const int left = lane_left<WA>(p.A.rows - a0);  // words of this lane that exist
     const int64_t part = (word0 + (int64_t)at.a * T::kA) / (16 * WA) + (threadIdx.x >> 7);
@@ -315,7 +315,7 @@ __global__ __launch_bounds__(256, 1) void loss_dz_kernel(Product p, LossRows row
     using T = Tile<WA, WB, RING, SPLIT>;
     const Place at = place_of(blockIdx.x, p.ta, p.tb);
     T t;
-    t.multiply(p.A, p.B, (int64_t)at.a * T::kA, (int64_t)at.b * T::kB, 0, p.per * (SPLIT ? kSegments : 1), p.per, lds);
+    t.multiply(p.A, p.B, (int64_t)at.a * T::kA, (int64_t)at.b * T::kB, 0, p.stages, p.stages, lds);
     const int64_t a0 = (int64_t)at.a * T::kA + T::lane_a(), b0 = (int64_t)at.b * T::kB + T::lane_b();
     const int left = lane_left<WA>(p.A.rows - a0);
     const float even = smoothing / (float)rows.vocab;
@@ -390,10 +390,10 @@ __global__ __launch_bounds__(256, 1) void loss_grad_kernel(Product p, O* __restr
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     using T = Tile<WA, WB, RING, SPLIT>;
     const Place at = place_of(blockIdx.x, p.ta, p.tb);
-    const int pairs = p.per * (SPLIT ? kSegments : 1) / 2;
+    const int pairs = p.stages / 2;
     const int s0 = (int)((int64_t)pairs * blockIdx.y / gridDim.y) * 2, s1 = (int)((int64_t)pairs * (blockIdx.y + 1) / gridDim.y) * 2;
     T t;
-    t.multiply(p.A, p.B, (int64_t)at.a * T::kA, (int64_t)at.b * T::kB, s0, s1, p.per, lds);
+    t.multiply(p.A, p.B, (int64_t)at.a * T::kA, (int64_t)at.b * T::kB, s0, s1, p.stages, lds);
     const int64_t a0 = (int64_t)at.a * T::kA + T::lane_a(), b0 = (int64_t)at.b * T::kB + T::lane_b();
     const int left = lane_left<WA>(p.A.rows - a0);
     if (slices) {
@@ -466,14 +466,15 @@ struct Shape {
 // fast: 4096 x 4096 x 8192 takes 238 us in large tiles and 395 in middle ones), the fixed part 12, 6 and 4 us. The small
 // ones win where the large ones leave CUs idle or are mostly padding: 64 tokens, 8192 words of 512 in fp32 30 -> 17 us
 // for the logits.
-Shape shape_of(int64_t a, int64_t b, int64_t stages, bool may_cut) {
+Shape shape_of(int64_t a, int64_t b, int64_t k, int products, bool may_cut) {
     constexpr double kStage[3] = {0.88, 0.36, 0.15}, kFixed[3] = {12.0, 6.0, 4.0};
     Shape best{};
     double least = 1e300;
     for (int t = 0; t < 3; ++t) {
         const int64_t blocks = 8 >> t, tiles = ceil_div(a, 32 * blocks) * ceil_div(b, 32 * blocks);
-        // A range keeps at least eight stages.
-        for (int64_t r = 1; r == 1 || (may_cut && r <= stages / 8 && tiles * r <= 2 * kCus); r *= 2) {
+        // A range keeps at least eight stages' products, and two stages.
+        const int64_t stages = k / kStageK * products, most = std::min(stages / 8, k / kStageK / 2);
+        for (int64_t r = 1; r == 1 || (may_cut && r <= most && tiles * r <= 2 * kCus); r *= 2) {
             double us = (double)ceil_div(tiles * r, kCus) * ((double)ceil_div(stages, r) * kStage[t] + kFixed[t]);
             if (r > 1) us += 4.0 + (double)(r * a * b) * 8.0 / 4.5e6;
             if (us < least) {
@@ -486,7 +487,7 @@ Shape shape_of(int64_t a, int64_t b, int64_t stages, bool may_cut) {
 }
 
 struct Plan {
-    int terms, segments;
+    int terms, products;
     int64_t kd, kn, piece;       // padded cols, padded tokens, words of a piece
     bool direct_x, direct_w;     // hidden and weight serve as operands as they are
     Shape logits, dh, dw;
@@ -526,7 +527,7 @@ int64_t piece_of(const jorge_loss_shape& s, int64_t most, bool backward) {
 Plan plan_of(const jorge_loss_shape& s, bool backward, bool direct_x, bool direct_w) {
     Plan p{};
     p.terms = s.dtype == JORGE_F32 ? kTerms : 1;
-    p.segments = s.dtype == JORGE_F32 ? kSegments : 1;
+    p.products = s.dtype == JORGE_F32 ? 6 : 1;
     p.kd = round_up(s.cols, kPadK);
     p.kn = round_up(s.tokens, kPadK);
     p.direct_x = direct_x;
@@ -536,10 +537,10 @@ Plan plan_of(const jorge_loss_shape& s, bool backward, bool direct_x, bool direc
     if (!backward && direct_w) most = s.vocab;
     most = std::min(most, kMostTiles / ceil_div(std::max<int64_t>(1, s.tokens), 128) * 128);
     p.piece = piece_of(s, std::max<int64_t>(512, round_up(most, 256) - (most < s.vocab && most % 256 ? 256 : 0)), backward);
-    const int64_t words = std::min(p.piece, s.vocab), seg = p.segments;
-    p.logits = shape_of(words, s.tokens, seg * p.kd / kStageK, false);
-    p.dh = shape_of(s.cols, s.tokens, seg * round_up(words, kPadK) / kStageK, true);
-    p.dw = shape_of(s.cols, words, seg * p.kn / kStageK, true);
+    const int64_t words = std::min(p.piece, s.vocab);
+    p.logits = shape_of(words, s.tokens, p.kd, p.products, false);
+    p.dh = shape_of(s.cols, s.tokens, round_up(words, kPadK), p.products, true);
+    p.dw = shape_of(s.cols, words, p.kn, p.products, true);
     return p;
 }
 
@@ -682,9 +683,8 @@ jorge_status gradient(const Shape& sh, const Product& pr, T* out, int64_t ldo, i
         constexpr int WA = decltype(W)::value, RING = decltype(R)::value;
         const auto k = loss_grad_kernel<WA, WA, RING, sizeof(T) == 4, T>;
         if ((err = allow_lds(k, Tile<WA, WA, RING, sizeof(T) == 4>::kBytes)) != JORGE_OK) return;
-        // The first piece of a sum is the longest and has at least eight stages for each range; a short last one may
-        // add to fewer slices.
-        const int ranges = std::min(sh.ranges, pr.per * (sizeof(T) == 4 ? kSegments : 1) / 2);
+        // The first piece of a sum is the longest and fills every slice; a short last one may add to fewer.
+        const int ranges = std::min(sh.ranges, pr.stages / 2);
         k<<<dim3(pr.ta * pr.tb, ranges), dim3(256), Tile<WA, WA, RING, sizeof(T) == 4>::kBytes, st>>>(pr, out, ldo, slices, lda, first ? 0 : 1, scale);
     });
     if (err != JORGE_OK) return err;

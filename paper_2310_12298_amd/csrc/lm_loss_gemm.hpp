@@ -27,6 +27,8 @@
 
 #include "lm_common.hpp"
 
+#include <type_traits>
+
 namespace jorge_lm {
 
 constexpr int kStageK = 32;
@@ -39,11 +41,7 @@ struct Operand {
     int64_t rows;
 };
 
-// The order in which the terms of split operands are multiplied: the six products down to 2^-16 of the
-// whole, smallest first (term t of A with term u of B).
-constexpr int kTerms = 3, kSegments = 6;
-__device__ __forceinline__ int term_a(int seg) { return (0x001012 >> (4 * seg)) & 3; }
-__device__ __forceinline__ int term_b(int seg) { return (0x010210 >> (4 * seg)) & 3; }
+constexpr int kTerms = 3;  // of a split operand
 
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) const void global_void;
@@ -71,74 +69,80 @@ struct Tile {
         return (wave & 1) * 16 * WB + (lane & 15) * WB;
     }
 
-    // Stages [s0, s1) of the product of rows a0 .. of A and b0 .. of B; each segment (pair of terms) has
-    // `per` stages. s0, s1 and per are even, s1 > s0. lds: kBytes.
+    // Stages [s0, s1) of the product of rows a0 .. of A and b0 .. of B, of which each row has `stages` (32 k each).
+    // s0 and s1 are even, s1 > s0. lds: kBytes.
     __device__ __forceinline__ void multiply(const Operand& A, const Operand& B, int64_t a0, int64_t b0, int s0, int s1,
-                                             int per, char* lds) {
+                                             int stages, char* lds) {
         const int lane = threadIdx.x & 63;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-        // Where this lane's loads start: block n of the operand (n = wave * kLoads + v), row rho of it.
+        Loads load;
+        // Where this lane's loads start: block n of the operand (n = wave * kLoads + v), row rho of it. Bytes from the
+        // tile's first row to the end of its last one are what a load may reach.
         const int rho = lane >> 2, chunk = (lane & 3) ^ swizzle(rho);
-        unsigned offA[kLoadsA], offB[kLoadsB];
         const int limA = (int)(A.rows - a0 < kA ? A.rows - a0 : kA) - 1, limB = (int)(B.rows - b0 < kB ? B.rows - b0 : kB) - 1;
+        const unsigned K = (unsigned)(stages * kStageK), more = SPLIT ? kTerms - 1 : 0;
 #pragma unroll
         for (int v = 0; v < kLoadsA; ++v) {
             const int n = wave * kLoadsA + v, half = n / WA, i = n % WA;
             const int row = half * 16 * WA + (rho >> 2) * 4 * WA + 4 * i + (rho & 3);
-            offA[v] = (unsigned)(row < limA ? row : limA) * (unsigned)A.ld * 2u + chunk * 16u;
+            load.offA[v] = (unsigned)(row < limA ? row : limA) * (unsigned)A.ld * 2u + chunk * 16u;
         }
 #pragma unroll
         for (int v = 0; v < kLoadsB; ++v) {
             const int n = wave * kLoadsB + v, half = n / WB, j = n % WB;
             const int row = half * 16 * WB + rho * WB + j;
-            offB[v] = (unsigned)(row < limB ? row : limB) * (unsigned)B.ld * 2u + chunk * 16u;
+            load.offB[v] = (unsigned)(row < limB ? row : limB) * (unsigned)B.ld * 2u + chunk * 16u;
         }
-        // Bytes from the tile's first row to the end of its last one: what a load may reach.
-        const unsigned K = (unsigned)(per * kStageK), terms = SPLIT ? kTerms - 1 : 0;
-        const unsigned lenA = ((unsigned)limA * (unsigned)A.ld + terms * (unsigned)A.plane + K) * 2u;
-        const unsigned lenB = ((unsigned)limB * (unsigned)B.ld + terms * (unsigned)B.plane + K) * 2u;
-        // The loads of one stage after the other. What it takes to go on to the next stage is spread over the MFMAs
-        // of a step (the scalar unit runs beside them, but not beside a wait).
-        struct Loader {
-            const unsigned *offA, *offB;
-            __amdgpu_buffer_rsrc_t ra, rb;
-            int planeA, planeB;      // bytes
-            int per, seg, in, left, kA, kB, wave;  // in: bytes into the segment
-            char *lds, *to;
-            __device__ __forceinline__ void one(int v) {
-                if (v < kLoadsA)
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void*)(to + v * 1024), 16, offA[v], kA, 0, 0);
-                else
-                    __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                        rb, (lds_void*)(to + (2 * WA - wave * (kLoadsA - kLoadsB) + v - kLoadsA) * 1024), 16,
-                        offB[v - kLoadsA], kB, 0, 0);
-            }
-            __device__ __forceinline__ void slot(int n) { to = lds + n * kStageBytes + wave * kLoadsA * 1024; }
-            // Where no stage is left the last one is loaded again and not used: every wave always has the same
-            // number of loads in flight. Arithmetic, so that the loop's body stays one block.
-            __device__ __forceinline__ void next() {
-                --left;
-                const int on = left > 0 ? kStageK * 2 : 0;
-                if constexpr (SPLIT) {
-                    // Uniform, which the compiler does not see by itself.
-                    const int k = __builtin_amdgcn_readfirstlane(in + on), wrap = k == per * (kStageK * 2) ? 1 : 0;
-                    in = k - wrap * k;
-                    seg = __builtin_amdgcn_readfirstlane(seg + wrap);
-                    kA = term_a(seg) * planeA + in;
-                    kB = term_b(seg) * planeB + in;
-                } else {
-                    kA += on;
-                    kB = kA;
-                }
-            }
-        };
-        const int seg0 = SPLIT ? s0 / per : 0, in0 = (s0 - seg0 * per) * (kStageK * 2), pA = SPLIT ? (int)A.plane * 2 : 0,
-                  pB = SPLIT ? (int)B.plane * 2 : 0;
-        Loader load{offA, offB, resource(A.p + a0 * A.ld, lenA), resource(B.p + b0 * B.ld, lenB), pA, pB, per, seg0, in0, s1 - s0,
-                    term_a(seg0) * pA + in0, term_b(seg0) * pB + in0, wave, lds, lds};
+        load.ra = resource(A.p + a0 * A.ld, ((unsigned)limA * (unsigned)A.ld + more * (unsigned)A.plane + K) * 2u);
+        load.rb = resource(B.p + b0 * B.ld, ((unsigned)limB * (unsigned)B.ld + more * (unsigned)B.plane + K) * 2u);
+        load.k = s0 * (kStageK * 2);
+        load.left = s1 - s0;
         const int frag = (lane & 15) * 64 + (((lane >> 4) ^ swizzle(lane & 15)) * 16);
+#pragma unroll
+        for (int i = 0; i < WA; ++i)
+#pragma unroll
+            for (int j = 0; j < WB; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if constexpr (SPLIT) terms(load, (int)A.plane * 2, (int)B.plane * 2, s0, s1, frag, wave, lds);
+        else plain(load, s0, s1, frag, wave, lds);
+        wait_loads<0>();
+        __builtin_amdgcn_s_barrier();  // the ring is free for the epilogue
+    }
+
+private:
+    // The loads of one stage after the other.
+    struct Loads {
+        unsigned offA[kLoadsA], offB[kLoadsB];
+        __amdgpu_buffer_rsrc_t ra, rb;
+        int k, left;  // bytes into the rows, and stages left
+        __device__ __forceinline__ void a(int v, char* to, int at) const {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void*)to, 16, offA[v], at, 0, 0);
+        }
+        __device__ __forceinline__ void b(int v, char* to, int at) const {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void*)to, 16, offB[v], at, 0, 0);
+        }
+        // Where no stage is left the last one is loaded again and not used: every wave always has the same number of
+        // loads in flight, and the loop's body stays one block.
+        __device__ __forceinline__ void next() {
+            --left;
+            k += left > 0 ? kStageK * 2 : 0;
+        }
+    };
+
+    // After the last MFMA of all, the wait states that reading its result takes. They stand inside the loop, ahead of any
+    // place where the compiler, which does not see MFMAs in the asm, may copy an accumulator.
+    static __device__ __forceinline__ void settle(int s, int s1) {
+        asm volatile("s_cmp_lt_i32 %0, %1\n\ts_cbranch_scc1 1f\n\ts_nop 15\n\ts_nop 15\n1:" ::"s"(s), "s"(s1) : "scc");
+    }
+
+    // One product. A stage in the ring is A's blocks, then B's.
+    __device__ __forceinline__ void plain(Loads& load, int s0, int s1, int frag, int wave, char* lds) {
         const int fragA = frag + (wave >> 1) * WA * 1024, fragB = frag + (2 * WA + (wave & 1) * WB) * 1024;
         bf16x8 fa[2][WA], fb[2][WB];
+        const auto one = [&](int v, int slot) {
+            char* const to = lds + slot * kStageBytes;
+            if (v < kLoadsA) load.a(v, to + (wave * kLoadsA + v) * 1024, load.k);
+            else load.b(v - kLoadsA, to + (2 * WA + wave * kLoadsB + v - kLoadsA) * 1024, load.k);
+        };
         // Fragment f of a stage: first B's, which the first row of MFMAs needs together, then A's.
         const auto read = [&](int slot, int set, int f) {
             const char* const p = lds + slot * kStageBytes;
@@ -146,14 +150,9 @@ struct Tile {
             else fa[set][f - WB] = *reinterpret_cast<const bf16x8*>(p + fragA + (f - WB) * 1024);
         };
 #pragma unroll
-        for (int i = 0; i < WA; ++i)
-#pragma unroll
-            for (int j = 0; j < WB; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
         for (int r = 0; r < kRing - 1; ++r) {
-            load.slot(r);
 #pragma unroll
-            for (int v = 0; v < kLoads; ++v) load.one(v);
+            for (int v = 0; v < kLoads; ++v) one(v, r);
             load.next();
         }
         wait_loads<(kRing - 2) * kLoads>();
@@ -166,10 +165,10 @@ struct Tile {
             // new loads write was read by all before their last barrier but one.
             wait_loads<(kRing - 3) * kLoads>();
             __builtin_amdgcn_s_barrier();
-            const int ahead = slot + 1 == kRing ? 0 : slot + 1;
-            load.slot(slot == 0 ? kRing - 1 : slot - 1);
+            const int ahead = slot + 1 == kRing ? 0 : slot + 1, behind = slot == 0 ? kRing - 1 : slot - 1;
             // In this order: the fragment reads by twos in the first half, so that the next step need not wait for
-            // them, a load in every second group, and after the last load the way to the next stage.
+            // them, a load in every second group, and after the last load the way to the next stage (the scalar unit
+            // runs beside the MFMAs).
             constexpr int G = WA + WB, PER = WA * WB / G;
 #pragma unroll
             for (int g = 0; g < G; ++g) {
@@ -178,7 +177,7 @@ struct Tile {
                     read(ahead, set ^ 1, 2 * g);
                     read(ahead, set ^ 1, 2 * g + 1);
                 }
-                if (g % 2 == 0) load.one(g / 2);
+                if (g % 2 == 0) one(g / 2, behind);
                 if (g == G - 1) load.next();
 #pragma unroll
                 for (int m = g * PER; m < (g + 1) * PER; ++m) mfma(acc[m / WB][m % WB], fa[set][m / WB], fb[set][m % WB]);
@@ -189,12 +188,86 @@ struct Tile {
         for (int s = s0; s < s1; s += 2) {
             step(0);
             step(1);
-            // After the last MFMA of all, the wait states that reading its result takes. They stand inside the loop,
-            // ahead of any place where the compiler, which does not see MFMAs in the asm, may copy an accumulator.
-            asm volatile("s_cmp_lt_i32 %0, %1\n\ts_cbranch_scc1 1f\n\ts_nop 15\n\ts_nop 15\n1:" ::"s"(s + 2), "s"(s1) : "scc");
+            settle(s + 2, s1);
         }
-        wait_loads<0>();
-        __builtin_amdgcn_s_barrier();  // the ring is free for the epilogue
+    }
+
+    // Six products of the operands' terms, those down to 2^-16 of the whole, stage by stage in the order
+    //   A2 B0, A1 B0, A1 B1, A0 B1, A0 B2, A0 B0,
+    // in which each step exchanges one of the two factors. The ring holds planes of one term of one operand, in the
+    // order A2 B0 A1 B1 A0 B2, in which the steps come to need them: each step loads one plane and reads one plane's
+    // fragments, half of what six products of their own would.
+    __device__ __forceinline__ void terms(Loads& load, int planeA, int planeB, int s0, int s1, int frag, int wave, char* lds) {
+        static_assert(WA == WB, "planes of one size");
+        constexpr int kPlanes = 2 * kRing, kPlaneBytes = kStageBytes / 2;
+        static_assert((kPlanes & (kPlanes - 1)) == 0, "a power of two");
+        const int fragA = frag + (wave >> 1) * WA * 1024, fragB = frag + (wave & 1) * WB * 1024;
+        bf16x8 fa[2][WA], fb[3][WB];
+        // Load v of the plane that plays role r, to a slot.
+        const auto one = [&](int r, int v, int slot) {
+            char* const to = lds + slot * kPlaneBytes + (wave * kLoadsA + v) * 1024;
+            if (r % 2 == 0) load.a(v, to, load.k + (2 - r / 2) * planeA);
+            else load.b(v, to, load.k + r / 2 * planeB);
+        };
+        const auto read = [&](bool a, int set, int f, int slot) {
+            const char* const p = lds + slot * kPlaneBytes + f * 1024;
+            if (a) fa[set][f] = *reinterpret_cast<const bf16x8*>(p + fragA);
+            else fb[set][f] = *reinterpret_cast<const bf16x8*>(p + fragB);
+        };
+#pragma unroll
+        for (int n = 0; n < kPlanes; ++n) {
+#pragma unroll
+            for (int v = 0; v < kLoadsA; ++v) one(n % 6, v, n);
+            if (n % 6 == 5) load.next();
+        }
+        wait_loads<(kPlanes - 2) * kLoadsA>();
+        __builtin_amdgcn_s_barrier();
+#pragma unroll
+        for (int f = 0; f < WA; ++f) {
+            read(true, 0, f, 0);
+            read(false, 0, f, 1);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // plane 0's slot is written from step 0 on
+        int slot = 0;  // of plane n, n the number of the step
+        const auto step = [&](auto S) {
+            constexpr int k = decltype(S)::value % 6, P = decltype(S)::value / 6;
+            constexpr int useA = k == 1 || k == 2 ? P ^ 1 : P, useB = k == 4 ? 2 : k == 2 || k == 3 ? P ^ 1 : P;
+            // What the next step needs anew: plane n + 2. Its set's last use was before this step.
+            constexpr bool readA = k % 2 == 0;
+            constexpr int set = k == 2 ? P : k == 3 ? 2 : P ^ 1;
+            constexpr int role = (k + kPlanes) % 6;  // of plane n + kPlanes, which is loaded
+            // Plane n + 2 has landed for every wave once all have passed the barrier; plane n's fragments were read two
+            // steps ago, so its slot is free.
+            wait_loads<(kPlanes - 3) * kLoadsA>();
+            __builtin_amdgcn_s_barrier();
+            const int ahead = (slot + 2) & (kPlanes - 1);
+            constexpr int G = 2 * WA, PER = WA * WB / G;
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                __builtin_amdgcn_sched_barrier(0);
+                if (g < WA) read(readA, set, g, ahead);
+                else if ((g - WA) % 2 == 1) one(role, (g - WA) / 2, slot);
+                if (g == G - 1 && role == 5) load.next();
+#pragma unroll
+                for (int m = g * PER; m < (g + 1) * PER; ++m) mfma(acc[m / WB][m % WB], fa[useA][m / WB], fb[useB][m % WB]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            slot = (slot + 1) & (kPlanes - 1);
+        };
+        const auto chunk = [&](auto P) {
+            constexpr int b = decltype(P)::value * 6;
+            step(std::integral_constant<int, b>());
+            step(std::integral_constant<int, b + 1>());
+            step(std::integral_constant<int, b + 2>());
+            step(std::integral_constant<int, b + 3>());
+            step(std::integral_constant<int, b + 4>());
+            step(std::integral_constant<int, b + 5>());
+        };
+        for (int s = s0; s < s1; s += 2) {
+            chunk(std::integral_constant<int, 0>());
+            chunk(std::integral_constant<int, 1>());
+            settle(s + 2, s1);
+        }
     }
 
     // In place, in accumulator registers: left to the compiler the 64 accumulators wander between the two halves
