@@ -300,8 +300,8 @@ __global__ __launch_bounds__(256) void norm_partials_kernel(TensorBatch batch, d
     if (threadIdx.x == 0) partial[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-__global__ __launch_bounds__(1024) void norm_finish_kernel(const double* __restrict__ partial, int64_t n, float max_norm,
-                                                           float* __restrict__ out) {
+__global__ __launch_bounds__(1024) void norm_finish_kernel(const double* __restrict__ partial, int64_t n,
+                                                           float max_norm, float* __restrict__ out) {
     __shared__ double red[16];
     double s[4] = {};
     int64_t i = threadIdx.x;
@@ -332,7 +332,8 @@ jorge_status check_tensors(const jorge_adamw_tensor* t, int32_t n, bool step) {
     for (int32_t i = 0; i < n; ++i) {
         if (!known_dtype(t[i].dtype)) return bad("adamw: unknown element type");
         if (t[i].numel < 0) return bad("adamw: numel >= 0 is needed");
-        if (t[i].numel > (int64_t)1 << 38) return refuse(JORGE_ERR_UNSUPPORTED, "adamw: a tensor of more than 2^38 elements");
+        if (t[i].numel > (int64_t)1 << 38)
+            return refuse(JORGE_ERR_UNSUPPORTED, "adamw: a tensor of more than 2^38 elements");
         if (t[i].numel == 0) continue;
         if (!t[i].grad || (step && !t[i].param)) return bad("adamw: a tensor's pointer is null");
         const int64_t e = dtype_bytes(t[i].dtype);
@@ -348,8 +349,10 @@ jorge_status check_moments(const jorge_adamw_moments* m) {
     if (m->blocks < 0 || m->blocks > (int64_t)UINT32_MAX) return bad("adamw: blocks must be in [0, 2^32)");
     if (m->blocks == 0) return JORGE_OK;
     if (!m->exp_avg || !m->exp_avg_sq) return bad("adamw: the moments' buffers are needed");
-    if (!aligned(m->exp_avg, 16) || !aligned(m->exp_avg_sq, 16)) return bad("adamw: the moments must be aligned to 16 bytes");
-    if (m->bits == 8 && (!m->exp_avg_scale || !m->exp_avg_sq_scale)) return bad("adamw: 8-bit moments need their scales");
+    if (!aligned(m->exp_avg, 16) || !aligned(m->exp_avg_sq, 16))
+        return bad("adamw: the moments must be aligned to 16 bytes");
+    if (m->bits == 8 && (!m->exp_avg_scale || !m->exp_avg_sq_scale))
+        return bad("adamw: 8-bit moments need their scales");
     return JORGE_OK;
 }
 
@@ -401,7 +404,8 @@ jorge_status check_range(const jorge_adamw_moments* m, int32_t second, int64_t f
     if (st != JORGE_OK) return st;
     if (m->bits != 8) return bad("adamw: 32-bit moments are read and written in place");
     if (second != 0 && second != 1) return bad("adamw: second must be 0 or 1");
-    if (first < 0 || count < 0 || first > m->blocks || count > m->blocks - first) return bad("adamw: blocks outside the moments");
+    if (first < 0 || count < 0 || first > m->blocks || count > m->blocks - first)
+        return bad("adamw: blocks outside the moments");
     if (count > kMaxGroups) return refuse(JORGE_ERR_UNSUPPORTED, "adamw: too many blocks in one call");
     if (count > 0 && !p) return bad("adamw: a buffer is needed");
     return JORGE_OK;
@@ -427,11 +431,14 @@ jorge_status jorge_gradient_norm(const jorge_adamw_tensor* tensors, int32_t n, d
                                  void* workspace, int64_t workspace_bytes, void* hip_stream) {
     jorge_status st = check_tensors(tensors, n, false);
     if (st != JORGE_OK) return st;
-    if (!(max_norm >= 0.0) || !(max_norm - max_norm == 0.0)) return bad("gradient norm: max_norm must be finite and not negative");
+    if (!(max_norm >= 0.0) || !(max_norm - max_norm == 0.0))
+        return bad("gradient norm: max_norm must be finite and not negative");
     if (!out || !aligned(out, 4)) return bad("gradient norm: out is needed");
     const int64_t groups = norm_groups(tensors, n);
-    if (!workspace || !aligned(workspace, kAlign)) return bad("gradient norm: a workspace aligned to 256 bytes is needed");
-    if (workspace_bytes < round_up((groups + 1) * (int64_t)sizeof(double), kAlign)) return bad("gradient norm: the workspace is too small");
+    if (!workspace || !aligned(workspace, kAlign))
+        return bad("gradient norm: a workspace aligned to 256 bytes is needed");
+    if (workspace_bytes < round_up((groups + 1) * (int64_t)sizeof(double), kAlign))
+        return bad("gradient norm: the workspace is too small");
     const hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
     double* partial = (double*)workspace;
     double* at = partial;
@@ -465,7 +472,8 @@ jorge_status jorge_adamw_step(const jorge_adamw_tensor* tensors, int32_t n, cons
     if (t < 1) return bad("adamw: t >= 1 is needed");
     if (!(lr >= 0.0) || !(eps >= 0.0) || !(weight_decay >= 0.0) || !finite(lr) || !finite(eps) || !finite(weight_decay))
         return bad("adamw: lr, eps and weight_decay must be finite and not negative");
-    if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return bad("adamw: the betas must be in [0, 1)");
+    if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0))
+        return bad("adamw: the betas must be in [0, 1)");
     if (!aligned(clip, 4)) return bad("adamw: clip is not aligned");
     StepArgs a{};
     a.m = moments->exp_avg;
@@ -497,8 +505,8 @@ jorge_status jorge_adamw_step(const jorge_adamw_tensor* tensors, int32_t n, cons
     return JORGE_OK;
 }
 
-jorge_status jorge_adamw_read(const jorge_adamw_moments* moments, int32_t second, int64_t first, int64_t count, void* out,
-                              int32_t dtype, void* hip_stream) {
+jorge_status jorge_adamw_read(const jorge_adamw_moments* moments, int32_t second, int64_t first, int64_t count,
+                              void* out, int32_t dtype, void* hip_stream) {
     const jorge_status st = check_range(moments, second, first, count, out);
     if (st != JORGE_OK) return st;
     if (!known_dtype(dtype)) return bad("adamw: unknown element type");

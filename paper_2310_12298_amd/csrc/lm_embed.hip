@@ -220,7 +220,8 @@ struct SumArgs {
     float scale;
 };
 
-// blockIdx.x < sum_groups: four waves, a (chunk, slab of 64 wide pieces) each. Beyond: zero rows, a (64 rows, slab) each.
+// blockIdx.x < sum_groups: four waves, a (chunk, slab of 64 wide pieces) each. Beyond: zero rows, a (64 rows, slab)
+// each.
 template <typename T>
 __global__ __launch_bounds__(256) void embed_sums_kernel(SumArgs a, const T* __restrict__ dout, T* __restrict__ dtable,
                                                          int64_t sum_groups) {
@@ -305,11 +306,11 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(SumArgs a, const T* __r
 }
 
 // Adds the sums that the chunks of one run left, where a run starts in a chunk and goes on past its end. A workgroup
-// looks at the ends of kJoinWaves neighbouring chunks, a wave at each, for a slab of 4 LANES columns: LANES lanes take a
-// chunk's sums, a wave 64 / LANES chunks at a time. A wave adds a short run's sums by itself; a long run is shared by all
-// waves of the workgroup. Slabs of 64 columns serve narrow tables, where a long run would have too few CUs to itself (one
-// gets some 50 GB/s): 1024 chunks of 512 columns take 17 us, in slabs of 256 columns 27. Wide tables have enough slabs of
-// 256, and four times as many workgroups would cost more: 16384 tokens, 2048 columns 7 us against 13.
+// looks at the ends of kJoinWaves neighbouring chunks, a wave at each, for a slab of 4 LANES columns: LANES lanes take
+// a chunk's sums, a wave 64 / LANES chunks at a time. A wave adds a short run's sums by itself; a long run is shared by
+// all waves of the workgroup. Slabs of 64 columns serve narrow tables, where a long run would have too few CUs to
+// itself (one gets some 50 GB/s): 1024 chunks of 512 columns take 17 us, in slabs of 256 columns 27. Wide tables have
+// enough slabs of 256, and four times as many workgroups would cost more: 16384 tokens, 2048 columns 7 us against 13.
 constexpr int kJoinWaves = 8;
 constexpr int kJoinAlone = 16;  // chunks after the first that a wave adds alone
 
@@ -336,7 +337,8 @@ __global__ __launch_bounds__(kJoinWaves * 64) void embed_join_kernel(SumArgs a, 
     __shared__ int64_t run_part[kJoinWaves], run_last[kJoinWaves];  // long runs
     __shared__ uint32_t run_key[kJoinWaves];
     __shared__ int64_t run_first[kJoinWaves];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane / LANES, c = (blockIdx.y * LANES + lane % LANES) * 4;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane / LANES;
+    const int c = (blockIdx.y * LANES + lane % LANES) * 4;
     const int64_t stride = a.ldp, tails = a.chunks * stride;
     const auto write = [&](uint32_t key, const f32x4& t) {
         T* const out = dtable + (int64_t)key * a.lddt + c;
@@ -435,8 +437,10 @@ Work carve(void* base, int64_t count, int64_t cols) {
 jorge_status check(int64_t count, int64_t vocab, int64_t cols, int32_t dtype, double scale) {
     if (!known_dtype(dtype)) return bad("embedding: unknown element type");
     if (count < 0 || vocab < 1 || cols < 1) return bad("embedding: count >= 0, vocab >= 1 and cols >= 1 are needed");
-    if (count > JORGE_EMBED_MAX_TOKENS) return refuse(JORGE_ERR_UNSUPPORTED, "embedding: count above JORGE_EMBED_MAX_TOKENS");
-    if (vocab > JORGE_EMBED_MAX_VOCAB) return refuse(JORGE_ERR_UNSUPPORTED, "embedding: vocab above JORGE_EMBED_MAX_VOCAB");
+    if (count > JORGE_EMBED_MAX_TOKENS)
+        return refuse(JORGE_ERR_UNSUPPORTED, "embedding: count above JORGE_EMBED_MAX_TOKENS");
+    if (vocab > JORGE_EMBED_MAX_VOCAB)
+        return refuse(JORGE_ERR_UNSUPPORTED, "embedding: vocab above JORGE_EMBED_MAX_VOCAB");
     if (cols > JORGE_EMBED_MAX_COLS) return refuse(JORGE_ERR_UNSUPPORTED, "embedding: cols above JORGE_EMBED_MAX_COLS");
     if (!(scale - scale == 0.0)) return bad("embedding: scale must be finite");
     return JORGE_OK;
@@ -449,8 +453,8 @@ void forward(const int64_t* tokens, int64_t count, const void* table, int64_t ld
     const auto go = [&](auto L) {
         constexpr int lanes = decltype(L)::value;
         const dim3 grid((unsigned)ceil_div(count, 256 / lanes), (unsigned)ceil_div(pieces, lanes * kFwdItems));
-        embed_forward_kernel<T, lanes><<<grid, dim3(256), 0, s>>>(tokens, count, (const T*)table, ldt, vocab, cols, scale,
-                                                                  (T*)out, ldo);
+        embed_forward_kernel<T, lanes>
+            <<<grid, dim3(256), 0, s>>>(tokens, count, (const T*)table, ldt, vocab, cols, scale, (T*)out, ldo);
     };
     // Narrow rows share a wave.
     if (pieces <= 4) go(std::integral_constant<int, 4>());
@@ -497,15 +501,18 @@ jorge_status backward(const void* dout, int64_t lddo, const int64_t* tokens, int
     a.scale = (float)scale;
     const int64_t sum_groups = ceil_div(a.chunks * a.slabs, 4);
     const int64_t zero_groups = ceil_div(ceil_div(vocab, kZeroRows) * a.slabs, 4);
-    if (sum_groups + zero_groups > kMaxGroups) return refuse(JORGE_ERR_UNSUPPORTED, "embedding: vocab * cols is too large");
+    if (sum_groups + zero_groups > kMaxGroups)
+        return refuse(JORGE_ERR_UNSUPPORTED, "embedding: vocab * cols is too large");
     embed_sums_kernel<T><<<dim3((unsigned)(sum_groups + zero_groups)), dim3(256), 0, s>>>(a, (const T*)dout, (T*)dtable,
                                                                                          sum_groups);
     if (a.chunks > 1) {
         const unsigned groups = (unsigned)ceil_div(a.chunks - 1, kJoinWaves);
         if (cols <= 1024)
-            embed_join_kernel<T, 16><<<dim3(groups, (unsigned)ceil_div(cols, 64)), dim3(kJoinWaves * 64), 0, s>>>(a, (T*)dtable);
+            embed_join_kernel<T, 16>
+                <<<dim3(groups, (unsigned)ceil_div(cols, 64)), dim3(kJoinWaves * 64), 0, s>>>(a, (T*)dtable);
         else
-            embed_join_kernel<T, 64><<<dim3(groups, (unsigned)ceil_div(cols, 256)), dim3(kJoinWaves * 64), 0, s>>>(a, (T*)dtable);
+            embed_join_kernel<T, 64>
+                <<<dim3(groups, (unsigned)ceil_div(cols, 256)), dim3(kJoinWaves * 64), 0, s>>>(a, (T*)dtable);
     }
     return launched("embedding");
 }
@@ -517,9 +524,9 @@ using namespace jorge_lm;
 
 extern "C" {
 
-jorge_status jorge_embedding_forward(const int64_t* tokens, int64_t count, const void* table, int64_t ldt, int32_t dtype,
-                                     int64_t vocab, int64_t cols, double scale, void* out, int64_t ldo,
-                                     void* hip_stream) {
+jorge_status jorge_embedding_forward(const int64_t* tokens, int64_t count, const void* table, int64_t ldt,
+                                     int32_t dtype, int64_t vocab, int64_t cols, double scale, void* out,
+                                     int64_t ldo, void* hip_stream) {
     const jorge_status st = check(count, vocab, cols, dtype, scale);
     if (st != JORGE_OK) return st;
     if (ldt < cols || ldo < cols) return bad("embedding: a row stride is below cols");
@@ -548,9 +555,10 @@ jorge_status jorge_embedding_workspace(int64_t count, int64_t vocab, int64_t col
     return JORGE_OK;
 }
 
-jorge_status jorge_embedding_backward(const void* dout, int64_t lddo, const int64_t* tokens, int64_t count, int32_t dtype,
-                                      int64_t vocab, int64_t cols, double scale, int64_t padding, void* dtable,
-                                      int64_t lddt, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+jorge_status jorge_embedding_backward(const void* dout, int64_t lddo, const int64_t* tokens, int64_t count,
+                                      int32_t dtype, int64_t vocab, int64_t cols, double scale, int64_t padding,
+                                      void* dtable, int64_t lddt, void* workspace, int64_t workspace_bytes,
+                                      void* hip_stream) {
     const jorge_status st = check(count, vocab, cols, dtype, scale);
     if (st != JORGE_OK) return st;
     if (lddo < cols || lddt < cols) return bad("embedding: a row stride is below cols");

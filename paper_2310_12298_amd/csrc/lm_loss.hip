@@ -35,10 +35,10 @@ constexpr float kLog2e = 1.44269504088896341f;
 constexpr int kPadK = 64;      // K of every product is a multiple of two stages
 
 // ---------------------------------------------------------------- operands
-// Copies of a matrix that the products read: `flat`, its rows padded with zeros to ldf (a multiple of 64), and `turned`,
-// its transpose, padded to ldt (a multiple of 64) with zeros, which also stand in for the rows that `targets` (if
-// given) has no target for: what such a row holds must not reach a sum that it has no part in. Either may be null;
-// the terms of a row follow one another.
+// Copies of a matrix that the products read: `flat`, its rows padded with zeros to a multiple of 64, and `turned`, its
+// transpose, padded alike with zeros, which also stand in for the rows that `targets` (if given) has no target for:
+// what such a row holds must not reach a sum that it has no part in. Either may be null; the terms of a row follow one
+// another.
 struct Copies {
     const void* src;
     int64_t ld, rows;
@@ -236,8 +236,9 @@ __global__ __launch_bounds__(256, 1) void loss_forward_kernel(Product p, LossRow
 
 // Joins the parts' statistics of 64 tokens: 16 waves take every 16th part, ascending, and are joined in order.
 constexpr int kJoinWaves = 16;
-__global__ __launch_bounds__(kJoinWaves * 64) void loss_join_kernel(Stats in, int64_t parts, LossRows rows, float smoothing,
-                                                                    float* __restrict__ loss, float* __restrict__ lse) {
+__global__ __launch_bounds__(kJoinWaves * 64) void loss_join_kernel(Stats in, int64_t parts, LossRows rows,
+                                                                    float smoothing, float* __restrict__ loss,
+                                                                    float* __restrict__ lse) {
     __shared__ float lt[kJoinWaves][64], ls[kJoinWaves][64], la[kJoinWaves][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t i = (int64_t)blockIdx.x * 64 + lane, at = i < rows.tokens ? i : rows.tokens - 1;
@@ -309,8 +310,8 @@ struct DzOut {
 // dz of a piece: words word0 .. word0 + A.rows; the padding of both copies is written as 0.
 template <int WA, int WB, int RING, bool SPLIT>
 __global__ __launch_bounds__(256, 1) void loss_dz_kernel(Product p, LossRows rows, const float* __restrict__ lse,
-                                                         const float* __restrict__ row_grad, float smoothing, int64_t word0,
-                                                         DzOut out) {
+                                                         const float* __restrict__ row_grad, float smoothing,
+                                                         int64_t word0, DzOut out) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     using T = Tile<WA, WB, RING, SPLIT>;
     const Place at = place_of(blockIdx.x, p.ta, p.tb);
@@ -385,13 +386,15 @@ struct Scale {
 // C[b][a] over one of gridDim.y ranges of K, to out (whole: one range) or to the range's slice of fp32 sums
 // [ranges][B.rows][lda], added to it where `add`.
 template <int WA, int WB, int RING, bool SPLIT, typename O>
-__global__ __launch_bounds__(256, 1) void loss_grad_kernel(Product p, O* __restrict__ out, int64_t ldo, float* __restrict__ slices,
-                                                           int64_t lda, int add, Scale scale) {
+__global__ __launch_bounds__(256, 1) void loss_grad_kernel(Product p, O* __restrict__ out, int64_t ldo,
+                                                           float* __restrict__ slices, int64_t lda, int add,
+                                                           Scale scale) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     using T = Tile<WA, WB, RING, SPLIT>;
     const Place at = place_of(blockIdx.x, p.ta, p.tb);
     const int pairs = p.stages / 2;
-    const int s0 = (int)((int64_t)pairs * blockIdx.y / gridDim.y) * 2, s1 = (int)((int64_t)pairs * (blockIdx.y + 1) / gridDim.y) * 2;
+    const int s0 = (int)((int64_t)pairs * blockIdx.y / gridDim.y) * 2;
+    const int s1 = (int)((int64_t)pairs * (blockIdx.y + 1) / gridDim.y) * 2;
     T t;
     t.multiply(p.A, p.B, (int64_t)at.a * T::kA, (int64_t)at.b * T::kB, s0, s1, p.stages, lds);
     const int64_t a0 = (int64_t)at.a * T::kA + T::lane_a(), b0 = (int64_t)at.b * T::kB + T::lane_b();
@@ -429,8 +432,9 @@ __global__ __launch_bounds__(256, 1) void loss_grad_kernel(Product p, O* __restr
 
 // out[r][c] = scale times the sum of the slices, in order.
 template <typename O>
-__global__ __launch_bounds__(256) void loss_slices_kernel(const float* __restrict__ slices, int n, int64_t rows, int cols,
-                                                          int64_t lda, O* __restrict__ out, int64_t ldo, Scale scale) {
+__global__ __launch_bounds__(256) void loss_slices_kernel(const float* __restrict__ slices, int n, int64_t rows,
+                                                          int cols, int64_t lda, O* __restrict__ out, int64_t ldo,
+                                                          Scale scale) {
     const int64_t r = blockIdx.x;
     const float f = scale.value();
     for (int c = (blockIdx.y * 256 + threadIdx.x) * 4; c < cols; c += gridDim.y * 1024) {
@@ -462,10 +466,10 @@ struct Shape {
 };
 // The tile and the number of ranges that a model of the launch puts first: rounds of workgroups over the CUs, each the
 // stages of its range and a fixed part (the ring's first loads, the epilogue), and adding the ranges' sums up. A stage
-// takes 0.88, 0.36 and 0.15 us (tiles of 256, 128 and 64, all CUs busy; per flop the large one is 1.6 and 2.7 times as
-// fast: 4096 x 4096 x 8192 takes 238 us in large tiles and 395 in middle ones), the fixed part 12, 6 and 4 us. The small
-// ones win where the large ones leave CUs idle or are mostly padding: 64 tokens, 8192 words of 512 in fp32 30 -> 17 us
-// for the logits.
+// takes 0.88, 0.36 and 0.15 us (tiles of 256, 128 and 64, all CUs busy; per flop the large one is 1.6 and 2.7 times
+// as fast: 4096 x 4096 x 8192 takes 238 us in large tiles and 395 in middle ones), the fixed part 12, 6 and 4 us. The
+// small ones win where the large ones leave CUs idle or are mostly padding: 64 tokens, 8192 words of 512 in fp32 30 ->
+// 17 us for the logits.
 Shape shape_of(int64_t a, int64_t b, int64_t k, int products, bool may_cut) {
     constexpr double kStage[3] = {0.88, 0.36, 0.15}, kFixed[3] = {12.0, 6.0, 4.0};
     Shape best{};
@@ -502,9 +506,10 @@ constexpr int64_t kPieceElements = 1 << 26;
 // Tiles of one launch: its threads have to stay below 2^32.
 constexpr int64_t kMostTiles = 1 << 23;
 
-// Words of a piece, a multiple of 256 up to `most`: where the tiles are large, those that leave the CUs idle least in the
-// last round of a launch's tiles, over the whole vocabulary. A round of dz costs cols (and its exponentials, about 400
-// elements of K), one of dweight tokens; a piece's other launches about a thousand.
+// Words of a piece, a multiple of 256 up to `most`: where the tiles are large, those that leave the CUs idle least in
+// the last round of a launch's tiles, over the whole vocabulary. A round of dz costs cols (and its exponentials, about
+// 400 elements of K), one of dweight tokens; a piece's other launches about a thousand. (8192 tokens, 50001 words of
+// 2048: pieces of 8192 words rather than seven equal ones, 6.67 -> 6.50 ms.)
 int64_t piece_of(const jorge_loss_shape& s, int64_t most, bool backward) {
     const int64_t even = round_up(ceil_div(s.vocab, ceil_div(s.vocab, most)), 256);
     const int64_t tokens = ceil_div(s.tokens, 256), cols = ceil_div(s.cols, 256);
@@ -536,7 +541,8 @@ Plan plan_of(const jorge_loss_shape& s, bool backward, bool direct_x, bool direc
     int64_t most = kPieceElements / (s.dtype == JORGE_F32 ? 2 : 1) / std::max<int64_t>(1, backward ? p.kn : p.kd);
     if (!backward && direct_w) most = s.vocab;
     most = std::min(most, kMostTiles / ceil_div(std::max<int64_t>(1, s.tokens), 128) * 128);
-    p.piece = piece_of(s, std::max<int64_t>(512, round_up(most, 256) - (most < s.vocab && most % 256 ? 256 : 0)), backward);
+    most = most < s.vocab ? most / 256 * 256 : round_up(most, 256);
+    p.piece = piece_of(s, std::max<int64_t>(512, most), backward);
     const int64_t words = std::min(p.piece, s.vocab);
     p.logits = shape_of(words, s.tokens, p.kd, p.products, false);
     p.dh = shape_of(s.cols, s.tokens, round_up(words, kPadK), p.products, true);
@@ -580,7 +586,8 @@ Work carve(void* base, const jorge_loss_shape& s, const Plan& p, bool backward) 
 // their type and strides alone do not rule it out.
 int64_t workspace_bytes_of(const jorge_loss_shape& s, bool backward) {
     int64_t most = 0;
-    for (int k = 0; k < 4; ++k) most = std::max(most, carve(nullptr, s, plan_of(s, backward, k & 1, k & 2), backward).bytes);
+    for (int k = 0; k < 4; ++k)
+        most = std::max(most, carve(nullptr, s, plan_of(s, backward, k & 1, k & 2), backward).bytes);
     return most;
 }
 
@@ -598,7 +605,8 @@ Product product_of(const Shape& sh, const Operand& A, const Operand& B, int64_t 
 // Lets a kernel use the LDS of its ring (more than the default limit).
 template <typename K>
 jorge_status allow_lds(K* kernel, int bytes) {
-    if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes) != hipSuccess) {
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes) !=
+        hipSuccess) {
         (void)hipGetLastError();
         return refuse(JORGE_ERR_HIP, "cross entropy: no LDS for a tile");
     }
@@ -675,8 +683,8 @@ jorge_status forward(const jorge_loss_shape& s, const Plan& p, const Work& w, co
 
 // One gradient: out = scale * A-by-B, in slices where K is cut or the sum goes on (first, last: of the sum's pieces).
 template <typename T>
-jorge_status gradient(const Shape& sh, const Product& pr, T* out, int64_t ldo, int64_t cols, float* slices, bool first, bool last,
-                      const Scale& scale, hipStream_t st) {
+jorge_status gradient(const Shape& sh, const Product& pr, T* out, int64_t ldo, int64_t cols, float* slices, bool first,
+                      bool last, const Scale& scale, hipStream_t st) {
     jorge_status err = JORGE_OK;
     const int64_t lda = round_up(cols, 4);
     with_tile(sh, [&](auto W, auto R) {
@@ -685,7 +693,8 @@ jorge_status gradient(const Shape& sh, const Product& pr, T* out, int64_t ldo, i
         if ((err = allow_lds(k, Tile<WA, WA, RING, sizeof(T) == 4>::kBytes)) != JORGE_OK) return;
         // The first piece of a sum is the longest and fills every slice; a short last one may add to fewer.
         const int ranges = std::min(sh.ranges, pr.stages / 2);
-        k<<<dim3(pr.ta * pr.tb, ranges), dim3(256), Tile<WA, WA, RING, sizeof(T) == 4>::kBytes, st>>>(pr, out, ldo, slices, lda, first ? 0 : 1, scale);
+        k<<<dim3(pr.ta * pr.tb, ranges), dim3(256), Tile<WA, WA, RING, sizeof(T) == 4>::kBytes, st>>>(
+            pr, out, ldo, slices, lda, first ? 0 : 1, scale);
     });
     if (err != JORGE_OK) return err;
     if (slices && last)
@@ -695,9 +704,9 @@ jorge_status gradient(const Shape& sh, const Product& pr, T* out, int64_t ldo, i
 }
 
 template <typename T>
-jorge_status backward(const jorge_loss_shape& s, const Plan& p, const Work& w, const float* grad, int32_t kind, const void* hidden,
-                      const void* weight, const LossRows& rows, const float* lse, const float* total, void* dhidden,
-                      void* dweight, hipStream_t st) {
+jorge_status backward(const jorge_loss_shape& s, const Plan& p, const Work& w, const float* grad, int32_t kind,
+                      const void* hidden, const void* weight, const LossRows& rows, const float* lse,
+                      const float* total, void* dhidden, void* dweight, hipStream_t st) {
     const Scale scale{kind == JORGE_LOSS_ROWS ? nullptr : grad, kind == JORGE_LOSS_MEAN ? total + 1 : nullptr};
     const float* const row_grad = kind == JORGE_LOSS_ROWS ? grad : nullptr;
     const Operand x = operand_x(s, p, w, hidden);
@@ -706,7 +715,8 @@ jorge_status backward(const jorge_loss_shape& s, const Plan& p, const Work& w, c
     for (int64_t v0 = 0; v0 < s.vocab; v0 += p.piece) {
         const int64_t n = std::min(p.piece, s.vocab - v0), ldz = round_up(n, kPadK);
         const T* const from = (const T*)weight + v0 * s.ldw;
-        copy<T>(v0 ? Copies{} : copies_of(hidden, s.ldh, s.tokens, s.cols, w.x, p.kd, dweight ? w.xt : nullptr, p.kn, &rows),
+        copy<T>(v0 ? Copies{}
+                   : copies_of(hidden, s.ldh, s.tokens, s.cols, w.x, p.kd, dweight ? w.xt : nullptr, p.kn, &rows),
                 copies_of(from, s.ldw, n, s.cols, w.w, p.kd, dhidden ? w.wt : nullptr, ldz, nullptr), st);
         const Product pr = product_of(p.logits, operand_w(s, p, w, from, n), x, p.kd);
         const DzOut dz{w.dz, w.dzt, ldz, p.kn};
@@ -714,16 +724,21 @@ jorge_status backward(const jorge_loss_shape& s, const Plan& p, const Work& w, c
             constexpr int WA = decltype(W)::value, RING = decltype(R)::value;
             const auto k = loss_dz_kernel<WA, WA, RING, sizeof(T) == 4>;
             if ((err = allow_lds(k, Tile<WA, WA, RING, sizeof(T) == 4>::kBytes)) != JORGE_OK) return;
-            k<<<dim3(pr.ta * pr.tb), dim3(256), Tile<WA, WA, RING, sizeof(T) == 4>::kBytes, st>>>(pr, rows, lse, row_grad, (float)s.label_smoothing, v0, dz);
+            k<<<dim3(pr.ta * pr.tb), dim3(256), Tile<WA, WA, RING, sizeof(T) == 4>::kBytes, st>>>(
+                pr, rows, lse, row_grad, (float)s.label_smoothing, v0, dz);
         });
         if (err != JORGE_OK) return err;
         if (dhidden) {
-            const Product g = product_of(p.dh, {w.wt, p.terms * ldz, ldz, s.cols}, {w.dz, p.terms * ldz, ldz, s.tokens}, ldz);
-            if ((err = gradient(p.dh, g, (T*)dhidden, s.ldh, s.cols, w.dh, v0 == 0, v0 + n == s.vocab, scale, st)) != JORGE_OK) return err;
+            const Operand wt{w.wt, p.terms * ldz, ldz, s.cols}, z{w.dz, p.terms * ldz, ldz, s.tokens};
+            err = gradient(p.dh, product_of(p.dh, wt, z, ldz), (T*)dhidden, s.ldh, s.cols, w.dh, v0 == 0,
+                           v0 + n == s.vocab, scale, st);
+            if (err != JORGE_OK) return err;
         }
         if (dweight) {
-            const Product g = product_of(p.dw, xt, {w.dzt, p.terms * p.kn, p.kn, n}, p.kn);
-            if ((err = gradient(p.dw, g, (T*)dweight + v0 * s.ldw, s.ldw, s.cols, w.dw, true, true, scale, st)) != JORGE_OK) return err;
+            const Operand zt{w.dzt, p.terms * p.kn, p.kn, n};
+            err = gradient(p.dw, product_of(p.dw, xt, zt, p.kn), (T*)dweight + v0 * s.ldw, s.ldw, s.cols, w.dw, true,
+                           true, scale, st);
+            if (err != JORGE_OK) return err;
         }
     }
     return launched("cross entropy");
@@ -737,14 +752,21 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(T* p, int64_t ld, int64_
 jorge_status check(const jorge_loss_shape* s) {
     if (!s) return bad("cross entropy: a shape is needed");
     if (!known_dtype(s->dtype)) return bad("cross entropy: unknown element type");
-    if (s->tokens < 0 || s->cols < 1 || s->vocab < 1) return bad("cross entropy: tokens >= 0, cols >= 1 and vocab >= 1 are needed");
-    if (s->tokens > JORGE_LOSS_MAX_TOKENS) return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: tokens above JORGE_LOSS_MAX_TOKENS");
-    if (s->vocab > JORGE_LOSS_MAX_VOCAB) return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: vocab above JORGE_LOSS_MAX_VOCAB");
-    if (s->cols > JORGE_LOSS_MAX_COLS) return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: cols above JORGE_LOSS_MAX_COLS");
-    if (ceil_div(s->tokens, 64) * ceil_div(s->cols, 64) > 1 << 23) return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: tokens * cols above 2^35");
+    if (s->tokens < 0 || s->cols < 1 || s->vocab < 1)
+        return bad("cross entropy: tokens >= 0, cols >= 1 and vocab >= 1 are needed");
+    if (s->tokens > JORGE_LOSS_MAX_TOKENS)
+        return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: tokens above JORGE_LOSS_MAX_TOKENS");
+    if (s->vocab > JORGE_LOSS_MAX_VOCAB)
+        return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: vocab above JORGE_LOSS_MAX_VOCAB");
+    if (s->cols > JORGE_LOSS_MAX_COLS)
+        return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: cols above JORGE_LOSS_MAX_COLS");
+    if (ceil_div(s->tokens, 64) * ceil_div(s->cols, 64) > 1 << 23)
+        return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: tokens * cols above 2^35");
     if (s->ldh < s->cols || s->ldw < s->cols) return bad("cross entropy: a row stride is below cols");
-    if (s->ldh > (int64_t)1 << 22 || s->ldw > (int64_t)1 << 22) return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: a row stride above 2^22");
-    if (!(s->label_smoothing >= 0.0 && s->label_smoothing <= 1.0)) return bad("cross entropy: label_smoothing must be in [0, 1]");
+    if (s->ldh > (int64_t)1 << 22 || s->ldw > (int64_t)1 << 22)
+        return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: a row stride above 2^22");
+    if (!(s->label_smoothing >= 0.0 && s->label_smoothing <= 1.0))
+        return bad("cross entropy: label_smoothing must be in [0, 1]");
     return JORGE_OK;
 }
 
@@ -772,10 +794,12 @@ jorge_status jorge_cross_entropy_forward(const jorge_loss_shape* shape, const vo
     const int64_t e = dtype_bytes(s.dtype);
     if (!total || !aligned(total, 4)) return bad("cross entropy: total is needed");
     if (s.tokens > 0) {
-        if (!hidden || !weight || !targets || !loss || !lse) return bad("cross entropy: hidden, weight, targets, loss and lse are needed");
+        if (!hidden || !weight || !targets || !loss || !lse)
+            return bad("cross entropy: hidden, weight, targets, loss and lse are needed");
         if (!aligned(hidden, e) || !aligned(weight, e) || !aligned(targets, 8) || !aligned(loss, 4) || !aligned(lse, 4))
             return bad("cross entropy: a pointer is not aligned to its element");
-        if (!workspace || !aligned(workspace, kAlign)) return bad("cross entropy: a workspace aligned to 256 bytes is needed");
+        if (!workspace || !aligned(workspace, kAlign))
+            return bad("cross entropy: a workspace aligned to 256 bytes is needed");
         if (workspace_bytes < workspace_bytes_of(s, false)) return bad("cross entropy: the workspace is too small");
     }
     const LossRows rows{targets, s.tokens, s.vocab, s.ignore_index};
@@ -790,29 +814,34 @@ jorge_status jorge_cross_entropy_forward(const jorge_loss_shape* shape, const vo
     return forward<bf16>(s, p, w, hidden, weight, rows, loss, lse, total, q);
 }
 
-jorge_status jorge_cross_entropy_backward(const jorge_loss_shape* shape, const float* grad, int32_t kind, const void* hidden,
-                                          const void* weight, const int64_t* targets, const float* lse, const float* total,
-                                          void* dhidden, void* dweight, void* workspace, int64_t workspace_bytes,
-                                          void* hip_stream) {
+jorge_status jorge_cross_entropy_backward(const jorge_loss_shape* shape, const float* grad, int32_t kind,
+                                          const void* hidden, const void* weight, const int64_t* targets,
+                                          const float* lse, const float* total, void* dhidden, void* dweight,
+                                          void* workspace, int64_t workspace_bytes, void* hip_stream) {
     jorge_status st = check(shape);
     if (st != JORGE_OK) return st;
     const jorge_loss_shape& s = *shape;
     const int64_t e = dtype_bytes(s.dtype);
-    if (kind != JORGE_LOSS_ROWS && kind != JORGE_LOSS_SUM && kind != JORGE_LOSS_MEAN) return bad("cross entropy: unknown kind of gradient");
-    if (!aligned(dhidden, e) || !aligned(dweight, e)) return bad("cross entropy: a pointer is not aligned to its element");
+    if (kind != JORGE_LOSS_ROWS && kind != JORGE_LOSS_SUM && kind != JORGE_LOSS_MEAN)
+        return bad("cross entropy: unknown kind of gradient");
+    if (!aligned(dhidden, e) || !aligned(dweight, e))
+        return bad("cross entropy: a pointer is not aligned to its element");
     const hipStream_t q = reinterpret_cast<hipStream_t>(hip_stream);
     if (s.tokens == 0) {
         if (dweight) {
-            if (s.dtype == JORGE_F32) zero_rows_kernel<float><<<dim3((unsigned)s.vocab), dim3(256), 0, q>>>((float*)dweight, s.ldw, s.cols);
+            if (s.dtype == JORGE_F32)
+                zero_rows_kernel<float><<<dim3((unsigned)s.vocab), dim3(256), 0, q>>>((float*)dweight, s.ldw, s.cols);
             else zero_rows_kernel<bf16><<<dim3((unsigned)s.vocab), dim3(256), 0, q>>>((bf16*)dweight, s.ldw, s.cols);
         }
         return launched("cross entropy");
     }
     if (!grad || !hidden || !weight || !targets || !lse || !total)
         return bad("cross entropy: grad, hidden, weight, targets, lse and total are needed");
-    if (!aligned(grad, 4) || !aligned(hidden, e) || !aligned(weight, e) || !aligned(targets, 8) || !aligned(lse, 4) || !aligned(total, 4))
+    if (!aligned(grad, 4) || !aligned(hidden, e) || !aligned(weight, e) || !aligned(targets, 8) || !aligned(lse, 4) ||
+        !aligned(total, 4))
         return bad("cross entropy: a pointer is not aligned to its element");
-    if (!workspace || !aligned(workspace, kAlign)) return bad("cross entropy: a workspace aligned to 256 bytes is needed");
+    if (!workspace || !aligned(workspace, kAlign))
+        return bad("cross entropy: a workspace aligned to 256 bytes is needed");
     if (workspace_bytes < workspace_bytes_of(s, true)) return bad("cross entropy: the workspace is too small");
     if (!dhidden && !dweight) return JORGE_OK;
     const Plan p = plan_of(s, true, direct(s, hidden, s.ldh), direct(s, weight, s.ldw));

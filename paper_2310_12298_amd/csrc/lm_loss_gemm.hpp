@@ -79,7 +79,8 @@ struct Tile {
         // Where this lane's loads start: block n of the operand (n = wave * kLoads + v), row rho of it. Bytes from the
         // tile's first row to the end of its last one are what a load may reach.
         const int rho = lane >> 2, chunk = (lane & 3) ^ swizzle(rho);
-        const int limA = (int)(A.rows - a0 < kA ? A.rows - a0 : kA) - 1, limB = (int)(B.rows - b0 < kB ? B.rows - b0 : kB) - 1;
+        const int limA = (int)(A.rows - a0 < kA ? A.rows - a0 : kA) - 1;
+        const int limB = (int)(B.rows - b0 < kB ? B.rows - b0 : kB) - 1;
         const unsigned K = (unsigned)(stages * kStageK), more = SPLIT ? kTerms - 1 : 0;
 #pragma unroll
         for (int v = 0; v < kLoadsA; ++v) {
@@ -128,8 +129,8 @@ private:
         }
     };
 
-    // After the last MFMA of all, the wait states that reading its result takes. They stand inside the loop, ahead of any
-    // place where the compiler, which does not see MFMAs in the asm, may copy an accumulator.
+    // After the last MFMA of all, the wait states that reading its result takes. They stand inside the loop, ahead of
+    // any place where the compiler, which does not see MFMAs in the asm, may copy an accumulator.
     static __device__ __forceinline__ void settle(int s, int s1) {
         asm volatile("s_cmp_lt_i32 %0, %1\n\ts_cbranch_scc1 1f\n\ts_nop 15\n\ts_nop 15\n1:" ::"s"(s), "s"(s1) : "scc");
     }
@@ -180,7 +181,8 @@ private:
                 if (g % 2 == 0) one(g / 2, behind);
                 if (g == G - 1) load.next();
 #pragma unroll
-                for (int m = g * PER; m < (g + 1) * PER; ++m) mfma(acc[m / WB][m % WB], fa[set][m / WB], fb[set][m % WB]);
+                for (int m = g * PER; m < (g + 1) * PER; ++m)
+                    mfma(acc[m / WB][m % WB], fa[set][m / WB], fb[set][m % WB]);
             }
             __builtin_amdgcn_sched_barrier(0);
             slot = ahead;
@@ -197,7 +199,8 @@ private:
     // in which each step exchanges one of the two factors. The ring holds planes of one term of one operand, in the
     // order A2 B0 A1 B1 A0 B2, in which the steps come to need them: each step loads one plane and reads one plane's
     // fragments, half of what six products of their own would.
-    __device__ __forceinline__ void terms(Loads& load, int planeA, int planeB, int s0, int s1, int frag, int wave, char* lds) {
+    __device__ __forceinline__ void terms(Loads& load, int planeA, int planeB, int s0, int s1, int frag, int wave,
+                                          char* lds) {
         static_assert(WA == WB, "planes of one size");
         constexpr int kPlanes = 2 * kRing, kPlaneBytes = kStageBytes / 2;
         static_assert((kPlanes & (kPlanes - 1)) == 0, "a power of two");
@@ -249,7 +252,8 @@ private:
                 else if ((g - WA) % 2 == 1) one(role, (g - WA) / 2, slot);
                 if (g == G - 1 && role == 5) load.next();
 #pragma unroll
-                for (int m = g * PER; m < (g + 1) * PER; ++m) mfma(acc[m / WB][m % WB], fa[useA][m / WB], fb[useB][m % WB]);
+                for (int m = g * PER; m < (g + 1) * PER; ++m)
+                    mfma(acc[m / WB][m % WB], fa[useA][m / WB], fb[useB][m % WB]);
             }
             __builtin_amdgcn_sched_barrier(0);
             slot = (slot + 1) & (kPlanes - 1);

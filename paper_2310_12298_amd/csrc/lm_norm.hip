@@ -51,7 +51,8 @@ struct RowSum {
 // time); ITEMS 16-byte pieces per lane.
 template <typename T, typename P, int WAVES, int ITEMS>
 __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void norm_forward_kernel(
-    const T* x, int64_t ldx, const P* __restrict__ weight, const P* __restrict__ bias, T* y, int64_t ldy, float* __restrict__ mean_out, float* __restrict__ rstd_out, int64_t rows, int cols, float eps) {
+    const T* x, int64_t ldx, const P* __restrict__ weight, const P* __restrict__ bias, T* y, int64_t ldy,
+    float* __restrict__ mean_out, float* __restrict__ rstd_out, int64_t rows, int cols, float eps) {
     constexpr int N = Wide<T>::N, TEAMS = WAVES > 4 ? 1 : 4 / WAVES, LANES = WAVES * 64;
     __shared__ float red[TEAMS * 4 * WAVES];
     const int team = threadIdx.x / LANES, lane = threadIdx.x % LANES;
@@ -216,8 +217,9 @@ __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void norm_backward_ke
 // partial each, in ascending order, and their sums are added in wave order.
 constexpr int kSumWaves = 16;
 template <typename P>
-__global__ __launch_bounds__(kSumWaves * 64) void norm_sums_kernel(const float* __restrict__ partial, int parts, int cols,
-                                                                    P* __restrict__ dweight, P* __restrict__ dbias) {
+__global__ __launch_bounds__(kSumWaves * 64) void norm_sums_kernel(const float* __restrict__ partial, int parts,
+                                                                   int cols, P* __restrict__ dweight,
+                                                                   P* __restrict__ dbias) {
     __shared__ float lds[kSumWaves][64];
     P* const out = blockIdx.y ? dbias : dweight;
     if (!out) return;
@@ -311,16 +313,19 @@ void backward(const void* dy, int64_t lddy, const void* x, int64_t ldx, const fl
             const dim3 grid(groups), block(waves > 4 ? waves * 64 : 256);
             if (partial)
                 norm_backward_kernel<T, P, waves, items, true><<<grid, block, 0, stream>>>(
-                    (const T*)dy, lddy, (const T*)x, ldx, mean, rstd, (const P*)weight, (T*)dx, lddx, partial, rows, cols);
+                    (const T*)dy, lddy, (const T*)x, ldx, mean, rstd, (const P*)weight, (T*)dx, lddx, partial, rows,
+                    cols);
             else
                 norm_backward_kernel<T, P, waves, items, false><<<grid, block, 0, stream>>>(
-                    (const T*)dy, lddy, (const T*)x, ldx, mean, rstd, (const P*)weight, (T*)dx, lddx, partial, rows, cols);
+                    (const T*)dy, lddy, (const T*)x, ldx, mean, rstd, (const P*)weight, (T*)dx, lddx, partial, rows,
+                    cols);
         }
     });
 }
 
 // What every call of the pass checks.
-jorge_status check(int64_t rows, int64_t cols, int32_t dtype, int32_t param_dtype, const void* weight, const void* bias) {
+jorge_status check(int64_t rows, int64_t cols, int32_t dtype, int32_t param_dtype, const void* weight,
+                   const void* bias) {
     if (!known_dtype(dtype) || !known_dtype(param_dtype)) return bad("layer norm: unknown element type");
     if (rows < 0 || cols < 1) return bad("layer norm: rows >= 0 and cols >= 1 are needed");
     if (cols > JORGE_NORM_MAX_COLS) return refuse(JORGE_ERR_UNSUPPORTED, "layer norm: cols above JORGE_NORM_MAX_COLS");
@@ -384,8 +389,10 @@ jorge_status jorge_layernorm_backward(const void* dy, int64_t lddy, const void* 
     const bool sums = dweight || dbias;
     const int groups = groups_of(rows, cols, dtype);
     if (sums && rows > 0) {
-        if (!workspace || !aligned(workspace, kAlign)) return bad("layer norm: a workspace aligned to 256 bytes is needed");
-        if (workspace_bytes < round_up((int64_t)groups * 2 * cols * 4, kAlign)) return bad("layer norm: the workspace is too small");
+        if (!workspace || !aligned(workspace, kAlign))
+            return bad("layer norm: a workspace aligned to 256 bytes is needed");
+        if (workspace_bytes < round_up((int64_t)groups * 2 * cols * 4, kAlign))
+            return bad("layer norm: the workspace is too small");
     }
     const hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
     float* const partial = sums ? (float*)workspace : nullptr;

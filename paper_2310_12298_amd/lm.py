@@ -476,7 +476,8 @@ class AdamW:
         return out[0], out[1]
 
     def set_moment_values(self, exp_avg, exp_avg_sq):
-        """Takes the moments' values from flat fp32 tensors in the layout of moment_values (8 bits: rounded to nearest)."""
+        """Takes the moments' values from flat fp32 tensors in the layout of moment_values (8 bits: rounded to
+        nearest)."""
         for second, (k, v) in enumerate((("exp_avg", exp_avg), ("exp_avg_sq", exp_avg_sq))):
             v = _cuda(v, k, (torch.float32,)).contiguous()
             if v.shape != self.moments[k].shape:

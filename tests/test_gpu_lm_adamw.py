@@ -182,7 +182,7 @@ def test_steps_in_8_bits(dtype, scale):
 
 
 def test_8_bit_rounding_is_even_handed():
-    """A slow average follows its input in the mean: after many steps the 8-bit second moments add up to the 32-bit ones."""
+    """A slow average follows its input in the mean: after many steps the 8-bit moments add up to the 32-bit ones."""
     n = 1 << 16
     g = tensors([n], F32, seed=3)
     a, b = lm.AdamW(tensors([n], F32)), lm.AdamW(tensors([n], F32), bits=8)
@@ -268,7 +268,8 @@ def test_optimizer_groups_clip_together_and_resume():
 
     def groups(m):
         vec = [p for p in m.parameters() if p.dim() < 2]
-        return [{"params": [p for p in m.parameters() if p.dim() >= 2]}, {"params": vec, "weight_decay": 0.0, "lr": 2e-3}]
+        return [{"params": [p for p in m.parameters() if p.dim() >= 2]},
+                {"params": vec, "weight_decay": 0.0, "lr": 2e-3}]
 
     def backward(m, t):
         g = torch.Generator(device="cuda").manual_seed(t)
@@ -328,8 +329,8 @@ def test_refusals():
         with pytest.raises(ValueError):
             bad()
     before = [x.clone() for x in p]
-    for kw in (dict(lr=-1.0), dict(beta1=1.0), dict(beta2=-0.1), dict(eps=float("nan")), dict(weight_decay=float("inf")),
-               dict(max_norm=-1.0)):
+    for kw in (dict(lr=-1.0), dict(beta1=1.0), dict(beta2=-0.1), dict(eps=float("nan")),
+               dict(weight_decay=float("inf")), dict(max_norm=-1.0)):
         with pytest.raises(lm.JorgeError):
             opt.step(g, **kw)
     assert opt.t == 0 and all(torch.equal(x, y) for x, y in zip(before, p))

@@ -55,8 +55,9 @@ def some_tokens(kind, n, vocab):
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("kind", ["uniform", "one", "half", "sorted", "strays"])
-@pytest.mark.parametrize("n,vocab,cols", [(1, 1, 1), (2, 5, 3), (31, 7, 64), (32, 40, 65), (33, 257, 8), (1000, 100, 130),
-                                          (1025, 65536, 5), (4097, 300, 516), (16384, 999, 24), (16385, 4000, 12)])
+@pytest.mark.parametrize("n,vocab,cols", [(1, 1, 1), (2, 5, 3), (31, 7, 64), (32, 40, 65), (33, 257, 8),
+                                          (1000, 100, 130), (1025, 65536, 5), (4097, 300, 516), (16384, 999, 24),
+                                          (16385, 4000, 12)])
 def test_gradient(kind, n, vocab, cols, dtype):
     check_grad(some_tokens(kind, n, vocab), vocab, cols, dtype)
 
@@ -91,8 +92,9 @@ def test_padding_gets_no_gradient_and_strides_do_not_matter():
 
 
 def test_no_tokens():
-    assert torch.count_nonzero(lm.embedding_backward(torch.empty(0, 9, device="cuda"), torch.empty(0, dtype=torch.int64, device="cuda"), 6)) == 0
-    out = lm.embedding_forward(torch.empty(0, dtype=torch.int64, device="cuda"), torch.ones(3, 9, device="cuda"))
+    none = torch.empty(0, dtype=torch.int64, device="cuda")
+    assert torch.count_nonzero(lm.embedding_backward(torch.empty(0, 9, device="cuda"), none, 6)) == 0
+    out = lm.embedding_forward(none, torch.ones(3, 9, device="cuda"))
     assert out.shape == (0, 9)
 
 
@@ -140,10 +142,12 @@ def test_refusals():
     dout = torch.ones(4, 8, device="cuda")
     for bad in (lambda: lm.embedding_forward(tokens.float(), table), lambda: lm.embedding_forward(tokens, table.half()),
                 lambda: lm.embedding_forward(tokens.cpu(), table), lambda: lm.embedding_forward(tokens, table[0]),
-                lambda: lm.embedding_backward(dout[:3], tokens, 5), lambda: lm.embedding_backward(dout, tokens, 5, padding=5)):
+                lambda: lm.embedding_backward(dout[:3], tokens, 5),
+                lambda: lm.embedding_backward(dout, tokens, 5, padding=5)):
         with pytest.raises(ValueError):
             bad()
     for bad in (lambda: lm.embedding_forward(tokens, table, scale=float("nan")),
-                lambda: lm.embedding_backward(dout, tokens, 0), lambda: lm.embedding_backward(dout, tokens, (1 << 24) + 1)):
+                lambda: lm.embedding_backward(dout, tokens, 0),
+                lambda: lm.embedding_backward(dout, tokens, (1 << 24) + 1)):
         with pytest.raises(lm.JorgeError):
             bad()

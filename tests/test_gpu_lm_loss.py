@@ -42,15 +42,16 @@ def plain(h, w, t, smoothing, ignore, row_grad):
     dz = (torch.softmax(z, 1) - want) * g[:, None]
     dz[~live] = 0
     zerr = ((h * h) @ (w * w).t()).sqrt() * (h.shape[1] / 8 + 16) * U32
-    return dict(z=z, lse=lse, loss=loss, live=live, g=g, dz=dz, dh=dz @ w, dw=dz.t() @ (h * live[:, None]), zerr=zerr, p=torch.softmax(z, 1))
+    return dict(z=z, lse=lse, loss=loss, live=live, g=g, dz=dz, dh=dz @ w, dw=dz.t() @ (h * live[:, None]), zerr=zerr,
+                p=torch.softmax(z, 1))
 
 
 def close(got, want, room, what):
     got = got.double()
     assert got.shape == want.shape and bool(torch.isfinite(got).all()), what
     bad = ((got - want).abs() > room).nonzero()
-    assert len(bad) == 0, (what, len(bad), tuple(bad[0].tolist()), got[tuple(bad[0])].item(), want[tuple(bad[0])].item(),
-                           room.expand_as(want)[tuple(bad[0])].item())
+    at = tuple(bad[0].tolist()) if len(bad) else None
+    assert at is None, (what, len(bad), at, got[at].item(), want[at].item(), room.expand_as(want)[at].item())
 
 
 def check(h, w, t, smoothing=0.0, ignore=-100, reduction="mean"):
@@ -58,20 +59,22 @@ def check(h, w, t, smoothing=0.0, ignore=-100, reduction="mean"):
     gen = torch.Generator().manual_seed(1)
     per_row = torch.randn(n, generator=gen).cuda()
     one = torch.tensor(1.7, device="cuda")
-    row_grad = {"none": lambda live: per_row.double(), "sum": lambda live: torch.full_like(live, 1.7, dtype=torch.float64),
-                "mean": lambda live: 1.7 / live.sum().clamp(min=1) * torch.ones_like(live, dtype=torch.float64)}[reduction]
+    row_grad = {"none": lambda live: per_row.double(),
+                "sum": lambda live: torch.full_like(live, 1.7, dtype=torch.float64),
+                "mean": lambda live: 1.7 / live.sum().clamp(min=1) * live.double()}[reduction]
     want = plain(h, w, t, smoothing, ignore, row_grad)
     loss, lse, total = lm.cross_entropy_forward(h, w, t, ignore, smoothing)
     zroom = want["zerr"].max(1).values + want["z"].abs().max(1).values * 8 * U32
     lse_room = zroom + (want["lse"].abs() + 16) * 8 * U32
     close(lse, want["lse"], lse_room, "lse")
-    close(loss, want["loss"], (2 * lse_room + want["z"].abs().max(1).values * v ** 0.5 * smoothing * 8 * U32) , "loss")
+    close(loss, want["loss"], (2 * lse_room + want["z"].abs().max(1).values * v ** 0.5 * smoothing * 8 * U32), "loss")
     count = int(want["live"].sum())
     assert total[1].item() == count
     sums = want["loss"].sum()
     room = (2 * lse_room).sum() + sums.abs() * 4 * U32
     assert abs(total[0].item() - sums) <= room and abs(total[2].item() - sums / max(count, 1)) <= room / max(count, 1)
-    dh, dw = lm.cross_entropy_backward(per_row if reduction == "none" else one, h, w, t, lse, total, reduction, ignore, smoothing)
+    back = (per_row if reduction == "none" else one, h, w, t, lse, total, reduction, ignore, smoothing)
+    dh, dw = lm.cross_entropy_backward(*back)
     assert dh.dtype == dtype and dw.dtype == dtype
     # Errors of dz: those of p, and the rounding of each to the type that the products take.
     rel = want["zerr"] + lse_room[:, None] + (want["z"] - want["lse"][:, None]).abs() * 2 * U32 + 4 * U32
@@ -84,7 +87,7 @@ def check(h, w, t, smoothing=0.0, ignore=-100, reduction="mean"):
         room = 5 * room2.sqrt() + 40 * U32 * terms
         close(got, ref, room + UNIT[dtype] * (ref.abs() + room) + 1e-30, "gradient")
     assert torch.count_nonzero(dh[~live]) == 0
-    again = lm.cross_entropy_backward(per_row if reduction == "none" else one, h, w, t, lse, total, reduction, ignore, smoothing)
+    again = lm.cross_entropy_backward(*back)
     assert torch.equal(again[0], dh) and torch.equal(again[1], dw)           # the same bits again
 
 
@@ -175,7 +178,8 @@ def test_strides_and_odd_starts(dtype):
 
 
 def test_no_tokens():
-    h, w, t = torch.empty(0, 16, device="cuda"), torch.ones(5, 16, device="cuda"), torch.empty(0, dtype=torch.int64, device="cuda")
+    h, w = torch.empty(0, 16, device="cuda"), torch.ones(5, 16, device="cuda")
+    t = torch.empty(0, dtype=torch.int64, device="cuda")
     loss, lse, total = lm.cross_entropy_forward(h, w, t)
     assert loss.shape == (0,) and total.tolist() == [0.0, 0.0, 0.0]
     dh, dw = lm.cross_entropy_backward(torch.ones((), device="cuda"), h, w, t, lse, total)
@@ -197,7 +201,8 @@ def test_autograd_and_differences():
             x = plain(a, b, tc, 0.1, -100, lambda live: torch.ones_like(live, dtype=torch.float64))
             return x["loss"].sum() / (x["live"].sum() if reduction == "mean" else 1)
         gen = torch.Generator().manual_seed(2)
-        u, v = torch.randn(12, 20, generator=gen, dtype=torch.float64).cuda(), torch.randn(33, 20, generator=gen, dtype=torch.float64).cuda()
+        u = torch.randn(12, 20, generator=gen, dtype=torch.float64).cuda()
+        v = torch.randn(33, 20, generator=gen, dtype=torch.float64).cuda()
         want = slope(lambda x: f(x, wd), hd, u, 1e-5) + slope(lambda x: f(hd, x), wd, v, 1e-5)
         got = (h3.grad.view(12, 20).double() * u).sum() + (w.grad.double() * v).sum()
         assert abs(got - want) <= 1e-5 * (h3.grad.double().norm() * u.norm() + w.grad.double().norm() * v.norm())
@@ -211,7 +216,8 @@ def test_refusals():
     h, w, t = inputs(8, 16, 30, F32)
     for bad in (lambda: lm.cross_entropy_forward(h, w.bfloat16(), t), lambda: lm.cross_entropy_forward(h, w[:, :15], t),
                 lambda: lm.cross_entropy_forward(h, w, t[:7]), lambda: lm.cross_entropy_forward(h, w, t.float()),
-                lambda: lm.cross_entropy_forward(h.half(), w.half(), t), lambda: lm.linear_cross_entropy(h, w, t, reduction="max")):
+                lambda: lm.cross_entropy_forward(h.half(), w.half(), t),
+                lambda: lm.linear_cross_entropy(h, w, t, reduction="max")):
         with pytest.raises(ValueError):
             bad()
     with pytest.raises(lm.JorgeError):

@@ -41,7 +41,8 @@ def plain(x, w, b, eps, dy=None):
 
 def inputs(rows, cols, dtype, ptype, seed=0):
     g = torch.Generator().manual_seed(seed + 31 * rows + cols)
-    x = torch.randn(rows, cols, generator=g) * (0.2 + torch.rand(rows, 1, generator=g)) + torch.randn(rows, 1, generator=g)
+    x = torch.randn(rows, cols, generator=g) * (0.2 + torch.rand(rows, 1, generator=g))
+    x += torch.randn(rows, 1, generator=g)
     return [t.to(d).cuda() for t, d in ((x, dtype), (1 + 0.2 * torch.randn(cols, generator=g), ptype),
                                         (0.3 * torch.randn(cols, generator=g), ptype),
                                         (torch.randn(rows, cols, generator=g), dtype))]

@@ -112,7 +112,8 @@ def test_embedding_past_two_to_the_31_elements():
     assert torch.equal(out, table[tok])
     dtable = lm.embedding_backward(rows, tok, vocab)
     assert torch.equal(dtable[131072], rows[2]) and torch.equal(dtable[135001], rows[4])
-    within(dtable[139999], rows[1].double() + rows[3].double(), rows[1].double().abs() + rows[3].double().abs(), 1, "row")
+    one, two = rows[1].double(), rows[3].double()
+    within(dtable[139999], one + two, one.abs() + two.abs(), 1, "row")
     dtable[tok] = 0
     assert not bool(dtable.view(torch.int32).any())
 

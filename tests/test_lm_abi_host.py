@@ -49,19 +49,20 @@ def test_header_stands_alone(tmp_path, compiler):
 
 def test_layer_norm_refusals(lib):
     def forward(x=A, ldx=8, dtype=0, w=A, b=A, pd=0, y=A, ldy=8, mean=A, rstd=A, rows=4, cols=8, eps=1e-5):
-        return lib.jorge_layernorm_forward(P(x), ldx, dtype, P(w), P(b), pd, P(y), ldy, P(mean), P(rstd), rows, cols, eps,
-                                           None)
+        return lib.jorge_layernorm_forward(P(x), ldx, dtype, P(w), P(b), pd, P(y), ldy, P(mean), P(rstd), rows, cols,
+                                           eps, None)
     for kw, why in ((dict(dtype=2), "type"), (dict(pd=-1), "type"), (dict(rows=-1), "rows"), (dict(cols=0), "cols"),
                     (dict(eps=-1.0), "eps"), (dict(eps=float("nan")), "eps"), (dict(eps=float("inf")), "eps"),
-                    (dict(ldx=7), "stride"), (dict(ldy=7), "stride"), (dict(x=None), "x and y"), (dict(mean=None), "mean"),
+                    (dict(ldx=7), "stride"), (dict(ldy=7), "stride"), (dict(x=None), "x and y"),
+                    (dict(mean=None), "mean"),
                     (dict(x=A + 2), "aligned"), (dict(w=A + 1), "aligned")):
         refused(lib, forward(**kw), INVALID, why)
     refused(lib, forward(cols=16385, ldx=16385, ldy=16385), UNSUPPORTED, "MAX_COLS")
     assert forward(rows=0, x=None, y=None) == 0        # nothing to do
 
     def backward(dy=A, x=A, mean=A, w=A, dx=A, dw=A, rows=4, cols=8, ld=8, ws=A, n=1 << 20):
-        return lib.jorge_layernorm_backward(P(dy), ld, P(x), ld, 0, P(mean), P(A), P(w), 0, P(dx), ld, P(dw), P(A), rows,
-                                            cols, P(ws), n, None)
+        return lib.jorge_layernorm_backward(P(dy), ld, P(x), ld, 0, P(mean), P(A), P(w), 0, P(dx), ld, P(dw), P(A),
+                                            rows, cols, P(ws), n, None)
     for kw, why in ((dict(dy=None), "needed"), (dict(mean=None), "needed"), (dict(ws=None), "workspace"),
                     (dict(ws=A + 16), "workspace"), (dict(n=100), "too small"), (dict(ld=7), "stride")):
         refused(lib, backward(**kw), INVALID, why)
@@ -90,10 +91,11 @@ def test_cross_entropy_refusals(lib):
         return lm.LossShape(tokens, cols, vocab, ldh, ldw, dtype, 0, ignore, smoothing)
 
     def forward(h=A, w=A, t=A, loss=A, total=A, ws=A, size=1 << 30, **kw):
-        return lib.jorge_cross_entropy_forward(ctypes.byref(shape(**kw)), P(h), P(w), P(t), P(loss), P(A), P(total), P(ws),
-                                               size, None)
-    for kw, why in ((dict(tokens=-1), "tokens"), (dict(cols=0), "cols"), (dict(vocab=0), "vocab"), (dict(dtype=4), "type"),
-                    (dict(ldh=7), "stride"), (dict(ldw=7), "stride"), (dict(smoothing=1.01), "smoothing"),
+        return lib.jorge_cross_entropy_forward(ctypes.byref(shape(**kw)), P(h), P(w), P(t), P(loss), P(A), P(total),
+                                               P(ws), size, None)
+    for kw, why in ((dict(tokens=-1), "tokens"), (dict(cols=0), "cols"), (dict(vocab=0), "vocab"),
+                    (dict(dtype=4), "type"), (dict(ldh=7), "stride"), (dict(ldw=7), "stride"),
+                    (dict(smoothing=1.01), "smoothing"),
                     (dict(smoothing=float("nan")), "smoothing"), (dict(h=None), "needed"), (dict(t=A + 4), "aligned"),
                     (dict(w=A + 1), "aligned"), (dict(total=None), "total"), (dict(ws=A + 8), "workspace"),
                     (dict(size=64), "too small")):
@@ -103,9 +105,10 @@ def test_cross_entropy_refusals(lib):
         refused(lib, forward(**kw), UNSUPPORTED, why)
 
     def backward(kind=0, grad=A, lse=A, dh=A, ws=A, size=1 << 30, **kw):
-        return lib.jorge_cross_entropy_backward(ctypes.byref(shape(**kw)), P(grad), kind, P(A), P(A), P(A), P(lse), P(A),
-                                                P(dh), P(A), P(ws), size, None)
-    for kw, why in ((dict(kind=3), "kind"), (dict(kind=-1), "kind"), (dict(grad=None), "needed"), (dict(lse=None), "needed"),
+        return lib.jorge_cross_entropy_backward(ctypes.byref(shape(**kw)), P(grad), kind, P(A), P(A), P(A), P(lse),
+                                                P(A), P(dh), P(A), P(ws), size, None)
+    for kw, why in ((dict(kind=3), "kind"), (dict(kind=-1), "kind"), (dict(grad=None), "needed"),
+                    (dict(lse=None), "needed"),
                     (dict(dh=A + 1), "aligned"), (dict(ws=None), "workspace"), (dict(size=64), "too small")):
         refused(lib, backward(**kw), INVALID, why)
     n = I64()
@@ -163,7 +166,8 @@ def test_workspaces_are_multiples_of_256(lib):
 
 def test_operators_need_a_gpu_tensor():
     import torch
-    for call in (lambda: lm.layer_norm_forward(torch.ones(2, 3)), lambda: lm.embedding_forward(torch.zeros(2).long(), torch.ones(2, 3)),
+    for call in (lambda: lm.layer_norm_forward(torch.ones(2, 3)),
+                 lambda: lm.embedding_forward(torch.zeros(2).long(), torch.ones(2, 3)),
                  lambda: lm.AdamW([torch.ones(3)])):
         with pytest.raises(ValueError, match="CUDA"):
             call()
