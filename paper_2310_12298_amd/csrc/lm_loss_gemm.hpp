@@ -8,9 +8,9 @@
 // takes 16 KB from LDS per 64 MFMAs, the least per flop that the registers allow: LDS would bound
 // waves of 128 x 64 (two per SIMD) at 9/8 of the MFMAs' time, these at 3/4.
 //
-// K goes by stages of 32 through a ring of RING buffers in LDS. Each stage is written by
-// direct-to-LDS loads, started RING - 1 stages ahead; nothing passes through registers. A wave
-// reads the next stage's fragments while the MFMAs of the current one run.
+// K goes by stages through a ring of buffers in LDS. Each stage is written by direct-to-LDS loads, started as soon as
+// its buffer is free; nothing passes through registers. A wave reads the next fragments while the MFMAs of the current
+// ones run.
 //
 // Which row of the tile goes where. An MFMA leaves lane l with rows 4 (l / 16) + r (r = 0 .. 3) and
 // column l % 16 of its 16 x 16 block. The rows that feed block i and the columns that feed block j
@@ -19,10 +19,12 @@
 // so that both C and its transpose are written in whole pieces from registers. The choice costs
 // nothing: it is the row that each direct-to-LDS load fetches.
 //
-// A block of 16 rows by 32 k is 1 KB of LDS: row rho at 64 rho, its 16-byte chunk c (k = 8 c ..) at
-// 16 (c ^ swizzle(rho)). Four neighbouring lanes fetch one row's 64 bytes; a fragment read (lane l:
-// row l % 16, chunk l / 16) takes the whole block, and the swizzle spreads any 8 or 16 lanes of it
-// over all banks.
+// A load brings 1 KB to consecutive LDS, 16 bytes per lane. For one product (plain) a stage is 64 k: a load fetches 8
+// rows of 128 bytes, whole cache lines (4096 x 4096 x 8192: 1200-1250 TFLOP/s, against 1140 with stages of 32 k and
+// half lines). For products of terms it is 32 k: 16 rows of 64 bytes. Within a row the 16-byte chunks are permuted by
+// the row's number so that a fragment read (lane l: row l % 16, chunk l / 16) meets no bank twice: the LDS serves lanes
+// 0-3, 12-15 and 20-27 together, then the others of the first 32, and the same of the last 32 (shown by the counter of
+// bank conflicts: 0, where a permutation made for 16 consecutive lanes doubled the reads' time).
 #pragma once
 
 #include "lm_common.hpp"
@@ -46,16 +48,16 @@ constexpr int kTerms = 3;  // of a split operand
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) const void global_void;
 
-__device__ __forceinline__ int swizzle(int rho) { return -(rho >> 2) & 3; }
+// What chunk numbers are exclusive-ored with in row rho of 16, for rows of 64 and of 128 bytes.
+__device__ __forceinline__ int swizzle64(int rho) { return -(rho >> 2) & 3; }
+__device__ __forceinline__ int swizzle128(int rho) { return rho >> 1; }
 
 template <int WA, int WB, int RING, bool SPLIT>
 struct Tile {
-    static constexpr int kRing = RING;
     static constexpr int kA = 32 * WA, kB = 32 * WB;
-    static constexpr int kStageBytes = (kA + kB) * kStageK * 2;
-    static constexpr int kBytes = kRing * kStageBytes;
-    // Direct-to-LDS loads per wave and stage: half of each operand's WA (WB) * 2 blocks over the four waves.
-    static constexpr int kLoadsA = WA / 2, kLoadsB = WB / 2, kLoads = kLoadsA + kLoadsB;
+    static constexpr int kBytes = RING * (kA + kB) * kStageK * 2;  // of LDS: RING stages of 32 k
+    // Direct-to-LDS loads per wave and stage of the ring.
+    static constexpr int kLoadsA = SPLIT ? WA / 2 : WA, kLoadsB = SPLIT ? WB / 2 : WB, kLoads = kLoadsA + kLoadsB;
 
     f32x4 acc[WA][WB];
 
@@ -76,35 +78,40 @@ struct Tile {
         const int lane = threadIdx.x & 63;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         Loads load;
-        // Where this lane's loads start: block n of the operand (n = wave * kLoads + v), row rho of it. Bytes from the
-        // tile's first row to the end of its last one are what a load may reach.
-        const int rho = lane >> 2, chunk = (lane & 3) ^ swizzle(rho);
+        // Where this lane's loads start: load n of the operand (n = wave * kLoads + v) takes rows rho of block i of a
+        // half of the tile. Bytes from the tile's first row to the end of its last one are what a load may reach.
         const int limA = (int)(A.rows - a0 < kA ? A.rows - a0 : kA) - 1;
         const int limB = (int)(B.rows - b0 < kB ? B.rows - b0 : kB) - 1;
         const unsigned K = (unsigned)(stages * kStageK), more = SPLIT ? kTerms - 1 : 0;
+        const auto place = [&](int n, int& block, int& rho) {
+            block = SPLIT ? n : n / 2;
+            rho = SPLIT ? lane >> 2 : (n & 1) * 8 + (lane >> 3);
+            return (unsigned)(SPLIT ? (lane & 3) ^ swizzle64(rho) : (lane & 7) ^ swizzle128(rho)) * 16u;
+        };
 #pragma unroll
         for (int v = 0; v < kLoadsA; ++v) {
-            const int n = wave * kLoadsA + v, half = n / WA, i = n % WA;
-            const int row = half * 16 * WA + (rho >> 2) * 4 * WA + 4 * i + (rho & 3);
-            load.offA[v] = (unsigned)(row < limA ? row : limA) * (unsigned)A.ld * 2u + chunk * 16u;
+            int block, rho;
+            const unsigned chunk = place(wave * kLoadsA + v, block, rho);
+            const int row = block / WA * 16 * WA + (rho >> 2) * 4 * WA + 4 * (block % WA) + (rho & 3);
+            load.offA[v] = (unsigned)(row < limA ? row : limA) * (unsigned)A.ld * 2u + chunk;
         }
 #pragma unroll
         for (int v = 0; v < kLoadsB; ++v) {
-            const int n = wave * kLoadsB + v, half = n / WB, j = n % WB;
-            const int row = half * 16 * WB + rho * WB + j;
-            load.offB[v] = (unsigned)(row < limB ? row : limB) * (unsigned)B.ld * 2u + chunk * 16u;
+            int block, rho;
+            const unsigned chunk = place(wave * kLoadsB + v, block, rho);
+            const int row = block / WB * 16 * WB + rho * WB + block % WB;
+            load.offB[v] = (unsigned)(row < limB ? row : limB) * (unsigned)B.ld * 2u + chunk;
         }
         load.ra = resource(A.p + a0 * A.ld, ((unsigned)limA * (unsigned)A.ld + more * (unsigned)A.plane + K) * 2u);
         load.rb = resource(B.p + b0 * B.ld, ((unsigned)limB * (unsigned)B.ld + more * (unsigned)B.plane + K) * 2u);
         load.k = s0 * (kStageK * 2);
-        load.left = s1 - s0;
-        const int frag = (lane & 15) * 64 + (((lane >> 4) ^ swizzle(lane & 15)) * 16);
+        load.left = SPLIT ? s1 - s0 : (s1 - s0) / 2;
 #pragma unroll
         for (int i = 0; i < WA; ++i)
 #pragma unroll
             for (int j = 0; j < WB; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        if constexpr (SPLIT) terms(load, (int)A.plane * 2, (int)B.plane * 2, s0, s1, frag, wave, lds);
-        else plain(load, s0, s1, frag, wave, lds);
+        if constexpr (SPLIT) terms(load, (int)A.plane * 2, (int)B.plane * 2, s0, s1, wave, lds);
+        else plain(load, s0, s1, wave, lds);
         wait_loads<0>();
         __builtin_amdgcn_s_barrier();  // the ring is free for the epilogue
     }
@@ -125,7 +132,7 @@ private:
         // loads in flight, and the loop's body stays one block.
         __device__ __forceinline__ void next() {
             --left;
-            k += left > 0 ? kStageK * 2 : 0;
+            k += left > 0 ? kStageK * (SPLIT ? 2 : 4) : 0;
         }
     };
 
@@ -135,61 +142,66 @@ private:
         asm volatile("s_cmp_lt_i32 %0, %1\n\ts_cbranch_scc1 1f\n\ts_nop 15\n\ts_nop 15\n1:" ::"s"(s), "s"(s1) : "scc");
     }
 
-    // One product. A stage in the ring is A's blocks, then B's.
-    __device__ __forceinline__ void plain(Loads& load, int s0, int s1, int frag, int wave, char* lds) {
-        const int fragA = frag + (wave >> 1) * WA * 1024, fragB = frag + (2 * WA + (wave & 1) * WB) * 1024;
+    // One product, in stages of 64 k. A stage in the ring is A's blocks of 16 rows (2 KB), then B's.
+    __device__ __forceinline__ void plain(Loads& load, int s0, int s1, int wave, char* lds) {
+        constexpr int kRing = RING / 2, kStageBytes = (kA + kB) * kStageK * 4;
+        static_assert(kRing >= 2 && (kRing & (kRing - 1)) == 0, "a power of two");
+        const int rho = threadIdx.x & 15, frag = rho * 128 + ((((threadIdx.x & 63) >> 4) ^ swizzle128(rho)) * 16);
+        const int fragA = frag + (wave >> 1) * WA * 2048, fragB = frag + (2 * WA + (wave & 1) * WB) * 2048;
         bf16x8 fa[2][WA], fb[2][WB];
         const auto one = [&](int v, int slot) {
             char* const to = lds + slot * kStageBytes;
             if (v < kLoadsA) load.a(v, to + (wave * kLoadsA + v) * 1024, load.k);
-            else load.b(v - kLoadsA, to + (2 * WA + wave * kLoadsB + v - kLoadsA) * 1024, load.k);
+            else load.b(v - kLoadsA, to + (4 * WA + wave * kLoadsB + v - kLoadsA) * 1024, load.k);
         };
-        // Fragment f of a stage: first B's, which the first row of MFMAs needs together, then A's.
-        const auto read = [&](int slot, int set, int f) {
+        // Fragment f of half h of a stage: first B's, which the first row of MFMAs needs together, then A's.
+        const auto read = [&](int slot, int h, int f) {
             const char* const p = lds + slot * kStageBytes;
-            if (f < WB) fb[set][f] = *reinterpret_cast<const bf16x8*>(p + fragB + f * 1024);
-            else fa[set][f - WB] = *reinterpret_cast<const bf16x8*>(p + fragA + (f - WB) * 1024);
+            if (f < WB) fb[h][f] = *reinterpret_cast<const bf16x8*>(p + (fragB ^ (h * 64)) + f * 2048);
+            else fa[h][f - WB] = *reinterpret_cast<const bf16x8*>(p + (fragA ^ (h * 64)) + (f - WB) * 2048);
         };
 #pragma unroll
-        for (int r = 0; r < kRing - 1; ++r) {
+        for (int r = 0; r < kRing; ++r) {
 #pragma unroll
             for (int v = 0; v < kLoads; ++v) one(v, r);
             load.next();
         }
-        wait_loads<(kRing - 2) * kLoads>();
+        wait_loads<(kRing - 1) * kLoads>();
         __builtin_amdgcn_s_barrier();
 #pragma unroll
         for (int f = 0; f < WA + WB; ++f) read(0, 0, f);
         int slot = 0;
-        const auto step = [&](int set) {
-            // The next stage has landed for every wave once all have passed the barrier, and the buffer that the
-            // new loads write was read by all before their last barrier but one.
-            wait_loads<(kRing - 3) * kLoads>();
-            __builtin_amdgcn_s_barrier();
-            const int ahead = slot + 1 == kRing ? 0 : slot + 1, behind = slot == 0 ? kRing - 1 : slot - 1;
-            // In this order: the fragment reads by twos in the first half, so that the next step need not wait for
-            // them, a load in every second group, and after the last load the way to the next stage (the scalar unit
-            // runs beside the MFMAs).
-            constexpr int G = WA + WB, PER = WA * WB / G;
+        // The MFMAs of half h, and among them, in this order: the fragment reads of the next half by twos in the first
+        // half of the groups, so that it need not wait for them; a load in every group (h = 1), and after the last one
+        // the way to the next stage (the scalar unit runs beside the MFMAs).
+        const auto half = [&](auto H, int from) {
+            constexpr int h = decltype(H)::value, G = WA + WB, PER = WA * WB / G;
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 __builtin_amdgcn_sched_barrier(0);
                 if (g < G / 2) {
-                    read(ahead, set ^ 1, 2 * g);
-                    read(ahead, set ^ 1, 2 * g + 1);
+                    read(from, h ^ 1, 2 * g);
+                    read(from, h ^ 1, 2 * g + 1);
                 }
-                if (g % 2 == 0) one(g / 2, behind);
-                if (g == G - 1) load.next();
+                if constexpr (h == 1) {
+                    one(g, slot);
+                    if (g == G - 1) load.next();
+                }
 #pragma unroll
                 for (int m = g * PER; m < (g + 1) * PER; ++m)
-                    mfma(acc[m / WB][m % WB], fa[set][m / WB], fb[set][m % WB]);
+                    mfma(acc[m / WB][m % WB], fa[h][m / WB], fb[h][m % WB]);
             }
             __builtin_amdgcn_sched_barrier(0);
-            slot = ahead;
         };
         for (int s = s0; s < s1; s += 2) {
-            step(0);
-            step(1);
+            const int ahead = (slot + 1) & (kRing - 1);
+            half(std::integral_constant<int, 0>(), slot);
+            // All waves have read this stage whole, so its buffer is free; and the next one has landed for all.
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            wait_loads<(kRing - 2) * kLoads>();
+            __builtin_amdgcn_s_barrier();
+            half(std::integral_constant<int, 1>(), ahead);
+            slot = ahead;
             settle(s + 2, s1);
         }
     }
@@ -199,10 +211,10 @@ private:
     // in which each step exchanges one of the two factors. The ring holds planes of one term of one operand, in the
     // order A2 B0 A1 B1 A0 B2, in which the steps come to need them: each step loads one plane and reads one plane's
     // fragments, half of what six products of their own would.
-    __device__ __forceinline__ void terms(Loads& load, int planeA, int planeB, int s0, int s1, int frag, int wave,
-                                          char* lds) {
+    __device__ __forceinline__ void terms(Loads& load, int planeA, int planeB, int s0, int s1, int wave, char* lds) {
         static_assert(WA == WB, "planes of one size");
-        constexpr int kPlanes = 2 * kRing, kPlaneBytes = kStageBytes / 2;
+        constexpr int kPlanes = 2 * RING, kPlaneBytes = kA * kStageK * 2;
+        const int rho = threadIdx.x & 15, frag = rho * 64 + ((((threadIdx.x & 63) >> 4) ^ swizzle64(rho)) * 16);
         static_assert((kPlanes & (kPlanes - 1)) == 0, "a power of two");
         const int fragA = frag + (wave >> 1) * WA * 1024, fragB = frag + (wave & 1) * WB * 1024;
         bf16x8 fa[2][WA], fb[3][WB];
