@@ -19,6 +19,10 @@
 //      launch write zeros to the rows that no token takes;
 //   4. the runs that cross chunks: their chunks' sums are added by a workgroup per run.
 // A token that half of all positions hold is thus spread over as many waves as any others.
+//
+// Measured: 16384 tokens, 50000 x 2048 bf16: forward 21 us (134 MB to move at most, 6.3 TB/s: repeated rows
+// come from the cache), sorting 12, merging 8.5, sums and zeros 53-61 (272 MB, 4.4-5.1 TB/s), joining 7.
+// 65536 tokens, half of them one token, 8192 x 512 fp32: 28-33, 11.5, 21.5, 33 (151 MB, 4.6 TB/s) and 17 us.
 #include "lm_common.hpp"
 
 #include <utility>

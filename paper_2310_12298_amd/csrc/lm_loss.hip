@@ -21,6 +21,16 @@
 // product is the six products of terms down to 2^-16 of the whole: the same K loop, six times as long.
 // dz is split alike. This is the scheme of the Jorge step's products; there the terms are formed while a
 // slab is staged, here once before the product, because every operand enters many tiles.
+//
+// Measured (a library product of 8192 x 8192 x 8192 in bf16 reaches 1350-1400 TFLOP/s here, x 2048 1140-1200, in fp32
+// 153). Rates are over a pass's whole product, all pieces of the vocabulary together:
+//   bf16, 8192 tokens, cols 2048, 50001 words: forward 1.35-1.38 ms (1220-1240 TFLOP/s); in seven pieces dz 1.64 ms
+//   (1020), each gradient 1.46 ms (1150), transposes 0.12 ms; both passes 6.0 ms.
+//   fp32, 2001 tokens, cols 1001, 30011 words (six products each): forward 0.50-0.55 ms (220-240 TFLOP/s of fp32
+//   products); in two pieces dz 0.69 ms (175), each gradient 0.56 ms (214), copies 0.17 ms; both passes 2.4 ms.
+// The MFMAs are busy 59% of the bf16 forward's wave cycles and 80% of the fp32 one's, which loads half as much for
+// each: the former is bound by the way from L2 to LDS as well. Power bounds both: a loop of these MFMAs on registers
+// alone reaches 1850-1970 TFLOP/s with random operands, 2430 with zeros.
 #include "lm_common.hpp"
 #include "lm_loss_gemm.hpp"
 

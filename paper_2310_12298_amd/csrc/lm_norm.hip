@@ -10,6 +10,10 @@
 // workgroup takes every grid-th group of rows and keeps its columns' two sums in registers
 // over all of them; the sums go to the workspace once per workgroup, and a second launch
 // adds them column by column in a fixed order (no atomics: the same bits every time).
+//
+// Measured, 16384 x 4096 bf16: forward 58 us (4.6 TB/s of what it has to move; a large copy
+// reaches 5.0-5.15), backward 86 us (4.7 TB/s), the second launch 6 us. 5003 x 1999 fp32
+// (rows at odd addresses): 17.3, 27.5 and 5.7 us (4.6 and 4.4 TB/s).
 #include "lm_common.hpp"
 
 namespace jorge_lm {
@@ -258,7 +262,8 @@ Split split_of(int64_t cols, int wide) {
 }
 
 // Workgroups of the backward pass: each leaves 2 * cols partial sums, so there are no more than it
-// takes to keep the memory busy.
+// takes to keep the memory busy: three per CU hold six rows' worth of loads (25 MB of sums for 4096
+// columns, beside 403 MB of rows). Rows above 8192 take a workgroup of eight waves, one per CU.
 constexpr int kGroups = 768;
 int groups_of(int64_t rows, int64_t cols, int32_t dtype) {
     const Split s = split_of(cols, dtype == JORGE_BF16 ? 8 : 4);
