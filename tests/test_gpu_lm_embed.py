@@ -62,6 +62,14 @@ def test_gradient(kind, n, vocab, cols, dtype):
     check_grad(some_tokens(kind, n, vocab), vocab, cols, dtype)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cols", [1, 2, 4, 5, 9, 16, 23, 33, 64, 127, 128, 129, 256, 257])
+def test_rows_without_tokens(cols, dtype):
+    """A wave looks for the tokens of 64 rows: vocabularies that end inside them, and rows of every width."""
+    for n in (3, 1500, 2048, 2049):
+        check_grad(some_tokens("uniform", n, 200 if n < 100 else 5003), 200 if n < 100 else 5003, cols, dtype)
+
+
 @pytest.mark.parametrize("kind", ["uniform", "half", "one"])
 def test_gradient_over_several_tiles_and_merges(kind):
     check_grad(some_tokens(kind, 16384 * 3 + 77, 70000), 70000, 4, F32)
