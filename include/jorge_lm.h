@@ -144,9 +144,11 @@ jorge_status jorge_cross_entropy_forward(const jorge_loss_shape* shape, const vo
  *   dz_iv = g_i (p_iv - (1 - e) [v = target_i] - e / vocab),
  *   dhidden = dz weight,  dweight = dz^T hidden.
  * dhidden, dweight: written whole; either may be NULL. bfloat16 inputs: dz (without g where that is one
- * number) is rounded to bfloat16 for the two products, whose sums are fp32. fp32 inputs: every product is
- * formed from three-term bfloat16 splits as the Jorge step's are (jorge.h), dz included: values above 3.39e38
- * count as infinite, and a sum over K elements takes 6 K / 32 roundings of its fp32 accumulator. */
+ * number) is rounded to bfloat16 for the two products, whose sums are fp32: rows of dweight of words that are
+ * no row's target, sums of such rounded terms alone, err by some 2.2e-3 of their size instead of the 1.7e-3 of
+ * their own rounding; dhidden and the other rows by 1.7e-3. fp32 inputs: every product is formed from three-term
+ * bfloat16 splits as the Jorge step's are (jorge.h), dz included: values above 3.39e38 count as infinite, and a
+ * sum over K elements takes 6 K / 32 roundings of its fp32 accumulator. */
 jorge_status jorge_cross_entropy_backward(const jorge_loss_shape* shape, const float* grad, int32_t kind,
                                           const void* hidden, const void* weight, const int64_t* targets,
                                           const float* lse, const float* total, void* dhidden, void* dweight,

@@ -1,0 +1,38 @@
+"""Cross entropy over a vocabulary on the GPU where it is called in less usual ways, against the formula in 64 bits or
+against the usual call's bits."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2310_12298_amd import lm  # noqa: E402
+from test_gpu_lm_loss import BF16, F32, inputs, plain  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+def one(value=1.0):
+    return torch.tensor(value, device="cuda")
+
+
+def relative(got, want):
+    return ((got.double() - want).norm() / want.norm()).item()
+
+
+@pytest.mark.parametrize("dtype,of_targets,of_others", [
+    # A rounding to eight bits errs evenly within 2^-8 of the power of two at or below a value: 2^-8 / sqrt(3) of it at
+    # most. Rows of words without a target have one such error in each term of their sums, independently, and one more.
+    (BF16, 2 ** -8 / 3 ** 0.5, 2 ** -8 * (2 / 3) ** 0.5),
+    # Three-term splits: the sums' own roundings, independent: sqrt(6 512 / 32) of a logit of size two, and
+    # sqrt(6 8192 / 32) of dhidden's sums, 1.2e-6 and 2.3e-6; twice that together.
+    (F32, 5e-6, 5e-6)])
+def test_whom_the_rounding_of_dz_costs(dtype, of_targets, of_others):
+    h, w, t = inputs(1024, 512, 8192, dtype, ignored=0.0)
+    t = (t % 500)                                            # few words are targets
+    loss, lse, total = lm.cross_entropy_forward(h, w, t)
+    dh, dw = lm.cross_entropy_backward(one(), h, w, t, lse, total)
+    want = plain(h, w, t, 0.0, -100, lambda live: torch.full_like(live, 1 / 1024, dtype=torch.float64))
+    hit = torch.zeros(8192, dtype=torch.bool, device="cuda")
+    hit[t] = True
+    assert relative(dh, want["dh"]) < of_targets
+    assert relative(dw[hit], want["dw"][hit]) < of_targets
+    assert relative(dw[~hit], want["dw"][~hit]) < of_others
