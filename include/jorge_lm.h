@@ -199,9 +199,10 @@ jorge_status jorge_gradient_norm_workspace(const jorge_adamw_tensor* tensors, in
 jorge_status jorge_gradient_norm(const jorge_adamw_tensor* tensors, int32_t n, double max_norm, float* out,
                                  void* workspace, int64_t workspace_bytes, void* hip_stream);
 
-/* Step t >= 1 of n tensors. tensors, moments: host, read before the call returns. clip: one float, the factor
- * of the gradients (out + 1 of jorge_gradient_norm), or NULL for 1. lr, eps, weight_decay >= 0, 0 <= beta1,
- * beta2 < 1, all finite. Scalars are formed in fp64 and enter the step as floats. */
+/* Step t >= 1 of n tensors: t counts a tensor's own steps, and tensors that have taken different numbers of them
+ * go in calls of their own (with the same moments). tensors, moments: host, read before the call returns. clip: one
+ * float, the factor of the gradients (out + 1 of jorge_gradient_norm), or NULL for 1. lr, eps, weight_decay >= 0,
+ * 0 <= beta1, beta2 < 1, all finite. Scalars are formed in fp64 and enter the step as floats. */
 jorge_status jorge_adamw_step(const jorge_adamw_tensor* tensors, int32_t n, const jorge_adamw_moments* moments,
                               int64_t t, double lr, double beta1, double beta2, double eps, double weight_decay,
                               const float* clip, void* hip_stream);

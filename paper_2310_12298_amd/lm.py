@@ -373,8 +373,9 @@ class AdamW:
     bits: 32, or 8 for moments of a byte per element with a scale per block of 256, rounded by random
     bits made from seed, the step and the element's place (include/jorge_lm.h has the format). moments:
     existing flat buffers to take over instead of zeros, as `moments` of another AdamW over tensors of
-    the same sizes. t: the number of steps taken. norm: after a step with max_norm, the gradients' global
-    norm before clipping (a device tensor).
+    the same sizes. steps: of each tensor, the steps it has taken; a tensor without a gradient takes none, and
+    its bias corrections (and random bits) go by its own count. t: the most of them; setting it sets them all.
+    norm: after a step with max_norm, the gradients' global norm before clipping (a device tensor).
     """
 
     def __init__(self, params, bits=32, seed=0, moments=None):
@@ -411,8 +412,21 @@ class AdamW:
         self._moments = AdamWMoments(*(_ptr(self.moments.get(k)) for k in (
             "exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale")), total, self.bits, self.seed)
 
+    @property
+    def t(self):
+        return self._t if self._steps is None else max(self._steps)
+
+    @t.setter
+    def t(self, value):
+        self._t, self._steps = int(value), None               # _steps: one count each, where they differ
+
+    @property
+    def steps(self):
+        return [self._t] * len(self.params) if self._steps is None else list(self._steps)
+
     def _gradients(self, grads):
-        """Puts the gradients' pointers into the table; a parameter without one (None) takes no part."""
+        """Puts the gradients' pointers into the table; a parameter without one (None) takes no part. Returns
+        temporaries to keep until the launch, and whether every parameter takes part."""
         if len(grads) != len(self.params):
             raise ValueError(f"grads: expected {len(self.params)} tensors, got {len(grads)}")
         keep, ptrs, numel = [], [], self._numel
@@ -431,13 +445,14 @@ class AdamW:
             ptrs.append(g.data_ptr())
         self._table["grad"] = ptrs
         self._table["numel"] = numel
-        return keep
+        return keep, numel is self._numel
 
     def step(self, grads=None, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, max_norm=0.0, clip=None):
         """One step from the gradients (default: each parameter's .grad; None entries are left as they
         are). max_norm > 0 scales all gradients to that global norm if theirs is larger; clip: the factor
         itself, one fp32 number on the device (of another gradient_norm call)."""
-        keep = self._gradients([p.grad for p in self.params] if grads is None else grads)
+        grads = [p.grad for p in self.params] if grads is None else grads
+        keep, whole = self._gradients(grads)
         for p, (dtype, shape, stride, device) in zip(self.params, self._layout):
             if p.dtype is not dtype or p.get_device() != device or p.shape != shape or p.stride() != stride:
                 raise ValueError("a parameter's type, device, shape or layout has changed since it was handed over")
@@ -449,15 +464,35 @@ class AdamW:
             self.norm, clip = out[0], out[1:]
         elif clip is not None and (_cuda(clip, "clip", (torch.float32,)).numel() != 1):
             raise ValueError("clip: one number is needed")
-        _check(self.lib, self.lib.jorge_adamw_step(self._tensors, len(self.params), ctypes.byref(self._moments),
-                                                   self.t + 1, float(lr), float(beta1), float(beta2), float(eps),
-                                                   float(weight_decay), _ptr(clip), _stream()))
-        self.t += 1
+        hyper = (float(lr), float(beta1), float(beta2), float(eps), float(weight_decay), _ptr(clip), _stream())
+        if whole and self._steps is None:
+            self._launch(self._t + 1, hyper)
+            self._t += 1
+        else:
+            steps = self.steps
+            given = [i for i, g in enumerate(grads) if g is not None]
+            counts = sorted({steps[i] for i in given}) or [self.t]
+            if len(counts) > 1:
+                numel = self._table["numel"].copy()
+            for t in counts:                                  # a call for each count of steps among the tensors
+                if len(counts) > 1:
+                    part = [i for i in given if steps[i] == t]
+                    self._table["numel"] = 0
+                    self._table["numel"][part] = numel[part]
+                self._launch(t + 1, hyper)
+            for i in given:
+                steps[i] += 1
+            self._t, self._steps = (steps[0], None) if len(set(steps)) == 1 else (None, steps)
         del keep
+
+    def _launch(self, t, hyper):
+        """Step t of the table's tensors."""
+        _check(self.lib, self.lib.jorge_adamw_step(self._tensors, len(self.params), ctypes.byref(self._moments), t,
+                                                   *hyper))
 
     def gradient_norm(self, grads=None, max_norm=0.0):
         """[norm, clip factor] of the gradients on the device, without a step (see gradient_norm)."""
-        keep = self._gradients([p.grad for p in self.params] if grads is None else grads)
+        keep, _ = self._gradients([p.grad for p in self.params] if grads is None else grads)
         out = _gradient_norm(self.lib, self._tensors, len(self.params), max_norm)
         del keep
         return out
@@ -489,14 +524,20 @@ class AdamW:
                                                             int(self.blocks[-1]), v.data_ptr(), _stream()))
 
     def state_dict(self):
-        return {"t": self.t, "bits": self.bits, "seed": self.seed, **{k: v.cpu() for k, v in self.moments.items()}}
+        return {"t": self.t, "steps": self.steps, "bits": self.bits, "seed": self.seed,
+                **{k: v.cpu() for k, v in self.moments.items()}}
 
     def load_state_dict(self, sd):
         if sd["bits"] != self.bits or any(sd[k].shape != v.shape for k, v in self.moments.items()):
             raise ValueError("the state is of another set of tensors or of other bits")
+        steps = [int(t) for t in sd.get("steps", [])]         # absent: all tensors took t steps
+        if steps and len(steps) != len(self.params):
+            raise ValueError("the state is of another set of tensors or of other bits")
         for k, v in self.moments.items():
             v.copy_(sd[k])
         self.t, self.seed = int(sd["t"]), int(sd["seed"])
+        if len(set(steps)) > 1:
+            self._t, self._steps = None, steps
         self._moments.seed = self.seed
 
 

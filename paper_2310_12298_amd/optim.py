@@ -192,7 +192,8 @@ class AdamWOptimizer(torch.optim.Optimizer):
     Hyperparameters (per group): lr, betas, eps, weight_decay (decoupled, lr-scaled). max_norm > 0 clips
     the gradients of all groups together by their global norm, which `norm` then holds on the device.
     bits: 32, or 8 for moments of one byte per element; seed: of their random rounding. The moments of a
-    group live in its handle's flat buffers. A parameter without a gradient is left as it is.
+    group live in its handle's flat buffers. A parameter without a gradient is left as it is: moments, weight and
+    the count of its steps, by which its bias corrections go.
     """
 
     def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,

@@ -1,0 +1,98 @@
+"""AdamW on the GPU as programs meet it: parameters whose gradients come and go, states, autograd, refused handles."""
+import io
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from lm_check import within  # noqa: E402
+from paper_2310_12298_amd import lm  # noqa: E402
+from paper_2310_12298_amd.optim import AdamWOptimizer  # noqa: E402
+from test_gpu_lm_adamw import BF16, F32, HP, flat, formula, tensors  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+SIZES = [300, 5, 1000, 257, 64]
+# Which tensors have a gradient at each step: the second's come late, the third's every other time, the fourth's once.
+GIVEN = [(0, 4), (0, 2, 4), (0, 4), (0, 1, 2, 4), (0, 1, 4), (), (0, 1, 2, 3, 4), (1, 3)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("bits", [32, 8])
+def test_each_parameter_counts_its_own_steps(bits, dtype):
+    params = tensors(SIZES, dtype)
+    opt, taken = lm.AdamW(params, bits=bits, seed=3), [0] * len(SIZES)
+    for k, given in enumerate(GIVEN):
+        grads = [g if i in given else None for i, g in enumerate(tensors(SIZES, dtype, seed=k + 1, scale=0.1))]
+        old = [p.clone() for p in params]
+        p, g = flat(opt, params), flat(opt, [torch.zeros_like(q) if x is None else x for q, x in zip(params, grads)])
+        m, v = (x.double().cpu() for x in opt.moment_values())
+        opt.step(grads, **HP)
+        after = [x.double().cpu() for x in opt.moment_values()]
+        for i, b in enumerate(opt.blocks[:-1]):
+            s = slice(b * lm.BLOCK, b * lm.BLOCK + SIZES[i])
+            if i in given:
+                taken[i] += 1
+                p1, _, _, _, _, size = formula(p[s], g[s], m[s], v[s], taken[i], **HP)
+                within(params[i], p1, size, 24, f"step {k}, parameter {i}")
+            else:
+                assert torch.equal(params[i], old[i])
+                assert torch.equal(after[0][s], m[s]) and torch.equal(after[1][s], v[s])
+        assert opt.steps == taken and opt.t == max(taken)
+
+
+def test_optimizer_agrees_with_torch_where_gradients_come_late():
+    def make():
+        torch.manual_seed(1)
+        return [torch.nn.Parameter(torch.randn(n, device="cuda")) for n in SIZES]
+    a, b = make(), make()
+    opt = AdamWOptimizer([{"params": a[:3]}, {"params": a[3:]}], lr=1e-2, weight_decay=0.1, max_norm=1.0)
+    ref = torch.optim.AdamW([{"params": b[:3]}, {"params": b[3:]}], lr=1e-2, weight_decay=0.1)
+    for k, given in enumerate(GIVEN):
+        for i, (p, q) in enumerate(zip(a, b)):
+            gen = torch.Generator(device="cuda").manual_seed(10 * k + i)
+            p.grad = torch.randn(p.shape, generator=gen, device="cuda") if i in given else None
+            q.grad = None if p.grad is None else p.grad.clone()
+        opt.step()
+        torch.nn.utils.clip_grad_norm_(b, 1.0)
+        ref.step()
+        for p, q in zip(a, b):
+            assert torch.allclose(p, q, rtol=1e-5, atol=1e-6)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_counts_of_steps_are_part_of_the_state(bits):
+    params = tensors(SIZES, F32)
+    opt = lm.AdamW(params, bits=bits, seed=3)
+
+    def step(o, k, given):
+        o.step([g if i in given else None for i, g in enumerate(tensors(SIZES, F32, seed=k))], **HP)
+    step(opt, 1, (0, 1))
+    step(opt, 2, (0, 4))
+    buf = io.BytesIO()
+    torch.save(opt.state_dict(), buf)
+    buf.seek(0)
+    twin = lm.AdamW([p.clone() for p in params], bits=bits)
+    twin.load_state_dict(torch.load(buf, weights_only=True))
+    assert twin.steps == [2, 1, 0, 0, 1] and twin.t == 2
+    for o in (opt, twin):
+        step(o, 3, (0, 1, 2, 3, 4))
+    for x, y in zip(opt.params, twin.params):
+        assert torch.equal(x, y)
+    old = opt.state_dict()
+    del old["steps"]                                          # a state that holds one count for all
+    twin.load_state_dict(old)
+    assert twin.steps == [3] * 5
+    short = opt.state_dict()
+    short["steps"] = short["steps"][:4]
+    with pytest.raises(ValueError):
+        twin.load_state_dict(short)
+
+
+def test_a_step_without_any_gradient_checks_and_changes_nothing():
+    params = tensors(SIZES, F32)
+    opt, old = lm.AdamW(params), [p.clone() for p in params]
+    opt.step([None] * len(SIZES), **HP)
+    with pytest.raises(lm.JorgeError):
+        opt.step([None] * len(SIZES), lr=-1.0)
+    assert opt.t == 0 and all(torch.equal(x, y) for x, y in zip(params, old))
