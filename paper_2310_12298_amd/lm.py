@@ -483,6 +483,9 @@ class AdamW:
             for i in given:
                 steps[i] += 1
             self._t, self._steps = (steps[0], None) if len(set(steps)) == 1 else (None, steps)
+        # What autograd saved of a parameter no longer holds: a backward pass that needs it has to say so.
+        torch.autograd.graph.increment_version(
+            self.params if whole else [p for p, g in zip(self.params, grads) if g is not None])
         del keep
 
     def _launch(self, t, hyper):

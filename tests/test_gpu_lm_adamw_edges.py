@@ -96,3 +96,25 @@ def test_a_step_without_any_gradient_checks_and_changes_nothing():
     with pytest.raises(lm.JorgeError):
         opt.step([None] * len(SIZES), lr=-1.0)
     assert opt.t == 0 and all(torch.equal(x, y) for x, y in zip(params, old))
+
+
+@pytest.mark.parametrize("optimizer", [False, True])
+def test_a_step_between_forward_and_backward_is_noticed(optimizer):
+    w, u = (torch.nn.Parameter(torch.randn(8, 8, device="cuda")) for _ in range(2))
+    x = torch.randn(8, 8, device="cuda", requires_grad=True)
+    opt = AdamWOptimizer([w, u]) if optimizer else lm.AdamW([w, u])
+    loss, other = (x @ w).square().sum(), (x @ u).square().sum()
+    w.grad, before = torch.ones_like(w), (w._version, u._version)
+    opt.step()
+    assert w._version > before[0] and u._version == before[1]
+    other.backward()                                          # u had no gradient and stands as it was
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+
+
+def test_parameters_made_in_inference_mode_are_stepped():
+    with torch.inference_mode():
+        p = torch.ones(300, device="cuda")
+    opt = lm.AdamW([p])
+    opt.step([torch.ones(300, device="cuda")], lr=0.5, weight_decay=0.0)
+    assert bool((p == 0.5).all())
