@@ -12,7 +12,8 @@
  * reused as soon as the stream has executed the call, and need not be cleared).
  * Every call queues its work on hip_stream (a hipStream_t; NULL = the null
  * stream) of the current device and returns without waiting. Nothing is
- * allocated, so the calls may be captured into a graph.
+ * allocated, so the calls may be captured into a graph; what they take by value
+ * is fixed then, which for jorge_adamw_step is t and the rates (see there).
  *
  * Pointers are device pointers unless the comment says "host". Matrices are
  * row-major with a row stride in elements (ld* >= columns). Elements are fp32 or
@@ -202,7 +203,9 @@ jorge_status jorge_gradient_norm(const jorge_adamw_tensor* tensors, int32_t n, d
 /* Step t >= 1 of n tensors: t counts a tensor's own steps, and tensors that have taken different numbers of them
  * go in calls of their own (with the same moments). tensors, moments: host, read before the call returns. clip: one
  * float, the factor of the gradients (out + 1 of jorge_gradient_norm), or NULL for 1. lr, eps, weight_decay >= 0,
- * 0 <= beta1, beta2 < 1, all finite. Scalars are formed in fp64 and enter the step as floats. */
+ * 0 <= beta1, beta2 < 1, all finite. Scalars are formed in fp64 and enter the step as floats. A call captured into
+ * a graph repeats its step t: replays have the bias corrections, rates and random bits of that one step, so they are
+ * no sequence of steps, and 8-bit moments rounded by the same bits every time are not right in the mean. */
 jorge_status jorge_adamw_step(const jorge_adamw_tensor* tensors, int32_t n, const jorge_adamw_moments* moments,
                               int64_t t, double lr, double beta1, double beta2, double eps, double weight_decay,
                               const float* clip, void* hip_stream);

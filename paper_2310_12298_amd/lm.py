@@ -11,6 +11,7 @@ fallback: a missing library raises.
 from __future__ import annotations
 
 import ctypes
+import warnings
 
 import numpy as np
 import torch
@@ -376,6 +377,10 @@ class AdamW:
     the same sizes. steps: of each tensor, the steps it has taken; a tensor without a gradient takes none, and
     its bias corrections (and random bits) go by its own count. t: the most of them; setting it sets them all.
     norm: after a step with max_norm, the gradients' global norm before clipping (a device tensor).
+
+    A step captured into a graph is one step for good: replays repeat its count, rates and random bits, and
+    advance nothing here. Capture the passes of a training step, and take the step itself outside; a warning
+    says so at a capture.
     """
 
     def __init__(self, params, bits=32, seed=0, moments=None):
@@ -464,6 +469,8 @@ class AdamW:
             self.norm, clip = out[0], out[1:]
         elif clip is not None and (_cuda(clip, "clip", (torch.float32,)).numel() != 1):
             raise ValueError("clip: one number is needed")
+        if torch.cuda.is_current_stream_capturing():
+            warnings.warn("a captured AdamW step repeats its own step count, rates and random bits at every replay")
         hyper = (float(lr), float(beta1), float(beta2), float(eps), float(weight_decay), _ptr(clip), _stream())
         if whole and self._steps is None:
             self._launch(self._t + 1, hyper)

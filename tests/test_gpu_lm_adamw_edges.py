@@ -118,3 +118,22 @@ def test_parameters_made_in_inference_mode_are_stepped():
     opt = lm.AdamW([p])
     opt.step([torch.ones(300, device="cuda")], lr=0.5, weight_decay=0.0)
     assert bool((p == 0.5).all())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_captured_step_warns_and_repeats_its_own_step(bits):
+    g = tensors([700], F32, seed=1)
+    a, b = (lm.AdamW(tensors([700], F32), bits=bits) for _ in range(2))
+    for o in (a, b):
+        o.step(g, **HP)
+    graph = torch.cuda.CUDAGraph()
+    with pytest.warns(UserWarning, match="every replay"):
+        with torch.cuda.graph(graph):
+            a.step(g, **HP)
+    for _ in range(4):
+        graph.replay()
+        b.t = 1
+        b.step(g, **HP)
+        torch.cuda.synchronize()
+        assert torch.equal(a.params[0], b.params[0])
+        assert all(torch.equal(x, y) for x, y in zip(a.moments.values(), b.moments.values()))
