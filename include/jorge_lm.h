@@ -26,8 +26,11 @@
  * Every call returns a jorge_status (jorge.h). Arguments are checked before any
  * work is queued: a call that is refused writes nothing. jorge_lm_last_error
  * tells why the calling thread's last refused or failed call was. No C++
- * exception crosses the ABI. Sums are formed in an order that depends on the
- * shapes alone: the same inputs give the same bits.
+ * exception crosses the ABI. Sums are formed in an order that timing has no part
+ * in: the same inputs at the same alignment and strides give the same bits. The
+ * order follows from the shapes; for the embedding's gradient also from the
+ * tokens, and for the forward loss of bfloat16 inputs also from whether weight
+ * can be read in place (cols a multiple of 64, ldw of 8, 16-byte alignment).
  */
 #ifndef JORGE_LM_H
 #define JORGE_LM_H

@@ -5,7 +5,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from paper_2310_12298_amd import lm  # noqa: E402
-from test_gpu_lm_loss import BF16, F32, inputs, plain  # noqa: E402
+from test_gpu_lm_loss import BF16, F32, check, inputs, plain  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -36,3 +36,21 @@ def test_whom_the_rounding_of_dz_costs(dtype, of_targets, of_others):
     assert relative(dh, want["dh"]) < of_targets
     assert relative(dw[hit], want["dw"][hit]) < of_targets
     assert relative(dw[~hit], want["dw"][~hit]) < of_others
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,d,v", [(128, 4096, 32000), (162, 1984, 35280), (70, 200, 900)])
+def test_weight_that_cannot_be_read_in_place(n, d, v, dtype):
+    """It goes in pieces of the vocabulary, whose tiles may differ from those of weight in place: both hold against
+    64 bits, each gives the same bits again, and so does the backward pass of both."""
+    h, w, t = inputs(n, d, v, dtype)
+    lse, total = lm.cross_entropy_forward(h, w, t)[1:]
+    grads = lm.cross_entropy_backward(one(), h, w, t, lse, total)
+    for start, pad in ((1, 0), (0, 8), (3, 1)):
+        hold = torch.full((v * (d + pad) + start,), float("nan"), dtype=dtype, device="cuda")
+        x = hold[start:].view(v, d + pad)[:, :d]
+        x.copy_(w)
+        check(h, x, t)
+        assert all(torch.equal(a, b) for a, b in zip(*(lm.cross_entropy_forward(h, x, t) for _ in range(2))))
+        got = lm.cross_entropy_backward(one(), h, x, t, lse, total)
+        assert all(torch.equal(a, b) for a, b in zip(got, grads))
