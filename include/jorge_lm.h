@@ -114,10 +114,11 @@ jorge_status jorge_embedding_backward(const void* dout, int64_t lddo, const int6
  * A target outside [0, vocab), or equal to ignore_index, is no target: loss_i = 0, and the row
  * takes no part in the sums and gradients (its lse_i is written). */
 
-/* Largest tokens, vocab and cols. */
+/* Largest tokens, vocab, cols and row strides; tokens * cols ends at 2^35. */
 #define JORGE_LOSS_MAX_TOKENS (1 << 21)
 #define JORGE_LOSS_MAX_VOCAB  (1 << 22)
 #define JORGE_LOSS_MAX_COLS   32768
+#define JORGE_LOSS_MAX_STRIDE (1 << 22)
 
 /* What grad of the backward pass is the gradient of. */
 #define JORGE_LOSS_ROWS 0 /* of every loss_i: tokens floats        */

@@ -786,8 +786,8 @@ jorge_status check(const jorge_loss_shape* s) {
     if (ceil_div(s->tokens, 64) * ceil_div(s->cols, 64) > 1 << 23)
         return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: tokens * cols above 2^35");
     if (s->ldh < s->cols || s->ldw < s->cols) return bad("cross entropy: a row stride is below cols");
-    if (s->ldh > (int64_t)1 << 22 || s->ldw > (int64_t)1 << 22)
-        return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: a row stride above 2^22");
+    if (s->ldh > JORGE_LOSS_MAX_STRIDE || s->ldw > JORGE_LOSS_MAX_STRIDE)
+        return refuse(JORGE_ERR_UNSUPPORTED, "cross entropy: a row stride above JORGE_LOSS_MAX_STRIDE (2^22)");
     if (!(s->label_smoothing >= 0.0 && s->label_smoothing <= 1.0))
         return bad("cross entropy: label_smoothing must be in [0, 1]");
     return JORGE_OK;

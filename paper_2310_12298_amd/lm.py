@@ -266,8 +266,20 @@ def embedding(tokens, table, scale=1.0, padding=None):
 
 
 # ---------------------------------------------------------------- cross entropy
-def _loss_args(hidden, weight, targets, ignore_index, label_smoothing):
-    h, w, t = _matrix(hidden, "hidden"), _matrix(weight, "weight"), _int64s(targets, "targets")
+LOSS_MAX_STRIDE = 1 << 22                     # JORGE_LOSS_MAX_STRIDE
+
+
+def _loss_matrix(t, what, gradients):
+    """_matrix, copied to dense rows where the row stride is more than the call takes, or, as its gradient will be
+    written in that stride, than twice the width."""
+    m = _matrix(t, what)
+    most = 2 * m.shape[1] if gradients else LOSS_MAX_STRIDE
+    return m.contiguous() if m.shape[0] > 1 and m.stride(0) > most else m
+
+
+def _loss_args(hidden, weight, targets, ignore_index, label_smoothing, gradients=False):
+    h, w = _loss_matrix(hidden, "hidden", gradients), _loss_matrix(weight, "weight", gradients)
+    t = _int64s(targets, "targets")
     if weight.dim() != 2 or h.shape[1] != w.shape[1]:
         raise ValueError("weight: a matrix with a row of hidden's width per word is needed")
     if h.dtype != w.dtype:
@@ -302,7 +314,7 @@ def cross_entropy_backward(grad, hidden, weight, targets, lse, total, reduction=
     """(dhidden, dweight) from lse and total of cross_entropy_forward. grad: the gradient of every row's
     loss (reduction "none"), or of their sum or mean (one number, on the device)."""
     lib = load_operators()
-    h, w, t, shape = _loss_args(hidden, weight, targets, ignore_index, label_smoothing)
+    h, w, t, shape = _loss_args(hidden, weight, targets, ignore_index, label_smoothing, gradients=True)
     kind = REDUCTIONS[reduction]
     g = _cuda(grad, "grad").float().contiguous()
     if g.numel() != (h.shape[0] if kind == 0 else 1):
@@ -313,7 +325,7 @@ def cross_entropy_backward(grad, hidden, weight, targets, lse, total, reduction=
     n = _I64(0)
     _check(lib, lib.jorge_cross_entropy_workspace(ctypes.byref(shape), 1, ctypes.byref(n)))
     ws = _workspace(n.value)
-    # In the inputs' own row strides, as the call writes them.
+    # In the matrices' own row strides, as the call writes them.
     dh = torch.empty((h.shape[0], shape.ldh), dtype=h.dtype, device=h.device) if need_hidden else None
     dw = torch.empty((w.shape[0], shape.ldw), dtype=w.dtype, device=w.device) if need_weight else None
     _check(lib, lib.jorge_cross_entropy_backward(ctypes.byref(shape), g.data_ptr(), kind, h.data_ptr(), w.data_ptr(),

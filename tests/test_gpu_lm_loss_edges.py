@@ -54,3 +54,32 @@ def test_weight_that_cannot_be_read_in_place(n, d, v, dtype):
         assert all(torch.equal(a, b) for a, b in zip(*(lm.cross_entropy_forward(h, x, t) for _ in range(2))))
         got = lm.cross_entropy_backward(one(), h, x, t, lse, total)
         assert all(torch.equal(a, b) for a, b in zip(got, grads))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_last_tokens_of_long_sequences(dtype):
+    """hidden[:, -1]: rows further apart than the C call takes, both passes and through autograd."""
+    n, length, d, v = 3, 9000, 512, 700
+    h, w, t = inputs(n, d, v, dtype, ignored=0.0)
+    whole = torch.zeros(n, length, d, dtype=dtype, device="cuda")
+    whole[:, -1] = h
+    last = whole[:, -1]
+    assert last.stride(0) > lm.LOSS_MAX_STRIDE
+    base = lm.cross_entropy_forward(h, w, t)
+    assert all(torch.equal(a, b) for a, b in zip(lm.cross_entropy_forward(last, w, t), base))
+    want = lm.cross_entropy_backward(one(), h, w, t, *base[1:])
+    assert all(torch.equal(a, b) for a, b in zip(lm.cross_entropy_backward(one(), last, w, t, *base[1:]), want))
+    whole.requires_grad_()
+    lm.linear_cross_entropy(whole[:, -1], w, t).backward()
+    assert torch.equal(whole.grad[:, -1], want[0]) and torch.count_nonzero(whole.grad[:, :-1]) == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gradients_of_narrow_slices_take_no_more_than_twice_their_size(dtype):
+    h, w, t = inputs(64, 128, 300, dtype)
+    wide_h, wide_w = (torch.full((m.shape[0], 5000), float("nan"), dtype=dtype, device="cuda") for m in (h, w))
+    wide_h[:, 8:136], wide_w[:, 16:144] = h, w
+    base = lm.cross_entropy_forward(h, w, t)
+    got = lm.cross_entropy_backward(one(), wide_h[:, 8:136], wide_w[:, 16:144], t, *base[1:])
+    for a, b in zip(got, lm.cross_entropy_backward(one(), h, w, t, *base[1:])):
+        assert torch.equal(a, b) and a.untyped_storage().nbytes() <= 2 * b.numel() * b.element_size()
