@@ -13,8 +13,8 @@
 //   written both ways round, so that both products below have K-contiguous operands;
 //   dhidden += dz weight      (K: the piece's words; the sum over the pieces in fp32)
 //   dweight  = dz^T hidden    (K: the tokens; whole, as a piece holds all tokens)
-// A piece is as large as keeps dz within a fixed number of elements, so the memory does not grow with
-// the vocabulary.
+// A piece is as large as keeps dz, and the copies of weight that the products read, within a fixed number of elements,
+// so the memory does not grow with the vocabulary.
 //
 // dz of bf16 inputs is the one value here that is held in fewer than 32 bits, because the matrix instructions take it
 // so; in two bfloat16 terms it would double both gradients' products (2.9 ms more of 6.0 for 8192 tokens of 2048, 50001
@@ -521,8 +521,12 @@ bool direct(const jorge_loss_shape& s, const void* p, int64_t ld) {
     return s.dtype == JORGE_BF16 && s.cols % kPadK == 0 && ld % 8 == 0 && aligned(p, 16);
 }
 
-// Elements of one layout of dz: what bounds the backward pass's workspace.
+// What bounds the workspaces, whatever the vocabulary: elements of one layout of dz (forward: of weight's copy), and, where
+// tokens are few and weight outgrows dz, those of each of the backward pass's two copies of it, terms together: 1 GiB. In
+// 2^29 elements a piece keeps enough tiles for the CUs: 64 tokens, 128256 words of 4096 in fp32 take 4.43 ms and 2.1 GB,
+// in 2^28 4.80 and 1.1, with weight copied whole 4.26 and 6.4; 1 token, 262144 words of 8192 in bf16 5.42 ms, 5.85, 5.05.
 constexpr int64_t kPieceElements = 1 << 26;
+constexpr int64_t kCopyElements = 1 << 29;
 // Tiles of one launch: its threads have to stay below 2^32.
 constexpr int64_t kMostTiles = 1 << 23;
 
@@ -562,6 +566,7 @@ Plan plan_of(const jorge_loss_shape& s, bool backward, bool direct_x, bool direc
     // that it can be read in place. The whole vocabulary's tile for its pieces too would cost those (500 tokens of
     // 8192, 128256 words at an odd address: 3.62 against 2.23 ms), the pieces' tile for the whole the usual call.
     int64_t most = kPieceElements / (s.dtype == JORGE_F32 ? 2 : 1) / std::max<int64_t>(1, backward ? p.kn : p.kd);
+    if (backward) most = std::min(most, kCopyElements / (p.terms * p.kd));
     if (!backward && direct_w) most = s.vocab;
     most = std::min(most, kMostTiles / ceil_div(std::max<int64_t>(1, s.tokens), 128) * 128);
     most = most < s.vocab ? most / 256 * 256 : round_up(most, 256);

@@ -83,3 +83,9 @@ def test_gradients_of_narrow_slices_take_no_more_than_twice_their_size(dtype):
     got = lm.cross_entropy_backward(one(), wide_h[:, 8:136], wide_w[:, 16:144], t, *base[1:])
     for a, b in zip(got, lm.cross_entropy_backward(one(), h, w, t, *base[1:])):
         assert torch.equal(a, b) and a.untyped_storage().nbytes() <= 2 * b.numel() * b.element_size()
+
+
+@pytest.mark.parametrize("n,d,v,dtype", [(5, 4096, 60000, F32), (66, 4096, 60001, F32), (3, 16384, 40000, BF16)])
+def test_few_tokens_over_several_pieces(n, d, v, dtype):
+    """Pieces that weight's copies bound, not dz."""
+    check(*inputs(n, d, v, dtype))

@@ -25,3 +25,21 @@ def test_row_strides_of_the_loss_end_where_the_header_says(lib):  # noqa: F811
         refused(lib, lib.jorge_cross_entropy_workspace(ctypes.byref(s), 0, ctypes.byref(n)), UNSUPPORTED, "MAX_STRIDE")
     s = lm.LossShape(4, 8, 5, lm.LOSS_MAX_STRIDE, lm.LOSS_MAX_STRIDE, 1, 0, -100, 0.0)
     assert lib.jorge_cross_entropy_workspace(ctypes.byref(s), 1, ctypes.byref(n)) == 0
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("tokens", [1, 63, 64, 700, 8192])
+def test_the_loss_of_few_tokens_copies_no_whole_weight(lib, tokens, dtype):  # noqa: F811
+    def size(vocab, back, cols=4096):
+        s, n = lm.LossShape(tokens, cols, vocab, cols, cols, dtype, 0, -100, 0.0), I64()
+        assert lib.jorge_cross_entropy_workspace(ctypes.byref(s), back, ctypes.byref(n)) == 0
+        return n.value
+    terms = 1 if dtype else 3
+    for cols in (4096, 16384):
+        # Twice 1 GiB of weight's copies; dz both ways round, 2^26 elements (fp32: half as many, of three terms);
+        # hidden's two copies; the sums of its gradient, and two products' slices: 512 tiles of 256 x 256 floats each.
+        most = 2 * 2 ** 30 + 2 * 2 * 2 ** 26 * (1 if dtype else 1.5) + 2 * 2 * terms * (tokens + 64) * cols
+        most += 4 * tokens * cols + 2 * 512 * 256 * 256 * 4
+        assert size(1 << 22, 1, cols) < most
+        # Pieces of equal length are at least half as long as they may be.
+        assert size(1 << 22, 1, cols) < 2 * size(1 << 18, 1, cols)
