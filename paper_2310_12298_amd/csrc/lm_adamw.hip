@@ -404,6 +404,9 @@ int64_t norm_groups(const jorge_adamw_tensor* t, int32_t n) {
     return g;
 }
 
+// Blocks of moments that one launch reads or writes: a wave or less each, and a grid holds fewer than 2^32 threads.
+constexpr int64_t kBlocksPerLaunch = 1 << 24;
+
 jorge_status check_range(const jorge_adamw_moments* m, int32_t second, int64_t first, int64_t count, const void* p) {
     const jorge_status st = check_moments(m);
     if (st != JORGE_OK) return st;
@@ -411,7 +414,6 @@ jorge_status check_range(const jorge_adamw_moments* m, int32_t second, int64_t f
     if (second != 0 && second != 1) return bad("adamw: second must be 0 or 1");
     if (first < 0 || count < 0 || first > m->blocks || count > m->blocks - first)
         return bad("adamw: blocks outside the moments");
-    if (count > kMaxGroups) return refuse(JORGE_ERR_UNSUPPORTED, "adamw: too many blocks in one call");
     if (count > 0 && !p) return bad("adamw: a buffer is needed");
     return JORGE_OK;
 }
@@ -518,15 +520,22 @@ jorge_status jorge_adamw_read(const jorge_adamw_moments* moments, int32_t second
     if (!aligned(out, dtype_bytes(dtype))) return bad("adamw: out is not aligned to its element");
     if (count == 0) return JORGE_OK;
     const hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
-    const uint8_t* const codes = (const uint8_t*)(second ? moments->exp_avg_sq : moments->exp_avg) + first * kBlock;
-    const uint8_t* const scales = (second ? moments->exp_avg_sq_scale : moments->exp_avg_scale) + first;
-    const dim3 grid((unsigned)ceil_div(count * kBlock, 256 * 16)), block(256);
-    if (dtype == JORGE_F32) {
-        if (second) moments_read_kernel<false, float><<<grid, block, 0, s>>>(codes, scales, count, (float*)out);
-        else moments_read_kernel<true, float><<<grid, block, 0, s>>>(codes, scales, count, (float*)out);
-    } else {
-        if (second) moments_read_kernel<false, bf16><<<grid, block, 0, s>>>(codes, scales, count, (bf16*)out);
-        else moments_read_kernel<true, bf16><<<grid, block, 0, s>>>(codes, scales, count, (bf16*)out);
+    const uint8_t* codes = (const uint8_t*)(second ? moments->exp_avg_sq : moments->exp_avg) + first * kBlock;
+    const uint8_t* scales = (second ? moments->exp_avg_sq_scale : moments->exp_avg_scale) + first;
+    for (int64_t left = count; left > 0;) {
+        const int64_t n = left < kBlocksPerLaunch ? left : kBlocksPerLaunch;
+        const dim3 grid((unsigned)ceil_div(n * kBlock, 256 * 16)), block(256);
+        if (dtype == JORGE_F32) {
+            if (second) moments_read_kernel<false, float><<<grid, block, 0, s>>>(codes, scales, n, (float*)out);
+            else moments_read_kernel<true, float><<<grid, block, 0, s>>>(codes, scales, n, (float*)out);
+        } else {
+            if (second) moments_read_kernel<false, bf16><<<grid, block, 0, s>>>(codes, scales, n, (bf16*)out);
+            else moments_read_kernel<true, bf16><<<grid, block, 0, s>>>(codes, scales, n, (bf16*)out);
+        }
+        left -= n;
+        codes += n * kBlock;
+        scales += n;
+        out = (char*)out + n * kBlock * dtype_bytes(dtype);
     }
     return launched("adamw");
 }
@@ -538,11 +547,18 @@ jorge_status jorge_adamw_write(const jorge_adamw_moments* moments, int32_t secon
     if (!aligned(values, 4)) return bad("adamw: values is not aligned to its element");
     if (count == 0) return JORGE_OK;
     const hipStream_t s = reinterpret_cast<hipStream_t>(hip_stream);
-    uint8_t* const codes = (uint8_t*)(second ? moments->exp_avg_sq : moments->exp_avg) + first * kBlock;
-    uint8_t* const scales = (second ? moments->exp_avg_sq_scale : moments->exp_avg_scale) + first;
-    const dim3 grid((unsigned)ceil_div(count, 4)), block(256);
-    if (second) moments_write_kernel<false><<<grid, block, 0, s>>>(codes, scales, count, values);
-    else moments_write_kernel<true><<<grid, block, 0, s>>>(codes, scales, count, values);
+    uint8_t* codes = (uint8_t*)(second ? moments->exp_avg_sq : moments->exp_avg) + first * kBlock;
+    uint8_t* scales = (second ? moments->exp_avg_sq_scale : moments->exp_avg_scale) + first;
+    for (int64_t left = count; left > 0;) {
+        const int64_t n = left < kBlocksPerLaunch ? left : kBlocksPerLaunch;
+        const dim3 grid((unsigned)ceil_div(n, 4)), block(256);
+        if (second) moments_write_kernel<false><<<grid, block, 0, s>>>(codes, scales, n, values);
+        else moments_write_kernel<true><<<grid, block, 0, s>>>(codes, scales, n, values);
+        left -= n;
+        codes += n * kBlock;
+        scales += n;
+        values += n * kBlock;
+    }
     return launched("adamw");
 }
 

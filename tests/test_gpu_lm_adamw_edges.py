@@ -137,3 +137,34 @@ def test_a_captured_step_warns_and_repeats_its_own_step(bits):
         torch.cuda.synchronize()
         assert torch.equal(a.params[0], b.params[0])
         assert all(torch.equal(x, y) for x, y in zip(a.moments.values(), b.moments.values()))
+
+
+def test_8_bit_moments_past_two_to_the_31_elements_are_read_and_written():
+    """More blocks than a launch takes (2^24) too: 2^24 + 70 of them, and the values around every boundary."""
+    blocks = (1 << 24) + 70
+    n, last = blocks * lm.BLOCK, lm.BLOCK * 200
+    opt = lm.AdamW([torch.empty(n, dtype=BF16, device="cuda")], bits=8)
+    g = torch.Generator(device="cuda").manual_seed(0)
+    for k in opt.moments:
+        code = opt.moments[k]
+        code[-last:] = torch.randint(1, 200, (min(last, code.numel()),), generator=g, device="cuda").to(torch.uint8)[
+            :code[-last:].numel()]
+    few = lm.AdamW([torch.empty(last, dtype=BF16, device="cuda")], bits=8, moments={
+        k: x[-(last if x.numel() == n else 200):].clone() for k, x in opt.moments.items()})
+    for x, y in zip(opt.moment_values(BF16), few.moment_values(BF16)):
+        assert torch.equal(x[-last:], y) and not bool(x[:-last].view(torch.int32).any())
+    del x, y
+    values = [x.clone() for x in few.moment_values()]
+    values[0] *= -1
+    wide = torch.zeros(n, device="cuda")
+    both = []
+    for v in values:
+        wide[-last:] = v
+        both.append(wide.clone() if not both else wide)
+    opt.set_moment_values(*both)
+    few.set_moment_values(*values)
+    for k, x in opt.moments.items():
+        end = last if x.numel() == n else 200
+        assert torch.equal(x[-end:], few.moments[k])
+    del wide, both
+    assert all(torch.equal(x[-last:], y) for x, y in zip(opt.moment_values(BF16), few.moment_values(BF16)))

@@ -43,3 +43,17 @@ def test_the_loss_of_few_tokens_copies_no_whole_weight(lib, tokens, dtype):  # n
         assert size(1 << 22, 1, cols) < most
         # Pieces of equal length are at least half as long as they may be.
         assert size(1 << 22, 1, cols) < 2 * size(1 << 18, 1, cols)
+
+
+NO_GPU = pytest.mark.skipif(torch.cuda.is_available(), reason="accepted calls would follow made-up addresses")
+HIP_ERROR = -3                                        # JORGE_ERR_HIP: where there is no GPU, a launch that was let through
+
+
+@NO_GPU
+def test_8_bit_moments_are_read_and_written_at_any_size(lib):  # noqa: F811
+    blocks = (1 << 23) + 300                          # 2^31 elements and more
+    ms = lm.AdamWMoments(P(A), P(A), P(A), P(A), blocks, 8, 0)
+    for second in (0, 1):
+        for dtype in (0, 1):
+            assert lib.jorge_adamw_read(ctypes.byref(ms), second, 0, blocks, P(A), dtype, None) == HIP_ERROR
+        assert lib.jorge_adamw_write(ctypes.byref(ms), second, 0, blocks, P(A), None) == HIP_ERROR
