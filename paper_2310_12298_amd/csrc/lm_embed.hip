@@ -509,10 +509,13 @@ jorge_status backward(const void* dout, int64_t lddo, const int64_t* tokens, int
     a.ldp = (int)partial_row(cols);
     a.slabs = (int)ceil_div(cols, 64 * Wide<T>::N);
     a.scale = (float)scale;
+    // The largest of tokens, rows and columns fit in one grid (fewer than 2^32 threads): at most 4096 chunks, 64 rows or a
+    // chunk per wave and slab.
+    constexpr int64_t kMostSlabs = JORGE_EMBED_MAX_COLS / (64 * 4);
+    static_assert((4096 + JORGE_EMBED_MAX_VOCAB / kZeroRows) * kMostSlabs / 4 + 2 < (1ll << 32) / 256, "one launch");
+    static_assert(JORGE_EMBED_MAX_TOKENS / 4096 <= 4096, "4096 chunks of up to 4096");
     const int64_t sum_groups = ceil_div(a.chunks * a.slabs, 4);
     const int64_t zero_groups = ceil_div(ceil_div(vocab, kZeroRows) * a.slabs, 4);
-    if (sum_groups + zero_groups > kMaxGroups)
-        return refuse(JORGE_ERR_UNSUPPORTED, "embedding: vocab * cols is too large");
     embed_sums_kernel<T><<<dim3((unsigned)(sum_groups + zero_groups)), dim3(256), 0, s>>>(a, (const T*)dout, (T*)dtable,
                                                                                          sum_groups);
     if (a.chunks > 1) {

@@ -57,3 +57,14 @@ def test_8_bit_moments_are_read_and_written_at_any_size(lib):  # noqa: F811
         for dtype in (0, 1):
             assert lib.jorge_adamw_read(ctypes.byref(ms), second, 0, blocks, P(A), dtype, None) == HIP_ERROR
         assert lib.jorge_adamw_write(ctypes.byref(ms), second, 0, blocks, P(A), None) == HIP_ERROR
+
+
+@NO_GPU
+@pytest.mark.parametrize("count", [0, 5, defined("JORGE_EMBED_MAX_TOKENS")])
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_the_largest_table_is_not_refused_after_its_tokens_are_sorted(lib, count, dtype):  # noqa: F811
+    vocab, cols = defined("JORGE_EMBED_MAX_VOCAB"), defined("JORGE_EMBED_MAX_COLS")
+    n = I64()
+    assert lib.jorge_embedding_workspace(count, vocab, cols, ctypes.byref(n)) == 0
+    assert lib.jorge_embedding_backward(P(A), cols, P(A), count, dtype, vocab, cols, 1.0, -1, P(A), cols, P(A), n.value,
+                                        None) == HIP_ERROR
