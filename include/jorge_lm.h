@@ -148,7 +148,8 @@ jorge_status jorge_cross_entropy_forward(const jorge_loss_shape* shape, const vo
  * loss_i (0 without a target) and p = exp(z - lse):
  *   dz_iv = g_i (p_iv - (1 - e) [v = target_i] - e / vocab),
  *   dhidden = dz weight,  dweight = dz^T hidden.
- * dhidden, dweight: written whole; either may be NULL. bfloat16 inputs: dz (without g where that is one
+ * dhidden, dweight: written whole; either may be NULL. A row of dhidden without a target is 0, whatever grad and
+ * weight hold, and so is all of both where no row has a target. bfloat16 inputs: dz (without g where that is one
  * number) is rounded to bfloat16 for the two products, whose sums are fp32: rows of dweight of words that are
  * no row's target, sums of such rounded terms alone, err by some 2.2e-3 of their size instead of the 1.7e-3 of
  * their own rounding; dhidden and the other rows by 1.7e-3. fp32 inputs: every product is formed from three-term

@@ -395,20 +395,24 @@ __global__ __launch_bounds__(256, 1) void loss_dz_kernel(Product p, LossRows row
     }
 }
 
-// What a gradient is multiplied by after its product: grad[0] (or 1), over the number of rows with a target for a mean.
+// What a gradient is multiplied by after its product: grad[0] (or 1), over the number of rows with a target for a mean;
+// 0 where no row has one, whatever grad is.
 struct Scale {
     const float *grad, *count;
+    bool mean;
     __device__ __forceinline__ float value() const {
-        return (grad ? *grad : 1.0f) / (count ? fmaxf(*count, 1.0f) : 1.0f);
+        const float n = *count;
+        return n > 0.0f ? (grad ? *grad : 1.0f) / (mean ? n : 1.0f) : 0.0f;
     }
 };
 
 // C[b][a] over one of gridDim.y ranges of K, to out (whole: one range) or to the range's slice of fp32 sums
-// [ranges][B.rows][lda], added to it where `add`.
+// [ranges][B.rows][lda], added to it where `add`. rows: of B's rows, where those are tokens; one without a target gets 0,
+// not 0 times what the scale or A may hold.
 template <int WA, int WB, int RING, bool SPLIT, typename O>
 __global__ __launch_bounds__(256, 1) void loss_grad_kernel(Product p, O* __restrict__ out, int64_t ldo,
                                                            float* __restrict__ slices, int64_t lda, int add,
-                                                           Scale scale) {
+                                                           Scale scale, LossRows rows) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     using T = Tile<WA, WB, RING, SPLIT>;
     const Place at = place_of(blockIdx.x, p.ta, p.tb);
@@ -440,23 +444,26 @@ __global__ __launch_bounds__(256, 1) void loss_grad_kernel(Product p, O* __restr
     constexpr int N = Wide<O>::N;
 #pragma unroll
     for (int j = 0; j < WB; ++j)
-        if (b0 + j < p.B.rows)
+        if (b0 + j < p.B.rows) {
+            const bool none = rows.targets && rows.target(b0 + j) < 0;
 #pragma unroll
             for (int i = 0; i < WA; i += N / 4) {
                 float v[N];
 #pragma unroll
-                for (int e = 0; e < N; ++e) v[e] = t.acc[i + e / 4][j][e & 3] * f;
+                for (int e = 0; e < N; ++e) v[e] = none ? 0.0f : t.acc[i + e / 4][j][e & 3] * f;
                 if (4 * i < left) store_wide(out + (b0 + j) * ldo + a0 + 4 * i, left - 4 * i, v);
             }
+        }
 }
 
-// out[r][c] = scale times the sum of the slices, in order.
+// out[r][c] = scale times the sum of the slices, in order (rows: as above).
 template <typename O>
 __global__ __launch_bounds__(256) void loss_slices_kernel(const float* __restrict__ slices, int n, int64_t rows,
                                                           int cols, int64_t lda, O* __restrict__ out, int64_t ldo,
-                                                          Scale scale) {
+                                                          Scale scale, LossRows targets) {
     const int64_t r = blockIdx.x;
     const float f = scale.value();
+    const bool none = targets.targets && targets.target(r) < 0;
     for (int c = (blockIdx.y * 256 + threadIdx.x) * 4; c < cols; c += gridDim.y * 1024) {
         const float* p = slices + r * lda + c;
         f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -471,7 +478,7 @@ __global__ __launch_bounds__(256) void loss_slices_kernel(const float* __restric
         O* const o = out + r * ldo + c;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (c + e < cols) o[e] = (O)(s[e] * f);
+            if (c + e < cols) o[e] = (O)(none ? 0.0f : s[e] * f);
     }
 }
 
@@ -712,7 +719,7 @@ jorge_status forward(const jorge_loss_shape& s, const Plan& p, const Work& w, co
 // One gradient: out = scale * A-by-B, in slices where K is cut or the sum goes on (first, last: of the sum's pieces).
 template <typename T>
 jorge_status gradient(const Shape& sh, const Product& pr, T* out, int64_t ldo, int64_t cols, float* slices, bool first,
-                      bool last, const Scale& scale, hipStream_t st) {
+                      bool last, const Scale& scale, const LossRows& rows, hipStream_t st) {
     jorge_status err = JORGE_OK;
     const int64_t lda = round_up(cols, 4);
     with_tile(sh, [&](auto W, auto R) {
@@ -722,12 +729,12 @@ jorge_status gradient(const Shape& sh, const Product& pr, T* out, int64_t ldo, i
         // The first piece of a sum is the longest and fills every slice; a short last one may add to fewer.
         const int ranges = std::min(sh.ranges, pr.stages / 2);
         k<<<dim3(pr.ta * pr.tb, ranges), dim3(256), Tile<WA, WA, RING, sizeof(T) == 4>::kBytes, st>>>(
-            pr, out, ldo, slices, lda, first ? 0 : 1, scale);
+            pr, out, ldo, slices, lda, first ? 0 : 1, scale, rows);
     });
     if (err != JORGE_OK) return err;
     if (slices && last)
         loss_slices_kernel<T><<<dim3((unsigned)pr.B.rows, (unsigned)ceil_div(cols, 1024)), dim3(256), 0, st>>>(
-            slices, sh.ranges, pr.B.rows, (int)cols, lda, out, ldo, scale);
+            slices, sh.ranges, pr.B.rows, (int)cols, lda, out, ldo, scale, rows);
     return JORGE_OK;
 }
 
@@ -735,7 +742,7 @@ template <typename T>
 jorge_status backward(const jorge_loss_shape& s, const Plan& p, const Work& w, const float* grad, int32_t kind,
                       const void* hidden, const void* weight, const LossRows& rows, const float* lse,
                       const float* total, void* dhidden, void* dweight, hipStream_t st) {
-    const Scale scale{kind == JORGE_LOSS_ROWS ? nullptr : grad, kind == JORGE_LOSS_MEAN ? total + 1 : nullptr};
+    const Scale scale{kind == JORGE_LOSS_ROWS ? nullptr : grad, total + 1, kind == JORGE_LOSS_MEAN};
     const float* const row_grad = kind == JORGE_LOSS_ROWS ? grad : nullptr;
     const Operand x = operand_x(s, p, w, hidden);
     const Operand xt{w.xt, p.terms * p.kn, p.kn, s.cols};
@@ -759,13 +766,13 @@ jorge_status backward(const jorge_loss_shape& s, const Plan& p, const Work& w, c
         if (dhidden) {
             const Operand wt{w.wt, p.terms * ldz, ldz, s.cols}, z{w.dz, p.terms * ldz, ldz, s.tokens};
             err = gradient(p.dh, product_of(p.dh, wt, z, ldz), (T*)dhidden, s.ldh, s.cols, w.dh, v0 == 0,
-                           v0 + n == s.vocab, scale, st);
+                           v0 + n == s.vocab, scale, rows, st);
             if (err != JORGE_OK) return err;
         }
         if (dweight) {
             const Operand zt{w.dzt, p.terms * p.kn, p.kn, n};
             err = gradient(p.dw, product_of(p.dw, xt, zt, p.kn), (T*)dweight + v0 * s.ldw, s.ldw, s.cols, w.dw, true,
-                           true, scale, st);
+                           true, scale, LossRows{}, st);
             if (err != JORGE_OK) return err;
         }
     }

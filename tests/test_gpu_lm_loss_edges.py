@@ -89,3 +89,28 @@ def test_gradients_of_narrow_slices_take_no_more_than_twice_their_size(dtype):
 def test_few_tokens_over_several_pieces(n, d, v, dtype):
     """Pieces that weight's copies bound, not dz."""
     check(*inputs(n, d, v, dtype))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,d,v", [(90, 72, 300), (40, 64, 9000), (4000, 64, 20000)])
+def test_rows_without_a_target_get_no_gradient_whatever_comes_in(n, d, v, dtype):
+    """The upstream gradient of a step whose loss overflowed, and weights that have: a masked row's gradient stays 0.
+    Sizes with one range of K, with several, and with several pieces of the vocabulary."""
+    h, w, t = inputs(n, d, v, dtype)
+    t[0] = -100
+    masked = t < 0
+    lse, total = lm.cross_entropy_forward(h, w, t)[1:]
+    for reduction in ("mean", "sum", "none"):
+        for value in (float("inf"), float("nan")):
+            grad = torch.full((n,), value, device="cuda") if reduction == "none" else one(value)
+            dh, dw = lm.cross_entropy_backward(grad, h, w, t, lse, total, reduction)
+            assert torch.count_nonzero(dh[masked]) == 0 and not bool(torch.isfinite(dh[~masked]).any())
+            none = torch.full_like(t, -100)
+            total0 = lm.cross_entropy_forward(h, w, none)[2]
+            for x in lm.cross_entropy_backward(grad, h, w, none, lse, total0, reduction):
+                assert torch.count_nonzero(x) == 0
+    bad = w.clone()
+    bad[3, 5] = float("inf")
+    lse, total = lm.cross_entropy_forward(h, bad, t)[1:]
+    dh = lm.cross_entropy_backward(one(), h, bad, t, lse, total)[0]
+    assert torch.count_nonzero(dh[masked]) == 0
