@@ -520,10 +520,10 @@ class AdamW:
         return out
 
     def moment_values(self, dtype=torch.float32):
-        """The two moments' values as flat tensors of dtype, in the layout of `moments` (parameter i starts
+        """The two moments' values as new flat tensors of dtype, in the layout of `moments` (parameter i starts
         at blocks[i] * 256)."""
         if self.bits == 32:
-            return self.moments["exp_avg"].to(dtype), self.moments["exp_avg_sq"].to(dtype)
+            return tuple(self.moments[k].to(dtype, copy=True) for k in ("exp_avg", "exp_avg_sq"))
         total, out = int(self.blocks[-1]), []
         for second in (0, 1):
             v = torch.empty(total * BLOCK, dtype=dtype, device="cuda")

@@ -168,3 +168,14 @@ def test_8_bit_moments_past_two_to_the_31_elements_are_read_and_written():
         assert torch.equal(x[-end:], few.moments[k])
     del wide, both
     assert all(torch.equal(x[-last:], y) for x, y in zip(opt.moment_values(BF16), few.moment_values(BF16)))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_moment_values_stay_as_they_were_read(bits):
+    opt = lm.AdamW(tensors(SIZES, F32), bits=bits)
+    opt.step(tensors(SIZES, F32, seed=1), **HP)
+    read = opt.moment_values()
+    kept = [x.clone() for x in read]
+    opt.step(tensors(SIZES, F32, seed=2), **HP)
+    assert all(torch.equal(x, y) for x, y in zip(read, kept))
+    assert not torch.equal(opt.moment_values()[0], kept[0])
