@@ -549,18 +549,27 @@ class AdamW:
         return {"t": self.t, "steps": self.steps, "bits": self.bits, "seed": self.seed,
                 **{k: v.cpu() for k, v in self.moments.items()}}
 
+    def check_state_dict(self, sd):
+        """Raises ValueError unless load_state_dict would take sd whole."""
+        held = all(isinstance(sd.get(k), torch.Tensor) and sd[k].shape == v.shape and sd[k].dtype == v.dtype
+                   for k, v in self.moments.items())
+        if not held or sd.get("bits") != self.bits or len(sd.get("steps", self.params)) != len(self.params):
+            raise ValueError("the state is of another set of tensors or of other bits")
+        if not all(int(t) >= 0 for t in [sd.get("t", -1), *sd.get("steps", [])]):
+            raise ValueError("the state holds no count of steps")
+        if not 0 <= int(sd.get("seed", -1)) < 1 << 32:
+            raise ValueError("the state's seed must be in [0, 2^32)")
+
     def load_state_dict(self, sd):
-        if sd["bits"] != self.bits or any(sd[k].shape != v.shape for k, v in self.moments.items()):
-            raise ValueError("the state is of another set of tensors or of other bits")
-        steps = [int(t) for t in sd.get("steps", [])]         # absent: all tensors took t steps
-        if steps and len(steps) != len(self.params):
-            raise ValueError("the state is of another set of tensors or of other bits")
+        """Takes over what state_dict returned (its moments are copied); changes nothing if it is refused."""
+        self.check_state_dict(sd)
         for k, v in self.moments.items():
             v.copy_(sd[k])
         self.t, self.seed = int(sd["t"]), int(sd["seed"])
+        self._moments.seed = self.seed
+        steps = [int(t) for t in sd.get("steps", [])]         # absent: all tensors took t steps
         if len(set(steps)) > 1:
             self._t, self._steps = None, steps
-        self._moments.seed = self.seed
 
 
 def _dense(t):

@@ -240,6 +240,8 @@ class AdamWOptimizer(torch.optim.Optimizer):
         held = sd.pop("adamw")
         if len(held) != len(self._handles):
             raise ValueError("the state is of another number of parameter groups")
+        for h, rec in zip(self._handles, held):   # all or nothing
+            h.check_state_dict(rec)
         super().load_state_dict(sd)
         for h, rec in zip(self._handles, held):
             h.load_state_dict(rec)

@@ -179,3 +179,34 @@ def test_moment_values_stay_as_they_were_read(bits):
     opt.step(tensors(SIZES, F32, seed=2), **HP)
     assert all(torch.equal(x, y) for x, y in zip(read, kept))
     assert not torch.equal(opt.moment_values()[0], kept[0])
+
+
+def test_a_refused_state_changes_nothing():
+    opt = lm.AdamW(tensors(SIZES, F32), bits=8, seed=4)
+    opt.step(tensors(SIZES, F32, seed=1), **HP)
+    good = opt.state_dict()
+    twin = lm.AdamW(tensors(SIZES, F32), bits=8)
+    for change in ({"t": None}, {"t": -1}, {"seed": None}, {"seed": 1 << 32}, {"exp_avg_sq": None}, {"steps": [1] * 4},
+                   {"steps": [1, 1, 1, 1, -1]}, {"exp_avg_scale": good["exp_avg_scale"].int()}, {"bits": 32}):
+        bad = {k: v for k, v in {**good, **change}.items() if v is not None}
+        with pytest.raises(ValueError):
+            twin.load_state_dict(bad)
+        assert twin.t == 0 and twin.seed == 0 and not any(bool(x.any()) for x in twin.moments.values())
+    twin.load_state_dict(good)
+    assert twin.t == 1 and twin.seed == 4 and all(torch.equal(opt.moments[k], x) for k, x in twin.moments.items())
+
+
+def test_a_state_that_one_group_refuses_changes_no_group():
+    def make(sizes):
+        ps = [torch.nn.Parameter(p) for p in tensors(sizes, F32)]
+        return AdamWOptimizer([{"params": ps[:1]}, {"params": ps[1:], "lr": 0.5}], lr=0.25)
+    a, b = make([30, 600]), make([30, 300])
+    for g in a.param_groups:
+        g["lr"] = 0.125
+        for p in g["params"]:
+            p.grad = torch.ones_like(p)
+    a.step()
+    with pytest.raises(ValueError):
+        b.load_state_dict(a.state_dict())
+    assert [g["lr"] for g in b.param_groups] == [0.25, 0.5]
+    assert all(h.t == 0 and not any(bool(x.any()) for x in h.moments.values()) for h in b._handles)
