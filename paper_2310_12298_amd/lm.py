@@ -406,6 +406,9 @@ class AdamW:
         for i, p in enumerate(self.params):
             if not _dense(_cuda(p, f"parameter {i}")):
                 raise ValueError(f"parameter {i}: a dense tensor is needed")
+        spans = sorted((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size()) for p in self.params if p.numel())
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            raise ValueError("parameters: no two may share memory (both would be stepped at once)")
         self._numel = [p.numel() for p in self.params]
         self._layout = [(p.dtype, p.shape, p.stride(), p.get_device()) for p in self.params]
         self.blocks = np.cumsum([0] + [-(-n // BLOCK) for n in self._numel])

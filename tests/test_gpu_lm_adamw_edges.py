@@ -210,3 +210,14 @@ def test_a_state_that_one_group_refuses_changes_no_group():
         b.load_state_dict(a.state_dict())
     assert [g["lr"] for g in b.param_groups] == [0.25, 0.5]
     assert all(h.t == 0 and not any(bool(x.any()) for x in h.moments.values()) for h in b._handles)
+
+
+def test_parameters_that_share_memory_are_refused():
+    hold = tensors([1000], F32)[0]
+    for params in ([hold, hold], [hold[:600], hold[599:]], [hold[10:20], hold.view(10, 100)]):
+        with pytest.raises(ValueError, match="share memory"):
+            lm.AdamW(params)
+    lm.AdamW([hold[600:], hold[:0], hold[:600], hold[600:600]])
+    q = torch.nn.Parameter(tensors([8], F32)[0])
+    with pytest.warns(UserWarning), pytest.raises(ValueError, match="share memory"):
+        AdamWOptimizer([q, q])
