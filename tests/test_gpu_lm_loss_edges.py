@@ -114,3 +114,29 @@ def test_rows_without_a_target_get_no_gradient_whatever_comes_in(n, d, v, dtype)
     lse, total = lm.cross_entropy_forward(h, bad, t)[1:]
     dh = lm.cross_entropy_backward(one(), h, bad, t, lse, total)[0]
     assert torch.count_nonzero(dh[masked]) == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,d,v,start", [(150, 96, 700, 0), (150, 96, 700, 1), (4000, 64, 20000, 0), (5, 4096, 60000, 0)])
+def test_one_gradient_alone_has_the_same_bits(n, d, v, start, dtype):
+    h, w, t = inputs(n, d, v, dtype)
+    hold = torch.zeros(v * d + start, dtype=dtype, device="cuda")
+    x = hold[start:].view(v, d)
+    x.copy_(w)
+    lse, total = lm.cross_entropy_forward(h, x, t)[1:]
+    dh, dw = lm.cross_entropy_backward(one(), h, x, t, lse, total)
+    a = lm.cross_entropy_backward(one(), h, x, t, lse, total, need_weight=False)
+    b = lm.cross_entropy_backward(one(), h, x, t, lse, total, need_hidden=False)
+    assert a[1] is None and b[0] is None and torch.equal(a[0], dh) and torch.equal(b[1], dw)
+    assert lm.cross_entropy_backward(one(), h, x, t, lse, total, need_hidden=False, need_weight=False) == (None, None)
+
+
+def test_autograd_forms_only_the_gradients_that_are_asked_for():
+    h, w, t = inputs(30, 40, 90, F32)
+    want = []
+    for a, b in ((True, True), (True, False), (False, True)):
+        x, y = h.clone().requires_grad_(a), w.clone().requires_grad_(b)
+        lm.linear_cross_entropy(x, y, t).backward()
+        want = want or [x.grad, y.grad]
+        for g, ref, asked in ((x.grad, want[0], a), (y.grad, want[1], b)):
+            assert torch.equal(g, ref) if asked else g is None
