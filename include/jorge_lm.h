@@ -180,7 +180,7 @@ jorge_status jorge_cross_entropy_backward(const jorge_loss_shape* shape, const f
 typedef struct jorge_adamw_tensor {
     void*       param;  /* numel elements of dtype, updated in place; no two tensors' may overlap */
     const void* grad;   /* numel elements of dtype                   */
-    int64_t     numel;  /* >= 0                                      */
+    int64_t     numel;  /* >= 0, at most 2^38                        */
     int64_t     block;  /* the tensor's first block in the moments' buffers; the tensors' blocks ascend
                            without overlap */
     int32_t     dtype;  /* JORGE_F32 or JORGE_BF16                   */

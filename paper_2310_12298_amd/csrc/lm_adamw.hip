@@ -332,12 +332,14 @@ __global__ __launch_bounds__(1024) void norm_finish_kernel(const double* __restr
 }
 
 // ---------------------------------------------------------------- host
+constexpr int64_t kMostElements = (int64_t)1 << 38;  // of a tensor
+
 jorge_status check_tensors(const jorge_adamw_tensor* t, int32_t n, bool step) {
     if (n < 0 || (n > 0 && !t)) return bad("adamw: n >= 0 tensors are needed");
     for (int32_t i = 0; i < n; ++i) {
         if (!known_dtype(t[i].dtype)) return bad("adamw: unknown element type");
         if (t[i].numel < 0) return bad("adamw: numel >= 0 is needed");
-        if (t[i].numel > (int64_t)1 << 38)
+        if (t[i].numel > kMostElements)
             return refuse(JORGE_ERR_UNSUPPORTED, "adamw: a tensor of more than 2^38 elements");
         if (t[i].numel == 0) continue;
         if (!t[i].grad || (step && !t[i].param)) return bad("adamw: a tensor's pointer is null");
@@ -428,8 +430,11 @@ extern "C" {
 jorge_status jorge_gradient_norm_workspace(const jorge_adamw_tensor* tensors, int32_t n, int64_t* bytes) {
     if (!bytes) return bad("gradient norm: bytes is needed");
     if (n < 0 || (n > 0 && !tensors)) return bad("gradient norm: n >= 0 tensors are needed");
-    for (int32_t i = 0; i < n; ++i)
+    for (int32_t i = 0; i < n; ++i) {
         if (tensors[i].numel < 0) return bad("gradient norm: numel >= 0 is needed");
+        if (tensors[i].numel > kMostElements)
+            return refuse(JORGE_ERR_UNSUPPORTED, "gradient norm: a tensor of more than 2^38 elements");
+    }
     *bytes = round_up((norm_groups(tensors, n) + 1) * (int64_t)sizeof(double), kAlign);
     return JORGE_OK;
 }

@@ -68,3 +68,11 @@ def test_the_largest_table_is_not_refused_after_its_tokens_are_sorted(lib, count
     assert lib.jorge_embedding_workspace(count, vocab, cols, ctypes.byref(n)) == 0
     assert lib.jorge_embedding_backward(P(A), cols, P(A), count, dtype, vocab, cols, 1.0, -1, P(A), cols, P(A), n.value,
                                         None) == HIP_ERROR
+
+
+def test_a_gradient_too_large_for_the_norm_has_no_workspace(lib):  # noqa: F811
+    n = I64()
+    for numel, want in ((1 << 38, 0), ((1 << 38) + 1, UNSUPPORTED), ((1 << 63) - 1, UNSUPPORTED), (-1, INVALID)):
+        ts = (lm.AdamWTensor * 1)(lm.AdamWTensor(0, A, numel, 0, 0, 0))
+        assert lib.jorge_gradient_norm_workspace(ts, 1, ctypes.byref(n)) == want
+    assert n.value > (1 << 38) // (1 << 14) * 8       # of the one that was taken
