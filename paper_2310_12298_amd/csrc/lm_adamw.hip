@@ -8,8 +8,9 @@
 // makes the largest magnitude of an 8-bit block a sum-like exchange within one wave.
 //
 // Measured: 25.5 M fp32 weights in 54 tensors, 32-bit moments: 110-119 us (6.0-6.5 TB/s; a large copy reaches
-// 5.0-5.15, but part of these 408 MB stays in the 256 MB cache behind L2); the norm of their gradients 25 us
-// (4.0 TB/s, what a large sum reaches) and 4 us to finish. 168 M weights, 8-bit moments: 544 us (4.9 TB/s);
+// 5.0-5.15, but part of these 408 MB stays in the 256 MB cache behind L2); the norm of their gradients 25.5 us
+// (4.0 TB/s, as torch's sum of 1 GiB; their bytes at a copy's rate would take 20) and 4 us to finish. 168 M weights,
+// 8-bit moments: 544 us (4.9 TB/s);
 // reading both moments back 2 x 85 us (5.9 TB/s).
 //
 // The step's arithmetic rounds every operation once (no contraction), so that the same

@@ -18,11 +18,13 @@
 //      go on in its neighbours: their sums go to the workspace. Other waves of the same
 //      launch write zeros to the rows that no token takes;
 //   4. the runs that cross chunks: their chunks' sums are added by a workgroup per run.
-// A token that half of all positions hold is thus spread over as many waves as any others.
+// A token that half of all positions hold is thus spread over as many waves as any others; what it adds is the join of
+// its chunks (all tokens equal against a Zipf distribution: 16384 of 2048 columns 54 against 49 us, 65536 of 512 76
+// against 68).
 //
 // Measured: 16384 tokens, 50000 x 2048 bf16: forward 21 us (134 MB to move at most, 6.3 TB/s: repeated rows
-// come from the cache), sorting 12, merging 8.5, sums and zeros 53-61 (272 MB, 4.4-5.1 TB/s), joining 7.
-// 65536 tokens, half of them one token, 8192 x 512 fp32: 28-33, 11.5, 21.5, 33 (151 MB, 4.6 TB/s) and 17 us.
+// come from the cache), sorting 12, merging 8.5, sums and zeros 53-62 (272 MB, 4.4-5.1 TB/s), joining 7.
+// 65536 tokens, half of them one token, 8192 x 512 fp32: 28-33, 11.5, 21.5, 33 (151 MB, 4.6 TB/s) and 16 us.
 #include "lm_common.hpp"
 
 #include <utility>
@@ -315,6 +317,9 @@ __global__ __launch_bounds__(256) void embed_sums_kernel(SumArgs a, const T* __r
 // all waves of the workgroup. Slabs of 64 columns serve narrow tables, where a long run would have too few CUs to
 // itself (one gets some 50 GB/s): 1024 chunks of 512 columns take 17 us, in slabs of 256 columns 27. Wide tables have
 // enough slabs of 256, and four times as many workgroups would cost more: 16384 tokens, 2048 columns 7 us against 13.
+// The whole gradient of 4000 bf16 rows, 65536 tokens, with either, Zipf-distributed and all equal: 512 columns 65 and
+// 71 us in narrow slabs, 62 and 93 in wide ones; 1024 columns 82 and 85 against 73 and 102; 1536 columns 100 and 108
+// against 86 and 117; 2048 columns 142 and 141 against 121 and 140.
 constexpr int kJoinWaves = 8;
 constexpr int kJoinAlone = 16;  // chunks after the first that a wave adds alone
 
@@ -417,6 +422,10 @@ __global__ __launch_bounds__(kJoinWaves * 64) void embed_join_kernel(SumArgs a, 
 // 32 entries (which are one chunk, with nothing to join) and up to 4096 it is 16: a wave sums a chunk's rows in turn,
 // which is much of a short call's time. Gradient of a 4000 x 512 fp32 table in chunks of 32, 16 and 8: 64 tokens 19.3,
 // 14.4, 14.4 us; 1651 tokens 24.1, 19.0, 18.5; 4096 tokens 27.8, 22.9, 23.4, and all of them equal 24.4, 24.8, 27.2.
+// Over 23 to 8192 columns, 20 to 65536 tokens, Zipf-distributed or all equal, and 8 to 128 entries a chunk (80 cases),
+// the rule's length takes at most 15% longer than the best, but for 4096 rows of 8192 fp32 columns that are all equal
+// (63 against 48 us in 32), 6000 of 23 (36 against 31 in 16), and 16384 or 65536 equal ones of 2048 columns and more
+// (16 to 24%, in 64 or 128).
 int chunk_of(int64_t count) {
     int c = count > 32 && count <= 4096 ? 16 : 32;
     while (ceil_div(count, c) > 4096 && c < 4096) c *= 2;
@@ -509,8 +518,8 @@ jorge_status backward(const void* dout, int64_t lddo, const int64_t* tokens, int
     a.ldp = (int)partial_row(cols);
     a.slabs = (int)ceil_div(cols, 64 * Wide<T>::N);
     a.scale = (float)scale;
-    // The largest of tokens, rows and columns fit in one grid (fewer than 2^32 threads): at most 4096 chunks, 64 rows or a
-    // chunk per wave and slab.
+    // The largest of tokens, rows and columns fit in one grid (fewer than 2^32 threads): at most 4096 chunks, and 64
+    // rows or a chunk per wave and slab.
     constexpr int64_t kMostSlabs = JORGE_EMBED_MAX_COLS / (64 * 4);
     static_assert((4096 + JORGE_EMBED_MAX_VOCAB / kZeroRows) * kMostSlabs / 4 + 2 < (1ll << 32) / 256, "one launch");
     static_assert(JORGE_EMBED_MAX_TOKENS / 4096 <= 4096, "4096 chunks of up to 4096");

@@ -24,8 +24,9 @@
 // targets stay at 1.66e-3, their own rounding: the target's -1 is exact and makes up most of them. fp32 inputs have
 // dz in three terms.
 //
-// Transposed copies of weight's piece and of hidden cost a hundredth of the time of the
-// products that they feed.
+// The copies of weight's piece and of hidden, padded, transposed or split, cost 4% of the time of the gradients'
+// products in bf16 and 15% in fp32 at the sizes below, and more the fewer tokens there are: of 64 tokens' 84 us with
+// 8192 words of 512 in fp32 they are a quarter.
 //
 // fp32 operands are split into three bfloat16 terms that sum to them exactly (in bfloat16's range), and a
 // product is the six products of terms down to 2^-16 of the whole: the same K loop, six times as long.
@@ -34,10 +35,10 @@
 //
 // Measured (a library product of 8192 x 8192 x 8192 in bf16 reaches 1350-1400 TFLOP/s here, x 2048 1140-1200, in fp32
 // 153). Rates are over a pass's whole product, all pieces of the vocabulary together:
-//   bf16, 8192 tokens, cols 2048, 50001 words: forward 1.35-1.38 ms (1220-1240 TFLOP/s); in seven pieces dz 1.64 ms
-//   (1020), each gradient 1.46 ms (1150), transposes 0.12 ms; both passes 6.0 ms.
-//   fp32, 2001 tokens, cols 1001, 30011 words (six products each): forward 0.50-0.55 ms (220-240 TFLOP/s of fp32
-//   products); in two pieces dz 0.69 ms (175), each gradient 0.56 ms (214), copies 0.17 ms; both passes 2.4 ms.
+//   bf16, 8192 tokens, cols 2048, 50001 words: forward 1.33-1.38 ms (1210-1260 TFLOP/s); in seven pieces dz 1.66 ms
+//   (1010), each gradient 1.49 ms (1120), transposes 0.12 ms; both passes 6.0 ms.
+//   fp32, 2001 tokens, cols 1001, 30011 words (six products each): forward 0.50-0.56 ms (215-240 TFLOP/s of fp32
+//   products); in two pieces dz 0.70 ms (172), each gradient 0.57 ms (211), copies 0.17 ms; both passes 2.4 ms.
 // The MFMAs are busy 59% of the bf16 forward's wave cycles and 80% of the fp32 one's, which loads half as much for
 // each: the former is bound by the way from L2 to LDS as well. Power bounds both: a loop of these MFMAs on registers
 // alone reaches 1850-1970 TFLOP/s with random operands, 2430 with zeros.
@@ -407,8 +408,8 @@ struct Scale {
 };
 
 // C[b][a] over one of gridDim.y ranges of K, to out (whole: one range) or to the range's slice of fp32 sums
-// [ranges][B.rows][lda], added to it where `add`. rows: of B's rows, where those are tokens; one without a target gets 0,
-// not 0 times what the scale or A may hold.
+// [ranges][B.rows][lda], added to it where `add`. rows: of B's rows, where those are tokens; one without a target gets
+// 0, not 0 times what the scale or A may hold.
 template <int WA, int WB, int RING, bool SPLIT, typename O>
 __global__ __launch_bounds__(256, 1) void loss_grad_kernel(Product p, O* __restrict__ out, int64_t ldo,
                                                            float* __restrict__ slices, int64_t lda, int add,
@@ -528,10 +529,11 @@ bool direct(const jorge_loss_shape& s, const void* p, int64_t ld) {
     return s.dtype == JORGE_BF16 && s.cols % kPadK == 0 && ld % 8 == 0 && aligned(p, 16);
 }
 
-// What bounds the workspaces, whatever the vocabulary: elements of one layout of dz (forward: of weight's copy), and, where
-// tokens are few and weight outgrows dz, those of each of the backward pass's two copies of it, terms together: 1 GiB. In
-// 2^29 elements a piece keeps enough tiles for the CUs: 64 tokens, 128256 words of 4096 in fp32 take 4.43 ms and 2.1 GB,
-// in 2^28 4.80 and 1.1, with weight copied whole 4.26 and 6.4; 1 token, 262144 words of 8192 in bf16 5.42 ms, 5.85, 5.05.
+// What bounds the workspaces, whatever the vocabulary: elements of one layout of dz (forward: of weight's copy), and,
+// where tokens are few and weight outgrows dz, those of each of the backward pass's two copies of it, terms together:
+// 1 GiB. In 2^29 elements a piece keeps enough tiles for the CUs: 64 tokens, 128256 words of 4096 in fp32 take 4.43 ms
+// and 2.1 GB, in 2^28 4.80 and 1.1, with weight copied whole 4.26 and 6.4; 1 token, 262144 words of 8192 in bf16 5.42,
+// 5.85 and 5.05 ms.
 constexpr int64_t kPieceElements = 1 << 26;
 constexpr int64_t kCopyElements = 1 << 29;
 // Tiles of one launch: its threads have to stay below 2^32.
@@ -568,10 +570,10 @@ Plan plan_of(const jorge_loss_shape& s, bool backward, bool direct_x, bool direc
     p.kn = round_up(s.tokens, kPadK);
     p.direct_x = direct_x;
     p.direct_w = direct_w;
-    // Without copies of weight the forward pass needs no pieces. A piece may take another tile than the whole vocabulary
-    // does, which groups the words of a row's sums otherwise: lse's last bits depend on whether bf16 weight lies so
-    // that it can be read in place. The whole vocabulary's tile for its pieces too would cost those (500 tokens of
-    // 8192, 128256 words at an odd address: 3.62 against 2.23 ms), the pieces' tile for the whole the usual call.
+    // Without copies of weight the forward pass needs no pieces. A piece may take another tile than the whole
+    // vocabulary does, which groups the words of a row's sums otherwise: lse's last bits depend on whether bf16 weight
+    // lies so that it can be read in place. The whole vocabulary's tile for its pieces too would cost those (500 tokens
+    // of 8192, 128256 words at an odd address: 3.62 against 2.23 ms), the pieces' tile for the whole the usual call.
     int64_t most = kPieceElements / (s.dtype == JORGE_F32 ? 2 : 1) / std::max<int64_t>(1, backward ? p.kn : p.kd);
     if (backward) most = std::min(most, kCopyElements / (p.terms * p.kd));
     if (!backward && direct_w) most = s.vocab;

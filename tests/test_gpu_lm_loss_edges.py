@@ -117,7 +117,8 @@ def test_rows_without_a_target_get_no_gradient_whatever_comes_in(n, d, v, dtype)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("n,d,v,start", [(150, 96, 700, 0), (150, 96, 700, 1), (4000, 64, 20000, 0), (5, 4096, 60000, 0)])
+@pytest.mark.parametrize("n,d,v,start", [(150, 96, 700, 0), (150, 96, 700, 1), (4000, 64, 20000, 0),
+                                         (5, 4096, 60000, 0)])
 def test_one_gradient_alone_has_the_same_bits(n, d, v, start, dtype):
     h, w, t = inputs(n, d, v, dtype)
     hold = torch.zeros(v * d + start, dtype=dtype, device="cuda")

@@ -46,7 +46,7 @@ def test_the_loss_of_few_tokens_copies_no_whole_weight(lib, tokens, dtype):  # n
 
 
 NO_GPU = pytest.mark.skipif(torch.cuda.is_available(), reason="accepted calls would follow made-up addresses")
-HIP_ERROR = -3                                        # JORGE_ERR_HIP: where there is no GPU, a launch that was let through
+HIP_ERROR = -3                                        # JORGE_ERR_HIP: of a launch, where there is no GPU
 
 
 @NO_GPU
