@@ -554,8 +554,7 @@ class AdamW:
 
     def check_state_dict(self, sd):
         """Raises ValueError unless load_state_dict would take sd whole."""
-        held = all(isinstance(sd.get(k), torch.Tensor) and sd[k].shape == v.shape and sd[k].dtype == v.dtype
-                   for k, v in self.moments.items())
+        held = all(isinstance(sd.get(k), torch.Tensor) and sd[k].shape == v.shape for k, v in self.moments.items())
         if not held or sd.get("bits") != self.bits or len(sd.get("steps", self.params)) != len(self.params):
             raise ValueError("the state is of another set of tensors or of other bits")
         if not all(int(t) >= 0 for t in [sd.get("t", -1), *sd.get("steps", [])]):
