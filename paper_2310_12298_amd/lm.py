@@ -538,10 +538,12 @@ class AdamW:
     def set_moment_values(self, exp_avg, exp_avg_sq):
         """Takes the moments' values from flat fp32 tensors in the layout of moment_values (8 bits: rounded to
         nearest)."""
-        for second, (k, v) in enumerate((("exp_avg", exp_avg), ("exp_avg_sq", exp_avg_sq))):
-            v = _cuda(v, k, (torch.float32,)).contiguous()
+        values = {"exp_avg": exp_avg, "exp_avg_sq": exp_avg_sq}
+        for k, v in values.items():
+            values[k] = _cuda(v, k, (torch.float32,)).contiguous()
             if v.shape != self.moments[k].shape:
                 raise ValueError(f"{k}: {self.moments[k].numel()} values are needed")
+        for second, (k, v) in enumerate(values.items()):
             if self.bits == 32:
                 self.moments[k].copy_(v)
             else:

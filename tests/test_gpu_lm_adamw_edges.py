@@ -223,3 +223,16 @@ def test_parameters_that_share_memory_are_refused():
     q = torch.nn.Parameter(tensors([8], F32)[0])
     with pytest.warns(UserWarning), pytest.raises(ValueError, match="share memory"):
         AdamWOptimizer([q, q])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_refused_moment_values_change_nothing(bits):
+    opt = lm.AdamW(tensors(SIZES, F32), bits=bits)
+    n = opt.moments["exp_avg"].numel()
+    ones = torch.ones(n, device="cuda")
+    for bad in (ones[1:], ones.bfloat16(), ones.cpu(), None):
+        with pytest.raises(ValueError):
+            opt.set_moment_values(ones, bad)
+        assert not any(bool(x.any()) for x in opt.moments.values())
+    opt.set_moment_values(ones, ones)
+    assert all(torch.equal(x, ones) for x in opt.moment_values())
