@@ -160,6 +160,65 @@ jorge_status jorge_cross_entropy_backward(const jorge_loss_shape* shape, const f
                                           const float* lse, const float* total, void* dhidden, void* dweight,
                                           void* workspace, int64_t workspace_bytes, void* hip_stream);
 
+/* ---------------------------------------------------------------- linear layers
+ * With act one of JORGE_ACT_* (gelu with the error function, silu(z) = z sigmoid(z)):
+ *   linear:        z = x weight^T + bias,  y = act(z) + residual;
+ *   gated linear:  g = x gate^T,  u = x up^T,  y = act(g) u.
+ * Gradients, with z, g and u formed again from x:
+ *   linear:        dz = dy act'(z),  dx = dz weight,  dweight = dz^T x,  dbias = sum over tokens of dz
+ *                  (the residual's gradient is dy);
+ *   gated linear:  dg = dy u act'(g),  du = dy act(g),  dx = dg gate + du up,  dgate = dg^T x,  dup = du^T x.
+ * relu's derivative at 0 is 0. bfloat16: dz, dg and du are rounded to bfloat16 for the products, whose sums are fp32
+ * (dbias is summed before that); a gradient then errs by some 2.4e-3 of its size instead of the 1.7e-3 of its own
+ * rounding. fp32: up to 64 tokens forward are multiplied in fp32; the other products are formed from three-term
+ * bfloat16 splits as the Jorge step's are (jorge.h): values above 3.39e38 count as infinite. */
+#define JORGE_ACT_NONE    0
+#define JORGE_ACT_RELU    1
+#define JORGE_ACT_GELU    2
+#define JORGE_ACT_SILU    3
+#define JORGE_ACT_SIGMOID 4
+
+/* Largest tokens, cols, outs and row strides; tokens * max(cols, outs) ends at 2^34. */
+#define JORGE_LINEAR_MAX_TOKENS (1 << 21)
+#define JORGE_LINEAR_MAX_COLS   32768
+#define JORGE_LINEAR_MAX_OUTS   (1 << 18)
+#define JORGE_LINEAR_MAX_STRIDE (1 << 22)
+
+typedef struct jorge_linear_shape {
+    int64_t tokens, cols, outs;  /* >= 1 (tokens may be 0); x: tokens x cols, a weight: outs x cols  */
+    int64_t ldx, ldw, ldu;       /* row strides of x, of weight (gate), of up (gated linear)         */
+    int64_t ldy, ldr;            /* of y (forward) or dy (backward), of residual                     */
+    int32_t dtype, bias_dtype;   /* of x, the weights, residual, y and their gradients; of bias and dbias */
+    int32_t activation;          /* JORGE_ACT_*                                                      */
+    int32_t reserved;            /* 0 */
+} jorge_linear_shape;
+
+/* Bytes of workspace of the forward (backward = 0) or backward pass of the linear (gated = 0) or gated linear layer
+ * (host pointers); 0 where none is needed. */
+jorge_status jorge_linear_workspace(const jorge_linear_shape* shape, int32_t gated, int32_t backward, int64_t* bytes);
+
+/* shape: host. bias: outs elements, residual: tokens x outs; each may be NULL. y may be residual (with ldy = ldr). */
+jorge_status jorge_linear_forward(const jorge_linear_shape* shape, const void* x, const void* weight, const void* bias,
+                                  const void* residual, void* y, void* workspace, int64_t workspace_bytes,
+                                  void* hip_stream);
+
+/* dx: tokens x cols, dweight: outs x cols, dbias: outs; each written whole unless NULL (dweight and dbias zeros where
+ * tokens is 0). ldr is not read. */
+jorge_status jorge_linear_backward(const jorge_linear_shape* shape, const void* dy, const void* x, const void* weight,
+                                   const void* bias, void* dx, int64_t lddx, void* dweight, int64_t lddw, void* dbias,
+                                   void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* bias_dtype and ldr are not read. */
+jorge_status jorge_gated_linear_forward(const jorge_linear_shape* shape, const void* x, const void* gate,
+                                        const void* up, void* y, void* workspace, int64_t workspace_bytes,
+                                        void* hip_stream);
+
+/* dgate, dup: outs x cols in the stride lddw; either both or neither. */
+jorge_status jorge_gated_linear_backward(const jorge_linear_shape* shape, const void* dy, const void* x,
+                                         const void* gate, const void* up, void* dx, int64_t lddx, void* dgate,
+                                         void* dup, int64_t lddw, void* workspace, int64_t workspace_bytes,
+                                         void* hip_stream);
+
 /* ---------------------------------------------------------------- AdamW
  * Step t of every element p of every tensor, with g its gradient times the clip factor:
  *   m <- m + (1 - beta1) (g - m),  v <- v + (1 - beta2) (g^2 - v),

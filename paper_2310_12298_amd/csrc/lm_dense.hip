@@ -1,0 +1,932 @@
+// The linear layer y = act(x weight^T + bias) + residual and the gated projection y = act(x gate^T) * (x up^T), forward
+// and backward, for gfx950.
+//
+// Bound by the matrix products: 2 tokens cols outs flops a matrix forward and twice that backward, and once more
+// backward where an activation's argument is formed again rather than kept: kept in 32 bits it would take four bytes
+// for every two of y, and rounded to bfloat16 it would put a second rounding into every gradient.
+//
+// Forward: a tile of products stays in registers for bias, activation, product of the pair and residual. The gated
+// projection's tile is of the same columns of both matrices (Tile's PAIR), so that a lane holds both factors.
+//
+// Backward:
+//   dz = dy act'(z)  (gated: dgate = dy u act'(g), dup = dy act(g), side by side as one matrix of 2 outs columns)
+//   dx = dz weight       (K: the columns of dz)
+//   dweight = dz^T x     (K: the tokens)
+// dz is written both ways round from the registers of the tile that forms z again, so that both products have
+// K-contiguous operands; bfloat16 inputs: rounded to bfloat16 for that, as the matrix instructions take it (a gradient,
+// a sum of such terms, errs by up to 2.4e-3 of its size instead of the 1.7e-3 of its own rounding). Without an
+// activation dz is dy as it is. dbias is summed from the unrounded dz.
+//
+// Few tokens, forward: bound by reading the weights once. A workgroup takes 16 of their rows, its eight waves cut K,
+// and nothing goes through LDS but the sums; fp32 then runs on the fp32 MFMAs, as splits would cost three times the
+// bytes.
+#include "lm_product.hpp"
+
+#include <math.h>
+
+namespace jorge_lm {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896341f;
+
+// ---------------------------------------------------------------- activations
+// 1 / (1 + exp(-z)). exp(-z) = 2^t 2^r with t the rounded product -z log2(e) and r what its rounding left out (fp32).
+template <bool EXACT>
+__device__ __forceinline__ float logistic(float z) {
+    const float t = -z * kLog2e;
+    float e = __builtin_amdgcn_exp2f(t);
+    if constexpr (EXACT) {
+        const float r = __builtin_fmaf(-z, kLog2e, -t) - z * 1.925963033500e-8f;
+        e = __builtin_fmaf(e, r * 0.693147180559945f, e);
+    }
+    const float s = __builtin_amdgcn_rcpf(1.0f + e);
+    // Beyond 88 the steps above overflow, and the sigmoid is 0 or 1 to the last bit. A NaN passes both comparisons by.
+    return z < -88.0f ? 0.0f : z > 88.0f ? 1.0f : s;
+}
+struct Acted {
+    float a, d;  // act(z), act'(z)
+};
+// EXACT: fp32 results; otherwise they will be rounded to bfloat16.
+template <bool EXACT>
+__device__ __forceinline__ Acted acted(int act, float z) {
+    switch (act) {
+        case JORGE_ACT_RELU: return {z > 0.0f || z != z ? z : 0.0f, z > 0.0f ? 1.0f : z != z ? z : 0.0f};
+        case JORGE_ACT_GELU: {
+            const float phi = 0.5f + 0.5f * erff(z * 0.707106781186547524f);
+            const float density = 0.398942280401432678f * __builtin_amdgcn_exp2f(-0.5f * z * z * kLog2e);
+            return {z * phi, phi + z * density};
+        }
+        case JORGE_ACT_SILU: {
+            const float s = logistic<EXACT>(z);
+            return {z * s, s * (1.0f + z * (1.0f - s))};
+        }
+        case JORGE_ACT_SIGMOID: {
+            const float s = logistic<EXACT>(z);
+            return {s, s * (1.0f - s)};
+        }
+        default: return {z, 1.0f};
+    }
+}
+
+// ---------------------------------------------------------------- epilogues
+// M consecutive elements at p, of which `left` exist.
+template <int M, typename T>
+__device__ __forceinline__ void load_some(const T* p, int left, float (&f)[M]) {
+    typedef T V __attribute__((ext_vector_type(M), aligned(sizeof(T))));
+    if (left >= M) {
+        const V v = *reinterpret_cast<const V*>(p);
+#pragma unroll
+        for (int e = 0; e < M; ++e) f[e] = (float)v[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < M; ++e) f[e] = e < left ? (float)p[e] : 0.0f;
+    }
+}
+template <int M, typename T>
+__device__ __forceinline__ void store_some(T* p, int left, const float (&f)[M]) {
+    typedef T V __attribute__((ext_vector_type(M), aligned(sizeof(T))));
+    if (left >= M) {
+        V v;
+#pragma unroll
+        for (int e = 0; e < M; ++e) v[e] = (T)f[e];
+        *reinterpret_cast<V*>(p) = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < M; ++e)
+            if (e < left) p[e] = (T)f[e];
+    }
+}
+
+// A bias vector of either type, or none.
+struct Bias {
+    const void* p;
+    int bf;
+    template <int M>
+    __device__ __forceinline__ void load(int64_t c, int left, float (&f)[M]) const {
+        if (!p) {
+#pragma unroll
+            for (int e = 0; e < M; ++e) f[e] = 0.0f;
+        } else if (bf) load_some<M>((const bf16*)p + c, left, f);
+        else load_some<M>((const float*)p + c, left, f);
+    }
+};
+
+// What a product becomes. z: x weight^T, u: x up^T (gated).
+template <typename T>
+struct Finish {
+    Bias bias;
+    const T* residual;
+    T* y;
+    int64_t ldr, ldy;
+    int act;
+    // M elements of row `row` from column c on, of which `left` exist. y may be residual: read before it is written.
+    template <int M, bool PAIR>
+    __device__ __forceinline__ void store(int64_t row, int64_t c, int left, const float (&z)[M],
+                                          const float (&u)[M]) const {
+        if (left <= 0) return;
+        float f[M], b[M], r[M];
+        if constexpr (!PAIR) {
+            bias.template load<M>(c, left, b);
+            if (residual) load_some<M>(residual + row * ldr + c, left, r);
+        }
+#pragma unroll
+        for (int e = 0; e < M; ++e) {
+            f[e] = acted<sizeof(T) == 4>(act, PAIR ? z[e] : z[e] + b[e]).a;
+            if constexpr (PAIR) f[e] *= u[e];
+            else if (residual) f[e] += r[e];
+        }
+        store_some<M>(y + row * ldy + c, left, f);
+    }
+};
+
+// A wave's part of a tile, row by row: 16 rows (tokens) of column j of its accumulators go through LDS, so that a lane
+// gets 8 consecutive columns of a row (8 of both matrices, PAIR) and a row's stores are whole cache lines. The body is
+// in a loop: unrolled over all accumulators, activations would spill them. f(row, column, z, u): of the wave's part.
+template <int WA, bool PAIR>
+struct Rows {
+    static constexpr int kCols = PAIR ? 8 * WA : 16 * WA;          // of a row, of one matrix
+    static constexpr int kLd = 16 * WA + 4;                        // the odd 16 bytes spread 16 rows over all banks
+    static constexpr int kLanes = kCols / 8, kPasses = kLanes / 4; // lanes to a row; passes of 64 / kLanes rows
+    static_assert(kPasses >= 1, "a pass takes whole rows");
+    float* at;                                                     // this wave's area
+    __device__ __forceinline__ explicit Rows(char* lds)
+        : at(reinterpret_cast<float*>(lds) + (threadIdx.x >> 6) * 16 * kLd) {}
+    // Where this lane's own accumulators of column j lie: row lane % 16, piece i.
+    __device__ __forceinline__ f32x4* piece(int i) const {
+        const int lane = threadIdx.x & 63;
+        const int c = PAIR ? (i / (WA / 2)) * 8 * WA + (lane >> 4) * 2 * WA + 4 * (i % (WA / 2))
+                           : (lane >> 4) * 4 * WA + 4 * i;
+        return reinterpret_cast<f32x4*>(at + (lane & 15) * kLd + c);
+    }
+    static __device__ __forceinline__ void fence() {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+    template <typename ACC, typename F>
+    __device__ __forceinline__ void each(const ACC& acc, int j, F&& f) const {
+        fence();
+#pragma unroll
+        for (int i = 0; i < WA; ++i) *piece(i) = acc[i][j];
+        fence();
+        const int lane = threadIdx.x & 63;
+#pragma unroll 1
+        for (int pass = 0; pass < kPasses; ++pass) {
+            const int row = pass * (64 / kLanes) + lane / kLanes, c = lane % kLanes * 8;
+            float z[8], u[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                z[e] = at[row * kLd + c + e];
+                u[e] = PAIR ? at[row * kLd + kCols + c + e] : 0.0f;
+            }
+            f(row, c, z, u);
+        }
+    }
+};
+
+// Of a workgroup's range of K (blockIdx.y of gridDim.y), its stages.
+struct Range {
+    int s0, s1;
+    __device__ __forceinline__ Range(int stages) {
+        const int pairs = stages / 2;
+        s0 = (int)((int64_t)pairs * blockIdx.y / gridDim.y) * 2;
+        s1 = (int)((int64_t)pairs * (blockIdx.y + 1) / gridDim.y) * 2;
+    }
+};
+
+// A product of one matrix (A) or two (A and A2) with B's rows.
+struct Dense {
+    Product p;
+    Operand A2;
+};
+
+// Tiles of y, or, where K is cut, of its sums: slices [ranges][tokens][lda], the second matrix's columns lda / 2 on.
+template <int WA, int RING, bool SPLIT, bool PAIR, typename T>
+__global__ __launch_bounds__(256, 1) void dense_forward_kernel(Dense d, Finish<T> out, float* __restrict__ slices,
+                                                               int64_t lda) {
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    using Q = Tile<WA, WA, RING, SPLIT, PAIR>;
+    const Place at = place_of(blockIdx.x, d.p.ta, d.p.tb);
+    const Range k(d.p.stages);
+    Q t;
+    t.multiply(d.p.A, d.A2, d.p.B, (int64_t)at.a * Q::kRowsA, (int64_t)at.b * Q::kB, k.s0, k.s1, d.p.stages, lds);
+    const int64_t a0 = (int64_t)at.a * Q::kRowsA + Q::lane_a(), b0 = (int64_t)at.b * Q::kB + Q::lane_b();
+    const int left = left_of<Q::kLaneA>(d.p.A.rows - a0);
+    constexpr int kUp = PAIR ? WA / 2 : 0;
+    if (slices) {
+#pragma unroll
+        for (int j = 0; j < WA; ++j)
+            if (b0 + j < d.p.B.rows) {
+                f32x4* const q = reinterpret_cast<f32x4*>(slices + (blockIdx.y * d.p.B.rows + b0 + j) * lda + a0);
+                // Past the last column up to a multiple of four there is room.
+#pragma unroll
+                for (int i = 0; i < Q::kLaneA / 4; ++i)
+                    if (4 * i < left) {
+                        q[i] = t.acc[i][j];
+                        if constexpr (PAIR) q[i + lda / 8] = t.acc[i + kUp][j];
+                    }
+            }
+        return;
+    }
+    const Rows<WA, PAIR> rows(lds);
+    const int64_t wa = (int64_t)at.a * Q::kRowsA + (threadIdx.x >> 7) * (Q::kRowsA / 2);
+    const int64_t wb = (int64_t)at.b * Q::kB + ((threadIdx.x >> 6) & 1) * (Q::kB / 2);
+#pragma unroll
+    for (int j = 0; j < WA; ++j)
+        rows.each(t.acc, j, [&](int row, int c, const float(&z)[8], const float(&u)[8]) {
+            const int64_t token = wb + row * WA + j;
+            if (token < d.p.B.rows) out.template store<8, PAIR>(token, wa + c, left_of<8>(d.p.A.rows - wa - c), z, u);
+        });
+}
+
+// The sum of n slices at p, a fixed distance apart, in order.
+__device__ __forceinline__ f32x4 sum_slices(const float* p, int n, int64_t apart) {
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+    int k = 0;
+    for (; k + 4 <= n; k += 4) {
+        f32x4 v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = *reinterpret_cast<const f32x4*>(p + (k + u) * apart);
+        s += (v[0] + v[1]) + (v[2] + v[3]);
+    }
+    for (; k < n; ++k) s += *reinterpret_cast<const f32x4*>(p + k * apart);
+    return s;
+}
+
+template <bool PAIR, typename T>
+__global__ __launch_bounds__(256) void dense_join_kernel(const float* __restrict__ slices, int n, int64_t rows,
+                                                         int cols, int64_t lda, Finish<T> out) {
+    const int64_t r = blockIdx.x;
+    for (int c = (blockIdx.y * 256 + threadIdx.x) * 4; c < cols; c += gridDim.y * 1024) {
+        const float* const p = slices + r * lda + c;
+        const f32x4 a = sum_slices(p, n, rows * lda), b = PAIR ? sum_slices(p + lda / 2, n, rows * lda) : a;
+        const float z[4] = {a[0], a[1], a[2], a[3]}, u[4] = {b[0], b[1], b[2], b[3]};
+        out.template store<4, PAIR>(r, c, cols - c, z, u);
+    }
+}
+
+// ---------------------------------------------------------------- few tokens
+constexpr int kFewWaves = 8, kFewTokens = 64;  // the most tokens of the kernel below
+
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef __bf16 bf16x8u __attribute__((ext_vector_type(8), aligned(2)));
+
+// A lane's piece of a row for one step along K: 16 bytes, zeros past the end.
+template <typename T>
+struct Piece;
+template <>
+struct Piece<bf16> {
+    static constexpr int K = 32, E = 8;  // elements of K of a step, of a lane's piece
+    bf16x8 v;
+    __device__ __forceinline__ void load(const bf16* p, int left) {
+        if (left >= E) v = *reinterpret_cast<const bf16x8u*>(p);
+        else
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = e < left ? p[e] : (bf16)0.0f;
+    }
+    static __device__ __forceinline__ void mma(f32x4& c, const Piece& a, const Piece& b) {
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
+    }
+};
+template <>
+struct Piece<float> {
+    static constexpr int K = 16, E = 4;
+    f32x4 v;
+    __device__ __forceinline__ void load(const float* p, int left) {
+        if (left >= E) v = *reinterpret_cast<const f32x4u*>(p);
+        else
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = e < left ? p[e] : 0.0f;
+    }
+    // The four MFMAs take the same elements of both operands, so which k each is does not matter.
+    static __device__ __forceinline__ void mma(f32x4& c, const Piece& a, const Piece& b) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[e], b.v[e], c, 0, 0, 0);
+    }
+};
+
+struct FewRows {
+    const void *x, *w, *u;
+    int64_t ldx, ldw, ldu, outs;
+    int tokens, cols;
+};
+
+// Rows 16 blockIdx.x .. of the weights (of both), all tokens (up to 16 NT). An MFMA leaves lane l with rows
+// 4 (l / 16) + r of the weights and token l % 16.
+template <typename T, int NT, bool PAIR>
+__global__ __launch_bounds__(kFewWaves * 64) void dense_few_kernel(FewRows in, Finish<T> out) {
+    using P = Piece<T>;
+    constexpr int MATS = PAIR ? 2 : 1, U = NT == 1 ? 4 : 2;  // steps whose loads are started together
+    __shared__ float sums[kFewWaves][MATS][NT][64][4];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = (lane >> 4) * P::E;
+    const int64_t row0 = (int64_t)blockIdx.x * 16, row = row0 + (lane & 15);
+    const T* const w[2] = {(const T*)in.w + (row < in.outs ? row : in.outs - 1) * in.ldw + at,
+                           PAIR ? (const T*)in.u + (row < in.outs ? row : in.outs - 1) * in.ldu + at : nullptr};
+    const T* x[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int i = n * 16 + (lane & 15);
+        x[n] = (const T*)in.x + (int64_t)(i < in.tokens ? i : in.tokens - 1) * in.ldx + at;
+    }
+    f32x4 acc[MATS][NT] = {};
+    // Wave w takes the steps from w / 8 to (w + 1) / 8 of all.
+    const int steps = (in.cols + P::K - 1) / P::K;
+    const int s0 = steps * wave / kFewWaves, s1 = steps * (wave + 1) / kFewWaves;
+    int s = s0;
+    const auto some = [&](auto COUNT) {
+        constexpr int C = decltype(COUNT)::value;
+        P a[C][MATS], b[C][NT];
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int k = (s + c) * P::K, left = in.cols - k - at;
+#pragma unroll
+            for (int m = 0; m < MATS; ++m) a[c][m].load(w[m] + k, left);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) b[c][n].load(x[n] + k, left);
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int m = 0; m < MATS; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) P::mma(acc[m][n], a[c][m], b[c][n]);
+        s += C;
+    };
+    while (s + U <= s1) some(std::integral_constant<int, U>());
+    while (s < s1) some(std::integral_constant<int, 1>());
+#pragma unroll
+    for (int m = 0; m < MATS; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) *reinterpret_cast<f32x4*>(sums[wave][m][n][lane]) = acc[m][n];
+    __syncthreads();
+    if ((int)threadIdx.x >= 64 * NT) return;
+    const int n = threadIdx.x >> 6, token = n * 16 + (lane & 15);
+    f32x4 v[2] = {};
+#pragma unroll
+    for (int m = 0; m < MATS; ++m)
+#pragma unroll
+        for (int k = 0; k < kFewWaves; ++k) v[m] += *reinterpret_cast<const f32x4*>(sums[k][m][n][lane]);
+    if (token >= in.tokens) return;
+    const int64_t c = row0 + (lane >> 4) * 4;
+    const float z[4] = {v[0][0], v[0][1], v[0][2], v[0][3]}, u[4] = {v[1][0], v[1][1], v[1][2], v[1][3]};
+    out.template store<4, PAIR>(token, c, left_of<4>(in.outs - c), z, u);
+}
+
+// ---------------------------------------------------------------- backward
+struct DzOut {
+    bf16 *dz, *dzt;            // [tokens][terms][matrices * kf], [matrices * outs][terms][kn]
+    int64_t kf, kn;            // outs and tokens, padded to multiples of 64
+    float* bias;               // [parts][outs] sums of dz over 16 WA tokens each, or null
+};
+
+template <int WA, int RING, bool SPLIT, bool PAIR, typename T>
+__global__ __launch_bounds__(256, 1) void dense_dz_kernel(Dense d, const T* __restrict__ dy, int64_t ldy, Bias bias,
+                                                          int act, DzOut out) {
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    using Q = Tile<WA, WA, RING, SPLIT, PAIR>;
+    const Place at = place_of(blockIdx.x, d.p.ta, d.p.tb);
+    Q t;
+    t.multiply(d.p.A, d.A2, d.p.B, (int64_t)at.a * Q::kRowsA, (int64_t)at.b * Q::kB, 0, d.p.stages, d.p.stages, lds);
+    const int64_t a0 = (int64_t)at.a * Q::kRowsA + Q::lane_a(), b0 = (int64_t)at.b * Q::kB + Q::lane_b();
+    const int64_t outs = d.p.A.rows, tokens = d.p.B.rows;
+    constexpr int L = Q::kLaneA, kUp = PAIR ? WA / 2 : 0, MATS = PAIR ? 2 : 1;
+    const int left = left_of<L>(outs - a0);
+    constexpr int terms = SPLIT ? kTerms : 1;
+    const Rows<WA, PAIR> rows(lds);
+    const int64_t wa = (int64_t)at.a * Q::kRowsA + (threadIdx.x >> 7) * (Q::kRowsA / 2);
+    const int64_t wb = (int64_t)at.b * Q::kB + ((threadIdx.x >> 6) & 1) * (Q::kB / 2);
+#pragma unroll
+    for (int j = 0; j < WA; ++j) {
+        rows.each(t.acc, j, [&](int row, int c, float(&z)[8], float(&u)[8]) {
+            const int64_t token = wb + row * WA + j;
+            const int n = token < tokens ? left_of<8>(outs - wa - c) : 0;
+            float b[8] = {}, g[8] = {};
+            if constexpr (!PAIR) bias.template load<8>(wa + c, n, b);
+            if (n) load_some<8>(dy + token * ldy + wa + c, n, g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const Acted f = acted<sizeof(T) == 4>(act, z[e] + b[e]);
+                // Selected: rows and columns past the end hold copies of the last one.
+                z[e] = e < n ? (PAIR ? g[e] * u[e] * f.d : g[e] * f.d) : 0.0f;
+                u[e] = e < n ? g[e] * f.a : 0.0f;
+            }
+            float* const back = rows.at + row * rows.kLd + c;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                back[e] = z[e];
+                if constexpr (PAIR) back[rows.kCols + e] = u[e];
+            }
+            if (out.dz && token < tokens && wa + c < out.kf) {
+                bf16* const dz = out.dz + token * terms * MATS * out.kf + wa + c;
+                store_terms<terms>(dz, MATS * out.kf, z);
+                if constexpr (PAIR) store_terms<terms>(dz + out.kf, MATS * out.kf, u);
+            }
+        });
+        Rows<WA, PAIR>::fence();
+#pragma unroll
+        for (int i = 0; i < WA; ++i) t.acc[i][j] = *rows.piece(i);
+    }
+    if (!PAIR && out.bias) {
+        const int64_t part = b0 / (16 * WA);
+#pragma unroll
+        for (int i = 0; i < WA; ++i) {
+            f32x4 s = t.acc[i][0];
+#pragma unroll
+            for (int j = 1; j < WA; ++j) s += t.acc[i][j];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+#pragma unroll
+                for (int off = 1; off < 16; off *= 2) s[r] += __shfl_xor(s[r], off);
+                if ((threadIdx.x & 15) == 0 && 4 * i + r < left) out.bias[part * outs + a0 + 4 * i + r] = s[r];
+            }
+        }
+    }
+#pragma unroll
+    for (int term = 0; term < terms; ++term) {
+#pragma unroll
+        for (int m = 0; m < MATS; ++m) {
+            bf16* const dzt = out.dzt + term * out.kn + b0;
+            if (out.dzt && b0 < out.kn)
+#pragma unroll
+                for (int i = 0; i < L; ++i)
+                    if (i < left) {
+                        typedef __bf16 V __attribute__((ext_vector_type(WA)));
+                        V o;
+#pragma unroll
+                        for (int j = 0; j < WA; ++j) o[j] = (bf16)t.acc[i / 4 + m * kUp][j][i & 3];
+                        *reinterpret_cast<V*>(dzt + (m * outs + a0 + i) * terms * out.kn) = o;
+                    }
+        }
+        if constexpr (SPLIT)
+#pragma unroll
+            for (int j = 0; j < WA; ++j)
+#pragma unroll
+                for (int i = 0; i < WA; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) t.acc[i][j][r] -= (float)(bf16)t.acc[i][j][r];
+    }
+}
+
+// Where a gradient goes: rows [0, first) to one matrix, the others to a second.
+template <typename T>
+struct Target {
+    T *one, *two;
+    int64_t first, ld;
+    __device__ __forceinline__ T* row(int64_t r) const { return r < first ? one + r * ld : two + (r - first) * ld; }
+};
+
+// C[b][a] over one of gridDim.y ranges of K, whole (one range) or into the range's slice [ranges][B.rows][lda].
+template <int WA, int RING, bool SPLIT, typename T>
+__global__ __launch_bounds__(256, 1) void dense_grad_kernel(Product p, Target<T> out, float* __restrict__ slices,
+                                                            int64_t lda) {
+    extern __shared__ __attribute__((aligned(1024))) char lds[];
+    using Q = Tile<WA, WA, RING, SPLIT>;
+    const Place at = place_of(blockIdx.x, p.ta, p.tb);
+    const Range k(p.stages);
+    Q t;
+    t.multiply(p.A, p.B, (int64_t)at.a * Q::kA, (int64_t)at.b * Q::kB, k.s0, k.s1, p.stages, lds);
+    const int64_t a0 = (int64_t)at.a * Q::kA + Q::lane_a(), b0 = (int64_t)at.b * Q::kB + Q::lane_b();
+    const int left = left_of<4 * WA>(p.A.rows - a0);
+    if (slices) {
+#pragma unroll
+        for (int j = 0; j < WA; ++j)
+            if (b0 + j < p.B.rows) {
+                f32x4* const q = reinterpret_cast<f32x4*>(slices + (blockIdx.y * p.B.rows + b0 + j) * lda + a0);
+#pragma unroll
+                for (int i = 0; i < WA; ++i)
+                    if (4 * i < left) q[i] = t.acc[i][j];
+            }
+        return;
+    }
+    const Rows<WA, false> rows(lds);
+    const int64_t wa = (int64_t)at.a * Q::kA + (threadIdx.x >> 7) * (Q::kA / 2);
+    const int64_t wb = (int64_t)at.b * Q::kB + ((threadIdx.x >> 6) & 1) * (Q::kB / 2);
+#pragma unroll
+    for (int j = 0; j < WA; ++j)
+        rows.each(t.acc, j, [&](int row, int c, const float(&z)[8], const float(&)[8]) {
+            const int64_t b = wb + row * WA + j;
+            const int n = left_of<8>(p.A.rows - wa - c);
+            if (b < p.B.rows && n) store_some<8>(out.row(b) + wa + c, n, z);
+        });
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void dense_slices_kernel(const float* __restrict__ slices, int n, int64_t rows,
+                                                           int cols, int64_t lda, Target<T> out) {
+    const int64_t r = blockIdx.x;
+    for (int c = (blockIdx.y * 256 + threadIdx.x) * 4; c < cols; c += gridDim.y * 1024) {
+        const f32x4 s = sum_slices(slices + r * lda + c, n, rows * lda);
+        const float v[4] = {s[0], s[1], s[2], s[3]};
+        store_some<4>(out.row(r) + c, cols - c, v);
+    }
+}
+
+// Sums of dy's columns over kBiasRows rows, four columns a lane: a part [outs] per blockIdx.y.
+constexpr int kBiasRows = 128;
+template <typename T>
+__global__ __launch_bounds__(256) void dense_columns_kernel(const T* __restrict__ dy, int64_t ldy, int64_t tokens,
+                                                            int64_t outs, float* __restrict__ parts) {
+    __shared__ f32x4 sums[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = ((int64_t)blockIdx.x * 64 + lane) * 4, r0 = (int64_t)blockIdx.y * kBiasRows;
+    const int left = left_of<4>(outs - c);
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (left > 0)
+        for (int64_t r = r0 + wave; r < r0 + kBiasRows && r < tokens; r += 4) {
+            float f[4];
+            load_some<4>(dy + r * ldy + c, left, f);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] += f[e];
+        }
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave) return;
+    s = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < left) parts[blockIdx.y * outs + c + e] = s[e];
+}
+// dbias: the parts of 64 columns added up by 16 waves, each every 16th, and those in order.
+__global__ __launch_bounds__(1024) void dense_bias_kernel(const float* __restrict__ parts, int64_t n, int64_t outs,
+                                                          void* __restrict__ dbias, int bf) {
+    __shared__ float sums[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    float s = 0.0f;
+    if (c < outs)
+        for (int64_t k = wave; k < n; k += 16) s += parts[k * outs + c];
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (wave || c >= outs) return;
+#pragma unroll
+    for (int w = 1; w < 16; ++w) s += sums[w][lane];
+    if (bf) ((bf16*)dbias)[c] = (bf16)s;
+    else ((float*)dbias)[c] = s;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void dense_zero_kernel(T* p, int64_t ld, int64_t cols) {
+    for (int64_t c = threadIdx.x; c < cols; c += 256) p[blockIdx.x * ld + c] = (T)0.0f;
+}
+
+// ---------------------------------------------------------------- host
+constexpr const char* kNoLds = "dense product: no LDS for a tile";
+
+struct Plan {
+    int terms, products, mats;       // mats: 2 for the gated projection
+    int64_t kd, kf, kn;              // cols, outs and tokens, padded
+    bool few;                        // forward: the kernel for few tokens
+    bool direct_x, direct_w, direct_dy;
+    bool dz;                         // dz differs from dy
+    Shape z, dx, dw;
+};
+struct Wanted {
+    bool backward, dx, dw, db;
+};
+
+bool readable(int32_t dtype, int64_t cols, const void* p, int64_t ld) {
+    return dtype == JORGE_BF16 && cols % kPadK == 0 && ld % 8 == 0 && aligned(p, 16);
+}
+
+Plan plan_of(const jorge_linear_shape& s, int mats, const Wanted& want, bool direct_x, bool direct_w, bool direct_dy) {
+    Plan p{};
+    p.terms = s.dtype == JORGE_F32 ? kTerms : 1;
+    p.products = s.dtype == JORGE_F32 ? 6 : 1;
+    p.mats = mats;
+    p.kd = round_up(s.cols, kPadK);
+    p.kf = round_up(s.outs, kPadK);
+    p.kn = round_up(s.tokens, kPadK);
+    p.direct_x = direct_x;
+    p.direct_w = direct_w;
+    p.direct_dy = direct_dy;
+    p.few = !want.backward && s.tokens <= kFewTokens;
+    p.dz = mats == 2 || s.activation != JORGE_ACT_NONE;
+    p.z = shape_of(mats * s.outs, s.tokens, p.kd, p.products, !want.backward);
+    // A pair's tile of 64 x 64 holds 32 columns of each, which padding to 64 would leave without a tile.
+    if (mats == 2 && p.z.blocks == 2) p.z.blocks = 4;
+    if (want.backward) {
+        p.dx = shape_of(s.cols, s.tokens, mats * p.kf, p.products, true);
+        p.dw = shape_of(s.cols, mats * s.outs, p.kn, p.products, true);
+    }
+    return p;
+}
+
+struct Work {
+    bf16 *x, *w, *u;          // K-contiguous copies
+    bf16 *xt, *wt;            // transposes; wt: of both matrices side by side
+    bf16 *dz, *dzt;
+    float *z, *dx, *dw;       // slices
+    float* bias;
+    int64_t bytes, ldz, ldc;
+};
+int64_t bias_parts(const jorge_linear_shape& s, const Plan& p) {
+    return p.dz ? ceil_div(s.tokens, 32 * p.z.blocks) * 2 : ceil_div(s.tokens, kBiasRows);
+}
+Work carve(void* base, const jorge_linear_shape& s, const Plan& p, const Wanted& want) {
+    Carve c{(char*)base};
+    Work w{};
+    w.ldz = p.mats * round_up(s.outs, 4);
+    w.ldc = round_up(s.cols, 4);
+    const bool z = !want.backward || (p.dz && (want.dx || want.dw || want.db));
+    if (z && !p.few) {
+        if (!p.direct_x) w.x = c.take<bf16>(p.terms * s.tokens * p.kd);
+        if (!p.direct_w) w.w = c.take<bf16>(p.terms * s.outs * p.kd);
+        if (!p.direct_w && p.mats == 2) w.u = c.take<bf16>(p.terms * s.outs * p.kd);
+    }
+    if (!want.backward) {
+        if (!p.few && p.z.ranges > 1) w.z = c.take<float>(p.z.ranges * s.tokens * w.ldz);
+    } else {
+        if (want.dw) w.xt = c.take<bf16>(p.terms * s.cols * p.kn);
+        if (want.dx) w.wt = c.take<bf16>(p.terms * s.cols * p.mats * p.kf);
+        if (want.dx && (p.dz || !p.direct_dy)) w.dz = c.take<bf16>(p.terms * s.tokens * p.mats * p.kf);
+        if (want.dw) w.dzt = c.take<bf16>(p.terms * p.mats * s.outs * p.kn);
+        if (want.dx && p.dx.ranges > 1) w.dx = c.take<float>(p.dx.ranges * s.tokens * w.ldc);
+        if (want.dw && p.dw.ranges > 1) w.dw = c.take<float>(p.dw.ranges * p.mats * s.outs * w.ldc);
+        if (want.db) w.bias = c.take<float>(bias_parts(s, p) * s.outs);
+    }
+    w.bytes = c.used;
+    return w;
+}
+// What serves in place depends on addresses: room for every copy is asked for.
+int64_t workspace_of(const jorge_linear_shape& s, int mats, bool backward) {
+    const Wanted want{backward, backward, backward, backward && mats == 1};
+    return carve(nullptr, s, plan_of(s, mats, want, false, false, false), want).bytes;
+}
+
+template <typename F>
+void with_pair_tile(const Shape& s, F&& f) {
+    if (s.blocks == 8) f(std::integral_constant<int, 8>(), std::integral_constant<int, 4>());
+    else if (s.deep) f(std::integral_constant<int, 4>(), std::integral_constant<int, 8>());
+    else f(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
+}
+
+// The product of x with the weights: ta counts tiles of kRowsA rows.
+Dense dense_of(const jorge_linear_shape& s, const Plan& p, const Work& w, const void* x, const void* weight,
+               const void* up) {
+    const Operand X = p.direct_x ? Operand{(const bf16*)x, s.ldx, 0, s.tokens}
+                                 : Operand{w.x, p.terms * p.kd, p.kd, s.tokens};
+    const Operand W = p.direct_w ? Operand{(const bf16*)weight, s.ldw, 0, s.outs}
+                                 : Operand{w.w, p.terms * p.kd, p.kd, s.outs};
+    const Operand U = p.direct_w ? Operand{(const bf16*)up, s.ldu, 0, s.outs}
+                                 : Operand{w.u, p.terms * p.kd, p.kd, s.outs};
+    Dense d{product_of(p.z, W, X, p.kd), p.mats == 2 ? U : W};
+    d.p.ta = (int)ceil_div(s.outs, 32 * p.z.blocks / p.mats);
+    return d;
+}
+
+template <typename T, bool PAIR>
+jorge_status forward(const jorge_linear_shape& s, const Plan& p, const Work& w, const void* x, const void* weight,
+                     const void* up, const Finish<T>& out, hipStream_t st) {
+    if (p.few) {
+        const FewRows in{x, weight, up, s.ldx, s.ldw, s.ldu, s.outs, (int)s.tokens, (int)s.cols};
+        const dim3 grid((unsigned)ceil_div(s.outs, 16)), block(kFewWaves * 64);
+        if (s.tokens <= 16) dense_few_kernel<T, 1, PAIR><<<grid, block, 0, st>>>(in, out);
+        else if (s.tokens <= 32) dense_few_kernel<T, 2, PAIR><<<grid, block, 0, st>>>(in, out);
+        else dense_few_kernel<T, 4, PAIR><<<grid, block, 0, st>>>(in, out);
+        return launched("dense product");
+    }
+    copy<T>(copies_of(x, s.ldx, s.tokens, s.cols, w.x, p.kd, nullptr, 0),
+            copies_of(weight, s.ldw, s.outs, s.cols, w.w, p.kd, nullptr, 0), st,
+            copies_of(up, s.ldu, s.outs, s.cols, w.u, p.kd, nullptr, 0));
+    const Dense d = dense_of(s, p, w, x, weight, up);
+    jorge_status err = JORGE_OK;
+    const int ranges = p.z.ranges;
+    const auto run = [&](auto WA, auto RING) {
+        constexpr int B = decltype(WA)::value, R = decltype(RING)::value, bytes = Tile<B, B, R, sizeof(T) == 4>::kBytes;
+        const auto k = dense_forward_kernel<B, R, sizeof(T) == 4, PAIR, T>;
+        if ((err = allow_lds(k, bytes, kNoLds)) != JORGE_OK) return;
+        k<<<dim3(d.p.ta * d.p.tb, ranges), dim3(256), bytes, st>>>(d, out, w.z, w.ldz);
+    };
+    if constexpr (PAIR) with_pair_tile(p.z, run);
+    else with_tile(p.z, run);
+    if (err != JORGE_OK) return err;
+    if (w.z)
+        dense_join_kernel<PAIR, T><<<dim3((unsigned)s.tokens, (unsigned)ceil_div(s.outs, 1024)), dim3(256), 0, st>>>(
+            w.z, ranges, s.tokens, (int)s.outs, w.ldz, out);
+    return launched("dense product");
+}
+
+template <typename T>
+jorge_status gradient(const Shape& sh, const Product& pr, const Target<T>& out, int64_t cols, float* slices,
+                      hipStream_t st) {
+    jorge_status err = JORGE_OK;
+    const int64_t lda = round_up(cols, 4);
+    with_tile(sh, [&](auto WA, auto RING) {
+        constexpr int B = decltype(WA)::value, R = decltype(RING)::value, bytes = Tile<B, B, R, sizeof(T) == 4>::kBytes;
+        const auto k = dense_grad_kernel<B, R, sizeof(T) == 4, T>;
+        if ((err = allow_lds(k, bytes, kNoLds)) != JORGE_OK) return;
+        k<<<dim3(pr.ta * pr.tb, sh.ranges), dim3(256), bytes, st>>>(pr, out, slices, lda);
+    });
+    if (err == JORGE_OK && slices)
+        dense_slices_kernel<T><<<dim3((unsigned)pr.B.rows, (unsigned)ceil_div(cols, 1024)), dim3(256), 0, st>>>(
+            slices, sh.ranges, pr.B.rows, (int)cols, lda, out);
+    return err;
+}
+
+struct Gradients {
+    void *dx, *dweight, *dup, *dbias;
+    int64_t lddx, lddw;
+};
+
+template <typename T, bool PAIR>
+jorge_status backward(const jorge_linear_shape& s, const Plan& p, const Work& w, const void* dy, const void* x,
+                      const void* weight, const void* up, const Bias& bias, const Gradients& out, hipStream_t st) {
+    const int64_t kz = p.mats * p.kf;
+    bf16* const ut = w.wt && PAIR ? w.wt + p.kf : nullptr;
+    copy<T>(copies_of(x, s.ldx, s.tokens, s.cols, w.x, p.kd, w.xt, p.kn),
+            copies_of(weight, s.ldw, s.outs, s.cols, w.w, p.kd, w.wt, kz), st,
+            PAIR ? copies_of(up, s.ldu, s.outs, s.cols, w.u, p.kd, ut, kz)
+                 : p.dz ? Copies{} : copies_of(dy, s.ldy, s.tokens, s.outs, w.dz, p.kf, w.dzt, p.kn));
+    jorge_status err = JORGE_OK;
+    if (p.dz) {
+        const Dense d = dense_of(s, p, w, x, weight, up);
+        const DzOut z{w.dz, w.dzt, p.kf, p.kn, w.bias};
+        const auto run = [&](auto WA, auto RING) {
+            constexpr int B = decltype(WA)::value, R = decltype(RING)::value;
+            constexpr int bytes = Tile<B, B, R, sizeof(T) == 4>::kBytes;
+            const auto k = dense_dz_kernel<B, R, sizeof(T) == 4, PAIR, T>;
+            if ((err = allow_lds(k, bytes, kNoLds)) != JORGE_OK) return;
+            k<<<dim3(d.p.ta * d.p.tb), dim3(256), bytes, st>>>(d, (const T*)dy, s.ldy, bias, s.activation, z);
+        };
+        if constexpr (PAIR) with_pair_tile(p.z, run);
+        else with_tile(p.z, run);
+        if (err != JORGE_OK) return err;
+    } else if (w.bias) {
+        dense_columns_kernel<T><<<dim3((unsigned)ceil_div(s.outs, 256), (unsigned)bias_parts(s, p)), dim3(256), 0,
+                                  st>>>((const T*)dy, s.ldy, s.tokens, s.outs, w.bias);
+    }
+    if (out.dbias)
+        dense_bias_kernel<<<dim3((unsigned)ceil_div(s.outs, 64)), dim3(1024), 0, st>>>(
+            w.bias, bias_parts(s, p), s.outs, out.dbias, bias.bf);
+    if (out.dx) {
+        const Operand wt{w.wt, p.terms * kz, kz, s.cols};
+        const Operand z = w.dz ? Operand{w.dz, p.terms * kz, kz, s.tokens}
+                               : Operand{(const bf16*)dy, s.ldy, 0, s.tokens};
+        err = gradient<T>(p.dx, product_of(p.dx, wt, z, kz), {(T*)out.dx, nullptr, s.tokens, out.lddx}, s.cols, w.dx,
+                          st);
+        if (err != JORGE_OK) return err;
+    }
+    if (out.dweight) {
+        const Operand xt{w.xt, p.terms * p.kn, p.kn, s.cols}, zt{w.dzt, p.terms * p.kn, p.kn, p.mats * s.outs};
+        err = gradient<T>(p.dw, product_of(p.dw, xt, zt, p.kn), {(T*)out.dweight, (T*)out.dup, s.outs, out.lddw},
+                          s.cols, w.dw, st);
+        if (err != JORGE_OK) return err;
+    }
+    return launched("dense product");
+}
+
+jorge_status check(const jorge_linear_shape* s, bool gated) {
+    if (!s) return bad("linear: a shape is needed");
+    if (!known_dtype(s->dtype)) return bad("linear: unknown element type");
+    if (!gated && !known_dtype(s->bias_dtype)) return bad("linear: unknown element type of the bias");
+    if (s->activation < JORGE_ACT_NONE || s->activation > JORGE_ACT_SIGMOID) return bad("linear: unknown activation");
+    if (s->tokens < 0 || s->cols < 1 || s->outs < 1)
+        return bad("linear: tokens >= 0, cols >= 1 and outs >= 1 are needed");
+    if (s->tokens > JORGE_LINEAR_MAX_TOKENS)
+        return refuse(JORGE_ERR_UNSUPPORTED, "linear: tokens above JORGE_LINEAR_MAX_TOKENS");
+    if (s->cols > JORGE_LINEAR_MAX_COLS) return refuse(JORGE_ERR_UNSUPPORTED, "linear: cols above JORGE_LINEAR_MAX_COLS");
+    if (s->outs > JORGE_LINEAR_MAX_OUTS) return refuse(JORGE_ERR_UNSUPPORTED, "linear: outs above JORGE_LINEAR_MAX_OUTS");
+    if (ceil_div(s->tokens, 64) * ceil_div(std::max(s->cols, s->outs), 64) > 1 << 22)
+        return refuse(JORGE_ERR_UNSUPPORTED, "linear: tokens * max(cols, outs) above 2^34");
+    const int64_t strides[] = {s->ldx, s->ldw, gated ? s->ldu : s->ldw, s->ldy}, least[] = {s->cols, s->cols, s->cols,
+                                                                                            s->outs};
+    for (int i = 0; i < 4; ++i) {
+        if (strides[i] < least[i]) return bad("linear: a row stride is below its columns");
+        if (strides[i] > JORGE_LINEAR_MAX_STRIDE)
+            return refuse(JORGE_ERR_UNSUPPORTED, "linear: a row stride above JORGE_LINEAR_MAX_STRIDE (2^22)");
+    }
+    return JORGE_OK;
+}
+jorge_status check_workspace(const jorge_linear_shape& s, int mats, bool backward, const void* workspace,
+                             int64_t bytes) {
+    const int64_t need = workspace_of(s, mats, backward);
+    if (need == 0) return JORGE_OK;
+    if (!workspace || !aligned(workspace, kAlign)) return bad("linear: a workspace aligned to 256 bytes is needed");
+    if (bytes < need) return bad("linear: the workspace is too small");
+    return JORGE_OK;
+}
+
+jorge_status run_forward(const jorge_linear_shape& s, int mats, const void* x, const void* weight, const void* up,
+                         const void* bias, const void* residual, void* y, void* workspace, int64_t bytes, void* stream) {
+    const int64_t e = dtype_bytes(s.dtype);
+    if (s.tokens == 0) return JORGE_OK;
+    if (!x || !weight || !y || (mats == 2 && !up)) return bad("linear: x, the weights and y are needed");
+    if (!aligned(x, e) || !aligned(weight, e) || !aligned(up, e) || !aligned(y, e) || !aligned(residual, e) ||
+        !aligned(bias, dtype_bytes(s.bias_dtype)))
+        return bad("linear: a pointer is not aligned to its element");
+    if (residual && (s.ldr < s.outs)) return bad("linear: a row stride is below its columns");
+    const jorge_status st = check_workspace(s, mats, false, workspace, bytes);
+    if (st != JORGE_OK) return st;
+    const Wanted want{false, false, false, false};
+    const bool direct_w = readable(s.dtype, s.cols, weight, s.ldw) && (mats == 1 || readable(s.dtype, s.cols, up, s.ldu));
+    const Plan p = plan_of(s, mats, want, readable(s.dtype, s.cols, x, s.ldx), direct_w, false);
+    const Work w = carve(workspace, s, p, want);
+    const hipStream_t q = reinterpret_cast<hipStream_t>(stream);
+    const Bias b{bias, s.bias_dtype == JORGE_BF16};
+    if (s.dtype == JORGE_F32) {
+        const Finish<float> f{b, (const float*)residual, (float*)y, s.ldr, s.ldy, s.activation};
+        return mats == 2 ? forward<float, true>(s, p, w, x, weight, up, f, q)
+                         : forward<float, false>(s, p, w, x, weight, up, f, q);
+    }
+    const Finish<bf16> f{b, (const bf16*)residual, (bf16*)y, s.ldr, s.ldy, s.activation};
+    return mats == 2 ? forward<bf16, true>(s, p, w, x, weight, up, f, q)
+                     : forward<bf16, false>(s, p, w, x, weight, up, f, q);
+}
+
+template <typename T>
+void zero(void* p, int64_t rows, int64_t ld, int64_t cols, hipStream_t q) {
+    if (p) dense_zero_kernel<T><<<dim3((unsigned)rows), dim3(256), 0, q>>>((T*)p, ld, cols);
+}
+
+jorge_status run_backward(const jorge_linear_shape& s, int mats, const void* dy, const void* x, const void* weight,
+                          const void* up, const void* bias, const Gradients& g, void* workspace, int64_t bytes,
+                          void* stream) {
+    const int64_t e = dtype_bytes(s.dtype);
+    if (!aligned(g.dx, e) || !aligned(g.dweight, e) || !aligned(g.dup, e) ||
+        !aligned(g.dbias, dtype_bytes(s.bias_dtype)) || !aligned(bias, dtype_bytes(s.bias_dtype)))
+        return bad("linear: a pointer is not aligned to its element");
+    if (mats == 2 && !g.dweight != !g.dup) return bad("gated linear: dgate and dup go together");
+    if ((g.dx && g.lddx < s.cols) || (g.dweight && g.lddw < s.cols))
+        return bad("linear: a row stride is below its columns");
+    const hipStream_t q = reinterpret_cast<hipStream_t>(stream);
+    if (s.tokens == 0) {
+        if (s.dtype == JORGE_F32) {
+            zero<float>(g.dweight, s.outs, g.lddw, s.cols, q);
+            zero<float>(g.dup, s.outs, g.lddw, s.cols, q);
+        } else {
+            zero<bf16>(g.dweight, s.outs, g.lddw, s.cols, q);
+            zero<bf16>(g.dup, s.outs, g.lddw, s.cols, q);
+        }
+        if (s.bias_dtype == JORGE_F32) zero<float>(g.dbias, 1, s.outs, s.outs, q);
+        else zero<bf16>(g.dbias, 1, s.outs, s.outs, q);
+        return launched("dense product");
+    }
+    if (!dy || !x || !weight || (mats == 2 && !up)) return bad("linear: dy, x and the weights are needed");
+    if (!aligned(dy, e) || !aligned(x, e) || !aligned(weight, e) || !aligned(up, e))
+        return bad("linear: a pointer is not aligned to its element");
+    const jorge_status st = check_workspace(s, mats, true, workspace, bytes);
+    if (st != JORGE_OK) return st;
+    const Wanted want{true, g.dx != nullptr, g.dweight != nullptr, g.dbias != nullptr};
+    if (!want.dx && !want.dw && !want.db) return JORGE_OK;
+    const bool direct_w = readable(s.dtype, s.cols, weight, s.ldw) && (mats == 1 || readable(s.dtype, s.cols, up, s.ldu));
+    const Plan p = plan_of(s, mats, want, readable(s.dtype, s.cols, x, s.ldx), direct_w,
+                           readable(s.dtype, s.outs, dy, s.ldy));
+    const Work w = carve(workspace, s, p, want);
+    const Bias b{bias, s.bias_dtype == JORGE_BF16};
+    if (s.dtype == JORGE_F32)
+        return mats == 2 ? backward<float, true>(s, p, w, dy, x, weight, up, b, g, q)
+                         : backward<float, false>(s, p, w, dy, x, weight, up, b, g, q);
+    return mats == 2 ? backward<bf16, true>(s, p, w, dy, x, weight, up, b, g, q)
+                     : backward<bf16, false>(s, p, w, dy, x, weight, up, b, g, q);
+}
+
+}  // namespace
+}  // namespace jorge_lm
+
+using namespace jorge_lm;
+
+extern "C" {
+
+jorge_status jorge_linear_workspace(const jorge_linear_shape* shape, int32_t gated, int32_t backward, int64_t* bytes) {
+    if (!bytes) return bad("linear: bytes is needed");
+    const jorge_status st = check(shape, gated != 0);
+    if (st != JORGE_OK) return st;
+    *bytes = shape->tokens ? workspace_of(*shape, gated ? 2 : 1, backward != 0) : 0;
+    return JORGE_OK;
+}
+
+jorge_status jorge_linear_forward(const jorge_linear_shape* shape, const void* x, const void* weight, const void* bias,
+                                  const void* residual, void* y, void* workspace, int64_t workspace_bytes,
+                                  void* hip_stream) {
+    const jorge_status st = check(shape, false);
+    if (st != JORGE_OK) return st;
+    return run_forward(*shape, 1, x, weight, nullptr, bias, residual, y, workspace, workspace_bytes, hip_stream);
+}
+
+jorge_status jorge_linear_backward(const jorge_linear_shape* shape, const void* dy, const void* x, const void* weight,
+                                   const void* bias, void* dx, int64_t lddx, void* dweight, int64_t lddw, void* dbias,
+                                   void* workspace, int64_t workspace_bytes, void* hip_stream) {
+    const jorge_status st = check(shape, false);
+    if (st != JORGE_OK) return st;
+    return run_backward(*shape, 1, dy, x, weight, nullptr, bias, {dx, dweight, nullptr, dbias, lddx, lddw}, workspace,
+                        workspace_bytes, hip_stream);
+}
+
+jorge_status jorge_gated_linear_forward(const jorge_linear_shape* shape, const void* x, const void* gate,
+                                        const void* up, void* y, void* workspace, int64_t workspace_bytes,
+                                        void* hip_stream) {
+    const jorge_status st = check(shape, true);
+    if (st != JORGE_OK) return st;
+    return run_forward(*shape, 2, x, gate, up, nullptr, nullptr, y, workspace, workspace_bytes, hip_stream);
+}
+
+jorge_status jorge_gated_linear_backward(const jorge_linear_shape* shape, const void* dy, const void* x,
+                                         const void* gate, const void* up, void* dx, int64_t lddx, void* dgate,
+                                         void* dup, int64_t lddw, void* workspace, int64_t workspace_bytes,
+                                         void* hip_stream) {
+    const jorge_status st = check(shape, true);
+    if (st != JORGE_OK) return st;
+    return run_backward(*shape, 2, dy, x, gate, up, nullptr, {dx, dgate, dup, nullptr, lddx, lddw}, workspace,
+                        workspace_bytes, hip_stream);
+}
+
+}  // extern "C"

@@ -52,9 +52,15 @@ typedef __attribute__((address_space(1))) const void global_void;
 __device__ __forceinline__ int swizzle64(int rho) { return -(rho >> 2) & 3; }
 __device__ __forceinline__ int swizzle128(int rho) { return rho >> 1; }
 
-template <int WA, int WB, int RING, bool SPLIT>
+// PAIR: A is two matrices of the same shape and plane, and a tile half as many rows of each: a wave's blocks i < WA / 2
+// are of the first, the others of the second, so that a lane holds the same 2 WA rows of both:
+//   a = 2 WA (l / 16) + 4 i + r  of 8 WA rows, in blocks i and i + WA / 2.
+// The loads of waves 0 and 2 are then all of the first matrix, those of 1 and 3 of the second.
+template <int WA, int WB, int RING, bool SPLIT, bool PAIR = false>
 struct Tile {
     static constexpr int kA = 32 * WA, kB = 32 * WB;
+    static constexpr int kRowsA = PAIR ? 16 * WA : kA;             // of A (of each of two)
+    static constexpr int kLaneA = PAIR ? 2 * WA : 4 * WA;          // consecutive ones that a lane ends up with
     static constexpr int kBytes = RING * (kA + kB) * kStageK * 2;  // of LDS: RING stages of 32 k
     // Direct-to-LDS loads per wave and stage of the ring.
     static constexpr int kLoadsA = SPLIT ? WA / 2 : WA, kLoadsB = SPLIT ? WB / 2 : WB, kLoads = kLoadsA + kLoadsB;
@@ -64,7 +70,7 @@ struct Tile {
     // First a and first b of the calling lane's part of the tile.
     static __device__ __forceinline__ int lane_a() {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        return (wave >> 1) * 16 * WA + (lane >> 4) * 4 * WA;
+        return (wave >> 1) * (kRowsA / 2) + (lane >> 4) * kLaneA;
     }
     static __device__ __forceinline__ int lane_b() {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -75,12 +81,18 @@ struct Tile {
     // s0 and s1 are even, s1 > s0. lds: kBytes.
     __device__ __forceinline__ void multiply(const Operand& A, const Operand& B, int64_t a0, int64_t b0, int s0, int s1,
                                              int stages, char* lds) {
+        multiply(A, A, B, a0, b0, s0, s1, stages, lds);
+    }
+    // PAIR: of A1 and A2.
+    __device__ __forceinline__ void multiply(const Operand& A1, const Operand& A2, const Operand& B, int64_t a0,
+                                             int64_t b0, int s0, int s1, int stages, char* lds) {
         const int lane = threadIdx.x & 63;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const Operand& A = PAIR && (wave & 1) ? A2 : A1;
         Loads load;
         // Where this lane's loads start: load n of the operand (n = wave * kLoads + v) takes rows rho of block i of a
         // half of the tile. Bytes from the tile's first row to the end of its last one are what a load may reach.
-        const int limA = (int)(A.rows - a0 < kA ? A.rows - a0 : kA) - 1;
+        const int limA = (int)(A.rows - a0 < kRowsA ? A.rows - a0 : kRowsA) - 1;
         const int limB = (int)(B.rows - b0 < kB ? B.rows - b0 : kB) - 1;
         const unsigned K = (unsigned)(stages * kStageK), more = SPLIT ? kTerms - 1 : 0;
         const auto place = [&](int n, int& block, int& rho) {
@@ -92,7 +104,7 @@ struct Tile {
         for (int v = 0; v < kLoadsA; ++v) {
             int block, rho;
             const unsigned chunk = place(wave * kLoadsA + v, block, rho);
-            const int row = block / WA * 16 * WA + (rho >> 2) * 4 * WA + 4 * (block % WA) + (rho & 3);
+            const int row = block / WA * (kRowsA / 2) + (rho >> 2) * kLaneA + 4 * (block % (kLaneA / 4)) + (rho & 3);
             load.offA[v] = (unsigned)(row < limA ? row : limA) * (unsigned)A.ld * 2u + chunk;
         }
 #pragma unroll

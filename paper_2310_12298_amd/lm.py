@@ -22,11 +22,18 @@ _P, _I32, _I64, _F64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c
 BLOCK = 256                                   # elements of an 8-bit moment that share a scale
 DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 REDUCTIONS = {"none": 0, "sum": 1, "mean": 2}
+ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "gelu": 2, "silu": 3, "sigmoid": 4}
 
 
 class LossShape(ctypes.Structure):
     _fields_ = [("tokens", _I64), ("cols", _I64), ("vocab", _I64), ("ldh", _I64), ("ldw", _I64), ("dtype", _I32),
                 ("reserved", _I32), ("ignore_index", _I64), ("label_smoothing", _F64)]
+
+
+class LinearShape(ctypes.Structure):
+    _fields_ = [("tokens", _I64), ("cols", _I64), ("outs", _I64), ("ldx", _I64), ("ldw", _I64), ("ldu", _I64),
+                ("ldy", _I64), ("ldr", _I64), ("dtype", _I32), ("bias_dtype", _I32), ("activation", _I32),
+                ("reserved", _I32)]
 
 
 class AdamWTensor(ctypes.Structure):
@@ -41,6 +48,7 @@ class AdamWMoments(ctypes.Structure):
 
 
 _PT, _PM, _PS = ctypes.POINTER(AdamWTensor), ctypes.POINTER(AdamWMoments), ctypes.POINTER(LossShape)
+_PL = ctypes.POINTER(LinearShape)
 # name -> (restype, argtypes); mirrors include/jorge_lm.h
 _SIGNATURES = {
     "jorge_lm_last_error": (ctypes.c_char_p, []),
@@ -54,6 +62,11 @@ _SIGNATURES = {
     "jorge_cross_entropy_workspace": (_I32, [_PS, _I32, ctypes.POINTER(_I64)]),
     "jorge_cross_entropy_forward": (_I32, [_PS, _P, _P, _P, _P, _P, _P, _P, _I64, _P]),
     "jorge_cross_entropy_backward": (_I32, [_PS, _P, _I32, _P, _P, _P, _P, _P, _P, _P, _P, _I64, _P]),
+    "jorge_linear_workspace": (_I32, [_PL, _I32, _I32, ctypes.POINTER(_I64)]),
+    "jorge_linear_forward": (_I32, [_PL, _P, _P, _P, _P, _P, _P, _I64, _P]),
+    "jorge_linear_backward": (_I32, [_PL, _P, _P, _P, _P, _P, _I64, _P, _I64, _P, _P, _I64, _P]),
+    "jorge_gated_linear_forward": (_I32, [_PL, _P, _P, _P, _P, _P, _I64, _P]),
+    "jorge_gated_linear_backward": (_I32, [_PL, _P, _P, _P, _P, _P, _I64, _P, _P, _I64, _P, _I64, _P]),
     "jorge_gradient_norm_workspace": (_I32, [_PT, _I32, ctypes.POINTER(_I64)]),
     "jorge_gradient_norm": (_I32, [_PT, _I32, _F64, _P, _P, _I64, _P]),
     "jorge_adamw_step": (_I32, [_PT, _I32, _PM, _I64, _F64, _F64, _F64, _F64, _F64, _P, _P]),
@@ -358,6 +371,163 @@ def linear_cross_entropy(hidden, weight, targets, ignore_index=-100, label_smoot
     if reduction not in REDUCTIONS:
         raise ValueError(f"reduction: {reduction!r} is none of {sorted(REDUCTIONS)}")
     return _CrossEntropy.apply(hidden, weight, targets, ignore_index, label_smoothing, reduction)
+
+
+# ---------------------------------------------------------------- linear layers
+LINEAR_MAX_STRIDE = 1 << 22                   # JORGE_LINEAR_MAX_STRIDE
+
+
+def _rows(t, what):
+    """_matrix, copied to dense rows where the row stride is more than the call takes."""
+    m = _matrix(t, what)
+    return m.contiguous() if m.shape[0] > 1 and m.stride(0) > LINEAR_MAX_STRIDE else m
+
+
+def _activation(name):
+    if name not in ACTIVATIONS:
+        raise ValueError(f"activation: one of {[a for a in ACTIVATIONS if a]}, or None")
+    return ACTIVATIONS[name]
+
+
+def _weights(x, weights):
+    """x as a matrix, and weights that fit it and one another: (outs, cols) of x's type."""
+    m = _rows(x, "x")
+    ws = [_rows(w, what) for w, what in weights]
+    for w, (t, what) in zip(ws, weights):
+        if t.dim() != 2 or w.shape[1] != m.shape[1]:
+            raise ValueError(f"{what}: a matrix with rows of x's width is needed")
+        if w.dtype != x.dtype:
+            raise ValueError(f"{what} must have x's type")
+        if w.shape != ws[0].shape:
+            raise ValueError(f"{what}: shape {tuple(w.shape)}, not {tuple(ws[0].shape)}")
+    return m, ws
+
+
+def _linear_shape(m, w, u, ldy, ldr, bias, activation):
+    return LinearShape(m.shape[0], m.shape[1], w.shape[0], _ld(m), _ld(w), _ld(u), ldy, ldr, DTYPES[m.dtype],
+                       0 if bias is None else DTYPES[bias.dtype], activation, 0)
+
+
+def _linear_workspace(lib, shape, gated, backward):
+    n = _I64(0)
+    _check(lib, lib.jorge_linear_workspace(ctypes.byref(shape), gated, backward, ctypes.byref(n)))
+    return _workspace(n.value), n.value
+
+
+def linear_forward(x, weight, bias=None, activation=None, residual=None):
+    """activation(x @ weight.T + bias) + residual, of x's type. weight: (outs, cols); bias: fp32 or bfloat16;
+    residual: of x's type and y's shape. activation: "relu", "gelu", "silu", "sigmoid" or None."""
+    lib = load_operators()
+    act = _activation(activation)
+    m, (w,) = _weights(x, [(weight, "weight")])
+    outs = w.shape[0]
+    b = None if bias is None else _vector(bias, outs, "bias")
+    shape_y = x.shape[:-1] + (outs,)
+    r = None
+    if residual is not None:
+        if residual.shape != shape_y or residual.dtype != x.dtype:
+            raise ValueError("residual must have the result's shape and x's type")
+        r = _rows(residual, "residual")
+    y = torch.empty(shape_y, dtype=x.dtype, device=x.device)
+    shape = _linear_shape(m, w, w, outs, outs if r is None else _ld(r), b, act)
+    ws, n = _linear_workspace(lib, shape, 0, 0)
+    _check(lib, lib.jorge_linear_forward(ctypes.byref(shape), m.data_ptr(), w.data_ptr(), _ptr(b), _ptr(r),
+                                         y.data_ptr(), _ptr(ws), n, _stream(x)))
+    return y
+
+
+def linear_backward(dy, x, weight, bias=None, activation=None, need_x=True, need_weight=True, need_bias=True):
+    """(dx, dweight, dbias) of linear_forward; the residual's gradient is dy. dbias has bias's type (None without a
+    bias); what is not needed is None."""
+    lib = load_operators()
+    act = _activation(activation)
+    m, (w,) = _weights(x, [(weight, "weight")])
+    outs, cols = w.shape
+    if dy.shape != x.shape[:-1] + (outs,) or dy.dtype != x.dtype:
+        raise ValueError("dy must have the result's shape and x's type")
+    d = _rows(dy, "dy")
+    b = None if bias is None else _vector(bias, outs, "bias")
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_x else None
+    dw = torch.empty((outs, cols), dtype=x.dtype, device=x.device) if need_weight else None
+    db = torch.empty(outs, dtype=b.dtype, device=x.device) if need_bias and b is not None else None
+    shape = _linear_shape(m, w, w, _ld(d), outs, b, act)
+    ws, n = _linear_workspace(lib, shape, 0, 1)
+    _check(lib, lib.jorge_linear_backward(ctypes.byref(shape), d.data_ptr(), m.data_ptr(), w.data_ptr(), _ptr(b),
+                                          _ptr(dx), cols, _ptr(dw), cols, _ptr(db), _ptr(ws), n, _stream(x)))
+    return dx, dw, db
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, activation, residual):
+        ctx.save_for_backward(x, weight, bias)
+        ctx.activation = activation
+        return linear_forward(x, weight, bias, activation, residual)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        x, weight, bias = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dx, dw, db = linear_backward(dy, x, weight, bias, ctx.activation, *need[:3]) if any(need[:3]) else (None,) * 3
+        return dx, dw, db, None, dy if need[4] else None
+
+
+def linear(x, weight, bias=None, activation=None, residual=None):
+    """Differentiable activation(x @ weight.T + bias) + residual (see linear_forward)."""
+    return _Linear.apply(x, weight, bias, activation, residual)
+
+
+def gated_linear_forward(x, gate, up, activation="silu"):
+    """activation(x @ gate.T) * (x @ up.T), of x's type. gate, up: (outs, cols). activation: as in linear_forward."""
+    lib = load_operators()
+    act = _activation(activation)
+    m, (g, u) = _weights(x, [(gate, "gate"), (up, "up")])
+    y = torch.empty(x.shape[:-1] + (g.shape[0],), dtype=x.dtype, device=x.device)
+    shape = _linear_shape(m, g, u, g.shape[0], g.shape[0], None, act)
+    ws, n = _linear_workspace(lib, shape, 1, 0)
+    _check(lib, lib.jorge_gated_linear_forward(ctypes.byref(shape), m.data_ptr(), g.data_ptr(), u.data_ptr(),
+                                               y.data_ptr(), _ptr(ws), n, _stream(x)))
+    return y
+
+
+def gated_linear_backward(dy, x, gate, up, activation="silu", need_x=True, need_weights=True):
+    """(dx, dgate, dup) of gated_linear_forward; what is not needed is None."""
+    lib = load_operators()
+    act = _activation(activation)
+    m, (g, u) = _weights(x, [(gate, "gate"), (up, "up")])
+    outs, cols = g.shape
+    if dy.shape != x.shape[:-1] + (outs,) or dy.dtype != x.dtype:
+        raise ValueError("dy must have the result's shape and x's type")
+    d = _rows(dy, "dy")
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_x else None
+    dg, du = (torch.empty((outs, cols), dtype=x.dtype, device=x.device) if need_weights else None for _ in range(2))
+    shape = _linear_shape(m, g, u, _ld(d), outs, None, act)
+    ws, n = _linear_workspace(lib, shape, 1, 1)
+    _check(lib, lib.jorge_gated_linear_backward(ctypes.byref(shape), d.data_ptr(), m.data_ptr(), g.data_ptr(),
+                                                u.data_ptr(), _ptr(dx), cols, _ptr(dg), _ptr(du), cols, _ptr(ws), n,
+                                                _stream(x)))
+    return dx, dg, du
+
+
+class _GatedLinear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, gate, up, activation):
+        ctx.save_for_backward(x, gate, up)
+        ctx.activation = activation
+        return gated_linear_forward(x, gate, up, activation)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        need = ctx.needs_input_grad
+        dx, dg, du = gated_linear_backward(dy, *ctx.saved_tensors, ctx.activation, need[0], need[1] or need[2])
+        return dx, dg if need[1] else None, du if need[2] else None, None
+
+
+def gated_linear(x, gate, up, activation="silu"):
+    """Differentiable activation(x @ gate.T) * (x @ up.T) (see gated_linear_forward)."""
+    return _GatedLinear.apply(x, gate, up, activation)
 
 
 # ---------------------------------------------------------------- AdamW
