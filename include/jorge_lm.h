@@ -219,6 +219,61 @@ jorge_status jorge_gated_linear_backward(const jorge_linear_shape* shape, const 
                                          void* dup, int64_t lddw, void* workspace, int64_t workspace_bytes,
                                          void* hip_stream);
 
+/* ---------------------------------------------------------------- attention
+ * Of queries q (batch x q_tokens x heads x dim) over k and v (batch x kv_tokens x kv_heads x dim), heads / kv_heads
+ * consecutive heads to one of k and v, with z = scale q k^T over the keys that a query sees:
+ *   lse = log sum exp z,  o = sum exp(z - lse) v.
+ * A sequence b has q_lengths[b] queries and kv_lengths[b] keys (those of the whole batch where the pointer is NULL;
+ * values outside 0 .. tokens count as the nearest of them), from its first row on. A query sees every key of its
+ * sequence; with causal, query i stands at position kv length - q length + i and sees the keys up to its own position,
+ * with a window of w > 0 the last w of those. A query that sees nothing, or that is past its sequence's length, has
+ * o = 0, lse = minus infinity and no part in any gradient, whatever it holds; so has a key past its sequence's length,
+ * whose rows of k and v may hold anything. A value that is not finite in a key that a query may not see can reach the
+ * query if both are near the edge of the mask (in the same 64 keys): 0 times it is NaN.
+ * Gradients, from the o and lse of the forward pass, with p = exp(z - lse):
+ *   delta = do . o,  ds = scale p (do v^T - delta),  dq = ds k,  dk = ds^T q,  dv = p^T do,
+ * dk and dv summed over the heads that share them. bfloat16: p and ds are rounded to bfloat16 for their products, all
+ * else is fp32 (a gradient then errs by some 2.4e-3 of its size instead of the 1.7e-3 of its own rounding). fp32 is
+ * multiplied in fp32. */
+
+/* Largest dim, tokens, token stride, and batch * heads * tokens (of q or of k). */
+#define JORGE_ATTENTION_MAX_DIM    128
+#define JORGE_ATTENTION_MAX_TOKENS (1 << 22)
+#define JORGE_ATTENTION_MAX_STRIDE (1 << 22)
+#define JORGE_ATTENTION_MAX_ROWS   (1 << 26)
+
+/* A matrix of heads: element d of head h of token t of sequence b is data[b batch + t token + h head + d]. */
+typedef struct jorge_heads {
+    void*   data;
+    int64_t batch, token, head;  /* strides in elements, >= 0 */
+} jorge_heads;
+
+typedef struct jorge_attention_shape {
+    int64_t batch, q_tokens, kv_tokens; /* >= 0 */
+    int32_t heads, kv_heads, dim;       /* heads a multiple of kv_heads */
+    int32_t dtype;                      /* of q, k, v, out and their gradients */
+    double  scale;                      /* > 0, below 1e30 */
+    int32_t causal;                     /* 0 or 1 */
+    int32_t reserved;                   /* 0 */
+    int64_t window;                     /* 0 for none; needs causal */
+    const int64_t *q_lengths, *kv_lengths; /* device: batch numbers each, or NULL */
+    jorge_heads q, k, v;                /* their data is only read */
+} jorge_attention_shape;
+
+/* Bytes of workspace (host pointers; 0 where none is needed) of the forward pass (dout NULL) or the backward pass. It
+ * depends on the matrices' addresses and strides too: those whose rows do not lie in whole 16 bytes are copied. */
+jorge_status jorge_attention_workspace(const jorge_attention_shape* shape, const jorge_heads* dout, int64_t* bytes);
+
+/* shape, out: host. lse: batch x heads x q_tokens floats. */
+jorge_status jorge_attention_forward(const jorge_attention_shape* shape, const jorge_heads* out, float* lse,
+                                     void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* dq like q, dk and dv like k: each written whole unless NULL. */
+jorge_status jorge_attention_backward(const jorge_attention_shape* shape, const jorge_heads* dout,
+                                      const jorge_heads* out, const float* lse, const jorge_heads* dq,
+                                      const jorge_heads* dk, const jorge_heads* dv, void* workspace,
+                                      int64_t workspace_bytes, void* hip_stream);
+
 /* ---------------------------------------------------------------- AdamW
  * Step t of every element p of every tensor, with g its gradient times the clip factor:
  *   m <- m + (1 - beta1) (g - m),  v <- v + (1 - beta2) (g^2 - v),

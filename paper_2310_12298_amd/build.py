@@ -12,7 +12,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libjorge.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("jorge.hip", "lm_api.hip", "lm_norm.hip", "lm_embed.hip", "lm_loss.hip",
-                                           "lm_dense.hip", "lm_adamw.hip")]
+                                           "lm_dense.hip", "lm_attention.hip", "lm_adamw.hip")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

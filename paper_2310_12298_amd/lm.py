@@ -36,6 +36,16 @@ class LinearShape(ctypes.Structure):
                 ("reserved", _I32)]
 
 
+class Heads(ctypes.Structure):
+    _fields_ = [("data", _P), ("batch", _I64), ("token", _I64), ("head", _I64)]
+
+
+class AttentionShape(ctypes.Structure):
+    _fields_ = [("batch", _I64), ("q_tokens", _I64), ("kv_tokens", _I64), ("heads", _I32), ("kv_heads", _I32),
+                ("dim", _I32), ("dtype", _I32), ("scale", _F64), ("causal", _I32), ("reserved", _I32),
+                ("window", _I64), ("q_lengths", _P), ("kv_lengths", _P), ("q", Heads), ("k", Heads), ("v", Heads)]
+
+
 class AdamWTensor(ctypes.Structure):
     # Addresses as numbers, so that a numpy view of an array of these can set them by the column.
     _fields_ = [("param", ctypes.c_uint64), ("grad", ctypes.c_uint64), ("numel", _I64), ("block", _I64),
@@ -48,7 +58,7 @@ class AdamWMoments(ctypes.Structure):
 
 
 _PT, _PM, _PS = ctypes.POINTER(AdamWTensor), ctypes.POINTER(AdamWMoments), ctypes.POINTER(LossShape)
-_PL = ctypes.POINTER(LinearShape)
+_PL, _PA, _PH = ctypes.POINTER(LinearShape), ctypes.POINTER(AttentionShape), ctypes.POINTER(Heads)
 # name -> (restype, argtypes); mirrors include/jorge_lm.h
 _SIGNATURES = {
     "jorge_lm_last_error": (ctypes.c_char_p, []),
@@ -67,6 +77,9 @@ _SIGNATURES = {
     "jorge_linear_backward": (_I32, [_PL, _P, _P, _P, _P, _P, _I64, _P, _I64, _P, _P, _I64, _P]),
     "jorge_gated_linear_forward": (_I32, [_PL, _P, _P, _P, _P, _P, _I64, _P]),
     "jorge_gated_linear_backward": (_I32, [_PL, _P, _P, _P, _P, _P, _I64, _P, _P, _I64, _P, _I64, _P]),
+    "jorge_attention_workspace": (_I32, [_PA, _PH, ctypes.POINTER(_I64)]),
+    "jorge_attention_forward": (_I32, [_PA, _PH, _P, _P, _I64, _P]),
+    "jorge_attention_backward": (_I32, [_PA, _PH, _PH, _P, _PH, _PH, _PH, _P, _I64, _P]),
     "jorge_gradient_norm_workspace": (_I32, [_PT, _I32, ctypes.POINTER(_I64)]),
     "jorge_gradient_norm": (_I32, [_PT, _I32, _F64, _P, _P, _I64, _P]),
     "jorge_adamw_step": (_I32, [_PT, _I32, _PM, _I64, _F64, _F64, _F64, _F64, _F64, _P, _P]),
@@ -528,6 +541,108 @@ class _GatedLinear(torch.autograd.Function):
 def gated_linear(x, gate, up, activation="silu"):
     """Differentiable activation(x @ gate.T) * (x @ up.T) (see gated_linear_forward)."""
     return _GatedLinear.apply(x, gate, up, activation)
+
+
+# ---------------------------------------------------------------- attention
+ATTENTION_MAX_STRIDE = 1 << 22                # JORGE_ATTENTION_MAX_STRIDE
+
+
+def _heads(t, what, like=None):
+    """t (batch, tokens, heads, dim) with dense rows and a token stride that the call takes, as a tensor and a Heads."""
+    _cuda(t, what)
+    if t.dim() != 4:
+        raise ValueError(f"{what}: (batch, tokens, heads, dim) is needed")
+    if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
+        raise ValueError(f"{what}: shape {tuple(t.shape)} and type {t.dtype}, not {tuple(like.shape)} and {like.dtype}")
+    if (t.shape[3] > 1 and t.stride(3) != 1) or (t.shape[1] > 1 and t.stride(1) > ATTENTION_MAX_STRIDE):
+        t = t.contiguous()
+    strides = [s if n > 1 else 0 for s, n in zip(t.stride(), t.shape)]
+    return t, Heads(t.data_ptr(), *strides[:3])
+
+
+def _lengths(t, batch, what):
+    if t is None:
+        return None
+    t = _int64s(t, what)
+    if tuple(t.shape) != (batch,):
+        raise ValueError(f"{what}: one number per sequence is needed")
+    return t
+
+
+def _attention_args(q, k, v, scale, causal, window, q_lengths, kv_lengths):
+    (q, hq), (k, hk), (v, hv) = _heads(q, "q"), _heads(k, "k"), _heads(v, "v", k)
+    batch, nq, heads, dim = q.shape
+    if k.shape[0] != batch or k.shape[3] != dim or k.dtype != q.dtype:
+        raise ValueError("k and v must have q's batch, dim and type")
+    if dim < 1 or heads < 1 or k.shape[2] < 1 or heads % k.shape[2]:
+        raise ValueError("q's heads must be a positive multiple of k's, and dim at least 1")
+    if window is not None and (not causal or int(window) < 1):
+        raise ValueError("window: a positive number, with causal")
+    ql, kl = _lengths(q_lengths, batch, "q_lengths"), _lengths(kv_lengths, batch, "kv_lengths")
+    shape = AttentionShape(batch, nq, k.shape[1], heads, k.shape[2], dim, DTYPES[q.dtype],
+                           dim ** -0.5 if scale is None else float(scale), int(bool(causal)), 0,
+                           0 if window is None else int(window), _ptr(ql), _ptr(kl), hq, hk, hv)
+    return shape, (q, k, v, ql, kl)
+
+
+def attention_forward(q, k, v, scale=None, causal=False, window=None, q_lengths=None, kv_lengths=None):
+    """(out, lse) of softmax(scale q k^T) v. q, out: (batch, tokens, heads, dim); k, v: (batch, keys, kv_heads, dim),
+    heads / kv_heads consecutive heads to one of k and v; lse (log sum exp): (batch, heads, tokens) in fp32.
+    scale: 1 / sqrt(dim) unless given. q_lengths, kv_lengths: how many of its rows each sequence has (all without).
+    causal: the last query sees the last key, each one before it a key less; window: the last so many of those.
+    A query that sees nothing or is past its sequence's length has out 0 and lse minus infinity."""
+    lib = load_operators()
+    shape, (q, k, v, ql, kl) = _attention_args(q, k, v, scale, causal, window, q_lengths, kv_lengths)
+    n = _I64(0)
+    _check(lib, lib.jorge_attention_workspace(ctypes.byref(shape), None, ctypes.byref(n)))
+    ws = _workspace(n.value)
+    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
+    to = Heads(out.data_ptr(), *out.stride()[:3])
+    _check(lib, lib.jorge_attention_forward(ctypes.byref(shape), ctypes.byref(to), lse.data_ptr(), _ptr(ws), n.value,
+                                            _stream(q)))
+    return out, lse
+
+
+def attention_backward(dout, q, k, v, out, lse, scale=None, causal=False, window=None, q_lengths=None, kv_lengths=None,
+                       need_q=True, need_kv=True):
+    """(dq, dk, dv) from what attention_forward took and returned; what is not needed is None."""
+    lib = load_operators()
+    shape, (q, k, v, ql, kl) = _attention_args(q, k, v, scale, causal, window, q_lengths, kv_lengths)
+    (dout, hd), (out, ho) = _heads(dout, "dout", q), _heads(out, "out", q)
+    if _cuda(lse, "lse", (torch.float32,)).shape != (q.shape[0], q.shape[2], q.shape[1]) or not lse.is_contiguous():
+        raise ValueError("lse: as attention_forward returned it")
+    n = _I64(0)
+    _check(lib, lib.jorge_attention_workspace(ctypes.byref(shape), ctypes.byref(hd), ctypes.byref(n)))
+    ws = _workspace(n.value)
+    grads = [torch.empty(t.shape, dtype=t.dtype, device=t.device) if need else None
+             for t, need in ((q, need_q), (k, need_kv), (v, need_kv))]
+    to = [None if t is None else ctypes.byref(Heads(t.data_ptr(), *t.stride()[:3])) for t in grads]
+    _check(lib, lib.jorge_attention_backward(ctypes.byref(shape), ctypes.byref(hd), ctypes.byref(ho), lse.data_ptr(), *to,
+                                             _ptr(ws), n.value, _stream(q)))
+    return tuple(grads)
+
+
+class _Attention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, scale, causal, window, q_lengths, kv_lengths):
+        out, lse = attention_forward(q, k, v, scale, causal, window, q_lengths, kv_lengths)
+        ctx.save_for_backward(q, k, v, out, lse, q_lengths, kv_lengths)
+        ctx.more = (scale, causal, window)
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        q, k, v, out, lse, ql, kl = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dq, dk, dv = attention_backward(dout, q, k, v, out, lse, *ctx.more, ql, kl, need[0], need[1] or need[2])
+        return dq, dk if need[1] else None, dv if need[2] else None, None, None, None, None, None
+
+
+def attention(q, k, v, scale=None, causal=False, window=None, q_lengths=None, kv_lengths=None):
+    """Differentiable softmax attention (see attention_forward)."""
+    return _Attention.apply(q, k, v, scale, causal, window, q_lengths, kv_lengths)
 
 
 # ---------------------------------------------------------------- AdamW

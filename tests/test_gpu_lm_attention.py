@@ -1,0 +1,308 @@
+"""Attention on the GPU, both passes, against the formulas in 64 bits.
+
+Errors. A score is a sum of dim products: (dim + 8) roundings of scale sum |q||k|, the largest of which in a row is
+`dz`. A probability's relative error is then at most twice that, and a rounding of each of its exponent's terms and of
+the exponential; a sum over n terms adds n roundings of the terms' magnitudes. bfloat16 rounds p and ds once, 2^-8 of
+each, and delta is formed from the rounded o. A probability below 2^-126, the smallest normal number, counts as zero
+(exp2 gives no subnormal ones): that is off by less than 2^-126, whatever the rest.
+"""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from lm_check import U32, UNIT, slope, within  # noqa: E402
+from paper_2310_12298_amd import lm  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+INF = float("inf")
+TINY = 2.0 ** -126
+
+
+def seen_by(nq, nk, tq, tk, causal, window):
+    """(tq, tk) truth values: which keys a query sees."""
+    i, j = torch.arange(tq)[:, None], torch.arange(tk)[None, :]
+    seen = (i < nq) & (j < nk)
+    if causal:
+        at = nk - nq + i
+        seen &= j <= at
+        if window:
+            seen &= j > at - window
+    return seen
+
+
+def plain(q, k, v, dout=None, scale=None, causal=False, window=None, ql=None, kl=None):
+    """Results in 64 bits, and as "<name>_off" how far the call's may be before their own rounding."""
+    dt = q.dtype
+    q, k, v = (t.double().cpu() for t in (q, k, v))
+    b, tq, h, d = q.shape
+    tk, hk = k.shape[1], k.shape[2]
+    g = h // hk
+    scale = d ** -0.5 if scale is None else scale
+    low = UNIT[dt] if dt is BF16 else 0.0
+    names = ["out"] + (["dq", "dk", "dv"] if dout is not None else [])
+    shapes = {"out": q, "dq": q, "dk": k, "dv": v}
+    res = {n: torch.zeros_like(shapes[n]) for n in names}
+    res.update({n + "_off": torch.zeros_like(shapes[n]) for n in names})
+    res["lse"], res["lse_off"] = torch.full((b, h, tq), -INF).double(), torch.zeros(b, h, tq).double()
+    for n in range(b):
+        nq = tq if ql is None else min(max(int(ql[n]), 0), tq)
+        nk = tk if kl is None else min(max(int(kl[n]), 0), tk)
+        seen = seen_by(nq, nk, tq, tk, causal, window)
+        rows = seen.any(1)
+        if not rows.any():
+            continue
+        for m in range(h):
+            x, y, w = q[n, rows, m], k[n, :nk, m // g], v[n, :nk, m // g]
+            mask = seen[rows][:, :nk]
+            z = scale * (x @ y.t())
+            z[~mask] = -INF
+            zs = scale * (x.abs() @ y.abs().t()) * mask
+            lse = torch.logsumexp(z, 1)
+            p = torch.exp(z - lse[:, None])
+            o = p @ w
+            dz = (d + 8) * U32 * zs.max(1).values
+            top = torch.where(mask, z.abs(), 0.0).max(1).values + lse.abs()
+            rel = (2 * dz + U32 * (nk + 64 + 8 * top))[:, None]
+            osize = p @ w.abs()
+            ooff = osize * (rel + low) + TINY * (mask.double() @ w.abs())
+            res["out"][n, rows, m], res["out_off"][n, rows, m] = o, ooff
+            res["lse"][n, m, rows], res["lse_off"][n, m, rows] = lse, rel[:, 0]
+            if dout is None:
+                continue
+            do = dout[n, rows, m].double().cpu()
+            dp, delta = do @ w.t(), (do * o).sum(1, keepdim=True)
+            ds = p * (dp - delta)
+            dps = do.abs() @ w.abs().t()
+            doff = (do.abs() * (ooff + UNIT[dt] * (o.abs() + ooff))).sum(1, keepdim=True)
+            doff = doff + (d + 8) * U32 * (do.abs() * o.abs()).sum(1, keepdim=True)
+            soff = p * (rel * (dp.abs() + delta.abs()) * (1 + rel) + (d + 8) * U32 * dps + doff)
+            soff = soff + TINY * mask * (dp.abs() + delta.abs())
+            soff = soff + (low + 4 * U32) * (ds.abs() + soff)
+            poff = p * (rel + low * (1 + rel)) + TINY * mask
+            for name, at, got, off, size, terms in (
+                    ("dq", (n, rows, m), ds @ y, soff @ y.abs(), (ds.abs() + soff) @ y.abs(), nk),
+                    ("dk", (n, slice(0, nk), m // g), ds.t() @ x, soff.t() @ x.abs(), (ds.abs() + soff).t() @ x.abs(), nq),
+                    ("dv", (n, slice(0, nk), m // g), p.t() @ do, poff.t() @ do.abs(), (p + poff).t() @ do.abs(), nq)):
+                f = 1.0 if name == "dv" else scale
+                res[name][at] += f * got
+                res[name + "_off"][at] += f * (off + U32 * (terms * g + 64) * size)
+    return res
+
+
+def inputs(b, tq, tk, h, hk, d, dtype, seed=0, s=1.0):
+    g = torch.Generator().manual_seed(seed + 7 * tq + tk + 31 * d)
+    return [(torch.randn(shape, generator=g) * s).to(dtype).cuda()
+            for shape in ((b, tq, h, d), (b, tk, hk, d), (b, tk, hk, d), (b, tq, h, d))]
+
+
+def check(q, k, v, dout, ql=None, kl=None, **how):
+    lengths = {n: None if t is None else torch.as_tensor(t, device="cuda") for n, t in
+               (("q_lengths", ql), ("kv_lengths", kl))}
+    want = plain(q, k, v, dout, ql=ql, kl=kl, **how)
+    out, lse = lm.attention_forward(q, k, v, **how, **lengths)
+    assert out.shape == q.shape and out.dtype == q.dtype
+    none = want["lse"] == -INF
+    assert torch.equal(lse.cpu() == -INF, none)
+    within(lse.cpu()[~none], want["lse"][~none], want["lse_off"][~none] / U32, 1, "lse")
+    within(out, want["out"], want["out_off"] / U32, 1, "out")
+    assert torch.count_nonzero(out.cpu().transpose(1, 2)[none]) == 0
+    grads = lm.attention_backward(dout, q, k, v, out, lse, **how, **lengths)
+    for n, t in zip(("dq", "dk", "dv"), grads):
+        within(t, want[n], want[n + "_off"] / U32, 1, n)
+    return out, lse, grads
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("b,tq,tk,h,hk,d", [
+    (1, 1, 1, 1, 1, 64), (2, 1, 70, 4, 4, 64), (1, 1, 333, 8, 1, 128), (2, 3, 129, 6, 2, 40), (1, 31, 31, 1, 1, 8),
+    (1, 33, 65, 2, 1, 128), (2, 64, 64, 2, 2, 64), (1, 65, 63, 3, 1, 72), (2, 127, 200, 4, 2, 128),
+    (1, 129, 128, 2, 2, 1), (1, 200, 40, 2, 1, 33), (1, 300, 301, 3, 3, 127), (2, 257, 257, 4, 1, 96)])
+def test_sizes(b, tq, tk, h, hk, d, dtype, causal):
+    check(*inputs(b, tq, tk, h, hk, d, dtype), causal=causal)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("window", [1, 2, 31, 64, 100, 5000])
+@pytest.mark.parametrize("tq,tk", [(1, 300), (150, 150), (70, 260), (260, 70)])
+def test_windows(tq, tk, window, dtype):
+    check(*inputs(1, tq, tk, 4, 2, 64, dtype), causal=True, window=window)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("causal,window", [(False, None), (True, None), (True, 40)])
+def test_lengths(dtype, causal, window):
+    """Whole, empty, single, odd ones, ones outside the range; of the keys, of the queries, of both."""
+    some = [0, 1, 33, 64, 150, -3, 999]
+    other = [150, 64, 7, 0, 1, 20, 149]
+    q, k, v, dout = inputs(7, 150, 150, 4, 2, 72, dtype)
+    for ql, kl in ((None, some), (some, None), (some, some), (other, some)):
+        check(q, k, v, dout, ql, kl, causal=causal, window=window)
+    q, k, v, dout = inputs(7, 3, 150, 4, 2, 72, dtype)
+    check(q, k, v, dout, None, some, causal=causal, window=window)
+    check(q, k, v, dout, [3, 0, 1, 2, 3, 1, 2], some, causal=causal, window=window)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_keys_cut_into_ranges(dtype):
+    """Few workgroups over many keys, and few keys under many queries: sums joined from ranges."""
+    check(*inputs(1, 1, 9000, 8, 2, 128, dtype), causal=True)
+    check(*inputs(2, 4, 5001, 2, 2, 64, dtype), kl=[5001, 700])
+    check(*inputs(1, 100, 4000, 1, 1, 64, dtype), causal=True)
+    check(*inputs(1, 3000, 90, 2, 1, 128, dtype))
+    check(*inputs(1, 1000, 2500, 2, 1, 40, dtype), causal=True, window=900)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_scores_far_apart(dtype):
+    q, k, v, dout = inputs(1, 90, 200, 2, 1, 64, dtype, s=3.0)
+    check(q, k, v, dout, scale=1.0, causal=True)
+    check(q, k, v, dout, scale=1e-6)
+    order = torch.argsort((q.float()[0, :, 0] @ k.float()[0, :, 0].t())[0])   # growing scores: every tile a new maximum
+    check(q, k[:, order].contiguous(), v, dout, scale=0.7)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("d", [64, 40, 33])
+def test_strides_and_alignment(d, dtype):
+    q, k, v, dout = inputs(2, 77, 77, 6, 3, d, dtype)
+    how = dict(causal=True)
+    first = lm.attention_forward(q, k, v, **how)
+    grads = lm.attention_backward(dout, q, k, v, *first, **how)
+    n = q.shape[2] + 2 * k.shape[2]
+    rows = torch.empty(2, 77, n, d, dtype=dtype, device="cuda")               # as one projection leaves them
+    rows[:, :, :6], rows[:, :, 6:9], rows[:, :, 9:] = q, k, v
+    turned = [t.transpose(1, 2).contiguous().transpose(1, 2) for t in (q, k, v, dout)]
+    odd = [torch.empty(t.numel() + 3, dtype=dtype, device="cuda")[3:].view(t.shape).copy_(t) for t in (q, k, v, dout)]
+    dense = [t.permute(3, 0, 1, 2).contiguous().permute(1, 2, 3, 0) for t in (q, k, v, dout)]
+    for a, b, c, g in ([rows[:, :, :6], rows[:, :, 6:9], rows[:, :, 9:], dout], turned, odd, dense):
+        out = lm.attention_forward(a, b, c, **how)
+        assert torch.equal(out[0], first[0]) and torch.equal(out[1], first[1])
+        for x, y in zip(lm.attention_backward(g, a, b, c, *out, **how), grads):
+            assert torch.equal(x, y)
+    far = torch.zeros(2, 2, lm.ATTENTION_MAX_STRIDE + 8, dtype=dtype, device="cuda")
+    far = far[:, :, :3 * d].unflatten(2, (3, d)).copy_(k[:, :2])
+    assert torch.equal(lm.attention_forward(q, far, far)[0], lm.attention_forward(q, *(k[:, :2].contiguous(),) * 2)[0])
+    one = dout[:, :1, :1].expand_as(dout)                                     # a broadcast gradient
+    for x, y in zip(lm.attention_backward(one, q, k, v, *first, **how),
+                    lm.attention_backward(one.contiguous(), q, k, v, *first, **how)):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tq", [5, 150])
+def test_what_stands_past_the_lengths_reaches_nothing(tq, dtype):
+    q, k, v, dout = inputs(3, tq, 150, 4, 2, 64, dtype)
+    ql, kl = [tq, 2, tq - 3], [100, 0, 77]
+    lengths = dict(q_lengths=torch.tensor(ql, device="cuda"), kv_lengths=torch.tensor(kl, device="cuda"))
+    for how in (dict(), dict(causal=True), dict(causal=True, window=30)):
+        first = lm.attention_forward(q, k, v, **how, **lengths)
+        grads = lm.attention_backward(dout, q, k, v, *first, **how, **lengths)
+        for bad in (float("nan"), INF):
+            Q, K, V, G = (t.clone() for t in (q, k, v, dout))
+            for n in range(3):
+                K[n, kl[n]:], V[n, kl[n]:], Q[n, ql[n]:], G[n, ql[n]:] = bad, bad, bad, bad
+                if how:                                       # queries before the first key see nothing
+                    Q[n, :max(0, ql[n] - kl[n])], G[n, :max(0, ql[n] - kl[n])] = bad, bad
+            out = lm.attention_forward(Q, K, V, **how, **lengths)
+            assert torch.equal(out[0], first[0]) and torch.equal(out[1], first[1])
+            for x, y in zip(lm.attention_backward(G, Q, K, V, *out, **how, **lengths), grads):
+                assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tq", [2, 200])
+def test_nan_and_infinity_where_they_are_seen(tq, dtype):
+    q, k, v, dout = inputs(1, tq, 200, 2, 2, 64, dtype)
+    clean = lm.attention_forward(q, k, v, causal=True)
+    q[0, 1, 0] = float("nan")
+    out, lse = lm.attention_forward(q, k, v, causal=True)
+    assert bool(torch.isnan(out[0, 1, 0]).all()) and bool(torch.isnan(lse[0, 0, 1]))
+    out[0, 1, 0], lse[0, 0, 1] = clean[0][0, 1, 0], clean[1][0, 0, 1]
+    assert torch.equal(out, clean[0]) and torch.equal(lse, clean[1])
+    q, k, v, dout = inputs(1, tq, 200, 2, 2, 64, dtype)
+    v[0, 5, 1] = INF
+    out, lse = lm.attention_forward(q, k, v)
+    assert torch.equal(lse, lm.attention_forward(q, k, v.clamp(max=9))[1])
+    assert bool((out[0, :, 1] == INF).all()) and bool(torch.isfinite(out[0, :, 0]).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_nothing_to_do(dtype):
+    for b, tq, tk in ((0, 5, 5), (2, 0, 5), (2, 5, 0)):
+        q, k, v, dout = inputs(b, tq, tk, 4, 2, 64, dtype)
+        out, lse = lm.attention_forward(q, k, v)
+        assert out.shape == q.shape and torch.count_nonzero(out) == 0 and bool((lse == -INF).all())
+        for x, t in zip(lm.attention_backward(dout, q, k, v, out, lse), (q, k, v)):
+            assert x.shape == t.shape and torch.count_nonzero(x) == 0
+    q, k, v, dout = inputs(1, 40, 40, 4, 2, 64, dtype)
+    out, lse = lm.attention_forward(q, k, v)
+    every = lm.attention_backward(dout, q, k, v, out, lse)
+    dq, dk, dv = lm.attention_backward(dout, q, k, v, out, lse, need_kv=False)
+    assert torch.equal(dq, every[0]) and dk is None and dv is None
+    dq, dk, dv = lm.attention_backward(dout, q, k, v, out, lse, need_q=False)
+    assert dq is None and torch.equal(dk, every[1]) and torch.equal(dv, every[2])
+
+
+def test_gradients_agree_with_differences_and_repeat_themselves():
+    q, k, v, dout = inputs(2, 37, 50, 4, 2, 24, F32)
+    kl = torch.tensor([50, 21], device="cuda")
+    how = dict(causal=True, window=30)
+    grads = []
+    for _ in range(2):
+        leaves = [t.clone().requires_grad_() for t in (q, k, v)]
+        lm.attention(*leaves, **how, kv_lengths=kl).backward(dout)
+        grads.append([t.grad for t in leaves])
+    assert all(torch.equal(a, b) for a, b in zip(*grads))
+    ref = [t.double().cpu() for t in (q, k, v)]
+    seen = torch.stack([seen_by(37, int(n), 37, 50, True, 30) for n in kl.tolist()])[:, None]
+
+    def loss(t):
+        x, y, w = (a.transpose(1, 2) for a in t)
+        y, w = y.repeat_interleave(2, 1), w.repeat_interleave(2, 1)
+        z = (x @ y.transpose(2, 3) / 24 ** 0.5).masked_fill(~seen, -INF)
+        p = torch.where(seen, torch.softmax(z, 3), 0.0).nan_to_num(0.0)
+        return ((p @ w).transpose(1, 2) * dout.double().cpu()).sum()
+    g = torch.Generator().manual_seed(1)
+    for i, got in enumerate(grads[0]):
+        d = torch.randn(ref[i].shape, generator=g, dtype=torch.float64)
+        want = slope(lambda t: loss([t if j == i else r for j, r in enumerate(ref)]), ref[i], d, 1e-6)
+        got = got.double().cpu()
+        assert abs((got * d).sum() - want) <= 1e-5 * got.norm() * d.norm()
+
+
+def test_autograd_of_some_inputs_and_a_shared_one():
+    q, k, v, dout = inputs(1, 40, 40, 2, 2, 64, BF16)
+    leaf = k.clone().requires_grad_()
+    lm.attention(q, leaf, leaf, causal=True).backward(dout)
+    out, lse = lm.attention_forward(q, k, k, causal=True)
+    _, dk, dv = lm.attention_backward(dout, q, k, k, out, lse, causal=True)
+    assert torch.equal(leaf.grad, dk + dv)
+    leaf = q.clone().requires_grad_()
+    lm.attention(leaf, k, v).backward(dout)
+    assert leaf.grad is not None and torch.isfinite(leaf.grad).all()
+
+
+def test_refusals():
+    q, k, v, dout = inputs(2, 8, 8, 4, 2, 32, F32)
+    out, lse = lm.attention_forward(q, k, v)
+    n = torch.tensor([3, 4], device="cuda")
+    for bad in (lambda: lm.attention_forward(q.half(), k.half(), v.half()), lambda: lm.attention_forward(q.cpu(), k, v),
+                lambda: lm.attention_forward(q, k.bfloat16(), v.bfloat16()), lambda: lm.attention_forward(q, k, v[:, :7]),
+                lambda: lm.attention_forward(q[:1], k, v), lambda: lm.attention_forward(q[..., :31], k, v),
+                lambda: lm.attention_forward(q[:, :, :3], k, v), lambda: lm.attention_forward(q[0], k, v),
+                lambda: lm.attention_forward(q, k, v, window=4), lambda: lm.attention_forward(q, k, v, True, window=0),
+                lambda: lm.attention_forward(q, k, v, causal=True, window=0),
+                lambda: lm.attention_forward(q, k, v, kv_lengths=n[:1]),
+                lambda: lm.attention_forward(q, k, v, kv_lengths=n.float()),
+                lambda: lm.attention_backward(dout[:, :7], q, k, v, out, lse),
+                lambda: lm.attention_backward(dout.bfloat16(), q, k, v, out, lse),
+                lambda: lm.attention_backward(dout, q, k, v, out, lse[:, :, :7])):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: lm.attention_forward(q, k, v, scale=0.0), lambda: lm.attention_forward(q, k, v, scale=-1.0),
+                lambda: lm.attention_forward(q, k, v, scale=float("nan")),
+                lambda: lm.attention_forward(*[torch.zeros(1, 1, 1, 129, device="cuda")] * 3)):
+        with pytest.raises(lm.JorgeError):
+            bad()
