@@ -65,7 +65,7 @@ struct Sequence {
     __device__ __forceinline__ Sequence(const Call& c, int b) {
         const auto of = [&](const int64_t* p, int most) {
             const int64_t n = p ? p[b] : most;
-            return __builtin_amdgcn_readfirstlane((int)(n < 0 ? 0 : n > most ? most : n));
+            return (int)(n < 0 ? 0 : n > most ? most : n);
         };
         nq = of(c.q_lengths, c.q_tokens);
         nk = of(c.kv_lengths, c.kv_tokens);

@@ -145,6 +145,15 @@ def test_lengths(dtype, causal, window):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tq,h,hk", [(37, 1, 1), (777, 6, 2), (1, 3, 1), (5, 2, 2)])
+def test_an_empty_sequence_next_to_a_whole_one(tq, h, hk, dtype):
+    """Rows of two sequences share a wave wherever heads and queries are odd."""
+    q, k, v, dout = inputs(3, tq, 301, h, hk, 40, dtype)
+    for kl in ([0, 301, 150], [150, 0, 301], [301, 150, 0]):
+        check(q, k, v, dout, None, kl)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_keys_cut_into_ranges(dtype):
     """Few workgroups over many keys, and few keys under many queries: sums joined from ranges."""
     check(*inputs(1, 1, 9000, 8, 2, 128, dtype), causal=True)
