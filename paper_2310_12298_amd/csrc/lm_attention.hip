@@ -100,6 +100,12 @@ struct Work {
 };
 
 // ---------------------------------------------------------------- tiles
+// 4 rows of 16 elements, 8 bytes from each of 16 lanes, to lane i's column i of each row. In a function with a
+// restricted pointer: without what that says of aliases the compiler waits here for every direct-to-LDS load in flight.
+__device__ __forceinline__ s16x4 read_turned4(const lds_s16x4* __restrict__ p) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16(const_cast<lds_s16x4*>(p));
+}
+
 template <typename T, int D>
 struct Tile {
     static constexpr int kRow = D * (int)sizeof(T);       // bytes of a row
@@ -210,7 +216,7 @@ struct Tile {
                     for (int u = 0; u < 2; ++u) {
                         const char* const at =
                             tile + ((at_cols ^ (db * 64) ^ (u * 32)) + (kb * 32 + t * 16 + u * 8) * kRow);
-                        v[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+                        v[u] = read_turned4((const lds_s16x4*)at);
                     }
                     typedef short s16x8 __attribute__((ext_vector_type(8)));
                     const s16x8 a = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);

@@ -12,10 +12,11 @@
 //   dz = dy act'(z)  (gated: dgate = dy u act'(g), dup = dy act(g), side by side as one matrix of 2 outs columns)
 //   dx = dz weight       (K: the columns of dz)
 //   dweight = dz^T x     (K: the tokens)
-// dz is written both ways round from the registers of the tile that forms z again, so that both products have
-// K-contiguous operands; bfloat16 inputs: rounded to bfloat16 for that, as the matrix instructions take it (a gradient,
-// a sum of such terms, errs by up to 2.4e-3 of its size instead of the 1.7e-3 of its own rounding). Without an
-// activation dz is dy as it is. dbias is summed from the unrounded dz.
+// bfloat16: dz is rounded to it, as the matrix instructions take it (a gradient, a sum of such terms, errs by up to
+// 2.4e-3 of its size instead of the 1.7e-3 of its own rounding); weight, x and dz are read as they lie, K along their
+// rows or across them (Tile's TA and TB). fp32: dz is written both ways round, in three terms, from the registers of the
+// tile that forms z again, and x and weight are copied so. Without an activation dz is dy as it is. dbias is summed
+// from the unrounded dz.
 //
 // Few tokens, forward: bound by reading the weights once. A workgroup takes 16 of their rows, its eight waves cut K,
 // and nothing goes through LDS but the sums; fp32 then runs on the fp32 MFMAs, as splits would cost three times the
@@ -395,7 +396,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void dense_few_kernel(FewRows in, F
 
 // ---------------------------------------------------------------- backward
 struct DzOut {
-    bf16 *dz, *dzt;            // [tokens][terms][matrices * kf], [matrices * outs][terms][kn]
+    bf16 *dz, *dzt;            // [tokens][terms][matrices * kf], [matrices * outs][terms][kn] or null
     int64_t kf, kn;            // outs and tokens, padded to multiples of 64
     float* bias;               // [parts][outs] sums of dz over 16 WA tokens each, or null
 };
@@ -413,6 +414,7 @@ __global__ __launch_bounds__(256, 1) void dense_dz_kernel(Dense d, const T* __re
     constexpr int L = Q::kLaneA, kUp = PAIR ? WA / 2 : 0, MATS = PAIR ? 2 : 1;
     const int left = left_of<L>(outs - a0);
     constexpr int terms = SPLIT ? kTerms : 1;
+    const bool again = out.dzt || out.bias;  // whether dz is needed back in the registers
     const Rows<WA, PAIR> rows(lds);
     const int64_t wa = (int64_t)at.a * Q::kRowsA + (threadIdx.x >> 7) * (Q::kRowsA / 2);
     const int64_t wb = (int64_t)at.b * Q::kB + ((threadIdx.x >> 6) & 1) * (Q::kB / 2);
@@ -434,11 +436,12 @@ __global__ __launch_bounds__(256, 1) void dense_dz_kernel(Dense d, const T* __re
                 }
             });
             float* const back = rows.at + row * rows.kLd + c;
+            if (again)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                back[e] = z[e];
-                if constexpr (PAIR) back[rows.kCols + e] = u[e];
-            }
+                for (int e = 0; e < 8; ++e) {
+                    back[e] = z[e];
+                    if constexpr (PAIR) back[rows.kCols + e] = u[e];
+                }
             if (out.dz && token < tokens && wa + c < out.kf) {
                 bf16* const dz = out.dz + token * terms * MATS * out.kf + wa + c;
                 store_terms<terms>(dz, MATS * out.kf, z);
@@ -446,8 +449,9 @@ __global__ __launch_bounds__(256, 1) void dense_dz_kernel(Dense d, const T* __re
             }
         });
         Rows<WA, PAIR>::fence();
+        if (again)
 #pragma unroll
-        for (int i = 0; i < WA; ++i) t.acc[i][j] = *rows.piece(i);
+            for (int i = 0; i < WA; ++i) t.acc[i][j] = *rows.piece(i);
     }
     if (!PAIR && out.bias) {
         const int64_t part = b0 / (16 * WA);
@@ -490,46 +494,52 @@ __global__ __launch_bounds__(256, 1) void dense_dz_kernel(Dense d, const T* __re
     }
 }
 
-// Where a gradient goes: rows [0, first) to one matrix, the others to a second.
+// Where a gradient goes: rows [0, rows) to one matrix, those from `second` on to another one.
 template <typename T>
 struct Target {
     T *one, *two;
-    int64_t first, ld;
-    __device__ __forceinline__ T* row(int64_t r) const { return r < first ? one + r * ld : two + (r - first) * ld; }
+    int64_t rows, second, ld;
+    __device__ __forceinline__ T* row(int64_t r) const {  // null for a row that is none
+        if (r >= second) return two && r - second < rows ? two + (r - second) * ld : nullptr;
+        return r < rows ? one + r * ld : nullptr;
+    }
 };
 
 // C[b][a] over one of gridDim.y ranges of K, whole (one range) or into the range's slice [ranges][B.rows][lda].
-template <int WA, int RING, bool SPLIT, typename T>
+template <int WA, int RING, bool SPLIT, bool TA, bool TB, typename T>
 __global__ __launch_bounds__(256, 1) void dense_grad_kernel(Product p, Target<T> out, float* __restrict__ slices,
                                                             int64_t lda) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
-    using Q = Tile<WA, WA, RING, SPLIT>;
+    using Q = Tile<WA, WA, RING, SPLIT, false, TA, TB>;
     const Place at = place_of(blockIdx.x, p.ta, p.tb);
     const Range k(p.stages);
     Q t;
     t.multiply(p.A, p.B, (int64_t)at.a * Q::kA, (int64_t)at.b * Q::kB, k.s0, k.s1, p.stages, lds);
-    const int64_t a0 = (int64_t)at.a * Q::kA + Q::lane_a(), b0 = (int64_t)at.b * Q::kB + Q::lane_b();
+    const int64_t a0 = (int64_t)at.a * Q::kA + Q::lane_a();
+    const int64_t wa = (int64_t)at.a * Q::kA + (threadIdx.x >> 7) * (Q::kA / 2);
+    const int64_t wb = (int64_t)at.b * Q::kB + ((threadIdx.x >> 6) & 1) * (Q::kB / 2);
     const int left = left_of<4 * WA>(p.A.rows - a0);
     if (slices) {
 #pragma unroll
-        for (int j = 0; j < WA; ++j)
-            if (b0 + j < p.B.rows) {
-                f32x4* const q = reinterpret_cast<f32x4*>(slices + (blockIdx.y * p.B.rows + b0 + j) * lda + a0);
+        for (int j = 0; j < WA; ++j) {
+            const int64_t b = wb + Q::part_b(threadIdx.x & 15, j);
+            if (b < p.B.rows) {
+                f32x4* const q = reinterpret_cast<f32x4*>(slices + (blockIdx.y * p.B.rows + b) * lda + a0);
 #pragma unroll
                 for (int i = 0; i < WA; ++i)
                     if (4 * i < left) q[i] = t.acc[i][j];
             }
+        }
         return;
     }
     const Rows<WA, false> rows(lds);
-    const int64_t wa = (int64_t)at.a * Q::kA + (threadIdx.x >> 7) * (Q::kA / 2);
-    const int64_t wb = (int64_t)at.b * Q::kB + ((threadIdx.x >> 6) & 1) * (Q::kB / 2);
 #pragma unroll
     for (int j = 0; j < WA; ++j)
         rows.each(t.acc, j, [&](int row, int c, const float(&z)[8], const float(&)[8]) {
-            const int64_t b = wb + row * WA + j;
+            const int64_t b = wb + Q::part_b(row, j);
             const int n = left_of<8>(p.A.rows - wa - c);
-            if (b < p.B.rows && n) store_some<8>(out.row(b) + wa + c, n, z);
+            T* const to = b < p.B.rows ? out.row(b) : nullptr;
+            if (to && n) store_some<8>(to + wa + c, n, z);
         });
 }
 
@@ -537,10 +547,12 @@ template <typename T>
 __global__ __launch_bounds__(256) void dense_slices_kernel(const float* __restrict__ slices, int n, int64_t rows,
                                                            int cols, int64_t lda, Target<T> out) {
     const int64_t r = blockIdx.x;
+    T* const to = out.row(r);
+    if (!to) return;
     for (int c = (blockIdx.y * 256 + threadIdx.x) * 4; c < cols; c += gridDim.y * 1024) {
         const f32x4 s = sum_slices(slices + r * lda + c, n, rows * lda);
         const float v[4] = {s[0], s[1], s[2], s[3]};
-        store_some<4>(out.row(r) + c, cols - c, v);
+        store_some<4>(to + c, cols - c, v);
     }
 }
 
@@ -601,6 +613,8 @@ struct Plan {
     bool few;                        // forward: the kernel for few tokens
     bool direct_x, direct_w, direct_dy;
     bool dz;                         // dz differs from dy
+    bool turn;                       // bfloat16: operands are read across their rows, not transposed first
+    int64_t rows_w;                  // rows of the weights' gradients as one matrix
     Shape z, dx, dw;
 };
 struct Wanted {
@@ -624,12 +638,14 @@ Plan plan_of(const jorge_linear_shape& s, int mats, const Wanted& want, bool dir
     p.direct_dy = direct_dy;
     p.few = !want.backward && s.tokens <= kFewTokens;
     p.dz = mats == 2 || s.activation != JORGE_ACT_NONE;
+    p.turn = p.terms == 1;
+    p.rows_w = mats * (p.turn ? p.kf : s.outs);
     p.z = shape_of(mats * s.outs, s.tokens, p.kd, p.products, !want.backward);
     // A pair's tile of 64 x 64 holds 32 columns of each, which padding to 64 would leave without a tile.
     if (mats == 2 && p.z.blocks == 2) p.z.blocks = 4;
     if (want.backward) {
         p.dx = shape_of(s.cols, s.tokens, mats * p.kf, p.products, true);
-        p.dw = shape_of(s.cols, mats * s.outs, p.kn, p.products, true);
+        p.dw = shape_of(s.cols, p.rows_w, p.kn, p.products, true);
     }
     return p;
 }
@@ -651,20 +667,23 @@ Work carve(void* base, const jorge_linear_shape& s, const Plan& p, const Wanted&
     w.ldz = p.mats * round_up(s.outs, 4);
     w.ldc = round_up(s.cols, 4);
     const bool z = !want.backward || (p.dz && (want.dx || want.dw || want.db));
-    if (z && !p.few) {
-        if (!p.direct_x) w.x = c.take<bf16>(p.terms * s.tokens * p.kd);
-        if (!p.direct_w) w.w = c.take<bf16>(p.terms * s.outs * p.kd);
-        if (!p.direct_w && p.mats == 2) w.u = c.take<bf16>(p.terms * s.outs * p.kd);
+    if (!p.few) {
+        if (!p.direct_x && (z || (p.turn && want.dw))) w.x = c.take<bf16>(p.terms * s.tokens * p.kd);
+        if (!p.direct_w && (z || (p.turn && want.dx))) {
+            w.w = c.take<bf16>(p.terms * s.outs * p.kd);
+            if (p.mats == 2) w.u = c.take<bf16>(p.terms * s.outs * p.kd);
+        }
     }
     if (!want.backward) {
         if (!p.few && p.z.ranges > 1) w.z = c.take<float>(p.z.ranges * s.tokens * w.ldz);
     } else {
-        if (want.dw) w.xt = c.take<bf16>(p.terms * s.cols * p.kn);
-        if (want.dx) w.wt = c.take<bf16>(p.terms * s.cols * p.mats * p.kf);
-        if (want.dx && (p.dz || !p.direct_dy)) w.dz = c.take<bf16>(p.terms * s.tokens * p.mats * p.kf);
-        if (want.dw) w.dzt = c.take<bf16>(p.terms * p.mats * s.outs * p.kn);
+        const bool dz = want.dx || (p.turn && want.dw);
+        if (want.dw && !p.turn) w.xt = c.take<bf16>(p.terms * s.cols * p.kn);
+        if (want.dx && !p.turn) w.wt = c.take<bf16>(p.terms * s.cols * p.mats * p.kf);
+        if (dz && (p.dz || !p.direct_dy)) w.dz = c.take<bf16>(p.terms * s.tokens * p.mats * p.kf);
+        if (want.dw && !p.turn) w.dzt = c.take<bf16>(p.terms * p.mats * s.outs * p.kn);
         if (want.dx && p.dx.ranges > 1) w.dx = c.take<float>(p.dx.ranges * s.tokens * w.ldc);
-        if (want.dw && p.dw.ranges > 1) w.dw = c.take<float>(p.dw.ranges * p.mats * s.outs * w.ldc);
+        if (want.dw && p.dw.ranges > 1) w.dw = c.take<float>(p.dw.ranges * p.rows_w * w.ldc);
         if (want.db) w.bias = c.take<float>(bias_parts(s, p) * s.outs);
     }
     w.bytes = c.used;
@@ -683,16 +702,25 @@ void with_pair_tile(const Shape& s, F&& f) {
     else f(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
 }
 
+// x and the weights as operands, K along their rows.
+struct Operands {
+    Operand x, w, u;
+};
+Operands operands_of(const jorge_linear_shape& s, const Plan& p, const Work& w, const void* x, const void* weight,
+                     const void* up) {
+    const auto of = [&](bool direct, const void* at, int64_t ld, const bf16* copy, int64_t rows) {
+        return direct ? Operand{(const bf16*)at, ld, 0, rows} : Operand{copy, p.terms * p.kd, p.kd, rows};
+    };
+    return {of(p.direct_x, x, s.ldx, w.x, s.tokens), of(p.direct_w, weight, s.ldw, w.w, s.outs),
+            of(p.direct_w, up, s.ldu, w.u, s.outs)};
+}
+// An operand of `depth` rows, K across them; of `cols` elements each.
+Operand turned(const Operand& o, int64_t cols, int64_t depth, const bf16* p2 = nullptr, int64_t part = 0) {
+    return {o.p, o.ld, 0, cols, p2, depth, part};
+}
 // The product of x with the weights: ta counts tiles of kRowsA rows.
-Dense dense_of(const jorge_linear_shape& s, const Plan& p, const Work& w, const void* x, const void* weight,
-               const void* up) {
-    const Operand X = p.direct_x ? Operand{(const bf16*)x, s.ldx, 0, s.tokens}
-                                 : Operand{w.x, p.terms * p.kd, p.kd, s.tokens};
-    const Operand W = p.direct_w ? Operand{(const bf16*)weight, s.ldw, 0, s.outs}
-                                 : Operand{w.w, p.terms * p.kd, p.kd, s.outs};
-    const Operand U = p.direct_w ? Operand{(const bf16*)up, s.ldu, 0, s.outs}
-                                 : Operand{w.u, p.terms * p.kd, p.kd, s.outs};
-    Dense d{product_of(p.z, W, X, p.kd), p.mats == 2 ? U : W};
+Dense dense_of(const jorge_linear_shape& s, const Plan& p, const Operands& o) {
+    Dense d{product_of(p.z, o.w, o.x, p.kd), p.mats == 2 ? o.u : o.w};
     d.p.ta = (int)ceil_div(s.outs, 32 * p.z.blocks / p.mats);
     return d;
 }
@@ -711,7 +739,7 @@ jorge_status forward(const jorge_linear_shape& s, const Plan& p, const Work& w, 
     copy<T>(copies_of(x, s.ldx, s.tokens, s.cols, w.x, p.kd, nullptr, 0),
             copies_of(weight, s.ldw, s.outs, s.cols, w.w, p.kd, nullptr, 0), st,
             copies_of(up, s.ldu, s.outs, s.cols, w.u, p.kd, nullptr, 0));
-    const Dense d = dense_of(s, p, w, x, weight, up);
+    const Dense d = dense_of(s, p, operands_of(s, p, w, x, weight, up));
     jorge_status err = JORGE_OK;
     const int ranges = p.z.ranges;
     const auto run = [&](auto WA, auto RING) {
@@ -729,14 +757,14 @@ jorge_status forward(const jorge_linear_shape& s, const Plan& p, const Work& w, 
     return launched("dense product");
 }
 
-template <typename T>
+template <typename T, bool TA, bool TB>
 jorge_status gradient(const Shape& sh, const Product& pr, const Target<T>& out, int64_t cols, float* slices,
                       hipStream_t st) {
     jorge_status err = JORGE_OK;
     const int64_t lda = round_up(cols, 4);
     with_tile(sh, [&](auto WA, auto RING) {
         constexpr int B = decltype(WA)::value, R = decltype(RING)::value, bytes = Tile<B, B, R, sizeof(T) == 4>::kBytes;
-        const auto k = dense_grad_kernel<B, R, sizeof(T) == 4, T>;
+        const auto k = dense_grad_kernel<B, R, sizeof(T) == 4, TA, TB, T>;
         if ((err = allow_lds(k, bytes, kNoLds)) != JORGE_OK) return;
         k<<<dim3(pr.ta * pr.tb, sh.ranges), dim3(256), bytes, st>>>(pr, out, slices, lda);
     });
@@ -760,9 +788,10 @@ jorge_status backward(const jorge_linear_shape& s, const Plan& p, const Work& w,
             copies_of(weight, s.ldw, s.outs, s.cols, w.w, p.kd, w.wt, kz), st,
             PAIR ? copies_of(up, s.ldu, s.outs, s.cols, w.u, p.kd, ut, kz)
                  : p.dz ? Copies{} : copies_of(dy, s.ldy, s.tokens, s.outs, w.dz, p.kf, w.dzt, p.kn));
+    const Operands in = operands_of(s, p, w, x, weight, up);
     jorge_status err = JORGE_OK;
     if (p.dz) {
-        const Dense d = dense_of(s, p, w, x, weight, up);
+        const Dense d = dense_of(s, p, in);
         const DzOut z{w.dz, w.dzt, p.kf, p.kn, w.bias};
         const auto run = [&](auto WA, auto RING) {
             constexpr int B = decltype(WA)::value, R = decltype(RING)::value;
@@ -781,18 +810,20 @@ jorge_status backward(const jorge_linear_shape& s, const Plan& p, const Work& w,
     if (out.dbias)
         dense_bias_kernel<<<dim3((unsigned)ceil_div(s.outs, 64)), dim3(1024), 0, st>>>(
             w.bias, bias_parts(s, p), s.outs, out.dbias, bias.bf);
+    constexpr bool TURN = sizeof(T) == 2;
+    const Operand z = w.dz ? Operand{w.dz, p.terms * kz, kz, s.tokens} : Operand{(const bf16*)dy, s.ldy, 0, s.tokens};
     if (out.dx) {
-        const Operand wt{w.wt, p.terms * kz, kz, s.cols};
-        const Operand z = w.dz ? Operand{w.dz, p.terms * kz, kz, s.tokens}
-                               : Operand{(const bf16*)dy, s.ldy, 0, s.tokens};
-        err = gradient<T>(p.dx, product_of(p.dx, wt, z, kz), {(T*)out.dx, nullptr, s.tokens, out.lddx}, s.cols, w.dx,
-                          st);
+        const Operand a = TURN ? turned(in.w, s.cols, s.outs, PAIR ? in.u.p : nullptr, p.kf)
+                               : Operand{w.wt, p.terms * kz, kz, s.cols};
+        const Target<T> to{(T*)out.dx, nullptr, s.tokens, INT64_MAX, out.lddx};
+        err = gradient<T, TURN, false>(p.dx, product_of(p.dx, a, z, kz), to, s.cols, w.dx, st);
         if (err != JORGE_OK) return err;
     }
     if (out.dweight) {
-        const Operand xt{w.xt, p.terms * p.kn, p.kn, s.cols}, zt{w.dzt, p.terms * p.kn, p.kn, p.mats * s.outs};
-        err = gradient<T>(p.dw, product_of(p.dw, xt, zt, p.kn), {(T*)out.dweight, (T*)out.dup, s.outs, out.lddw},
-                          s.cols, w.dw, st);
+        const Operand a = TURN ? turned(in.x, s.cols, s.tokens) : Operand{w.xt, p.terms * p.kn, p.kn, s.cols};
+        const Operand zt = TURN ? turned(z, p.rows_w, s.tokens) : Operand{w.dzt, p.terms * p.kn, p.kn, p.rows_w};
+        const Target<T> to{(T*)out.dweight, (T*)out.dup, s.outs, p.rows_w / p.mats, out.lddw};
+        err = gradient<T, TURN, TURN>(p.dw, product_of(p.dw, a, zt, p.kn), to, s.cols, w.dw, st);
         if (err != JORGE_OK) return err;
     }
     return launched("dense product");
@@ -841,7 +872,7 @@ jorge_status run_forward(const jorge_linear_shape& s, int mats, const void* x, c
     const jorge_status st = check_workspace(s, mats, false, workspace, bytes);
     if (st != JORGE_OK) return st;
     const Wanted want{false, false, false, false};
-    const bool direct_w = readable(s.dtype, s.cols, weight, s.ldw) && (mats == 1 || readable(s.dtype, s.cols, up, s.ldu));
+    const bool direct_w = readable(s.dtype, s.cols, weight, s.ldw) && (mats == 1 || (readable(s.dtype, s.cols, up, s.ldu) && s.ldw == s.ldu));
     const Plan p = plan_of(s, mats, want, readable(s.dtype, s.cols, x, s.ldx), direct_w, false);
     const Work w = carve(workspace, s, p, want);
     const hipStream_t q = reinterpret_cast<hipStream_t>(stream);
@@ -891,7 +922,7 @@ jorge_status run_backward(const jorge_linear_shape& s, int mats, const void* dy,
     if (st != JORGE_OK) return st;
     const Wanted want{true, g.dx != nullptr, g.dweight != nullptr, g.dbias != nullptr};
     if (!want.dx && !want.dw && !want.db) return JORGE_OK;
-    const bool direct_w = readable(s.dtype, s.cols, weight, s.ldw) && (mats == 1 || readable(s.dtype, s.cols, up, s.ldu));
+    const bool direct_w = readable(s.dtype, s.cols, weight, s.ldw) && (mats == 1 || (readable(s.dtype, s.cols, up, s.ldu) && s.ldw == s.ldu));
     const Plan p = plan_of(s, mats, want, readable(s.dtype, s.cols, x, s.ldx), direct_w,
                            readable(s.dtype, s.outs, dy, s.ldy));
     const Work w = carve(workspace, s, p, want);

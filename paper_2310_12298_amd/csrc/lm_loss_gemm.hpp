@@ -37,16 +37,32 @@ constexpr int kStageK = 32;
 
 // One operand of a product: `rows` rows of K elements at a stride of ld elements. Rows past the end are
 // not read: the last one is, in their place. `plane`: elements between a row's terms, of a split operand.
+//
+// A turned operand (Tile's TA, TB) lies the other way round: K lines of `rows` elements (a multiple of 8, 16-byte
+// aligned) at a stride of ld. `depth` of the lines exist; the others count as zeros. It may be two such matrices, one
+// after the other along K: the second one, p2, begins at line `part` (a multiple of 64).
 struct Operand {
     const bf16* p;
     int64_t ld, plane;
     int64_t rows;
+    const bf16* p2 = nullptr;
+    int64_t depth = 0, part = 0;
 };
+constexpr unsigned kNowhere = 0x80000000u;  // an offset past every resource's end: a load brings zeros
 
 constexpr int kTerms = 3;  // of a split operand
 
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) const void global_void;
+
+// 4 lines of 16 elements, 8 bytes from each of 16 lanes, to lane i's column i of each line. In a function with a
+// restricted pointer: without what that says of aliases the compiler waits here for every direct-to-LDS load in flight,
+// the next stages' too, which the callers' own waits keep apart (2.5 times the time of a product).
+__device__ __forceinline__ s16x4 read_turned4(const lds_s16x4* __restrict__ p) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16(const_cast<lds_s16x4*>(p));
+}
 
 // What chunk numbers are exclusive-ored with in row rho of 16, for rows of 64 and of 128 bytes.
 __device__ __forceinline__ int swizzle64(int rho) { return -(rho >> 2) & 3; }
@@ -56,8 +72,15 @@ __device__ __forceinline__ int swizzle128(int rho) { return rho >> 1; }
 // are of the first, the others of the second, so that a lane holds the same 2 WA rows of both:
 //   a = 2 WA (l / 16) + 4 i + r  of 8 WA rows, in blocks i and i + WA / 2.
 // The loads of waves 0 and 2 are then all of the first matrix, those of 1 and 3 of the second.
-template <int WA, int WB, int RING, bool SPLIT, bool PAIR = false>
+//
+// TA, TB: the operand is turned. A stage then holds 64 lines of the tile's 32 WA elements, and a fragment is read by
+// ds_read_tr16, which gives lane l % 16 of 16 the elements in column l % 16 of 4 lines of 16. The columns of a block are
+// 4 times 4 consecutive ones, so B's block j has those that A's rule gives: b = 4 WB (n / 4) + 4 j + n % 4 for column n
+// of the block. The 16-byte chunks of a line are permuted by its number so that the 4 x 4 pieces of 8 bytes that 16
+// lanes read meet 16 chunks.
+template <int WA, int WB, int RING, bool SPLIT, bool PAIR = false, bool TA = false, bool TB = false>
 struct Tile {
+    static_assert(!SPLIT || (!TA && !TB), "terms are K-contiguous");
     static constexpr int kA = 32 * WA, kB = 32 * WB;
     static constexpr int kRowsA = PAIR ? 16 * WA : kA;             // of A (of each of two)
     static constexpr int kLaneA = PAIR ? 2 * WA : 4 * WA;          // consecutive ones that a lane ends up with
@@ -77,6 +100,17 @@ struct Tile {
         return (wave & 1) * 16 * WB + (lane & 15) * WB;
     }
 
+    // Which b of the wave's part column n of block j is.
+    static __device__ __forceinline__ int part_b(int n, int j) {
+        return TB ? (n >> 2) * 4 * WB + 4 * j + (n & 3) : n * WB + j;
+    }
+
+    // What a line's chunk numbers are exclusive-ored with, of a turned operand with W blocks to a wave.
+    template <int W>
+    static __device__ __forceinline__ int swizzle_line(int k) {
+        return W == 8 ? k & 3 : W == 4 ? (k & 1) | (k >> 1 & 1) << 3 : (k >> 1 & 1) << 2;
+    }
+
     // Stages [s0, s1) of the product of rows a0 .. of A and b0 .. of B, of which each row has `stages` (32 k each).
     // s0 and s1 are even, s1 > s0. lds: kBytes.
     __device__ __forceinline__ void multiply(const Operand& A, const Operand& B, int64_t a0, int64_t b0, int s0, int s1,
@@ -90,6 +124,9 @@ struct Tile {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const Operand& A = PAIR && (wave & 1) ? A2 : A1;
         Loads load;
+        if constexpr (TA) load.la = Lines(A, a0);
+        if constexpr (TB) load.lb = Lines(B, b0);
+        load.line = s0 * kStageK;
         // Where this lane's loads start: load n of the operand (n = wave * kLoads + v) takes rows rho of block i of a
         // half of the tile. Bytes from the tile's first row to the end of its last one are what a load may reach.
         const int limA = (int)(A.rows - a0 < kRowsA ? A.rows - a0 : kRowsA) - 1;
@@ -100,8 +137,18 @@ struct Tile {
             rho = SPLIT ? lane >> 2 : (n & 1) * 8 + (lane >> 3);
             return (unsigned)(SPLIT ? (lane & 3) ^ swizzle64(rho) : (lane & 7) ^ swizzle128(rho)) * 16u;
         };
+        // Of a turned operand: 1 KB is 16 / W lines of 32 W elements.
+        const auto line = [&](int n, auto W, int64_t there, unsigned ld) {
+            constexpr int w = decltype(W)::value, chunks = 4 * w;
+            const int k = n * (64 / chunks) + lane / chunks, chunk = (lane % chunks) ^ swizzle_line<w>(k);
+            return chunk * 8 < there ? (unsigned)k * ld * 2u + chunk * 16u : kNowhere;
+        };
 #pragma unroll
         for (int v = 0; v < kLoadsA; ++v) {
+            if constexpr (TA) {
+                load.offA[v] = line(wave * kLoadsA + v, std::integral_constant<int, WA>(), A.rows - a0, (unsigned)A.ld);
+                continue;
+            }
             int block, rho;
             const unsigned chunk = place(wave * kLoadsA + v, block, rho);
             const int row = block / WA * (kRowsA / 2) + (rho >> 2) * kLaneA + 4 * (block % (kLaneA / 4)) + (rho & 3);
@@ -109,13 +156,20 @@ struct Tile {
         }
 #pragma unroll
         for (int v = 0; v < kLoadsB; ++v) {
+            if constexpr (TB) {
+                load.offB[v] = line(wave * kLoadsB + v, std::integral_constant<int, WB>(), B.rows - b0, (unsigned)B.ld);
+                continue;
+            }
             int block, rho;
             const unsigned chunk = place(wave * kLoadsB + v, block, rho);
             const int row = block / WB * 16 * WB + rho * WB + block % WB;
             load.offB[v] = (unsigned)(row < limB ? row : limB) * (unsigned)B.ld * 2u + chunk;
         }
-        load.ra = resource(A.p + a0 * A.ld, ((unsigned)limA * (unsigned)A.ld + more * (unsigned)A.plane + K) * 2u);
-        load.rb = resource(B.p + b0 * B.ld, ((unsigned)limB * (unsigned)B.ld + more * (unsigned)B.plane + K) * 2u);
+        if constexpr (!TA)
+            load.ra = resource(A.p + a0 * A.ld, ((unsigned)limA * (unsigned)A.ld + more * (unsigned)A.plane + K) * 2u);
+        if constexpr (!TB)
+            load.rb = resource(B.p + b0 * B.ld, ((unsigned)limB * (unsigned)B.ld + more * (unsigned)B.plane + K) * 2u);
+        load.lines();
         load.k = s0 * (kStageK * 2);
         load.left = SPLIT ? s1 - s0 : (s1 - s0) / 2;
 #pragma unroll
@@ -129,22 +183,49 @@ struct Tile {
     }
 
 private:
+    // A turned operand from element `first` of its lines on: the 64 lines of a stage, of which those past `depth` are past
+    // the resource's end. Without branches: the loop's body stays one block.
+    struct Lines {
+        const bf16 *p, *p2;
+        int ld, depth, part, last;  // last: elements of a line from `first` on, in whole chunks
+        Lines() = default;
+        __device__ __forceinline__ Lines(const Operand& o, int64_t first)
+            : p(o.p + first), p2(o.p2 ? o.p2 + first : nullptr), ld((int)o.ld), depth((int)o.depth), part(o.p2 ? (int)o.part : 1 << 30),
+              last((int)((o.rows + 7) / 8 * 8 - first)) {}
+        __device__ __forceinline__ __amdgpu_buffer_rsrc_t stage(int line) const {
+            const bool two = line >= part;
+            const int at = two ? line - part : line, left = depth - at, n = left < 64 ? left : 64;
+            const unsigned bytes = (unsigned)((n - 1) * ld + last) * 2u;
+            return resource((two ? p2 : p) + (int64_t)at * ld, n > 0 ? bytes : 0u);
+        }
+    };
+
     // The loads of one stage after the other.
     struct Loads {
         unsigned offA[kLoadsA], offB[kLoadsB];
         __amdgpu_buffer_rsrc_t ra, rb;
         int k, left;  // bytes into the rows, and stages left
+        Lines la, lb; // turned operands
+        int line;     // of the stage's first one
         __device__ __forceinline__ void a(int v, char* to, int at) const {
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void*)to, 16, offA[v], at, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void*)to, 16, offA[v], TA ? 0 : at, 0, 0);
         }
         __device__ __forceinline__ void b(int v, char* to, int at) const {
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void*)to, 16, offB[v], at, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void*)to, 16, offB[v], TB ? 0 : at, 0, 0);
+        }
+        __device__ __forceinline__ void lines() {
+            if constexpr (TA) ra = la.stage(line);
+            if constexpr (TB) rb = lb.stage(line);
         }
         // Where no stage is left the last one is loaded again and not used: every wave always has the same number of
         // loads in flight, and the loop's body stays one block.
         __device__ __forceinline__ void next() {
             --left;
             k += left > 0 ? kStageK * (SPLIT ? 2 : 4) : 0;
+            if constexpr (TA || TB) {
+                line += left > 0 ? 2 * kStageK : 0;
+                lines();
+            }
         }
     };
 
@@ -160,7 +241,25 @@ private:
         static_assert(kRing >= 2 && (kRing & (kRing - 1)) == 0, "a power of two");
         const int rho = threadIdx.x & 15, frag = rho * 128 + ((((threadIdx.x & 63) >> 4) ^ swizzle128(rho)) * 16);
         const int fragA = frag + (wave >> 1) * WA * 2048, fragB = frag + (2 * WA + (wave & 1) * WB) * 2048;
+        // Of turned operands: line 8 (l / 16) + l % 16 / 4 of 32, elements 4 W (l % 4) .. + 3 of the wave's part; the next
+        // four lines are 4 further, whose chunks are permuted alike.
+        const int lane = threadIdx.x & 63, line = (lane >> 4) * 8 + (lane & 15) / 4;
+        const auto turned = [&](auto W, int part) {
+            constexpr int w = decltype(W)::value;
+            return line * (64 * w) + (((part * 2 * w + (lane & 3) * (w / 2)) ^ swizzle_line<w>(line)) * 16);
+        };
+        const int turnA = turned(std::integral_constant<int, WA>(), wave >> 1);
+        const int turnB = turned(std::integral_constant<int, WB>(), wave & 1) + kA * kStageK * 4;
         bf16x8 fa[2][WA], fb[2][WB];
+        // Block i of half h: chunk i / 2 of the lane's, its half i % 2.
+        const auto read_turned = [](const char* p, int at, auto W, int h, int i) {
+            constexpr int w = decltype(W)::value;
+            s16x4 v[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+                v[u] = read_turned4((const lds_s16x4*)(p + (at ^ (i / 2 * 16)) + (h * 32 + u * 4) * (64 * w) + (i & 1) * 8));
+            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        };
         const auto one = [&](int v, int slot) {
             char* const to = lds + slot * kStageBytes;
             if (v < kLoadsA) load.a(v, to + (wave * kLoadsA + v) * 1024, load.k);
@@ -169,8 +268,13 @@ private:
         // Fragment f of half h of a stage: first B's, which the first row of MFMAs needs together, then A's.
         const auto read = [&](int slot, int h, int f) {
             const char* const p = lds + slot * kStageBytes;
-            if (f < WB) fb[h][f] = *reinterpret_cast<const bf16x8*>(p + (fragB ^ (h * 64)) + f * 2048);
-            else fa[h][f - WB] = *reinterpret_cast<const bf16x8*>(p + (fragA ^ (h * 64)) + (f - WB) * 2048);
+            if (f < WB) {
+                if constexpr (TB) fb[h][f] = read_turned(p, turnB, std::integral_constant<int, WB>(), h, f);
+                else fb[h][f] = *reinterpret_cast<const bf16x8*>(p + (fragB ^ (h * 64)) + f * 2048);
+            } else {
+                if constexpr (TA) fa[h][f - WB] = read_turned(p, turnA, std::integral_constant<int, WA>(), h, f - WB);
+                else fa[h][f - WB] = *reinterpret_cast<const bf16x8*>(p + (fragA ^ (h * 64)) + (f - WB) * 2048);
+            }
         };
 #pragma unroll
         for (int r = 0; r < kRing; ++r) {

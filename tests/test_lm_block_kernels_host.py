@@ -35,5 +35,5 @@ def test_matrix_loops_neither_copy_nor_spill_accumulators(tmp_path):
             assert loop[mfmas[-1] + 1:].count("s_nop 15") == 2, name
             assert sum(t.startswith("v_mfma") for _, t in body) == len(mfmas), f"{name}: an MFMA outside the loop"
             seen += 1
-    # Types; linear: four tiles, gated: three, forward and dz; gradients: four tiles.
-    assert seen == 2 * (2 * (4 + 3) + 4)
+    # Types; linear: four tiles, gated: three, forward and dz; gradients: four tiles, of bfloat16 two ways round.
+    assert seen == 2 * 2 * (4 + 3) + 4 + 4 * 2
