@@ -85,16 +85,23 @@ struct Sequence {
     }
 };
 
-// Workgroup id's place: the key head (of all sequences), and the tile of its own rows. Workgroup g runs on XCD g mod 8;
-// each XCD takes a contiguous share, so that the tiles that read the same keys do so from one L2. Where the last tiles
-// have the most to do they come first.
+// Workgroup g's place: the key head (of all sequences), and the tile of its own rows. Workgroup g runs on XCD g mod 8:
+// tiles that read the same keys are put on one, so that they do so from one L2, and key heads are dealt out in turn, so
+// that a batch of unequal sequences loads all XCDs alike (three sequences of 1301, 650 and 0 keys in equal shares one
+// after the other: 1.4 times the time); the last ones, if they are no multiple of eight, are spread tile by tile. Where
+// the last tiles have the most to do they come first.
 struct Work {
     int bh, tile;
     __device__ __forceinline__ Work(int g, int total, int tiles, int heaviest_last) {
-        const int q = total / 8, r = total % 8, x = g % 8;
-        const int id = x * q + min(x, r) + g / 8;
-        bh = id / tiles;
-        tile = id - bh * tiles;
+        const int heads = total / tiles, whole = heads / 8, n = g / 8, x = g % 8;
+        if (n < whole * tiles) {
+            bh = n / tiles * 8 + x;
+            tile = n % tiles;
+        } else {
+            const int rest = (n - whole * tiles) * 8 + x;
+            bh = whole * 8 + rest / tiles;
+            tile = rest % tiles;
+        }
         if (heaviest_last) tile = tiles - 1 - tile;
     }
 };
@@ -106,15 +113,16 @@ __device__ __forceinline__ s16x4 read_turned4(const lds_s16x4* __restrict__ p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16(const_cast<lds_s16x4*>(p));
 }
 
+// Rows of D elements (32, 64, 96 or 128).
 template <typename T, int D>
 struct Tile {
-    static constexpr int kRow = D * (int)sizeof(T);       // bytes of a row
+    static constexpr int kRow = (D <= 64 ? 64 : 128) * (int)sizeof(T);  // bytes of a row in LDS
     static constexpr int kChunks = kRow / 16;
     static constexpr int kRows = sizeof(T) == 2 ? 64 : 32;
     static constexpr int kBlocks = kRows / 32;
     static constexpr int kBytes = kRows * kRow;
     static constexpr int kLoads = kBytes / 1024;          // wave-wide loads of 16 bytes a lane
-    static constexpr int kSteps = kRow / 32;              // of rows(): 16 bytes of either half of a wave
+    static constexpr int kSteps = D * (int)sizeof(T) / 32;  // of rows(): 16 bytes of either half of a wave
     static constexpr int kDims = D / 32;                  // blocks of 32 elements of a row
 
     // What a row's chunk numbers are exclusive-ored with.
@@ -201,6 +209,46 @@ struct Tile {
         return s;
     }
 
+    // S of every block of the tile. The reads run ahead of the products by one block's: a wave that waits for each
+    // fragment alone leaves the matrix cores idle three quarters of the time.
+    __device__ __forceinline__ void all_rows(const char* tile, const Own& own, f32x16 (&s)[kBlocks]) const {
+#pragma unroll
+        for (int kb = 0; kb < kBlocks; ++kb) s[kb] = rows(tile, kb, own);
+        if constexpr (sizeof(T) == 2) {
+            __builtin_amdgcn_sched_group_barrier(0x100, kSteps, 0);
+#pragma unroll
+            for (int i = 0; i < (kBlocks - 1) * kSteps; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, kSteps, 0);
+        } else order_rows(kBlocks);
+    }
+    // fp32: four products to a read; the reads run four ahead.
+    static __device__ __forceinline__ void order_rows(int products) {
+        constexpr int kAhead = 4;
+        __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+        for (int i = 0; i < products * kSteps - kAhead; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4 * kAhead, 0);
+    }
+
+    // The order of a backward kernel's two products by rows: the reads of one run while the one before it does.
+    static __device__ __forceinline__ void order() {
+        if constexpr (sizeof(T) == 2) {
+            __builtin_amdgcn_sched_group_barrier(0x100, kSteps, 0);
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, kSteps, 0);
+        } else order_rows(2);
+    }
+
     // acc[db] += the tile's rows of block kb, elements 32 db .., times p.
     __device__ __forceinline__ void cols(const char* tile, int kb, const f32x16& p, f32x16 (&acc)[kDims]) const {
         if constexpr (sizeof(T) == 2) {
@@ -235,6 +283,14 @@ struct Tile {
                             tile + ((at_cols ^ (db * 128) ^ ((g & 1) * 64) ^ (r * 16)) + (kb * 32 + g * 8 + r) * kRow));
                         acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p[4 * g + r], acc[db], 0, 0, 0);
                     }
+            constexpr int kAhead = 8;
+            __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+            for (int i = 0; i < 16 * kDims - kAhead; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
         }
     }
 
@@ -447,8 +503,7 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(Call c, Heads
         const char* const vt = kt + L::kBytes;
         if (!__any(k0 < hi && k0 + L::kRows > lo)) return;
         f32x16 z[L::kBlocks];
-#pragma unroll
-        for (int kb = 0; kb < L::kBlocks; ++kb) z[kb] = tile.rows(kt, kb, own);
+        tile.all_rows(kt, own, z);
         soft.template tile<T>(c, z, k0, lo, hi);
 #pragma unroll
         for (int kb = 0; kb < L::kBlocks; ++kb) tile.cols(vt, kb, z[kb], soft.acc);
@@ -592,39 +647,40 @@ __global__ __launch_bounds__(256) void attention_join_kernel(Call c, Output out,
 }
 
 // ---------------------------------------------------------------- backward
-// stats: [batch][head][token], the row's log2 sum exp (plus infinity where it sees nothing, so that every probability is
-// 0) and delta = do . o. 16 lanes to a row.
+// [batch][head][token]: the row's log2 sum exp (plus infinity where it sees nothing, so that every probability is 0) and
+// delta = do . o. Two lanes to a row, which add it up as attention_dq_kernel does where that forms it: dk and dv are the
+// same to the bit with and without dq.
 template <typename T>
 __global__ __launch_bounds__(256) void attention_delta_kernel(Call c, Heads o, Heads g, const float* __restrict__ lse,
                                                               float* __restrict__ lse2, float* __restrict__ delta) {
-    const int64_t id = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+    const int64_t id = (int64_t)blockIdx.x * 128 + (threadIdx.x >> 1);
     if (id >= (int64_t)c.batch * c.heads * c.q_tokens) return;
     // Neighbouring rows are heads of a token, as they lie in memory.
     const int h = (int)(id % c.heads);
     const int64_t bt = id / c.heads;
-    const int t = (int)(bt % c.q_tokens), b = (int)(bt / c.q_tokens), d0 = (threadIdx.x & 15) * 8;
+    const int t = (int)(bt % c.q_tokens), b = (int)(bt / c.q_tokens);
     const Sequence s(c, b);
     const T* const po = reinterpret_cast<const T*>(o.p + b * o.batch + t * o.token + h * o.head);
     const T* const pg = reinterpret_cast<const T*>(g.p + b * g.batch + t * g.token + h * g.head);
     const int64_t at = ((int64_t)b * c.heads + h) * c.q_tokens + t;
     const bool seen = s.hi(c, t) > s.lo(c, t);
+    constexpr int N = 16 / sizeof(T);
     float sum = 0.0f;
-    if (seen) {
-        typedef T V __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-        if (d0 + 8 <= c.dim) {
-            const V x = *reinterpret_cast<const V*>(po + d0), y = *reinterpret_cast<const V*>(pg + d0);
+    if (seen)
+        for (int d = (threadIdx.x & 1) * N; d < c.dim; d += 2 * N) {
+            typedef T V __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+            if (d + N <= c.dim) {
+                const V x = *reinterpret_cast<const V*>(po + d), y = *reinterpret_cast<const V*>(pg + d);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum += (float)x[e] * (float)y[e];
-        } else {
-            for (int e = d0; e < c.dim; ++e) sum += (float)po[e] * (float)pg[e];
+                for (int e = 0; e < N; ++e) sum = __builtin_fmaf((float)x[e], (float)y[e], sum);
+            } else {
+                for (int e = d; e < c.dim; ++e) sum = __builtin_fmaf((float)po[e], (float)pg[e], sum);
+            }
         }
-    }
-#pragma unroll
-    for (int off = 1; off < 16; off *= 2) sum += __shfl_xor(sum, off);
-    if ((threadIdx.x & 15) == 0) {
-        lse2[at] = seen ? lse[at] * kLog2e : INFINITY;
-        delta[at] = seen ? sum : 0.0f;
-    }
+    sum += __shfl_xor(sum, 1);
+    if (threadIdx.x & 1) return;
+    lse2[at] = seen ? lse[at] * kLog2e : INFINITY;
+    delta[at] = seen ? sum : 0.0f;
 }
 
 // Gradients of rows of one matrix: to it, or, where the streamed side is cut into ranges, the range's sums
@@ -634,10 +690,17 @@ struct Gradient {
     float* part;
 };
 
+// A row's log2 sum exp and delta: as attention_delta_kernel left them, or (o given) formed here from the row's o and
+// gradient, which saves reading the gradient twice, and left for attention_dkv_kernel.
+struct RowStats {
+    Heads o;
+    const float* lse;
+    float *lse2, *delta;
+};
+
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void attention_dq_kernel(Call c, Heads q, Heads k, Heads v, Heads g,
-                                                              const float* __restrict__ lse2,
-                                                              const float* __restrict__ delta, Gradient dq, int tiles) {
+                                                              RowStats stats, Gradient dq, int tiles) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     using L = Tile<T, D>;
     const Work at(blockIdx.x, gridDim.x, tiles, c.causal);
@@ -657,7 +720,25 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(Call c, Heads q, H
     const Two<L> fetch{{k.p + b * k.batch + hk * k.head, k.token, c.dim, wave},
                        {v.p + b * v.batch + hk * v.head, v.token, c.dim, wave}, span.lo, span.hi, wave};
     const int64_t stat = ((int64_t)b * c.heads + row.head) * c.q_tokens + row.token;
-    const float l2 = row.there ? lse2[stat] : INFINITY, de = row.there ? delta[stat] : 0.0f;
+    float l2 = INFINITY, de = 0.0f;
+    if (stats.o.p) {
+        typename L::Own o;
+        o.load(stats.o.p + b * stats.o.batch + row.token * stats.o.token + row.head * stats.o.head,
+               row.there && hi > lo, c.dim);
+#pragma unroll
+        for (int n = 0; n < L::kSteps; ++n)
+#pragma unroll
+            for (int e = 0; e < (int)(16 / sizeof(T)); ++e) de = __builtin_fmaf((float)o.f[n][e], (float)grad.f[n][e], de);
+        de += __shfl_xor(de, 32);
+        if (row.there && hi > lo) l2 = stats.lse[stat] * kLog2e;
+        if (row.there && lane < 32 && blockIdx.y == 0) {
+            stats.lse2[stat] = l2;
+            stats.delta[stat] = de;
+        }
+    } else if (row.there) {
+        l2 = stats.lse2[stat];
+        de = stats.delta[stat];
+    }
     f32x16 acc[L::kDims];
     clear(acc);
     stream<2 * L::kBytes>(span, lds, fetch, [&](int t, const char* kt) {
@@ -670,8 +751,8 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(Call c, Heads q, H
             f32x16 z = tile.rows(kt, kb, own);
             const f32x16 dp = tile.rows(vt, kb, grad);
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                z[i] = probability<T>(c, z[i], l2) * (dp[i] - de);
+            for (int i = 0; i < 16; ++i) z[i] = probability<T>(c, z[i], l2) * (dp[i] - de);
+            L::order();
             if (masked)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -692,8 +773,12 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(Call c, Heads q, H
              c.scale, hi > lo);
 }
 
+// Two waves to a SIMD where their registers allow it (a wave's k, v and sums of dk and dv take D of them for every four
+// bytes of T): with D = 96 in bfloat16 that takes 111 us where one wave takes 128 (5 sequences of up to 2011, 12 heads
+// of 80, window 512). At D = 128 two would spill in the loop (1.7 times the time); eight waves to a workgroup that keep
+// v in LDS instead took as long as four with one to a SIMD.
 template <typename T, int D>
-__global__ __launch_bounds__(256, 1) void attention_dkv_kernel(Call c, Heads q, Heads k, Heads v, Heads g,
+__global__ __launch_bounds__(256, D <= (sizeof(T) == 2 ? 96 : 64) ? 2 : 1) void attention_dkv_kernel(Call c, Heads q, Heads k, Heads v, Heads g,
                                                                const float* __restrict__ lse2,
                                                                const float* __restrict__ delta, Gradient dk,
                                                                Gradient dv, int tiles) {
@@ -738,6 +823,7 @@ __global__ __launch_bounds__(256, 1) void attention_dkv_kernel(Call c, Heads q, 
                         dp[i] = z[i] * (dp[i] - de[i & 3]);
                     }
                 }
+                L::order();
                 if (masked)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
@@ -820,7 +906,7 @@ struct Plan {
     bool few;                      // forward: the kernel for few rows
     int tiles, tiles_k;            // of own rows, of own keys
     int ranges, ranges_q, ranges_k;  // forward; dq (over keys); dk, dv (over queries)
-    int wide;                      // 64 or 128
+    int wide;                      // elements of a row as the kernels take it: 32, 64, 96 or 128
 };
 // Into how many ranges a launch of `groups` workgroups cuts `tiles` streamed tiles: enough that each CU has two
 // workgroups, of at least `least` tiles.
@@ -832,16 +918,16 @@ Plan plan_of(const jorge_attention_shape& s) {
     Plan p{};
     const int64_t group = s.heads / s.kv_heads, rows = s.q_tokens * group, bh = s.batch * s.kv_heads;
     const int tile = s.dtype == JORGE_F32 ? 32 : 64;
-    p.wide = s.dim <= 64 ? 64 : 128;
+    p.wide = (int)round_up(s.dim, 32);
     p.few = rows <= kOwn;
     p.tiles = (int)ceil_div(rows, 4 * kOwn);
     p.tiles_k = (int)ceil_div(s.kv_tokens, 4 * kOwn);
     // What a query sees at most, in tiles.
     const int64_t keys = s.window ? std::min<int64_t>(s.kv_tokens, s.window + 4 * kOwn / group + 1) : s.kv_tokens;
     const int64_t key_tiles = ceil_div(keys, tile), row_tiles = ceil_div(s.q_tokens, tile);
-    p.ranges = p.few ? cut(bh, key_tiles, 8) : cut(bh * p.tiles, key_tiles, 4);
-    p.ranges_q = cut(bh * p.tiles, key_tiles, 4);
-    p.ranges_k = cut(bh * p.tiles_k, row_tiles, 4);
+    p.ranges = p.few ? cut(bh, key_tiles, 8) : cut(bh * p.tiles, key_tiles, 2);
+    p.ranges_q = cut(bh * p.tiles, key_tiles, 2);
+    p.ranges_k = cut(bh * p.tiles_k, row_tiles, 2);
     return p;
 }
 
@@ -962,15 +1048,17 @@ jorge_status backward(const jorge_attention_shape& s, const Plan& p, const Space
     const Heads g = operand<T>(s, dout, s.q_tokens, s.heads, w.g, st);
     const int64_t rows = s.batch * s.heads * s.q_tokens, keys = s.batch * s.kv_heads * s.kv_tokens;
     const int bh = c.batch * c.kv_heads;
-    if (rows)
-        attention_delta_kernel<T><<<dim3((unsigned)ceil_div(rows, 16)), dim3(256), 0, st>>>(
+    // dq is formed first, and its kernel forms what dk's and dv's reads of a row too.
+    const bool fused = dq.data && rows && readable(s, out);
+    if (rows && !fused)
+        attention_delta_kernel<T><<<dim3((unsigned)ceil_div(rows, 128)), dim3(256), 0, st>>>(
             c, in_bytes(out, sizeof(T)), in_bytes(dout, sizeof(T)), lse, w.lse2, w.delta);
     jorge_status err;
     if (dq.data && rows) {
         if ((err = allow_lds(attention_dq_kernel<T, D>, 4 * L::kBytes)) != JORGE_OK) return err;
         const Gradient to{in_bytes(dq, sizeof(T)), w.part};
         attention_dq_kernel<T, D><<<dim3(bh * p.tiles, p.ranges_q), dim3(256), 4 * L::kBytes, st>>>(
-            c, q, k, v, g, w.lse2, w.delta, to, p.tiles);
+            c, q, k, v, g, {fused ? in_bytes(out, sizeof(T)) : Heads{}, lse, w.lse2, w.delta}, to, p.tiles);
         if (w.part)
             attention_sum_kernel<T, D><<<dim3((unsigned)ceil_div(rows, 8)), dim3(256), 0, st>>>(
                 to, p.ranges_q, s.q_tokens * c.group, rows, c.kv_heads, c.group, c.dim);
@@ -988,6 +1076,20 @@ jorge_status backward(const jorge_attention_shape& s, const Plan& p, const Space
                     to, p.ranges_k, s.kv_tokens, keys, c.kv_heads, 1, c.dim);
     }
     return launched("attention");
+}
+
+// f(an element, the row's width as a constant).
+template <typename F>
+jorge_status with_kernels(const jorge_attention_shape& s, const Plan& p, F&& f) {
+    const auto wide = [&](auto t) {
+        switch (p.wide) {
+            case 32: return f(t, std::integral_constant<int, 32>());
+            case 64: return f(t, std::integral_constant<int, 64>());
+            case 96: return f(t, std::integral_constant<int, 96>());
+            default: return f(t, std::integral_constant<int, 128>());
+        }
+    };
+    return s.dtype == JORGE_F32 ? wide(0.0f) : wide((bf16)0.0f);
 }
 
 // Strides that the kernels' offsets can hold: a tile's rows within 2^31 bytes.
@@ -1065,9 +1167,9 @@ jorge_status jorge_attention_forward(const jorge_attention_shape* shape, const j
     if ((st = check_workspace(carve(nullptr, s, p, nullptr).bytes, workspace, workspace_bytes)) != JORGE_OK) return st;
     const Space w = carve(workspace, s, p, nullptr);
     const hipStream_t q = reinterpret_cast<hipStream_t>(hip_stream);
-    if (s.dtype == JORGE_F32)
-        return p.wide == 64 ? forward<float, 64>(s, p, w, *out, lse, q) : forward<float, 128>(s, p, w, *out, lse, q);
-    return p.wide == 64 ? forward<bf16, 64>(s, p, w, *out, lse, q) : forward<bf16, 128>(s, p, w, *out, lse, q);
+    return with_kernels(s, p, [&](auto t, auto D) {
+        return forward<decltype(t), decltype(D)::value>(s, p, w, *out, lse, q);
+    });
 }
 
 jorge_status jorge_attention_backward(const jorge_attention_shape* shape, const jorge_heads* dout,
@@ -1096,11 +1198,9 @@ jorge_status jorge_attention_backward(const jorge_attention_shape* shape, const 
     const Space w = carve(workspace, s, p, &d);
     const hipStream_t q = reinterpret_cast<hipStream_t>(hip_stream);
     const jorge_heads& o = out ? *out : none;
-    if (s.dtype == JORGE_F32)
-        return p.wide == 64 ? backward<float, 64>(s, p, w, d, o, lse, gq, gk, gv, q)
-                            : backward<float, 128>(s, p, w, d, o, lse, gq, gk, gv, q);
-    return p.wide == 64 ? backward<bf16, 64>(s, p, w, d, o, lse, gq, gk, gv, q)
-                        : backward<bf16, 128>(s, p, w, d, o, lse, gq, gk, gv, q);
+    return with_kernels(s, p, [&](auto t, auto D) {
+        return backward<decltype(t), decltype(D)::value>(s, p, w, d, o, lse, gq, gk, gv, q);
+    });
 }
 
 }  // extern "C"
