@@ -170,13 +170,16 @@ jorge_status jorge_cross_entropy_backward(const jorge_loss_shape* shape, const f
  *   gated linear:  dg = dy u act'(g),  du = dy act(g),  dx = dg gate + du up,  dgate = dg^T x,  dup = du^T x.
  * relu's derivative at 0 is 0. bfloat16: dz, dg and du are rounded to bfloat16 for the products, whose sums are fp32
  * (dbias is summed before that); a gradient then errs by some 2.4e-3 of its size instead of the 1.7e-3 of its own
- * rounding. fp32: up to 64 tokens forward are multiplied in fp32; the other products are formed from three-term
+ * rounding. fp32: up to JORGE_LINEAR_FEW_TOKENS forward are multiplied in fp32; the other products are formed from three-term
  * bfloat16 splits as the Jorge step's are (jorge.h): values above 3.39e38 count as infinite. */
 #define JORGE_ACT_NONE    0
 #define JORGE_ACT_RELU    1
 #define JORGE_ACT_GELU    2
 #define JORGE_ACT_SILU    3
 #define JORGE_ACT_SIGMOID 4
+
+/* Up to so many tokens the forward passes need no workspace. */
+#define JORGE_LINEAR_FEW_TOKENS 64
 
 /* Largest tokens, cols, outs and row strides; tokens * max(cols, outs) ends at 2^34. */
 #define JORGE_LINEAR_MAX_TOKENS (1 << 21)

@@ -288,7 +288,8 @@ __global__ __launch_bounds__(256) void dense_join_kernel(const float* __restrict
 }
 
 // ---------------------------------------------------------------- few tokens
-constexpr int kFewWaves = 8, kFewTokens = 64;  // the most tokens of the kernel below
+constexpr int kFewWaves = 8, kFewTokens = JORGE_LINEAR_FEW_TOKENS;  // the most tokens of the kernel below
+static_assert(kFewTokens == 64, "16 NT");
 
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef __bf16 bf16x8u __attribute__((ext_vector_type(8), aligned(2)));

@@ -41,9 +41,11 @@ class Heads(ctypes.Structure):
 
 
 class AttentionShape(ctypes.Structure):
+    # q, k and v as their four fields each, which takes less time to fill in than a Heads.
     _fields_ = [("batch", _I64), ("q_tokens", _I64), ("kv_tokens", _I64), ("heads", _I32), ("kv_heads", _I32),
                 ("dim", _I32), ("dtype", _I32), ("scale", _F64), ("causal", _I32), ("reserved", _I32),
-                ("window", _I64), ("q_lengths", _P), ("kv_lengths", _P), ("q", Heads), ("k", Heads), ("v", Heads)]
+                ("window", _I64), ("q_lengths", _P), ("kv_lengths", _P),
+                *[(f"{t}_{n}", c) for t in "qkv" for n, c in Heads._fields_]]
 
 
 class AdamWTensor(ctypes.Structure):
@@ -118,7 +120,7 @@ def _cuda(t, what, dtypes=DTYPES):
         raise ValueError(f"{what}: a CUDA tensor is needed")
     if t.dtype not in dtypes:
         raise ValueError(f"{what}: unsupported type {t.dtype}")
-    if t.get_device() != torch.cuda.current_device():
+    if t.get_device() != torch._C._cuda_getDevice():      # as torch.cuda.current_device(), without its checks (0.4 us)
         raise ValueError(f"{what}: on device {t.get_device()}, not the current one")
     return t
 
@@ -388,6 +390,7 @@ def linear_cross_entropy(hidden, weight, targets, ignore_index=-100, label_smoot
 
 # ---------------------------------------------------------------- linear layers
 LINEAR_MAX_STRIDE = 1 << 22                   # JORGE_LINEAR_MAX_STRIDE
+LINEAR_FEW_TOKENS = 64                        # JORGE_LINEAR_FEW_TOKENS
 
 
 def _rows(t, what):
@@ -441,9 +444,9 @@ def linear_forward(x, weight, bias=None, activation=None, residual=None):
         if residual.shape != shape_y or residual.dtype != x.dtype:
             raise ValueError("residual must have the result's shape and x's type")
         r = _rows(residual, "residual")
-    y = torch.empty(shape_y, dtype=x.dtype, device=x.device)
+    y = x.new_empty(shape_y)
     shape = _linear_shape(m, w, w, outs, outs if r is None else _ld(r), b, act)
-    ws, n = _linear_workspace(lib, shape, 0, 0)
+    ws, n = (None, 0) if shape.tokens <= LINEAR_FEW_TOKENS else _linear_workspace(lib, shape, 0, 0)
     _check(lib, lib.jorge_linear_forward(ctypes.byref(shape), m.data_ptr(), w.data_ptr(), _ptr(b), _ptr(r),
                                          y.data_ptr(), _ptr(ws), n, _stream(x)))
     return y
@@ -496,9 +499,9 @@ def gated_linear_forward(x, gate, up, activation="silu"):
     lib = load_operators()
     act = _activation(activation)
     m, (g, u) = _weights(x, [(gate, "gate"), (up, "up")])
-    y = torch.empty(x.shape[:-1] + (g.shape[0],), dtype=x.dtype, device=x.device)
+    y = x.new_empty(x.shape[:-1] + (g.shape[0],))
     shape = _linear_shape(m, g, u, g.shape[0], g.shape[0], None, act)
-    ws, n = _linear_workspace(lib, shape, 1, 0)
+    ws, n = (None, 0) if shape.tokens <= LINEAR_FEW_TOKENS else _linear_workspace(lib, shape, 1, 0)
     _check(lib, lib.jorge_gated_linear_forward(ctypes.byref(shape), m.data_ptr(), g.data_ptr(), u.data_ptr(),
                                                y.data_ptr(), _ptr(ws), n, _stream(x)))
     return y
@@ -548,16 +551,18 @@ ATTENTION_MAX_STRIDE = 1 << 22                # JORGE_ATTENTION_MAX_STRIDE
 
 
 def _heads(t, what, like=None):
-    """t (batch, tokens, heads, dim) with dense rows and a token stride that the call takes, as a tensor and a Heads."""
+    """t (batch, tokens, heads, dim) with dense rows and a token stride that the call takes, and a Heads' fields of it."""
     _cuda(t, what)
     if t.dim() != 4:
         raise ValueError(f"{what}: (batch, tokens, heads, dim) is needed")
     if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
         raise ValueError(f"{what}: shape {tuple(t.shape)} and type {t.dtype}, not {tuple(like.shape)} and {like.dtype}")
-    if (t.shape[3] > 1 and t.stride(3) != 1) or (t.shape[1] > 1 and t.stride(1) > ATTENTION_MAX_STRIDE):
+    _, tokens, heads, dim = t.shape
+    batch_s, token_s, head_s, dim_s = t.stride()
+    if (dim_s != 1 and dim > 1) or (token_s > ATTENTION_MAX_STRIDE and tokens > 1):
         t = t.contiguous()
-    strides = [s if n > 1 else 0 for s, n in zip(t.stride(), t.shape)]
-    return t, Heads(t.data_ptr(), *strides[:3])
+        batch_s, token_s, head_s, dim_s = t.stride()
+    return t, (t.data_ptr(), batch_s, token_s if tokens > 1 else 0, head_s if heads > 1 else 0)
 
 
 def _lengths(t, batch, what):
@@ -581,7 +586,7 @@ def _attention_args(q, k, v, scale, causal, window, q_lengths, kv_lengths):
     ql, kl = _lengths(q_lengths, batch, "q_lengths"), _lengths(kv_lengths, batch, "kv_lengths")
     shape = AttentionShape(batch, nq, k.shape[1], heads, k.shape[2], dim, DTYPES[q.dtype],
                            dim ** -0.5 if scale is None else float(scale), int(bool(causal)), 0,
-                           0 if window is None else int(window), _ptr(ql), _ptr(kl), hq, hk, hv)
+                           0 if window is None else int(window), _ptr(ql), _ptr(kl), *hq, *hk, *hv)
     return shape, (q, k, v, ql, kl)
 
 
@@ -596,8 +601,8 @@ def attention_forward(q, k, v, scale=None, causal=False, window=None, q_lengths=
     n = _I64(0)
     _check(lib, lib.jorge_attention_workspace(ctypes.byref(shape), None, ctypes.byref(n)))
     ws = _workspace(n.value)
-    out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
+    out = q.new_empty(q.shape)
+    lse = q.new_empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32)
     to = Heads(out.data_ptr(), *out.stride()[:3])
     _check(lib, lib.jorge_attention_forward(ctypes.byref(shape), ctypes.byref(to), lse.data_ptr(), _ptr(ws), n.value,
                                             _stream(q)))
@@ -610,6 +615,7 @@ def attention_backward(dout, q, k, v, out, lse, scale=None, causal=False, window
     lib = load_operators()
     shape, (q, k, v, ql, kl) = _attention_args(q, k, v, scale, causal, window, q_lengths, kv_lengths)
     (dout, hd), (out, ho) = _heads(dout, "dout", q), _heads(out, "out", q)
+    hd, ho = Heads(*hd), Heads(*ho)
     if _cuda(lse, "lse", (torch.float32,)).shape != (q.shape[0], q.shape[2], q.shape[1]) or not lse.is_contiguous():
         raise ValueError("lse: as attention_forward returned it")
     n = _I64(0)
