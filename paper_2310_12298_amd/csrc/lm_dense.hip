@@ -146,11 +146,18 @@ struct Finish {
     __device__ __forceinline__ void store(int64_t row, int64_t c, int left, const float (&z)[M],
                                           const float (&u)[M]) const {
         if (left <= 0) return;
-        float f[M], b[M], r[M];
+        float b[M], r[M];
         if constexpr (!PAIR) {
             bias.template load<M>(c, left, b);
             if (residual) load_some<M>(residual + row * ldr + c, left, r);
         }
+        store<M, PAIR>(row, c, left, z, u, b, r);
+    }
+    // b: the bias, r: the residual (where there is one).
+    template <int M, bool PAIR>
+    __device__ __forceinline__ void store(int64_t row, int64_t c, int left, const float (&z)[M], const float (&u)[M],
+                                          const float (&b)[M], const float (&r)[M]) const {
+        float f[M];
         with_activation(act, [&](auto A) {
 #pragma unroll
             for (int e = 0; e < M; ++e) f[e] = acted<decltype(A)::value, sizeof(T) == 4>(PAIR ? z[e] : z[e] + b[e]).a;
@@ -162,47 +169,108 @@ struct Finish {
     }
 };
 
-// A wave's part of a tile, row by row: 16 rows (tokens) of column j of its accumulators go through LDS, so that a lane
-// gets 8 consecutive columns of a row (8 of both matrices, PAIR) and a row's stores are whole cache lines. The body is
-// in a loop: unrolled over all accumulators, activations would spill them. f(row, column, z, u): of the wave's part.
+// A wave's part of a tile, row by row: the rows (tokens) of four columns j of its accumulators at a time go through LDS,
+// so that a lane gets 8 consecutive columns of a row (8 of both matrices, PAIR) and a row's stores are whole cache lines.
+// The body is in a loop: unrolled over all accumulators, activations would spill them. What a row needs from memory is
+// loaded four passes ahead: a workgroup has its CU to itself, and nothing else would hide that time (dz of 8192 tokens,
+// 2048 -> 2 x 8192: 574 us with every load waited for, 515 so).
 template <int WA, bool PAIR>
 struct Rows {
     static constexpr int kCols = PAIR ? 8 * WA : 16 * WA;          // of a row, of one matrix
-    static constexpr int kLd = 16 * WA + 4;                        // the odd 16 bytes spread 16 rows over all banks
     static constexpr int kLanes = kCols / 8, kPasses = kLanes / 4; // lanes to a row; passes of 64 / kLanes rows
-    static_assert(kPasses >= 1, "a pass takes whole rows");
+    static constexpr int kJ = WA < 4 ? WA : 4, kAll = kJ * kPasses, kAhead = kAll < 4 ? kAll : 4;
+    static_assert(kPasses >= 1 && kAll % kAhead == 0, "a pass takes whole rows");
     float* at;                                                     // this wave's area
+    int c;                                                         // this lane's first column
     __device__ __forceinline__ explicit Rows(char* lds)
-        : at(reinterpret_cast<float*>(lds) + (threadIdx.x >> 6) * 16 * kLd) {}
-    // Where this lane's own accumulators of column j lie: row lane % 16, piece i.
-    __device__ __forceinline__ f32x4* piece(int i) const {
+        : at(reinterpret_cast<float*>(lds) + (threadIdx.x >> 6) * kJ * 256 * WA),
+          c((threadIdx.x & 63) % kLanes * 8) {}
+    // Piece of 4 columns of a row of the jj-th of the columns j; the pieces are permuted so that 16 rows meet all banks.
+    __device__ __forceinline__ f32x4* piece(int jj, int row, int n) const {
+        const int swizzled = n ^ (WA == 2 ? row >> 1 & 7 : row & 15);
+        return reinterpret_cast<f32x4*>(at + (jj * 16 + row) * 16 * WA + swizzled * 4);
+    }
+    // Piece i of this lane's own accumulators, of row lane % 16.
+    __device__ __forceinline__ f32x4* own(int jj, int i) const {
         const int lane = threadIdx.x & 63;
-        const int c = PAIR ? (i / (WA / 2)) * 8 * WA + (lane >> 4) * 2 * WA + 4 * (i % (WA / 2))
-                           : (lane >> 4) * 4 * WA + 4 * i;
-        return reinterpret_cast<f32x4*>(at + (lane & 15) * kLd + c);
+        const int n = PAIR ? i / (WA / 2) * 2 * WA + (lane >> 4) * (WA / 2) + i % (WA / 2) : (lane >> 4) * WA + i;
+        return piece(jj, lane & 15, n);
     }
     static __device__ __forceinline__ void fence() {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     }
-    template <typename ACC, typename F>
-    __device__ __forceinline__ void each(const ACC& acc, int j, F&& f) const {
-        fence();
+    __device__ __forceinline__ void put(int jj, int row, const float (&z)[8], const float (&u)[8]) const {
 #pragma unroll
-        for (int i = 0; i < WA; ++i) *piece(i) = acc[i][j];
-        fence();
-        const int lane = threadIdx.x & 63;
-#pragma unroll 1
-        for (int pass = 0; pass < kPasses; ++pass) {
-            const int row = pass * (64 / kLanes) + lane / kLanes, c = lane % kLanes * 8;
-            float z[8], u[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                z[e] = at[row * kLd + c + e];
-                u[e] = PAIR ? at[row * kLd + kCols + c + e] : 0.0f;
-            }
-            f(row, c, z, u);
+        for (int n = 0; n < 2; ++n) {
+            *piece(jj, row, c / 4 + n) = f32x4{z[4 * n], z[4 * n + 1], z[4 * n + 2], z[4 * n + 3]};
+            if constexpr (PAIR)
+                *piece(jj, row, (kCols + c) / 4 + n) = f32x4{u[4 * n], u[4 * n + 1], u[4 * n + 2], u[4 * n + 3]};
         }
+    }
+    // load(row, j): what row `row` of column j needs, started ahead; use(jj, row, j, z, u, that): its values. again: what
+    // use() has put back is wanted in the accumulators.
+    template <typename ACC, typename LOAD, typename USE>
+    __device__ __forceinline__ void each(ACC& acc, bool again, LOAD&& load, USE&& use) const {
+#pragma unroll
+        for (int j0 = 0; j0 < WA; j0 += kJ) {
+            decltype(load(0, 0)) ahead[kAhead];
+            const int lane_row = (threadIdx.x & 63) / kLanes;
+            const auto row_of = [&](int pass) { return pass % kPasses * (64 / kLanes) + lane_row; };
+#pragma unroll
+            for (int n = 0; n < kAhead; ++n) ahead[n] = load(row_of(n), j0 + n / kPasses);
+            fence();
+#pragma unroll
+            for (int jj = 0; jj < kJ; ++jj)
+#pragma unroll
+                for (int i = 0; i < WA; ++i) *own(jj, i) = acc[i][j0 + jj];
+            fence();
+#pragma unroll 1
+            for (int pass = 0; pass < kAll; pass += kAhead)
+#pragma unroll
+                for (int n = 0; n < kAhead; ++n) {
+                    const int jj = (pass + n) / kPasses, row = row_of(pass + n);
+                    float z[8], u[8];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const f32x4 a = *piece(jj, row, c / 4 + k);
+                        const f32x4 b = PAIR ? *piece(jj, row, (kCols + c) / 4 + k) : a;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            z[4 * k + e] = a[e];
+                            u[4 * k + e] = b[e];
+                        }
+                    }
+                    const auto now = ahead[n];
+                    if (pass + kAhead < kAll) ahead[n] = load(row_of(pass + kAhead + n), j0 + (pass + kAhead + n) / kPasses);
+                    use(jj, row, j0 + jj, z, u, now);
+                }
+            if (again) {
+                fence();
+#pragma unroll
+                for (int jj = 0; jj < kJ; ++jj)
+#pragma unroll
+                    for (int i = 0; i < WA; ++i) acc[i][j0 + jj] = *own(jj, i);
+            }
+        }
+    }
+};
+struct Nothing {};
+
+// 8 elements of a row as they lie, of which `left` exist.
+template <typename T>
+struct Raw {
+    typedef T V __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    V v;
+    __device__ __forceinline__ void load(const T* p, int left) {
+        if (left >= 8) v = *reinterpret_cast<const V*>(p);
+        else
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = e < left ? p[e] : (T)0.0f;
+    }
+    __device__ __forceinline__ void get(float (&f)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = (float)v[e];
     }
 };
 
@@ -253,11 +321,22 @@ __global__ __launch_bounds__(256, 1) void dense_forward_kernel(Dense d, Finish<T
     const Rows<WA, PAIR> rows(lds);
     const int64_t wa = (int64_t)at.a * Q::kRowsA + (threadIdx.x >> 7) * (Q::kRowsA / 2);
     const int64_t wb = (int64_t)at.b * Q::kB + ((threadIdx.x >> 6) & 1) * (Q::kB / 2);
-#pragma unroll
-    for (int j = 0; j < WA; ++j)
-        rows.each(t.acc, j, [&](int row, int c, const float(&z)[8], const float(&u)[8]) {
+    const int n = left_of<8>(d.p.A.rows - wa - rows.c);  // of this lane's columns
+    float bias[8] = {};
+    if constexpr (!PAIR) out.bias.template load<8>(wa + rows.c, n, bias);
+    rows.each(
+        t.acc, false,
+        [&](int row, int j) {
+            Raw<T> r{};
             const int64_t token = wb + row * WA + j;
-            if (token < d.p.B.rows) out.template store<8, PAIR>(token, wa + c, left_of<8>(d.p.A.rows - wa - c), z, u);
+            if (!PAIR && out.residual && n && token < d.p.B.rows) r.load(out.residual + token * out.ldr + wa + rows.c, n);
+            return r;
+        },
+        [&](int, int row, int j, const float(&z)[8], const float(&u)[8], const Raw<T>& raw) {
+            const int64_t token = wb + row * WA + j;
+            float r[8];
+            raw.get(r);
+            if (n && token < d.p.B.rows) out.template store<8, PAIR>(token, wa + rows.c, n, z, u, bias, r);
         });
 }
 
@@ -419,14 +498,22 @@ __global__ __launch_bounds__(256, 1) void dense_dz_kernel(Dense d, const T* __re
     const Rows<WA, PAIR> rows(lds);
     const int64_t wa = (int64_t)at.a * Q::kRowsA + (threadIdx.x >> 7) * (Q::kRowsA / 2);
     const int64_t wb = (int64_t)at.b * Q::kB + ((threadIdx.x >> 6) & 1) * (Q::kB / 2);
-#pragma unroll
-    for (int j = 0; j < WA; ++j) {
-        rows.each(t.acc, j, [&](int row, int c, float(&z)[8], float(&u)[8]) {
+    const int cols = left_of<8>(outs - wa - rows.c);     // of this lane's columns, how many exist
+    float b[8] = {};
+    if constexpr (!PAIR) bias.template load<8>(wa + rows.c, cols, b);
+    rows.each(
+        t.acc, again,
+        [&](int row, int j) {
+            Raw<T> r{};
             const int64_t token = wb + row * WA + j;
-            const int n = token < tokens ? left_of<8>(outs - wa - c) : 0;
-            float b[8] = {}, g[8] = {};
-            if constexpr (!PAIR) bias.template load<8>(wa + c, n, b);
-            if (n) load_some<8>(dy + token * ldy + wa + c, n, g);
+            if (cols && token < tokens) r.load(dy + token * ldy + wa + rows.c, cols);
+            return r;
+        },
+        [&](int jj, int row, int j, float(&z)[8], float(&u)[8], const Raw<T>& raw) {
+            const int64_t token = wb + row * WA + j;
+            const int n = token < tokens ? cols : 0;
+            float g[8];
+            raw.get(g);
             with_activation(act, [&](auto A) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -436,24 +523,13 @@ __global__ __launch_bounds__(256, 1) void dense_dz_kernel(Dense d, const T* __re
                     u[e] = e < n ? g[e] * f.a : 0.0f;
                 }
             });
-            float* const back = rows.at + row * rows.kLd + c;
-            if (again)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    back[e] = z[e];
-                    if constexpr (PAIR) back[rows.kCols + e] = u[e];
-                }
-            if (out.dz && token < tokens && wa + c < out.kf) {
-                bf16* const dz = out.dz + token * terms * MATS * out.kf + wa + c;
+            if (again) rows.put(jj, row, z, u);
+            if (out.dz && token < tokens && wa + rows.c < out.kf) {
+                bf16* const dz = out.dz + token * terms * MATS * out.kf + wa + rows.c;
                 store_terms<terms>(dz, MATS * out.kf, z);
                 if constexpr (PAIR) store_terms<terms>(dz + out.kf, MATS * out.kf, u);
             }
         });
-        Rows<WA, PAIR>::fence();
-        if (again)
-#pragma unroll
-            for (int i = 0; i < WA; ++i) t.acc[i][j] = *rows.piece(i);
-    }
     if (!PAIR && out.bias) {
         const int64_t part = b0 / (16 * WA);
 #pragma unroll
@@ -534,13 +610,13 @@ __global__ __launch_bounds__(256, 1) void dense_grad_kernel(Product p, Target<T>
         return;
     }
     const Rows<WA, false> rows(lds);
-#pragma unroll
-    for (int j = 0; j < WA; ++j)
-        rows.each(t.acc, j, [&](int row, int c, const float(&z)[8], const float(&)[8]) {
+    const int n = left_of<8>(p.A.rows - wa - rows.c);
+    rows.each(
+        t.acc, false, [](int, int) { return Nothing(); },
+        [&](int, int row, int j, const float(&z)[8], const float(&)[8], Nothing) {
             const int64_t b = wb + Q::part_b(row, j);
-            const int n = left_of<8>(p.A.rows - wa - c);
             T* const to = b < p.B.rows ? out.row(b) : nullptr;
-            if (to && n) store_some<8>(to + wa + c, n, z);
+            if (to && n) store_some<8>(to + wa + rows.c, n, z);
         });
 }
 
