@@ -231,8 +231,8 @@ jorge_status jorge_gated_linear_backward(const jorge_linear_shape* shape, const 
  * sequence; with causal, query i stands at position kv length - q length + i and sees the keys up to its own position,
  * with a window of w > 0 the last w of those. A query that sees nothing, or that is past its sequence's length, has
  * o = 0, lse = minus infinity and no part in any gradient, whatever it holds; so has a key past its sequence's length,
- * whose rows of k and v may hold anything. A value that is not finite in a key that a query may not see can reach the
- * query if both are near the edge of the mask (in the same 64 keys): 0 times it is NaN.
+ * whose rows of k and v may hold anything. What a key holds reaches no query that does not see it, and what a query or
+ * its gradient holds no key that the query does not see, infinities and NaN among it.
  * Gradients, from the o and lse of the forward pass, with p = exp(z - lse):
  *   delta = do . o,  ds = scale p (do v^T - delta),  dq = ds k,  dk = ds^T q,  dv = p^T do,
  * dk and dv summed over the heads that share them. bfloat16: p and ds are rounded to bfloat16 for their products, all

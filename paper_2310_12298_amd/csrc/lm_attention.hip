@@ -113,6 +113,14 @@ __device__ __forceinline__ s16x4 read_turned4(const lds_s16x4* __restrict__ p) {
     return __builtin_amdgcn_ds_read_tr16_b64_v4i16(const_cast<lds_s16x4*>(p));
 }
 
+template <int N>
+__device__ __forceinline__ void clear(f32x16 (&acc)[N]) {
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[n][r] = 0.0f;
+}
+
 // Rows of D elements (32, 64, 96 or 128).
 template <typename T, int D>
 struct Tile {
@@ -272,6 +280,15 @@ struct Tile {
                                                                       0);
                 }
             }
+            // The reads run 4 products ahead.
+            constexpr int kAhead = 4;
+            __builtin_amdgcn_sched_group_barrier(0x100, 2 * kAhead, 0);
+#pragma unroll
+            for (int i = 0; i < 2 * kDims - kAhead; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
         } else {
 #pragma unroll
             for (int g = 0; g < 4; ++g)
@@ -292,6 +309,54 @@ struct Tile {
             }
             __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
         }
+    }
+
+    // Whether a lane's column holds a NaN (both lanes of it know).
+    static __device__ __forceinline__ bool spoilt(const f32x16 (&acc)[kDims]) {
+        bool found = false;
+#pragma unroll
+        for (int db = 0; db < kDims; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) found |= acc[db][r] != acc[db][r];
+        return found | (bool)__shfl_xor((int)found, 32);
+    }
+    // A sum that cols() forms, formed again without the rows that a lane does not see: acc = sum of weight(i) times row i
+    // of x over the lane's own i of [first, last), element by element. 0 times an infinity or a NaN is a NaN, so a row
+    // with one among those of a tile at a mask's edge spoils the sums of the columns that do not see it. Called after all
+    // tiles, for columns with a NaN in their sum that nothing of their own explains. `again`: acc is added to.
+    template <typename W>
+    static __device__ __forceinline__ void add_seen(f32x16 (&acc)[kDims], bool again, const char* x, int64_t stride,
+                                                    int first, int last, int dim, W&& weight) {
+        typedef T V __attribute__((ext_vector_type(4)));
+        const int half = (threadIdx.x & 63) >> 5;
+        if (!again) clear(acc);
+#pragma unroll 1
+        for (int i = first; i < last; ++i) {
+            const float w = weight(i);
+            const T* const row = reinterpret_cast<const T*>(x + i * stride);
+#pragma unroll
+            for (int db = 0; db < kDims; ++db)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int at = db * 32 + g * 8 + half * 4;
+                    if (at >= dim) continue;
+                    const V v = *reinterpret_cast<const V*>(row + at);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[db][4 * g + e] = __builtin_fmaf(w, (float)v[e], acc[db][4 * g + e]);
+                }
+        }
+    }
+    // The product of two rows, by the two lanes that share a column.
+    static __device__ __forceinline__ float dot(const char* a, const char* b, int dim) {
+        typedef T V __attribute__((ext_vector_type(4)));
+        float s = 0.0f;
+#pragma unroll 1
+        for (int at = ((threadIdx.x & 63) >> 5) * 4; at < dim; at += 8) {
+            const V x = reinterpret_cast<const V*>(a)[at / 4], y = reinterpret_cast<const V*>(b)[at / 4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s = __builtin_fmaf((float)x[e], (float)y[e], s);
+        }
+        return s + __shfl_xor(s, 32);
     }
 
     // Row n's elements of acc times f, to a row of T or of floats; zeros for a row that has no part in anything, whose
@@ -328,14 +393,6 @@ __device__ __forceinline__ void wait_loads() {
 }
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-template <int N>
-__device__ __forceinline__ void clear(f32x16 (&acc)[N]) {
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) acc[n][r] = 0.0f;
-}
-
 // Tiles [t0, t1) of a range of streamed rows [lo, hi) cut into `of` parts, the y-th.
 struct Span {
     int lo, hi, t0, t1;
@@ -344,6 +401,9 @@ struct Span {
         t0 = a + (int)((int64_t)n * y / of);
         t1 = a + (int)((int64_t)n * (y + 1) / of);
     }
+    // The part's rows of a lane's [first, last).
+    __device__ __forceinline__ int from(int first, int rows) const { return max(first, t0 * rows); }
+    __device__ __forceinline__ int to(int last, int rows) const { return min(last, t1 * rows); }
 };
 
 __device__ __forceinline__ void barrier() {
@@ -433,28 +493,34 @@ struct Softmax {
 #pragma unroll
             for (int r = 0; r < 16; ++r) top = fmaxf(top, s[kb][r]);
         top = fmaxf(top, __shfl_xor(top, 32)) * c.scale2;
-        if (__any(top > base + kRoom || (base == -INFINITY && top > base))) {
-            const float to = fmaxf(base, top), f = to == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(base - to);
-            base = to;
+        const bool higher = top > base + kRoom || (base == -INFINITY && top > base);
+        if (__any(higher)) {
+            // For the columns that need it alone: a row's result does not depend on the others of its wave.
+            const float f = higher ? __builtin_amdgcn_exp2f(base - top) : 1.0f;
+            base = higher ? top : base;
             sum *= f;
 #pragma unroll
             for (int db = 0; db < TILE::kDims; ++db)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[db][r] *= f;
         }
-        const float at = base == -INFINITY ? 0.0f : base;
         float add = 0.0f;
 #pragma unroll
         for (int kb = 0; kb < TILE::kBlocks; ++kb)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                float z = __builtin_fmaf(s[kb][r], c.scale2, -at);
-                // A masked score stays at minus infinity, whatever the low part's sign.
-                if constexpr (sizeof(T) == 4) z = s[kb][r] == -INFINITY ? z : __builtin_fmaf(s[kb][r], c.scale2_low, z);
-                s[kb][r] = __builtin_amdgcn_exp2f(z);
+                s[kb][r] = weight<T>(c, s[kb][r]);
                 add += s[kb][r];
             }
         sum += add;
+    }
+    // A score's exponential, relative to the reference.
+    template <typename T>
+    __device__ __forceinline__ float weight(const Call& c, float s) const {
+        float z = __builtin_fmaf(s, c.scale2, base == -INFINITY ? 0.0f : -base);
+        // A masked score stays at minus infinity, whatever the low part's sign.
+        if constexpr (sizeof(T) == 4) z = s == -INFINITY ? z : __builtin_fmaf(s, c.scale2_low, z);
+        return __builtin_amdgcn_exp2f(z);
     }
 };
 
@@ -494,7 +560,8 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(Call c, Heads
     const Span span(s.lo(c, first), first < s.nq ? s.hi(c, last) : 0, L::kRows, blockIdx.y, gridDim.y);
     const L tile;
     typename L::Own own;
-    own.load(q.p + b * q.batch + row.token * q.token + row.head * q.head, row.there, c.dim);
+    const char* const qp = q.p + b * q.batch + row.token * q.token + row.head * q.head;
+    own.load(qp, row.there, c.dim);
     const Two<L> fetch{{k.p + b * k.batch + hk * k.head, k.token, c.dim, wave},
                        {v.p + b * v.batch + hk * v.head, v.token, c.dim, wave}, span.lo, span.hi, wave};
     Softmax<L> soft;
@@ -509,6 +576,13 @@ __global__ __launch_bounds__(256, 2) void attention_forward_kernel(Call c, Heads
         for (int kb = 0; kb < L::kBlocks; ++kb) tile.cols(vt, kb, z[kb], soft.acc);
     });
     if (!row.there) return;
+    if (L::spoilt(soft.acc) && soft.sum == soft.sum) {
+        const char* const kp = k.p + b * k.batch + hk * k.head;
+        L::add_seen(soft.acc, false, v.p + b * v.batch + hk * v.head, v.token, span.from(lo, L::kRows),
+                    span.to(hi, L::kRows), c.dim, [&](int i) {
+                        return soft.template weight<T>(c, L::dot(qp, kp + i * k.token, c.dim));
+                    });
+    }
     const float sum = soft.sum + __shfl_xor(soft.sum, 32);
     // A row that sees nothing is zero, its log sum exp minus infinity.
     const float f = hi > lo && soft.base != -INFINITY ? 1.0f / sum : hi > lo && sum != sum ? sum : 0.0f;
@@ -541,7 +615,8 @@ __global__ __launch_bounds__(256, 1) void attention_few_kernel(Call c, Heads q, 
     const Span span(s.lo(c, 0), s.hi(c, min((kOwn - 1) / c.group, s.nq - 1)), L::kRows, blockIdx.y, gridDim.y);
     const L tile;
     typename L::Own own;
-    own.load(q.p + b * q.batch + row.token * q.token + row.head * q.head, row.there, c.dim);
+    const char* const qp = q.p + b * q.batch + row.token * q.token + row.head * q.head;
+    own.load(qp, row.there, c.dim);
     const typename L::template Loader<1> lk(k.p + b * k.batch + hk * k.head, k.token, c.dim, 0);
     const typename L::template Loader<1> lv(v.p + b * v.batch + hk * v.head, v.token, c.dim, 0);
     char *const kt = lds + wave * 2 * L::kBytes, *const vt = kt + L::kBytes;
@@ -560,7 +635,8 @@ __global__ __launch_bounds__(256, 1) void attention_few_kernel(Call c, Heads q, 
         for (int kb = 0; kb < L::kBlocks; ++kb) z[kb] = tile.rows(kt, kb, own);
         wait_lds();
         lk.load(next, span.lo, span.hi, kt, 0);
-        soft.template tile<T>(c, z, t * L::kRows, lo, hi);
+        const int k0 = t * L::kRows;
+        soft.template tile<T>(c, z, k0, lo, hi);
         wait_loads<L::kLoads>();
 #pragma unroll
         for (int kb = 0; kb < L::kBlocks; ++kb) tile.cols(vt, kb, z[kb], soft.acc);
@@ -568,6 +644,15 @@ __global__ __launch_bounds__(256, 1) void attention_few_kernel(Call c, Heads q, 
         lv.load(next, span.lo, span.hi, vt, 0);
     }
     wait_loads<0>();
+    if (L::spoilt(soft.acc) && soft.sum == soft.sum && row.there) {
+        const char* const kp = k.p + b * k.batch + hk * k.head;
+        clear(soft.acc);
+        for (int n = span.t0 + wave; n < span.t1; n += 4)
+            L::add_seen(soft.acc, true, v.p + b * v.batch + hk * v.head, v.token, max(lo, n * L::kRows),
+                        min(hi, (n + 1) * L::kRows), c.dim, [&](int i) {
+                            return soft.template weight<T>(c, L::dot(qp, kp + i * k.token, c.dim));
+                        });
+    }
     __syncthreads();
     // The waves' references, sums and outputs: [wave][row], [wave][row][D + 4].
     float* const refs = reinterpret_cast<float*>(lds);
@@ -647,6 +732,13 @@ __global__ __launch_bounds__(256) void attention_join_kernel(Call c, Output out,
 }
 
 // ---------------------------------------------------------------- backward
+// A row's log2 sum exp for dk and dv. A row whose q or gradient is not finite has a lse or a delta that is not: it counts
+// as a NaN, which attention_dkv_kernel goes by.
+__device__ __forceinline__ float stat_of(float lse, float delta) {
+    const float x = lse * kLog2e;
+    return __builtin_fabsf(x) < INFINITY && __builtin_fabsf(delta) < INFINITY ? x : __builtin_nanf("");
+}
+
 // [batch][head][token]: the row's log2 sum exp (plus infinity where it sees nothing, so that every probability is 0) and
 // delta = do . o. Two lanes to a row, which add it up as attention_dq_kernel does where that forms it: dk and dv are the
 // same to the bit with and without dq.
@@ -679,7 +771,7 @@ __global__ __launch_bounds__(256) void attention_delta_kernel(Call c, Heads o, H
         }
     sum += __shfl_xor(sum, 1);
     if (threadIdx.x & 1) return;
-    lse2[at] = seen ? lse[at] * kLog2e : INFINITY;
+    lse2[at] = seen ? stat_of(lse[at], sum) : INFINITY;
     delta[at] = seen ? sum : 0.0f;
 }
 
@@ -714,9 +806,11 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(Call c, Heads q, H
     const Span span(s.lo(c, first), first < s.nq ? s.hi(c, last) : 0, L::kRows, blockIdx.y, gridDim.y);
     const L tile;
     typename L::Own own, grad;
-    own.load(q.p + b * q.batch + row.token * q.token + row.head * q.head, row.there, c.dim);
+    const char* const qp = q.p + b * q.batch + row.token * q.token + row.head * q.head;
+    const char* const gp = g.p + b * g.batch + row.token * g.token + row.head * g.head;
+    own.load(qp, row.there, c.dim);
     // A row that sees nothing has no part in anything, whatever its gradient is.
-    grad.load(g.p + b * g.batch + row.token * g.token + row.head * g.head, row.there && hi > lo, c.dim);
+    grad.load(gp, row.there && hi > lo, c.dim);
     const Two<L> fetch{{k.p + b * k.batch + hk * k.head, k.token, c.dim, wave},
                        {v.p + b * v.batch + hk * v.head, v.token, c.dim, wave}, span.lo, span.hi, wave};
     const int64_t stat = ((int64_t)b * c.heads + row.head) * c.q_tokens + row.token;
@@ -732,7 +826,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(Call c, Heads q, H
         de += __shfl_xor(de, 32);
         if (row.there && hi > lo) l2 = stats.lse[stat] * kLog2e;
         if (row.there && lane < 32 && blockIdx.y == 0) {
-            stats.lse2[stat] = l2;
+            stats.lse2[stat] = hi > lo ? stat_of(stats.lse[stat], de) : INFINITY;
             stats.delta[stat] = de;
         }
     } else if (row.there) {
@@ -745,7 +839,7 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(Call c, Heads q, H
         const int k0 = t * L::kRows;
         const char* const vt = kt + L::kBytes;
         if (!__any(k0 < hi && k0 + L::kRows > lo)) return;
-        const bool masked = __any(k0 < lo || k0 + L::kRows > hi);
+        const bool edge = __any(k0 < lo || k0 + L::kRows > hi);
 #pragma unroll
         for (int kb = 0; kb < L::kBlocks; ++kb) {
             f32x16 z = tile.rows(kt, kb, own);
@@ -753,16 +847,24 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(Call c, Heads q, H
 #pragma unroll
             for (int i = 0; i < 16; ++i) z[i] = probability<T>(c, z[i], l2) * (dp[i] - de);
             L::order();
-            if (masked)
+            if (edge) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int key = k0 + kb * 32 + row_of(i);
                     z[i] = key >= lo && key < hi ? z[i] : 0.0f;
                 }
+            }
             tile.cols(kt, kb, z, acc);
         }
     });
     if (!row.there) return;
+    if (L::spoilt(acc) && l2 == l2 && de == de) {
+        const char *const kp = k.p + b * k.batch + hk * k.head, *const vp = v.p + b * v.batch + hk * v.head;
+        L::add_seen(acc, false, kp, k.token, span.from(lo, L::kRows), span.to(hi, L::kRows), c.dim, [&](int i) {
+            const float p = probability<T>(c, L::dot(qp, kp + i * k.token, c.dim), l2);
+            return p * (L::dot(gp, vp + i * v.token, c.dim) - de);
+        });
+    }
     if (dq.part) {
         const int64_t rows = (int64_t)c.q_tokens * c.group;
         L::store(acc, dq.part + (((int64_t)blockIdx.y * c.batch * c.kv_heads + at.bh) * rows + r) * D, D, c.scale,
@@ -771,6 +873,25 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(Call c, Heads q, H
     }
     L::store(acc, reinterpret_cast<T*>(dq.g.p + b * dq.g.batch + row.token * dq.g.token + row.head * dq.g.head), c.dim,
              c.scale, hi > lo);
+}
+
+// Zeros in the place of the rows of a stage whose log2 sum exp is a NaN, in q's and the gradient's tile: 0 times an infinity
+// or a NaN is a NaN, which must not reach a key that does not see the row; p of one that does is a NaN by itself. Every
+// wave that uses the stage at a mask's edge writes the same zeros before it reads.
+template <typename TILE>
+__device__ __forceinline__ void without_spoilt_rows(char* stage) {
+    const int lane = threadIdx.x & 63;
+    const float* const stats = reinterpret_cast<const float*>(stage + 2 * TILE::kBytes);
+    const float mine = lane < TILE::kRows ? stats[lane] : 0.0f;
+    uint64_t bad = __ballot(mine != mine);
+    while (bad) {
+        const int row = __builtin_ctzll(bad);
+        bad &= bad - 1;
+        for (int at = lane * 4; at < 2 * TILE::kRow; at += 256) {
+            const int tile = at >= TILE::kRow;
+            *reinterpret_cast<float*>(stage + tile * TILE::kBytes + row * TILE::kRow + at - tile * TILE::kRow) = 0.0f;
+        }
+    }
 }
 
 // Two waves to a SIMD where their registers allow it (a wave's k, v and sums of dk and dv take D of them for every four
@@ -809,7 +930,8 @@ __global__ __launch_bounds__(256, D <= (sizeof(T) == 2 ? 96 : 64) ? 2 : 1) void 
             const int t0 = t * L::kRows;
             const char *const gt = qt + L::kBytes, *const st = gt + L::kBytes;
             if (!__any(t0 < hi && t0 + L::kRows > lo)) return;
-            const bool masked = __any(t0 < lo || t0 + L::kRows > hi);
+            const bool edge = __any(t0 < lo || t0 + L::kRows > hi);
+            if (edge) without_spoilt_rows<L>(const_cast<char*>(qt));
 #pragma unroll
             for (int kb = 0; kb < L::kBlocks; ++kb) {
                 f32x16 z = tile.rows(qt, kb, own), dp = tile.rows(gt, kb, val);
@@ -824,7 +946,7 @@ __global__ __launch_bounds__(256, D <= (sizeof(T) == 2 ? 96 : 64) ? 2 : 1) void 
                     }
                 }
                 L::order();
-                if (masked)
+                if (edge) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int row = t0 + kb * 32 + row_of(i);
@@ -832,6 +954,7 @@ __global__ __launch_bounds__(256, D <= (sizeof(T) == 2 ? 96 : 64) ? 2 : 1) void 
                         z[i] = seen ? z[i] : 0.0f;
                         dp[i] = seen ? dp[i] : 0.0f;
                     }
+                }
                 tile.cols(gt, kb, z, av);
                 tile.cols(qt, kb, dp, ak);
             }

@@ -221,6 +221,48 @@ def test_what_stands_past_the_lengths_reaches_nothing(tq, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("d", [24, 64, 96, 128])
+@pytest.mark.parametrize("tq,window", [(3, None), (150, None), (150, 40), (400, 70)])
+def test_nan_and_infinity_where_they_are_not_seen(tq, window, d, dtype):
+    """Keys of the future, keys before the window, and gradients and queries of rows that do not see a key, in the same
+    tile as those that do."""
+    tk, how = 400, dict(causal=True, window=window)
+    q, k, v, dout = inputs(1, tq, tk, 4, 2, d, dtype)
+    off, first = tk - tq, tk - tq + 1 + tq // 3                # the first key of the future for the rows before `rows`
+    rows = first - off
+    want = plain(q, k, v, dout, **how)
+    clean = lm.attention_forward(q, k, v, **how)
+    grads = lm.attention_backward(dout, q, k, v, *clean, **how)
+
+    def close(got, name, at):
+        within(got[at], want[name][at], want[name + "_off"][at] / U32, 1, name)
+    for bad in (float("nan"), INF, -INF):
+        K, V = k.clone(), v.clone()
+        K[:, first:, 0, 0], V[:, first:, 1, -1] = bad, bad
+        gone = max(0, off - (window or tk))                    # keys that no query sees any more
+        K[:, :gone], V[:, :gone] = bad, bad
+        for a, b in ((K, v), (k, V), (K, V)):
+            out, lse = lm.attention_forward(q, a, b, **how)
+            assert torch.equal(lse[:, :, :rows], clean[1][:, :, :rows])
+            close(out, "out", (slice(None), slice(0, rows)))
+            dq = lm.attention_backward(dout, q, a, b, out, lse, need_kv=False, **how)[0]
+            close(dq, "dq", (slice(None), slice(0, rows)))
+        if not bool(torch.isfinite(torch.tensor(bad))) and rows < tq and V is not v:
+            assert not bool(torch.isfinite(out[:, rows:].float()).all())
+        Q, G = q.clone(), dout.clone()
+        Q[:, :rows, 1], G[:, :rows, 2, 0] = bad, bad           # the rows before `rows` do not see the keys from `first` on
+        for a, b in ((Q, dout), (q, G), (Q, G)):
+            out, lse = lm.attention_forward(a, k, v, **how)
+            for got, ref in zip(lm.attention_backward(b, a, k, v, out, lse, **how)[1:], grads[1:]):
+                assert torch.equal(got[:, first:], ref[:, first:])
+            for got, ref in zip(lm.attention_backward(b, a, k, v, out, lse, need_q=False, **how)[1:], grads[1:]):
+                assert torch.equal(got[:, first:], ref[:, first:])
+        seen = max(0, off + rows - (window or tk))             # a key that the last of them sees
+        _, dk, dv = lm.attention_backward(G, q, k, v, *clean, **how)
+        assert not bool(torch.isfinite(dv[0, max(seen, first - 1), 1].float()).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("tq", [2, 200])
 def test_nan_and_infinity_where_they_are_seen(tq, dtype):
     q, k, v, dout = inputs(1, tq, 200, 2, 2, 64, dtype)
