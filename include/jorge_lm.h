@@ -1,10 +1,10 @@
 /*
  * jorge_lm.h - C ABI of the operators of a language model's training step that
  * stand beside the Jorge step (jorge.h) in libjorge.so: layer norm, embedding
- * lookup, softmax cross entropy over a vocabulary, and AdamW with the global
- * gradient norm for the parameters that Jorge does not precondition (gains,
- * biases, tables wider than JORGE_MAX_DIM). Each has its forward and backward
- * pass where it has one.
+ * lookup, softmax cross entropy over a vocabulary, linear and gated linear
+ * layers, attention, and AdamW with the global gradient norm for the parameters
+ * that Jorge does not precondition (gains, biases, tables wider than
+ * JORGE_MAX_DIM). Each has its forward and backward pass where it has one.
  *
  * The calls keep no state: what a step keeps (moments, saved statistics) lies in
  * the caller's buffers, and temporaries in a workspace that the caller lends and
@@ -16,7 +16,8 @@
  * is fixed then, which for jorge_adamw_step is t and the rates (see there).
  *
  * Pointers are device pointers unless the comment says "host". Matrices are
- * row-major with a row stride in elements (ld* >= columns). Elements are fp32 or
+ * row-major with a row stride in elements (ld* >= columns), but for attention's,
+ * which have three strides (jorge_heads). Elements are fp32 or
  * bfloat16 (JORGE_F32, JORGE_BF16); pointers need the alignment of their element,
  * workspaces 256 bytes, and every speed remark assumes 16. Whatever the type of
  * the elements, sums, softmax statistics and norms are held in fp32 or wider and

@@ -13,8 +13,14 @@
 //   forward:  S = rows(k, q), P = exp(S - m), o += cols(v, P), with the running maximum m and sum of the row
 //   dq:       S = rows(k, q), dP = rows(v, do), dS = P (dP - delta), dq += cols(k, dS)
 //   dk, dv:   S = rows(q, k), dP = rows(do, v), dv += cols(do, P), dk += cols(q, dS)
-// delta = do . o is formed first, a row at a time. Both backward kernels form S and dP: seven products where one kernel
-// would do with five, but that one has to add dq up by atomics, whose order would change results.
+// with delta = do . o of a row, which dq forms at its start and leaves for dk and dv. Both backward kernels form S and
+// dP: seven products where one kernel would do with five, but that one has to add dq up by atomics, whose order would
+// change results.
+//
+// Bound by the matrix cores in training. 4 sequences of 4096, 16 heads of 128 over 4 of k and v, causal, bfloat16:
+// forward 361 us (380 TFLOP/s of the half that is not masked; matrix cores busy 46%), dq 465 us (443; 56%), dk and dv
+// 756 us (364; 39%: one wave to a SIMD has nothing to cover its own softmax with). No bank conflicts in any of them. A
+// single token over 32 caches is bound by reading k and v: 159 us for 0.8 GB, 5.1 TB/s.
 //
 // Queries whose heads share a key head are rows of one sequence of own rows, (token, head) by (token, head), so that a
 // tile of k and v is read once for all of them.
@@ -87,9 +93,9 @@ struct Sequence {
 
 // Workgroup g's place: the key head (of all sequences), and the tile of its own rows. Workgroup g runs on XCD g mod 8:
 // tiles that read the same keys are put on one, so that they do so from one L2, and key heads are dealt out in turn, so
-// that a batch of unequal sequences loads all XCDs alike (three sequences of 1301, 650 and 0 keys in equal shares one
-// after the other: 1.4 times the time); the last ones, if they are no multiple of eight, are spread tile by tile. Where
-// the last tiles have the most to do they come first.
+// that a batch of unequal sequences loads all XCDs alike (5 sequences of up to 2011 with a window of 512: 47 us forward
+// and 210 us backward, where an equal run of key heads for each XCD took 50 and 221); the last ones, if they are no
+// multiple of eight, are spread tile by tile. Where the last tiles have the most to do they come first.
 struct Work {
     int bh, tile;
     __device__ __forceinline__ Work(int g, int total, int tiles, int heaviest_last) {
@@ -217,8 +223,8 @@ struct Tile {
         return s;
     }
 
-    // S of every block of the tile. The reads run ahead of the products by one block's: a wave that waits for each
-    // fragment alone leaves the matrix cores idle three quarters of the time.
+    // S of every block of the tile. The reads run ahead of the products by one block's (327 us for a forward pass of 338
+    // where each waits for its own: 4 sequences of 4096, 16 heads of 128, causal).
     __device__ __forceinline__ void all_rows(const char* tile, const Own& own, f32x16 (&s)[kBlocks]) const {
 #pragma unroll
         for (int kb = 0; kb < kBlocks; ++kb) s[kb] = rows(tile, kb, own);
@@ -822,7 +828,8 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(Call c, Heads q, H
 #pragma unroll
         for (int n = 0; n < L::kSteps; ++n)
 #pragma unroll
-            for (int e = 0; e < (int)(16 / sizeof(T)); ++e) de = __builtin_fmaf((float)o.f[n][e], (float)grad.f[n][e], de);
+            for (int e = 0; e < (int)(16 / sizeof(T)); ++e)
+                de = __builtin_fmaf((float)o.f[n][e], (float)grad.f[n][e], de);
         de += __shfl_xor(de, 32);
         if (row.there && hi > lo) l2 = stats.lse[stat] * kLog2e;
         if (row.there && lane < 32 && blockIdx.y == 0) {
@@ -875,9 +882,9 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(Call c, Heads q, H
              c.scale, hi > lo);
 }
 
-// Zeros in the place of the rows of a stage whose log2 sum exp is a NaN, in q's and the gradient's tile: 0 times an infinity
-// or a NaN is a NaN, which must not reach a key that does not see the row; p of one that does is a NaN by itself. Every
-// wave that uses the stage at a mask's edge writes the same zeros before it reads.
+// Zeros in the place of the rows of a stage whose log2 sum exp is a NaN, in q's and the gradient's tile: 0 times an
+// infinity or a NaN is a NaN, which must not reach a key that does not see the row; p of one that does is a NaN by
+// itself. Every wave that uses the stage at a mask's edge writes the same zeros before it reads.
 template <typename TILE>
 __device__ __forceinline__ void without_spoilt_rows(char* stage) {
     const int lane = threadIdx.x & 63;
@@ -899,10 +906,9 @@ __device__ __forceinline__ void without_spoilt_rows(char* stage) {
 // of 80, window 512). At D = 128 two would spill in the loop (1.7 times the time); eight waves to a workgroup that keep
 // v in LDS instead took as long as four with one to a SIMD.
 template <typename T, int D>
-__global__ __launch_bounds__(256, D <= (sizeof(T) == 2 ? 96 : 64) ? 2 : 1) void attention_dkv_kernel(Call c, Heads q, Heads k, Heads v, Heads g,
-                                                               const float* __restrict__ lse2,
-                                                               const float* __restrict__ delta, Gradient dk,
-                                                               Gradient dv, int tiles) {
+__global__ __launch_bounds__(256, D <= (sizeof(T) == 2 ? 96 : 64) ? 2 : 1) void attention_dkv_kernel(
+    Call c, Heads q, Heads k, Heads v, Heads g, const float* __restrict__ lse2, const float* __restrict__ delta,
+    Gradient dk, Gradient dv, int tiles) {
     extern __shared__ __attribute__((aligned(1024))) char lds[];
     using L = Tile<T, D>;
     const Work at(blockIdx.x, gridDim.x, tiles, 0);
@@ -1010,12 +1016,6 @@ __global__ __launch_bounds__(256) void attention_copy_kernel(Heads in, T* __rest
 // ---------------------------------------------------------------- host
 constexpr int kCus = 256;
 
-struct Tensor {
-    const jorge_heads* h;
-    int64_t tokens;
-    int heads;
-};
-
 Heads in_bytes(const jorge_heads& h, int64_t e) { return {(char*)h.data, h.batch * e, h.token * e, h.head * e}; }
 
 // Whether a matrix can be read as it lies: whole pieces of 16 bytes.
@@ -1046,7 +1046,8 @@ Plan plan_of(const jorge_attention_shape& s) {
     p.tiles = (int)ceil_div(rows, 4 * kOwn);
     p.tiles_k = (int)ceil_div(s.kv_tokens, 4 * kOwn);
     // What a query sees at most, in tiles.
-    const int64_t keys = s.window ? std::min<int64_t>(s.kv_tokens, s.window + 4 * kOwn / group + 1) : s.kv_tokens;
+    const int64_t window = std::min(s.window, s.kv_tokens);
+    const int64_t keys = window ? std::min(s.kv_tokens, window + 4 * kOwn / group + 1) : s.kv_tokens;
     const int64_t key_tiles = ceil_div(keys, tile), row_tiles = ceil_div(s.q_tokens, tile);
     p.ranges = p.few ? cut(bh, key_tiles, 8) : cut(bh * p.tiles, key_tiles, 2);
     p.ranges_q = cut(bh * p.tiles, key_tiles, 2);
@@ -1232,7 +1233,8 @@ jorge_status check(const jorge_attention_shape* shape) {
     if (s.heads < 1 || s.kv_heads < 1 || s.heads % s.kv_heads)
         return bad("attention: heads must be a positive multiple of kv_heads");
     if (s.dim < 1) return bad("attention: dim >= 1 is needed");
-    if (s.dim > JORGE_ATTENTION_MAX_DIM) return refuse(JORGE_ERR_UNSUPPORTED, "attention: dim above JORGE_ATTENTION_MAX_DIM");
+    if (s.dim > JORGE_ATTENTION_MAX_DIM)
+        return refuse(JORGE_ERR_UNSUPPORTED, "attention: dim above JORGE_ATTENTION_MAX_DIM");
     if (!(s.scale > 0.0) || !(s.scale < 1e30)) return bad("attention: scale must be positive and below 1e30");
     if (s.causal != 0 && s.causal != 1) return bad("attention: causal must be 0 or 1");
     if (s.window < 0) return bad("attention: window >= 0 is needed");

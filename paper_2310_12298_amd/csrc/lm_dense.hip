@@ -55,7 +55,7 @@ __device__ __forceinline__ Acted acted(float z) {
         case JORGE_ACT_GELU: {
             // The normal distribution's upper tail at |z| = sqrt(2) x, erfc(x) / 2, by the polynomial 7.1.26 of
             // Abramowitz and Stegun in 1 / (1 + p x) times exp(-x^2), off by at most 0.75e-7; the same exponential is
-            // the density. erff took 43 us of an epilogue over 4096 x 4096, this 9.
+            // the density. A forward pass of 4096 tokens, 1024 -> 4096, took 84 us with erff and 72 us with this.
             const float x = 0.707106781186547524f * __builtin_fabsf(z);
             const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.0f));
             const float bell = __builtin_amdgcn_exp2f(-kLog2e * x * x);
@@ -702,6 +702,11 @@ bool readable(int32_t dtype, int64_t cols, const void* p, int64_t ld) {
     return dtype == JORGE_BF16 && cols % kPadK == 0 && ld % 8 == 0 && aligned(p, 16);
 }
 
+bool weights_readable(const jorge_linear_shape& s, int mats, const void* weight, const void* up) {
+    return readable(s.dtype, s.cols, weight, s.ldw) &&
+           (mats == 1 || (readable(s.dtype, s.cols, up, s.ldu) && s.ldw == s.ldu));
+}
+
 Plan plan_of(const jorge_linear_shape& s, int mats, const Wanted& want, bool direct_x, bool direct_w, bool direct_dy) {
     Plan p{};
     p.terms = s.dtype == JORGE_F32 ? kTerms : 1;
@@ -949,7 +954,7 @@ jorge_status run_forward(const jorge_linear_shape& s, int mats, const void* x, c
     const jorge_status st = check_workspace(s, mats, false, workspace, bytes);
     if (st != JORGE_OK) return st;
     const Wanted want{false, false, false, false};
-    const bool direct_w = readable(s.dtype, s.cols, weight, s.ldw) && (mats == 1 || (readable(s.dtype, s.cols, up, s.ldu) && s.ldw == s.ldu));
+    const bool direct_w = weights_readable(s, mats, weight, up);
     const Plan p = plan_of(s, mats, want, readable(s.dtype, s.cols, x, s.ldx), direct_w, false);
     const Work w = carve(workspace, s, p, want);
     const hipStream_t q = reinterpret_cast<hipStream_t>(stream);
@@ -999,7 +1004,7 @@ jorge_status run_backward(const jorge_linear_shape& s, int mats, const void* dy,
     if (st != JORGE_OK) return st;
     const Wanted want{true, g.dx != nullptr, g.dweight != nullptr, g.dbias != nullptr};
     if (!want.dx && !want.dw && !want.db) return JORGE_OK;
-    const bool direct_w = readable(s.dtype, s.cols, weight, s.ldw) && (mats == 1 || (readable(s.dtype, s.cols, up, s.ldu) && s.ldw == s.ldu));
+    const bool direct_w = weights_readable(s, mats, weight, up);
     const Plan p = plan_of(s, mats, want, readable(s.dtype, s.cols, x, s.ldx), direct_w,
                            readable(s.dtype, s.outs, dy, s.ldy));
     const Work w = carve(workspace, s, p, want);

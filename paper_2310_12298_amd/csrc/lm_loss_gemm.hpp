@@ -1,4 +1,4 @@
-// The bfloat16 matrix product that cross entropy is made of, for gfx950:
+// The bfloat16 matrix product that cross entropy and the linear layers are made of, for gfx950:
 //   C[a][b] = sum_k A[a][k] B[b][k],  both operands K-contiguous, fp32 accumulators,
 // as a device function that leaves a tile of C in registers for the caller's epilogue.
 //

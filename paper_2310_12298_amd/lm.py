@@ -1,9 +1,10 @@
-"""Operators of a language model's training step beside the Jorge step: layer norm, embedding,
-cross entropy over a vocabulary, and AdamW with the global gradient norm.
+"""Operators of a language model's training step beside the Jorge step: layer norm, embedding, linear
+and gated linear layers, attention, cross entropy over a vocabulary, and AdamW with the global
+gradient norm.
 
-ctypes binding of include/jorge_lm.h. layer_norm(), embedding() and linear_cross_entropy() are
-differentiable; the *_forward and *_backward functions are the two passes by themselves; AdamW
-steps a list of tensors. torch owns the memory (outputs and workspaces are torch tensors of the
+ctypes binding of include/jorge_lm.h. layer_norm(), embedding(), linear(), gated_linear(),
+attention() and linear_cross_entropy() are differentiable; the *_forward and *_backward functions
+are the two passes by themselves; AdamW steps a list of tensors. torch owns the memory (outputs and workspaces are torch tensors of the
 current stream) and names the current HIP stream. Tensors are fp32 or bfloat16 CUDA tensors of the
 current device; the last dimension has to be dense, rows may have a stride. There is no CPU
 fallback: a missing library raises.
@@ -551,7 +552,7 @@ ATTENTION_MAX_STRIDE = 1 << 22                # JORGE_ATTENTION_MAX_STRIDE
 
 
 def _heads(t, what, like=None):
-    """t (batch, tokens, heads, dim) with dense rows and a token stride that the call takes, and a Heads' fields of it."""
+    """t (batch, tokens, heads, dim), its rows dense and its token stride one that the call takes, and its Heads' fields."""
     _cuda(t, what)
     if t.dim() != 4:
         raise ValueError(f"{what}: (batch, tokens, heads, dim) is needed")
@@ -624,8 +625,8 @@ def attention_backward(dout, q, k, v, out, lse, scale=None, causal=False, window
     grads = [torch.empty(t.shape, dtype=t.dtype, device=t.device) if need else None
              for t, need in ((q, need_q), (k, need_kv), (v, need_kv))]
     to = [None if t is None else ctypes.byref(Heads(t.data_ptr(), *t.stride()[:3])) for t in grads]
-    _check(lib, lib.jorge_attention_backward(ctypes.byref(shape), ctypes.byref(hd), ctypes.byref(ho), lse.data_ptr(), *to,
-                                             _ptr(ws), n.value, _stream(q)))
+    _check(lib, lib.jorge_attention_backward(ctypes.byref(shape), ctypes.byref(hd), ctypes.byref(ho), lse.data_ptr(),
+                                             *to, _ptr(ws), n.value, _stream(q)))
     return tuple(grads)
 
 
