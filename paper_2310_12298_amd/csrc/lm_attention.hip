@@ -17,10 +17,10 @@
 // dP: seven products where one kernel would do with five, but that one has to add dq up by atomics, whose order would
 // change results.
 //
-// Bound by the matrix cores in training. 4 sequences of 4096, 16 heads of 128 over 4 of k and v, causal, bfloat16:
-// forward 361 us (380 TFLOP/s of the half that is not masked; matrix cores busy 46%), dq 465 us (443; 56%), dk and dv
-// 756 us (364; 39%: one wave to a SIMD has nothing to cover its own softmax with). No bank conflicts in any of them. A
-// single token over 32 caches is bound by reading k and v: 159 us for 0.8 GB, 5.1 TB/s.
+// Bound by the matrix cores and the exponentials between their products in training. 4 sequences of 4096, 16 heads of
+// 128, causal, bfloat16: forward 361 us (762 TFLOP/s over what is not masked; matrix cores busy 46%), dq 465 us (887;
+// 56%), dk and dv 756 us (727; 39%: one wave to a SIMD has nothing to cover its own softmax with). No bank conflicts in
+// any of them. A single token over 32 caches is bound by reading k and v: 159 us for 0.8 GB, 5.1 TB/s.
 //
 // Queries whose heads share a key head are rows of one sequence of own rows, (token, head) by (token, head), so that a
 // tile of k and v is read once for all of them.
@@ -903,8 +903,9 @@ __device__ __forceinline__ void without_spoilt_rows(char* stage) {
 
 // Two waves to a SIMD where their registers allow it (a wave's k, v and sums of dk and dv take D of them for every four
 // bytes of T): with D = 96 in bfloat16 that takes 111 us where one wave takes 128 (5 sequences of up to 2011, 12 heads
-// of 80, window 512). At D = 128 two would spill in the loop (1.7 times the time); eight waves to a workgroup that keep
-// v in LDS instead took as long as four with one to a SIMD.
+// of 80, window 512). At D = 128 two would spill in the loop (1.7 times the time), and so would one that forms the scores
+// of a tile's second block between the exponentials of its first (1.75 times); eight waves to a workgroup that keep v in
+// LDS instead took as long as four with one to a SIMD.
 template <typename T, int D>
 __global__ __launch_bounds__(256, D <= (sizeof(T) == 2 ? 96 : 64) ? 2 : 1) void attention_dkv_kernel(
     Call c, Heads q, Heads k, Heads v, Heads g, const float* __restrict__ lse2, const float* __restrict__ delta,
@@ -978,12 +979,14 @@ __global__ __launch_bounds__(256, D <= (sizeof(T) == 2 ? 96 : 64) ? 2 : 1) void 
     write(av, dv, 1.0f);
 }
 
-// The sum of the ranges' gradients of a row, 32 lanes to it, in order. group: rows of a token.
+// The sum of the ranges' gradients of a row, 32 lanes to it, in order; of two matrices (blockIdx.y), of which one may be
+// none. group: rows of a token.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void attention_sum_kernel(Gradient out, int ranges, int64_t rows, int64_t all,
-                                                            int kv_heads, int group, int dim) {
+__global__ __launch_bounds__(256) void attention_sum_kernel(Gradient one, Gradient two, int ranges, int64_t rows,
+                                                            int64_t all, int kv_heads, int group, int dim) {
+    const Gradient& out = blockIdx.y ? two : one;
     const int64_t id = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (id >= all) return;
+    if (id >= all || !out.part) return;
     const int bh = (int)(id / rows), b = bh / kv_heads, r = (int)(id - bh * rows), d = (threadIdx.x & 31) * 4;
     if (d >= D) return;
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -1185,7 +1188,7 @@ jorge_status backward(const jorge_attention_shape& s, const Plan& p, const Space
             c, q, k, v, g, {fused ? in_bytes(out, sizeof(T)) : Heads{}, lse, w.lse2, w.delta}, to, p.tiles);
         if (w.part)
             attention_sum_kernel<T, D><<<dim3((unsigned)ceil_div(rows, 8)), dim3(256), 0, st>>>(
-                to, p.ranges_q, s.q_tokens * c.group, rows, c.kv_heads, c.group, c.dim);
+                to, {}, p.ranges_q, s.q_tokens * c.group, rows, c.kv_heads, c.group, c.dim);
     }
     if ((dk.data || dv.data) && keys) {
         constexpr int bytes = 4 * L::kBytes + 1024;
@@ -1194,10 +1197,9 @@ jorge_status backward(const jorge_attention_shape& s, const Plan& p, const Space
         const Gradient tv{in_bytes(dv, sizeof(T)), dv.data ? w.part_v : nullptr};
         attention_dkv_kernel<T, D><<<dim3(bh * p.tiles_k, p.ranges_k), dim3(256), bytes, st>>>(
             c, q, k, v, g, w.lse2, w.delta, tk, tv, p.tiles_k);
-        for (const Gradient& to : {tk, tv})
-            if (to.part)
-                attention_sum_kernel<T, D><<<dim3((unsigned)ceil_div(keys, 8)), dim3(256), 0, st>>>(
-                    to, p.ranges_k, s.kv_tokens, keys, c.kv_heads, 1, c.dim);
+        if (tk.part || tv.part)
+            attention_sum_kernel<T, D><<<dim3((unsigned)ceil_div(keys, 8), 2), dim3(256), 0, st>>>(
+                tk, tv, p.ranges_k, s.kv_tokens, keys, c.kv_heads, 1, c.dim);
     }
     return launched("attention");
 }
