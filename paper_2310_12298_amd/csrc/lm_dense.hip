@@ -274,13 +274,14 @@ struct Raw {
     }
 };
 
-// Of a workgroup's range of K (blockIdx.y of gridDim.y), its stages.
+// The stages of range n of `of` along K, if not given the workgroup's (blockIdx.y of gridDim.y).
 struct Range {
     int s0, s1;
-    __device__ __forceinline__ Range(int stages) {
+    __device__ __forceinline__ explicit Range(int stages) : Range(stages, blockIdx.y, gridDim.y) {}
+    __device__ __forceinline__ Range(int stages, int n, int of) {
         const int pairs = stages / 2;
-        s0 = (int)((int64_t)pairs * blockIdx.y / gridDim.y) * 2;
-        s1 = (int)((int64_t)pairs * (blockIdx.y + 1) / gridDim.y) * 2;
+        s0 = (int)((int64_t)pairs * n / of) * 2;
+        s1 = (int)((int64_t)pairs * (n + 1) / of) * 2;
     }
 };
 
@@ -479,6 +480,7 @@ struct DzOut {
     bf16 *dz, *dzt;            // [tokens][terms][matrices * kf], [matrices * outs][terms][kn] or null
     int64_t kf, kn;            // outs and tokens, padded to multiples of 64
     float* bias;               // [parts][outs] sums of dz over 16 WA tokens each, or null
+    int chunks;                // fp32, tiles up to 128 x 128: parts of K that are summed by themselves
 };
 
 template <int WA, int RING, bool SPLIT, bool PAIR, typename T>
@@ -488,7 +490,20 @@ __global__ __launch_bounds__(256, 1) void dense_dz_kernel(Dense d, const T* __re
     using Q = Tile<WA, WA, RING, SPLIT, PAIR>;
     const Place at = place_of(blockIdx.x, d.p.ta, d.p.tb);
     Q t;
-    t.multiply(d.p.A, d.A2, d.p.B, (int64_t)at.a * Q::kRowsA, (int64_t)at.b * Q::kB, 0, d.p.stages, d.p.stages, lds);
+    const auto sum = [&](const Range& k) {
+        t.multiply(d.p.A, d.A2, d.p.B, (int64_t)at.a * Q::kRowsA, (int64_t)at.b * Q::kB, k.s0, k.s1, d.p.stages, lds);
+    };
+    if constexpr (SPLIT && WA <= 4) {
+        f32x4 total[WA][WA] = {};
+#pragma unroll 1
+        for (int n = 0; n < out.chunks; ++n) {
+            sum(Range(d.p.stages, n, out.chunks));
+#pragma unroll
+            for (int i = 0; i < WA * WA; ++i) total[i / WA][i % WA] += t.acc[i / WA][i % WA];
+        }
+#pragma unroll
+        for (int i = 0; i < WA * WA; ++i) t.acc[i / WA][i % WA] = total[i / WA][i % WA];
+    } else sum(Range(d.p.stages, 0, 1));
     const int64_t a0 = (int64_t)at.a * Q::kRowsA + Q::lane_a(), b0 = (int64_t)at.b * Q::kB + Q::lane_b();
     const int64_t outs = d.p.A.rows, tokens = d.p.B.rows;
     constexpr int L = Q::kLaneA, kUp = PAIR ? WA / 2 : 0, MATS = PAIR ? 2 : 1;
@@ -692,6 +707,7 @@ struct Plan {
     bool dz;                         // dz differs from dy
     bool turn;                       // bfloat16: operands are read across their rows, not transposed first
     int64_t rows_w;                  // rows of the weights' gradients as one matrix
+    int chunks;                      // of K, in dense_dz_kernel
     Shape z, dx, dw;
 };
 struct Wanted {
@@ -705,6 +721,15 @@ bool readable(int32_t dtype, int64_t cols, const void* p, int64_t ld) {
 bool weights_readable(const jorge_linear_shape& s, int mats, const void* weight, const void* up) {
     return readable(s.dtype, s.cols, weight, s.ldw) &&
            (mats == 1 || (readable(s.dtype, s.cols, up, s.ldu) && s.ldw == s.ldu));
+}
+
+// fp32: the fewest ranges of a sum over K, a power of two. The accumulator's roundings leave an error that grows with the
+// root of K, 7e-7 of the sum at 2048 and 1.4e-6 at 8192; ranges of 1024 stay at 5e-7. Eight at most, as each is kept in
+// 32 bits.
+int64_t ranges_for(int64_t k) {
+    int64_t r = 1;
+    while (r < 8 && r * 1024 < k) r *= 2;
+    return r;
 }
 
 Plan plan_of(const jorge_linear_shape& s, int mats, const Wanted& want, bool direct_x, bool direct_w, bool direct_dy) {
@@ -722,12 +747,20 @@ Plan plan_of(const jorge_linear_shape& s, int mats, const Wanted& want, bool dir
     p.dz = mats == 2 || s.activation != JORGE_ACT_NONE;
     p.turn = p.terms == 1;
     p.rows_w = mats * (p.turn ? p.kf : s.outs);
-    p.z = shape_of(mats * s.outs, s.tokens, p.kd, p.products, !want.backward);
+    const auto least = [&](int64_t k) { return p.terms == 1 ? 1 : ranges_for(k); };
+    p.z = shape_of(mats * s.outs, s.tokens, p.kd, p.products, !want.backward, want.backward ? 1 : least(p.kd));
+    p.chunks = 1;
+    if (want.backward && least(p.kd) > 2) {
+        // dz needs its sums whole, and a tile of 256 x 256 leaves no registers for sums of two parts of K.
+        p.chunks = (int)least(p.kd);
+        if (p.z.blocks == 8) p.z.blocks = 4;
+        p.z.deep = ceil_div(mats * s.outs, 32 * p.z.blocks) * ceil_div(s.tokens, 32 * p.z.blocks) <= kCus;
+    }
     // A pair's tile of 64 x 64 holds 32 columns of each, which padding to 64 would leave without a tile.
     if (mats == 2 && p.z.blocks == 2) p.z.blocks = 4;
     if (want.backward) {
-        p.dx = shape_of(s.cols, s.tokens, mats * p.kf, p.products, true);
-        p.dw = shape_of(s.cols, p.rows_w, p.kn, p.products, true);
+        p.dx = shape_of(s.cols, s.tokens, mats * p.kf, p.products, true, least(mats * p.kf));
+        p.dw = shape_of(s.cols, p.rows_w, p.kn, p.products, true, least(p.kn));
     }
     return p;
 }
@@ -874,7 +907,7 @@ jorge_status backward(const jorge_linear_shape& s, const Plan& p, const Work& w,
     jorge_status err = JORGE_OK;
     if (p.dz) {
         const Dense d = dense_of(s, p, in);
-        const DzOut z{w.dz, w.dzt, p.kf, p.kn, w.bias};
+        const DzOut z{w.dz, w.dzt, p.kf, p.kn, w.bias, p.chunks};
         const auto run = [&](auto WA, auto RING) {
             constexpr int B = decltype(WA)::value, R = decltype(RING)::value;
             constexpr int bytes = Tile<B, B, R, sizeof(T) == 4>::kBytes;

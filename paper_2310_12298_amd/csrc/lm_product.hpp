@@ -138,7 +138,8 @@ struct Shape {
 // as fast: 4096 x 4096 x 8192 takes 238 us in large tiles and 395 in middle ones), the fixed part 12, 6 and 4 us. The
 // small ones win where the large ones leave CUs idle or are mostly padding: 64 tokens, 8192 words of 512 in fp32 30 ->
 // 17 us for the logits.
-Shape shape_of(int64_t a, int64_t b, int64_t k, int products, bool may_cut) {
+// least_ranges: a power of two, the fewest ranges that the caller takes.
+Shape shape_of(int64_t a, int64_t b, int64_t k, int products, bool may_cut, int64_t least_ranges = 1) {
     constexpr double kStage[3] = {0.88, 0.36, 0.15}, kFixed[3] = {12.0, 6.0, 4.0};
     Shape best{};
     double least = 1e300;
@@ -146,7 +147,7 @@ Shape shape_of(int64_t a, int64_t b, int64_t k, int products, bool may_cut) {
         const int64_t blocks = 8 >> t, tiles = ceil_div(a, 32 * blocks) * ceil_div(b, 32 * blocks);
         // A range keeps at least eight stages' products, and two stages.
         const int64_t stages = k / kStageK * products, most = std::min(stages / 8, k / kStageK / 2);
-        for (int64_t r = 1; r == 1 || (may_cut && r <= most && tiles * r <= 2 * kCus); r *= 2) {
+        for (int64_t r = least_ranges; r == least_ranges || (may_cut && r <= most && tiles * r <= 2 * kCus); r *= 2) {
             double us = (double)ceil_div(tiles * r, kCus) * ((double)ceil_div(stages, r) * kStage[t] + kFixed[t]);
             if (r > 1) us += 4.0 + (double)(r * a * b) * 8.0 / 4.5e6;
             if (us < least) {

@@ -327,3 +327,42 @@ def test_refusals():
             bad()
     with pytest.raises(lm.JorgeError):
         lm.linear_forward(torch.zeros(1, 32769, device="cuda"), torch.zeros(1, 32769, device="cuda"))
+
+
+@pytest.mark.parametrize("n,d,f,act", [(4096, 8192, 1536, None), (16384, 1030, 1100, None), (1500, 1000, 8192, "silu"),
+                                       (700, 8192, 600, "silu")])
+def test_long_sums_in_fp32_keep_their_precision(n, d, f, act):
+    """A sum over K of random terms, and the step that it is rounded to, grow with the root of K, and so do the roundings'
+    number and with it the sum's relative error, unless it is formed in ranges: their errors are independent and add up in
+    squares as the ranges do, so that the whole errs as one range does. A range has 1024 terms up to K = 8192 (eight
+    ranges), and K / 8 beyond. e is the error of a sum of 1024, measured. An argument's error e comes with the
+    activation's slope: for silu of normal arguments, of act'(z) it is at most e (act'' is at most 1/2, the root mean
+    square of act' 0.6) and of act(z) e (both have a root mean square of 0.6); and of u it is e. So a layer's gradients
+    err by at most sqrt(2) e and the pair's by sqrt(3) e; a tenth more is left for what joins the ranges."""
+    g = torch.Generator().manual_seed(n + d)
+    x, w, u = (rand(g, *s, d=F32, s=k) for s, k in (((n, d), 1.0), ((f, d), d ** -0.5), ((f, d), d ** -0.5)))
+    dy = rand(g, n, f, d=F32, s=1e-2)
+    X, W, U, DY = (t.double() for t in (x, w, u, dy))
+
+    def off(got, want):
+        return float((got.double() - want).norm() / want.norm())
+
+    a, b = rand(g, 4096, 1024, d=F32), rand(g, 4096, 1024, d=F32)      # enough tiles: its sums are of one range
+    e = 1.1 * off(lm.linear_forward(a, b), a.double() @ b.double().t())
+
+    def near(got, want, k, factor, what):
+        assert off(got, want) < factor ** 0.5 * max(1.0, k / 8192) ** 0.5 * e, f"{what}: {off(got, want):.2e}, e {e:.2e}"
+
+    a, da = both64(act, X @ W.t())
+    more = 2 if act else 1
+    near(lm.linear_forward(x, w, None, act), a, d, more, "y")
+    dx, dw, _ = lm.linear_backward(dy, x, w, None, act)
+    near(dx, DY * da @ W, f, more, "dx")
+    near(dw, (DY * da).t() @ X, n, more, "dweight")
+    if act:
+        near(lm.gated_linear_forward(x, w, u, act), a * (X @ U.t()), d, 3, "gated y")
+        dx, dw, du = lm.gated_linear_backward(dy, x, w, u, act)
+        dg, dv = DY * (X @ U.t()) * da, DY * a
+        near(dx, dg @ W + dv @ U, 2 * f, 3, "gated dx")
+        near(dw, dg.t() @ X, n, 3, "dgate")
+        near(du, dv.t() @ X, n, 3, "dup")
