@@ -745,12 +745,10 @@ __device__ __forceinline__ float stat_of(float lse, float delta) {
     return __builtin_fabsf(x) < INFINITY && __builtin_fabsf(delta) < INFINITY ? x : __builtin_nanf("");
 }
 
-// [batch][head][token]: the row's log2 sum exp (plus infinity where it sees nothing, so that every probability is 0) and
-// delta = do . o. Two lanes to a row, which add it up as attention_dq_kernel does where that forms it: dk and dv are the
-// same to the bit with and without dq.
+// delta = do . o, [batch][head][token], where o cannot be read in whole pieces of 16 bytes. Two lanes to a row, which add
+// it up as attention_dq_kernel does where that reads o: the results are the same to the bit.
 template <typename T>
-__global__ __launch_bounds__(256) void attention_delta_kernel(Call c, Heads o, Heads g, const float* __restrict__ lse,
-                                                              float* __restrict__ lse2, float* __restrict__ delta) {
+__global__ __launch_bounds__(256) void attention_delta_kernel(Call c, Heads o, Heads g, float* __restrict__ delta) {
     const int64_t id = (int64_t)blockIdx.x * 128 + (threadIdx.x >> 1);
     if (id >= (int64_t)c.batch * c.heads * c.q_tokens) return;
     // Neighbouring rows are heads of a token, as they lie in memory.
@@ -776,9 +774,7 @@ __global__ __launch_bounds__(256) void attention_delta_kernel(Call c, Heads o, H
             }
         }
     sum += __shfl_xor(sum, 1);
-    if (threadIdx.x & 1) return;
-    lse2[at] = seen ? stat_of(lse[at], sum) : INFINITY;
-    delta[at] = seen ? sum : 0.0f;
+    if (!(threadIdx.x & 1)) delta[at] = seen ? sum : 0.0f;
 }
 
 // Gradients of rows of one matrix: to it, or, where the streamed side is cut into ranges, the range's sums
@@ -788,14 +784,20 @@ struct Gradient {
     float* part;
 };
 
-// A row's log2 sum exp and delta: as attention_delta_kernel left them, or (o given) formed here from the row's o and
-// gradient, which saves reading the gradient twice, and left for attention_dkv_kernel.
+// A row's log2 sum exp (plus infinity where it sees nothing, so that every probability is 0) and delta, [batch][head]
+// [token], which attention_dq_kernel leaves for attention_dkv_kernel. delta is formed from the row's o and gradient, which
+// saves reading the gradient twice, or (no o) is there from attention_delta_kernel. o's rounding to bfloat16 puts an
+// error into delta that is an average over the keys that a row sees; where a workgroup's rows see few (kFewTiles), delta
+// is the sum of p dp instead, formed in a pass of its own: without it dq errs by 3.8e-3 of its size where rows see 2
+// keys, by 2.6e-3 at 96 and 2.4e-3 at 264, with it by 2.4e-3.
+constexpr int kFewTiles = 4;
 struct RowStats {
     Heads o;
     const float* lse;
     float *lse2, *delta;
 };
 
+// dq absent: only the rows' statistics.
 template <typename T, int D>
 __global__ __launch_bounds__(256, 2) void attention_dq_kernel(Call c, Heads q, Heads k, Heads v, Heads g,
                                                               RowStats stats, Gradient dq, int tiles) {
@@ -821,6 +823,8 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(Call c, Heads q, H
                        {v.p + b * v.batch + hk * v.head, v.token, c.dim, wave}, span.lo, span.hi, wave};
     const int64_t stat = ((int64_t)b * c.heads + row.head) * c.q_tokens + row.token;
     float l2 = INFINITY, de = 0.0f;
+    const Span all(span.lo, span.hi, L::kRows, 0, 1);
+    const bool few = sizeof(T) == 2 && all.t1 - all.t0 <= kFewTiles;
     if (stats.o.p) {
         typename L::Own o;
         o.load(stats.o.p + b * stats.o.batch + row.token * stats.o.token + row.head * stats.o.head,
@@ -832,14 +836,34 @@ __global__ __launch_bounds__(256, 2) void attention_dq_kernel(Call c, Heads q, H
                 de = __builtin_fmaf((float)o.f[n][e], (float)grad.f[n][e], de);
         de += __shfl_xor(de, 32);
         if (row.there && hi > lo) l2 = stats.lse[stat] * kLog2e;
-        if (row.there && lane < 32 && blockIdx.y == 0) {
-            stats.lse2[stat] = hi > lo ? stat_of(stats.lse[stat], de) : INFINITY;
-            stats.delta[stat] = de;
-        }
     } else if (row.there) {
-        l2 = stats.lse2[stat];
+        l2 = hi > lo ? stats.lse[stat] * kLog2e : INFINITY;
         de = stats.delta[stat];
     }
+    if constexpr (sizeof(T) == 2) {
+        if (few) {
+            de = 0.0f;
+            stream<2 * L::kBytes>(all, lds, fetch, [&](int t, const char* kt) {
+                const int k0 = t * L::kRows;
+                if (!__any(k0 < hi && k0 + L::kRows > lo)) return;
+#pragma unroll
+                for (int kb = 0; kb < L::kBlocks; ++kb) {
+                    const f32x16 z = tile.rows(kt, kb, own), dp = tile.rows(kt + L::kBytes, kb, grad);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int key = k0 + kb * 32 + row_of(i);
+                        de += key >= lo && key < hi ? probability<T>(c, z[i], l2) * dp[i] : 0.0f;
+                    }
+                }
+            });
+            de += __shfl_xor(de, 32);
+        }
+    }
+    if (row.there && lane < 32 && blockIdx.y == 0) {
+        stats.lse2[stat] = hi > lo ? stat_of(stats.lse[stat], de) : INFINITY;
+        stats.delta[stat] = de;
+    }
+    if (!dq.g.p) return;
     f32x16 acc[L::kDims];
     clear(acc);
     stream<2 * L::kBytes>(span, lds, fetch, [&](int t, const char* kt) {
@@ -1175,18 +1199,18 @@ jorge_status backward(const jorge_attention_shape& s, const Plan& p, const Space
     const Heads g = operand<T>(s, dout, s.q_tokens, s.heads, w.g, st);
     const int64_t rows = s.batch * s.heads * s.q_tokens, keys = s.batch * s.kv_heads * s.kv_tokens;
     const int bh = c.batch * c.kv_heads;
-    // dq is formed first, and its kernel forms what dk's and dv's reads of a row too.
-    const bool fused = dq.data && rows && readable(s, out);
+    // dq's kernel comes first and forms what dk's and dv's reads of a row too, also without dq.
+    const bool fused = readable(s, out);
     if (rows && !fused)
         attention_delta_kernel<T><<<dim3((unsigned)ceil_div(rows, 128)), dim3(256), 0, st>>>(
-            c, in_bytes(out, sizeof(T)), in_bytes(dout, sizeof(T)), lse, w.lse2, w.delta);
+            c, in_bytes(out, sizeof(T)), in_bytes(dout, sizeof(T)), w.delta);
     jorge_status err;
-    if (dq.data && rows) {
+    if (rows) {
         if ((err = allow_lds(attention_dq_kernel<T, D>, 4 * L::kBytes)) != JORGE_OK) return err;
-        const Gradient to{in_bytes(dq, sizeof(T)), w.part};
-        attention_dq_kernel<T, D><<<dim3(bh * p.tiles, p.ranges_q), dim3(256), 4 * L::kBytes, st>>>(
+        const Gradient to{in_bytes(dq, sizeof(T)), dq.data ? w.part : nullptr};
+        attention_dq_kernel<T, D><<<dim3(bh * p.tiles, dq.data ? p.ranges_q : 1), dim3(256), 4 * L::kBytes, st>>>(
             c, q, k, v, g, {fused ? in_bytes(out, sizeof(T)) : Heads{}, lse, w.lse2, w.delta}, to, p.tiles);
-        if (w.part)
+        if (to.part)
             attention_sum_kernel<T, D><<<dim3((unsigned)ceil_div(rows, 8)), dim3(256), 0, st>>>(
                 to, {}, p.ranges_q, s.q_tokens * c.group, rows, c.kv_heads, c.group, c.dim);
     }

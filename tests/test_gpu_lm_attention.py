@@ -357,3 +357,30 @@ def test_refusals():
                 lambda: lm.attention_forward(*[torch.zeros(1, 1, 1, 129, device="cuda")] * 3)):
         with pytest.raises(lm.JorgeError):
             bad()
+
+
+@pytest.mark.parametrize("batch,n,m,heads,kv_heads,dim,how", [
+    (15, 2, 2, 8, 8, 94, dict(causal=True)), (7, 1809, 2, 7, 7, 53, {}), (4, 300, 300, 4, 2, 64, dict(causal=True, window=4)),
+    (6, 96, 96, 8, 4, 80, dict(causal=True)), (3, 500, 21, 8, 2, 128, {})])
+def test_bfloat16_gradients_where_rows_see_few_keys(batch, n, m, heads, kv_heads, dim, how):
+    """dq and dk are rounded twice, each time by at most 2^-8 of a value, evenly: ds for its product and the result. The
+    root mean square of that is 2^-8 / sqrt(3) at most, and that of both sqrt(2) times as much, 3.2e-3 of the result
+    where the terms are independent. delta from the rounded o would add as much again where a row sees two keys."""
+    g = torch.Generator().manual_seed(n + m + dim)
+    q, dout = (torch.randn(batch, n, heads, dim, generator=g) for _ in range(2))
+    k, v = (torch.randn(batch, m, kv_heads, dim, generator=g) for _ in range(2))
+    q, k, v, dout = (t.bfloat16().cuda() for t in (q, k, v, dout))
+    out, lse = lm.attention_forward(q, k, v, **how)
+    Q, K, V = (t.double().requires_grad_() for t in (q, k, v))
+    wide = [t.repeat_interleave(heads // kv_heads, 2).transpose(1, 2) for t in (K, V)]
+    z = (Q.transpose(1, 2) @ wide[0].transpose(2, 3).contiguous()) * dim ** -0.5
+    at = torch.arange(n, device="cuda")[:, None] + m - n
+    key = torch.arange(m, device="cuda")[None]
+    seen = torch.ones(n, m, dtype=torch.bool, device="cuda")
+    if how:
+        seen = (key <= at) & (key > at - how.get("window", m))
+    z = torch.softmax(z.masked_fill(~seen, -float("inf")), -1)
+    want = torch.autograd.grad((z @ wide[1]).transpose(1, 2), (Q, K, V), dout.double())
+    for got, ref in zip(lm.attention_backward(dout, q, k, v, out, lse, **how)[:2], want):
+        off = float((got.double() - ref).norm() / ref.norm())
+        assert off < 2 ** 0.5 * 2 ** -8 / 3 ** 0.5, off
