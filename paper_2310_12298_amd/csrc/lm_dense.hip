@@ -586,6 +586,32 @@ __global__ __launch_bounds__(256, 1) void dense_dz_kernel(Dense d, const T* __re
     }
 }
 
+// fp32, K cut: dz (of both matrices) from the ranges' sums, in the place of the first range's.
+template <bool PAIR>
+__global__ __launch_bounds__(256) void dense_dz_join_kernel(float* slices, int n, int64_t rows, int cols, int64_t lda,
+                                                            const float* __restrict__ dy, int64_t ldy, Bias bias,
+                                                            int act) {
+    const int64_t r = blockIdx.x;
+    for (int c = (blockIdx.y * 256 + threadIdx.x) * 4; c < cols; c += gridDim.y * 1024) {
+        float* const p = slices + r * lda + c;
+        f32x4 z = sum_slices(p, n, rows * lda), u = PAIR ? sum_slices(p + lda / 2, n, rows * lda) : z;
+        float g[4], b[4] = {};
+        load_some<4>(dy + r * ldy + c, cols - c, g);
+        if constexpr (!PAIR) bias.template load<4>(c, cols - c, b);
+        with_activation(act, [&](auto A) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const Acted f = acted<decltype(A)::value, true>(z[e] + b[e]);
+                z[e] = PAIR ? g[e] * u[e] * f.d : g[e] * f.d;
+                u[e] = g[e] * f.a;
+            }
+        });
+        // Past the last column up to a multiple of four there is room.
+        *reinterpret_cast<f32x4*>(p) = z;
+        if constexpr (PAIR) *reinterpret_cast<f32x4*>(p + lda / 2) = u;
+    }
+}
+
 // Where a gradient goes: rows [0, rows) to one matrix, those from `second` on to another one.
 template <typename T>
 struct Target {
@@ -708,6 +734,7 @@ struct Plan {
     bool turn;                       // bfloat16: operands are read across their rows, not transposed first
     int64_t rows_w;                  // rows of the weights' gradients as one matrix
     int chunks;                      // of K, in dense_dz_kernel
+    bool cut;                        // fp32, backward: dz from ranges of K over workgroups
     Shape z, dx, dw;
 };
 struct Wanted {
@@ -756,6 +783,17 @@ Plan plan_of(const jorge_linear_shape& s, int mats, const Wanted& want, bool dir
         if (p.z.blocks == 8) p.z.blocks = 4;
         p.z.deep = ceil_div(mats * s.outs, 32 * p.z.blocks) * ceil_div(s.tokens, 32 * p.z.blocks) <= kCus;
     }
+    if (want.backward && p.dz && p.terms > 1) {
+        // Where tiles leave CUs idle K is cut for dz too, which is then formed by a launch of its own and split by
+        // another: 1515 tokens, 7854 -> 230, silu, both passes: 385 us whole, 324 cut.
+        const Shape cut = shape_of(mats * s.outs, s.tokens, p.kd, p.products, true, least(p.kd));
+        const double more = 10.0 + (double)(s.tokens * mats * s.outs) * 28.0 / 4.5e6;
+        p.cut = cut.ranges > 1 && cut.us + more < p.z.us;
+        if (p.cut) {
+            p.z = cut;
+            p.chunks = 1;
+        }
+    }
     // A pair's tile of 64 x 64 holds 32 columns of each, which padding to 64 would leave without a tile.
     if (mats == 2 && p.z.blocks == 2) p.z.blocks = 4;
     if (want.backward) {
@@ -774,7 +812,7 @@ struct Work {
     int64_t bytes, ldz, ldc;
 };
 int64_t bias_parts(const jorge_linear_shape& s, const Plan& p) {
-    return p.dz ? ceil_div(s.tokens, 32 * p.z.blocks) * 2 : ceil_div(s.tokens, kBiasRows);
+    return p.dz && !p.cut ? ceil_div(s.tokens, 32 * p.z.blocks) * 2 : ceil_div(s.tokens, kBiasRows);
 }
 Work carve(void* base, const jorge_linear_shape& s, const Plan& p, const Wanted& want) {
     Carve c{(char*)base};
@@ -793,6 +831,7 @@ Work carve(void* base, const jorge_linear_shape& s, const Plan& p, const Wanted&
         if (!p.few && p.z.ranges > 1) w.z = c.take<float>(p.z.ranges * s.tokens * w.ldz);
     } else {
         const bool dz = want.dx || (p.turn && want.dw);
+        if (p.cut && z) w.z = c.take<float>(p.z.ranges * s.tokens * w.ldz);
         if (want.dw && !p.turn) w.xt = c.take<bf16>(p.terms * s.cols * p.kn);
         if (want.dx && !p.turn) w.wt = c.take<bf16>(p.terms * s.cols * p.mats * p.kf);
         if (dz && (p.dz || !p.direct_dy)) w.dz = c.take<bf16>(p.terms * s.tokens * p.mats * p.kf);
@@ -905,7 +944,33 @@ jorge_status backward(const jorge_linear_shape& s, const Plan& p, const Work& w,
                  : p.dz ? Copies{} : copies_of(dy, s.ldy, s.tokens, s.outs, w.dz, p.kf, w.dzt, p.kn));
     const Operands in = operands_of(s, p, w, x, weight, up);
     jorge_status err = JORGE_OK;
-    if (p.dz) {
+    if constexpr (sizeof(T) == 4) {
+        if (p.cut) {
+            const Dense d = dense_of(s, p, in);
+            const auto run = [&](auto WA, auto RING) {
+                constexpr int B = decltype(WA)::value, R = decltype(RING)::value, bytes = Tile<B, B, R, true>::kBytes;
+                const auto k = dense_forward_kernel<B, R, true, PAIR, T>;
+                if ((err = allow_lds(k, bytes, kNoLds)) != JORGE_OK) return;
+                k<<<dim3(d.p.ta * d.p.tb, p.z.ranges), dim3(256), bytes, st>>>(d, Finish<T>{}, w.z, w.ldz);
+            };
+            if constexpr (PAIR) with_pair_tile(p.z, run);
+            else with_tile(p.z, run);
+            if (err != JORGE_OK) return err;
+            dense_dz_join_kernel<PAIR><<<dim3((unsigned)s.tokens, (unsigned)ceil_div(s.outs, 1024)), dim3(256), 0, st>>>(
+                w.z, p.z.ranges, s.tokens, (int)s.outs, w.ldz, (const T*)dy, s.ldy, bias, s.activation);
+            Copies split[2] = {};
+            for (int m = 0; m < p.mats; ++m) {
+                split[m] = copies_of(w.z + m * (w.ldz / 2), w.ldz, s.tokens, s.outs, w.dz ? w.dz + m * p.kf : nullptr,
+                                     p.kf, w.dzt ? w.dzt + m * s.outs * p.terms * p.kn : nullptr, p.kn);
+                split[m].padded_f = kz;
+            }
+            copy<T>(split[0], split[1], st);
+            if (w.bias)
+                dense_columns_kernel<T><<<dim3((unsigned)ceil_div(s.outs, 256), (unsigned)bias_parts(s, p)), dim3(256),
+                                          0, st>>>(w.z, w.ldz, s.tokens, s.outs, w.bias);
+        }
+    }
+    if (p.dz && !p.cut) {
         const Dense d = dense_of(s, p, in);
         const DzOut z{w.dz, w.dzt, p.kf, p.kn, w.bias, p.chunks};
         const auto run = [&](auto WA, auto RING) {
@@ -918,7 +983,7 @@ jorge_status backward(const jorge_linear_shape& s, const Plan& p, const Work& w,
         if constexpr (PAIR) with_pair_tile(p.z, run);
         else with_tile(p.z, run);
         if (err != JORGE_OK) return err;
-    } else if (w.bias) {
+    } else if (!p.dz && w.bias) {
         dense_columns_kernel<T><<<dim3((unsigned)ceil_div(s.outs, 256), (unsigned)bias_parts(s, p)), dim3(256), 0,
                                   st>>>((const T*)dy, s.ldy, s.tokens, s.outs, w.bias);
     }

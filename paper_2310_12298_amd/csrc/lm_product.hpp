@@ -131,6 +131,7 @@ struct Shape {
     int blocks;   // 8, 4 or 2: tiles of 256 x 256, 128 x 128 or 64 x 64
     int ranges;
     bool deep;    // a tile has its CU to itself: a ring of eight stages, else of four
+    double us;    // what the model expects
 };
 // The tile and the number of ranges that a model of the launch puts first: rounds of workgroups over the CUs, each the
 // stages of its range and a fixed part (the ring's first loads, the epilogue), and adding the ranges' sums up. A stage
@@ -152,7 +153,7 @@ Shape shape_of(int64_t a, int64_t b, int64_t k, int products, bool may_cut, int6
             if (r > 1) us += 4.0 + (double)(r * a * b) * 8.0 / 4.5e6;
             if (us < least) {
                 least = us;
-                best = {(int)blocks, (int)r, tiles * r <= kCus};
+                best = {(int)blocks, (int)r, tiles * r <= kCus, us};
             }
         }
     }

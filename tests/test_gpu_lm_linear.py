@@ -366,3 +366,25 @@ def test_long_sums_in_fp32_keep_their_precision(n, d, f, act):
         near(dx, dg @ W + dv @ U, 2 * f, 3, "gated dx")
         near(dw, dg.t() @ X, n, 3, "dgate")
         near(du, dv.t() @ X, n, 3, "dup")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,d,f", [(130, 4001, 70), (70, 2500, 129), (300, 6000, 5)])
+def test_few_tiles_of_long_rows(n, d, f, dtype):
+    """Where K is cut over workgroups backward too, and dz is formed from the ranges' sums."""
+    check_linear(n, d, f, dtype, "gelu", True, True)
+    check_linear(n, d, f, dtype, "sigmoid", False, False)
+    check_gated(n, d, f, dtype, "silu")
+
+
+def test_single_gradients_of_few_tiles_of_long_rows():
+    g = torch.Generator().manual_seed(4)
+    x, w, u, b, dy = (rand(g, *s, d=F32) for s in ((130, 4001), (70, 4001), (70, 4001), (70,), (130, 70)))
+    every = lm.linear_backward(dy, x, w, b, "silu")
+    for i in range(3):
+        alone = lm.linear_backward(dy, x, w, b, "silu", *[n == i for n in range(3)])
+        assert torch.equal(alone[i], every[i]) and sum(t is not None for t in alone) == 1
+    every = lm.gated_linear_backward(dy, x, w, u)
+    assert torch.equal(lm.gated_linear_backward(dy, x, w, u, need_weights=False)[0], every[0])
+    for one, both in zip(lm.gated_linear_backward(dy, x, w, u, need_x=False)[1:], every[1:]):
+        assert torch.equal(one, both)
