@@ -171,8 +171,9 @@ jorge_status jorge_cross_entropy_backward(const jorge_loss_shape* shape, const f
  *   gated linear:  dg = dy u act'(g),  du = dy act(g),  dx = dg gate + du up,  dgate = dg^T x,  dup = du^T x.
  * relu's derivative at 0 is 0. bfloat16: dz, dg and du are rounded to bfloat16 for the products, whose sums are fp32
  * (dbias is summed before that); a gradient then errs by some 2.4e-3 of its size instead of the 1.7e-3 of its own
- * rounding. fp32: up to JORGE_LINEAR_FEW_TOKENS forward are multiplied in fp32; the other products are formed from three-term
- * bfloat16 splits as the Jorge step's are (jorge.h): values above 3.39e38 count as infinite. */
+ * rounding. fp32: up to JORGE_LINEAR_FEW_TOKENS forward are multiplied in fp32; the other products are formed from
+ * three-term bfloat16 splits as the Jorge step's are (jorge.h): values above 3.39e38 count as infinite. Their sums over
+ * more than 1024 terms are formed in up to eight ranges, of which the workspace holds up to 1 GiB. */
 #define JORGE_ACT_NONE    0
 #define JORGE_ACT_RELU    1
 #define JORGE_ACT_GELU    2
@@ -237,8 +238,9 @@ jorge_status jorge_gated_linear_backward(const jorge_linear_shape* shape, const 
  * Gradients, from the o and lse of the forward pass, with p = exp(z - lse):
  *   delta = do . o,  ds = scale p (do v^T - delta),  dq = ds k,  dk = ds^T q,  dv = p^T do,
  * dk and dv summed over the heads that share them. bfloat16: p and ds are rounded to bfloat16 for their products, all
- * else is fp32 (a gradient then errs by some 2.4e-3 of its size instead of the 1.7e-3 of its own rounding). fp32 is
- * multiplied in fp32. */
+ * else is fp32 (a gradient then errs by some 2.4e-3 of its size instead of the 1.7e-3 of its own rounding); where rows
+ * see few keys, delta is the sum of p (do v^T), as o's rounding would not average out in it. fp32 is multiplied in
+ * fp32. */
 
 /* Largest dim, tokens, token stride, and batch * heads * tokens (of q or of k). */
 #define JORGE_ATTENTION_MAX_DIM    128

@@ -751,11 +751,11 @@ bool weights_readable(const jorge_linear_shape& s, int mats, const void* weight,
 }
 
 // fp32: the fewest ranges of a sum over K, a power of two. The accumulator's roundings leave an error that grows with the
-// root of K, 7e-7 of the sum at 2048 and 1.4e-6 at 8192; ranges of 1024 stay at 5e-7. Eight at most, as each is kept in
-// 32 bits.
-int64_t ranges_for(int64_t k) {
+// root of K, 7e-7 of the sum at 2048 and 1.4e-6 at 8192; ranges of 1024 stay at 5e-7. Eight at most, and no more than
+// 1 GiB of them, as each is kept in 32 bits (`sums` of them to a range; 0: in registers).
+int64_t ranges_for(int64_t k, int64_t sums) {
     int64_t r = 1;
-    while (r < 8 && r * 1024 < k) r *= 2;
+    while (r < 8 && r * 1024 < k && 2 * r * sums * 4 <= int64_t(1) << 30) r *= 2;
     return r;
 }
 
@@ -774,20 +774,21 @@ Plan plan_of(const jorge_linear_shape& s, int mats, const Wanted& want, bool dir
     p.dz = mats == 2 || s.activation != JORGE_ACT_NONE;
     p.turn = p.terms == 1;
     p.rows_w = mats * (p.turn ? p.kf : s.outs);
-    const auto least = [&](int64_t k) { return p.terms == 1 ? 1 : ranges_for(k); };
-    p.z = shape_of(mats * s.outs, s.tokens, p.kd, p.products, !want.backward, want.backward ? 1 : least(p.kd));
+    const auto least = [&](int64_t k, int64_t sums) { return p.terms == 1 ? 1 : ranges_for(k, sums); };
+    const int64_t sums_z = mats * s.outs * s.tokens;
+    p.z = shape_of(mats * s.outs, s.tokens, p.kd, p.products, !want.backward, want.backward ? 1 : least(p.kd, sums_z));
     p.chunks = 1;
-    if (want.backward && least(p.kd) > 2) {
+    if (want.backward && least(p.kd, 0) > 2) {
         // dz needs its sums whole, and a tile of 256 x 256 leaves no registers for sums of two parts of K.
-        p.chunks = (int)least(p.kd);
+        p.chunks = (int)least(p.kd, 0);
         if (p.z.blocks == 8) p.z.blocks = 4;
         p.z.deep = ceil_div(mats * s.outs, 32 * p.z.blocks) * ceil_div(s.tokens, 32 * p.z.blocks) <= kCus;
     }
     if (want.backward && p.dz && p.terms > 1) {
         // Where tiles leave CUs idle K is cut for dz too, which is then formed by a launch of its own and split by
         // another: 1515 tokens, 7854 -> 230, silu, both passes: 385 us whole, 324 cut.
-        const Shape cut = shape_of(mats * s.outs, s.tokens, p.kd, p.products, true, least(p.kd));
-        const double more = 10.0 + (double)(s.tokens * mats * s.outs) * 28.0 / 4.5e6;
+        const Shape cut = shape_of(mats * s.outs, s.tokens, p.kd, p.products, true, least(p.kd, sums_z));
+        const double more = 10.0 + (double)sums_z * 28.0 / 4.5e6;
         p.cut = cut.ranges > 1 && cut.us + more < p.z.us;
         if (p.cut) {
             p.z = cut;
@@ -797,8 +798,8 @@ Plan plan_of(const jorge_linear_shape& s, int mats, const Wanted& want, bool dir
     // A pair's tile of 64 x 64 holds 32 columns of each, which padding to 64 would leave without a tile.
     if (mats == 2 && p.z.blocks == 2) p.z.blocks = 4;
     if (want.backward) {
-        p.dx = shape_of(s.cols, s.tokens, mats * p.kf, p.products, true, least(mats * p.kf));
-        p.dw = shape_of(s.cols, p.rows_w, p.kn, p.products, true, least(p.kn));
+        p.dx = shape_of(s.cols, s.tokens, mats * p.kf, p.products, true, least(mats * p.kf, s.cols * s.tokens));
+        p.dw = shape_of(s.cols, p.rows_w, p.kn, p.products, true, least(p.kn, s.cols * p.rows_w));
     }
     return p;
 }
