@@ -242,7 +242,7 @@ jorge_status jorge_gated_linear_backward(const jorge_linear_shape* shape, const 
  * see few keys, delta is the sum of p (do v^T), as o's rounding would not average out in it. fp32 is multiplied in
  * fp32. */
 
-/* Largest dim, tokens, token stride, and batch * heads * tokens (of q or of k). */
+/* Largest dim, tokens, token stride, and rows: batch * heads * q_tokens of q, batch * kv_heads * kv_tokens of k. */
 #define JORGE_ATTENTION_MAX_DIM    128
 #define JORGE_ATTENTION_MAX_TOKENS (1 << 22)
 #define JORGE_ATTENTION_MAX_STRIDE (1 << 22)

@@ -1267,10 +1267,13 @@ jorge_status check(const jorge_attention_shape* shape) {
     if (s.window && !s.causal) return bad("attention: a window needs causal");
     if (s.q_tokens > JORGE_ATTENTION_MAX_TOKENS || s.kv_tokens > JORGE_ATTENTION_MAX_TOKENS)
         return refuse(JORGE_ERR_UNSUPPORTED, "attention: tokens above JORGE_ATTENTION_MAX_TOKENS");
-    // Lengths of launches: tiles of 128 rows, rows by the eight, copies' pieces by the 256.
+    // Lengths of launches: tiles of 128 rows, rows by the eight, copies' pieces by the 256; k and v have kv_heads.
     if (s.batch > 1 << 20 || s.heads > 1 << 20 || s.batch * s.heads > 1 << 22 ||
-        s.batch * s.heads * std::max<int64_t>(s.q_tokens, s.kv_tokens) > JORGE_ATTENTION_MAX_ROWS)
-        return refuse(JORGE_ERR_UNSUPPORTED, "attention: batch * heads * tokens above JORGE_ATTENTION_MAX_ROWS (2^26)");
+        s.batch * s.heads * s.q_tokens > JORGE_ATTENTION_MAX_ROWS)
+        return refuse(JORGE_ERR_UNSUPPORTED, "attention: batch * heads * q_tokens above JORGE_ATTENTION_MAX_ROWS (2^26)");
+    if (s.batch * s.kv_heads * s.kv_tokens > JORGE_ATTENTION_MAX_ROWS)
+        return refuse(JORGE_ERR_UNSUPPORTED,
+                      "attention: batch * kv_heads * kv_tokens above JORGE_ATTENTION_MAX_ROWS (2^26)");
     return JORGE_OK;
 }
 jorge_status check_inputs(const jorge_attention_shape& s) {

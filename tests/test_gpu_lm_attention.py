@@ -384,3 +384,16 @@ def test_bfloat16_gradients_where_rows_see_few_keys(batch, n, m, heads, kv_heads
     for got, ref in zip(lm.attention_backward(dout, q, k, v, out, lse, **how)[:2], want):
         off = float((got.double() - ref).norm() / ref.norm())
         assert off < 2 ** 0.5 * 2 ** -8 / 3 ** 0.5, off
+
+
+def test_many_sequences_over_long_caches_of_shared_heads():
+    """64 sequences of 64 heads over 8: 2^27 rows counted with q's heads, 2^24 of k and v."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    q = torch.randn(64, 1, 64, 8, generator=g, device="cuda").bfloat16()
+    k, v = (torch.randn(64, 32768, 8, 8, generator=g, device="cuda").bfloat16() for _ in range(2))
+    kl = torch.randint(1, 32769, (64,), generator=g, device="cuda")
+    out, lse = lm.attention_forward(q, k, v, causal=True, kv_lengths=kl)
+    for n in (0, 41, 63):
+        want = plain(q[n:n + 1], k[n:n + 1], v[n:n + 1], causal=True, kl=kl[n:n + 1])
+        within(lse[n:n + 1], want["lse"], want["lse_off"] / U32, 1, "lse")
+        within(out[n:n + 1], want["out"], want["out_off"] / U32, 1, "out")

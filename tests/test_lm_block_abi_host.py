@@ -179,6 +179,23 @@ def test_attention_workspaces(lib):  # noqa: F811
     assert size(batch=0) == 0
 
 
+def test_rows_of_q_and_of_k_are_limited_each_by_its_own_heads(lib):  # noqa: F811
+    """A step of generation for many sequences has few rows of q, with all heads, and many of k, with kv_heads."""
+    most = defined("JORGE_ATTENTION_MAX_ROWS")
+    n = I64()
+
+    def status(dout=None, **kw):
+        return lib.jorge_attention_workspace(ctypes.byref(attention_shape(**kw)), dout, ctypes.byref(n))
+    for batch, kv in ((64, 32768), (16, 131072)):
+        step = dict(batch=batch, q=1, kv=kv, heads=64, kv_heads=8, dim=128)
+        assert batch * 64 * kv > most >= batch * 8 * kv
+        assert status(**step) == 0 and status(heads(), **step) == 0
+    assert status(batch=1 << 10, q=1, kv=most >> 13, heads=64, kv_heads=8) == 0
+    refused(lib, status(batch=1 << 10, q=1, kv=(most >> 13) + 1, heads=64, kv_heads=8), UNSUPPORTED, "kv_heads")
+    assert status(batch=1 << 10, q=most >> 16, kv=1, heads=64, kv_heads=8) == 0
+    refused(lib, status(batch=1 << 10, q=(most >> 16) + 1, kv=1, heads=64, kv_heads=8), UNSUPPORTED, "q_tokens")
+
+
 @NO_GPU
 @pytest.mark.parametrize("dtype", [0, 1])
 def test_the_largest_sizes_are_launched(lib, dtype):  # noqa: F811
