@@ -169,11 +169,13 @@ jorge_status jorge_cross_entropy_backward(const jorge_loss_shape* shape, const f
  *   linear:        dz = dy act'(z),  dx = dz weight,  dweight = dz^T x,  dbias = sum over tokens of dz
  *                  (the residual's gradient is dy);
  *   gated linear:  dg = dy u act'(g),  du = dy act(g),  dx = dg gate + du up,  dgate = dg^T x,  dup = du^T x.
- * relu's derivative at 0 is 0. bfloat16: dz, dg and du are rounded to bfloat16 for the products, whose sums are fp32
- * (dbias is summed before that); a gradient then errs by some 2.4e-3 of its size instead of the 1.7e-3 of its own
- * rounding. fp32: up to JORGE_LINEAR_FEW_TOKENS forward are multiplied in fp32; the other products are formed from
- * three-term bfloat16 splits as the Jorge step's are (jorge.h): values above 3.39e38 count as infinite. Their sums over
- * more than 1024 terms are formed in up to eight ranges, of which the workspace holds up to 1 GiB. */
+ * relu's derivative at 0 is 0. gelu's normal distribution errs in fp32 by at most 20 roundings of itself, also in its
+ * tails, and in bfloat16 by 3e-7 of 1, which shows below arguments of -5. bfloat16: dz, dg and du are rounded to bfloat16
+ * for the products, whose sums are fp32 (dbias is summed before that); a gradient then errs by some 2.4e-3 of its size
+ * instead of the 1.7e-3 of its own rounding. fp32: up to JORGE_LINEAR_FEW_TOKENS forward are multiplied in fp32; the
+ * other products are formed from three-term bfloat16 splits as the Jorge step's are (jorge.h): values above 3.39e38
+ * count as infinite. Their sums over more than 1024 terms are formed in up to eight ranges, of which the workspace holds
+ * up to 1 GiB. */
 #define JORGE_ACT_NONE    0
 #define JORGE_ACT_RELU    1
 #define JORGE_ACT_GELU    2

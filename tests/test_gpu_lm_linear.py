@@ -388,3 +388,19 @@ def test_single_gradients_of_few_tiles_of_long_rows():
     assert torch.equal(lm.gated_linear_backward(dy, x, w, u, need_weights=False)[0], every[0])
     for one, both in zip(lm.gated_linear_backward(dy, x, w, u, need_x=False)[1:], every[1:]):
         assert torch.equal(one, both)
+
+
+@pytest.mark.parametrize("tokens", [60, 2400])
+def test_gelu_in_fp32_keeps_its_relative_precision(tokens):
+    """gelu(z) = z Phi(z) is as small as Phi for z below 0, and its derivative Phi + z phi is their sum. A tail in fp32
+    is off by 12 roundings of its polynomial, reciprocal and argument (evaluated on the host), 4 of the exponential and 2
+    of a reciprocal that is one unit in the last place off; two more are the products'. Its argument and the matrix
+    products are exact here (one column, weights of one)."""
+    z = torch.linspace(-10, 4, 2400, device="cuda")
+    z = z if tokens > lm.LINEAR_FEW_TOKENS else z[::40]
+    x, one, zz = z[:, None].contiguous(), torch.ones(1, 1, device="cuda"), z.double().cpu()
+    Phi, phi = 0.5 * torch.special.erfc(-zz / 2 ** 0.5), torch.exp(-0.5 * zz * zz) / (2 * torch.pi) ** 0.5
+    within(lm.linear_forward(x, one, None, "gelu")[:, 0], zz * Phi, zz.abs() * Phi, 20, "gelu")
+    within(lm.gated_linear_forward(x, one, one, "gelu")[:, 0], zz * zz * Phi, zz * zz * Phi, 21, "gated gelu")
+    dx = lm.linear_backward(torch.ones_like(x), x, one, None, "gelu", need_weight=False)[0]
+    within(dx[:, 0], Phi + zz * phi, Phi + zz.abs() * phi, 20, "gelu'")
