@@ -154,8 +154,9 @@ jorge_status jorge_cross_entropy_forward(const jorge_loss_shape* shape, const vo
  * number) is rounded to bfloat16 for the two products, whose sums are fp32: rows of dweight of words that are
  * no row's target, sums of such rounded terms alone, err by some 2.2e-3 of their size instead of the 1.7e-3 of
  * their own rounding; dhidden and the other rows by 1.7e-3. fp32 inputs: every product is formed from three-term
- * bfloat16 splits as the Jorge step's are (jorge.h), dz included: values above 3.39e38 count as infinite, and a
- * sum over K elements takes 6 K / 32 roundings of its fp32 accumulator. */
+ * bfloat16 splits as the Jorge step's are (jorge.h), dz included: values above 3.39e38 count as infinite, a
+ * product of two infinities or a sum beyond fp32's range may be NaN, and a sum over K elements takes 6 K / 32
+ * roundings of its fp32 accumulator. */
 jorge_status jorge_cross_entropy_backward(const jorge_loss_shape* shape, const float* grad, int32_t kind,
                                           const void* hidden, const void* weight, const int64_t* targets,
                                           const float* lse, const float* total, void* dhidden, void* dweight,
@@ -174,8 +175,8 @@ jorge_status jorge_cross_entropy_backward(const jorge_loss_shape* shape, const f
  * for the products, whose sums are fp32 (dbias is summed before that); a gradient then errs by some 2.4e-3 of its size
  * instead of the 1.7e-3 of its own rounding. fp32: up to JORGE_LINEAR_FEW_TOKENS forward are multiplied in fp32; the
  * other products are formed from three-term bfloat16 splits as the Jorge step's are (jorge.h): values above 3.39e38
- * count as infinite. Their sums over more than 1024 terms are formed in up to eight ranges, of which the workspace holds
- * up to 1 GiB. */
+ * count as infinite, and a product of two infinities or a sum beyond fp32's range may be NaN. Their sums over more than
+ * 1024 terms are formed in up to eight ranges, of which the workspace holds up to 1 GiB. */
 #define JORGE_ACT_NONE    0
 #define JORGE_ACT_RELU    1
 #define JORGE_ACT_GELU    2

@@ -608,7 +608,7 @@ __global__ __launch_bounds__(256, 1) void dense_dz_kernel(Dense d, const T* __re
                         typedef __bf16 V __attribute__((ext_vector_type(WA)));
                         V o;
 #pragma unroll
-                        for (int j = 0; j < WA; ++j) o[j] = (bf16)t.acc[i / 4 + m * kUp][j][i & 3];
+                        for (int j = 0; j < WA; ++j) o[j] = term_of(t.acc[i / 4 + m * kUp][j][i & 3], term == terms - 1);
                         *reinterpret_cast<V*>(dzt + (m * outs + a0 + i) * terms * out.kn) = o;
                     }
         }
@@ -618,7 +618,7 @@ __global__ __launch_bounds__(256, 1) void dense_dz_kernel(Dense d, const T* __re
 #pragma unroll
                 for (int i = 0; i < WA; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) t.acc[i][j][r] -= (float)(bf16)t.acc[i][j][r];
+                    for (int r = 0; r < 4; ++r) t.acc[i][j][r] -= (float)term_of(t.acc[i][j][r], false);
     }
 }
 

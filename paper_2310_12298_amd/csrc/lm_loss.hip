@@ -261,7 +261,7 @@ __global__ __launch_bounds__(256, 1) void loss_dz_kernel(Product p, LossRows row
                 for (int i = 0; i < WA; i += 2) {
                     bf16x8 o;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) o[e] = (bf16)t.acc[i + e / 4][j][e & 3];
+                    for (int e = 0; e < 8; ++e) o[e] = term_of(t.acc[i + e / 4][j][e & 3], term == terms - 1);
                     if (a0 + 4 * i < out.words)
                         *reinterpret_cast<bf16x8*>(dz + (b0 + j) * terms * out.words + 4 * i) = o;
                 }
@@ -274,7 +274,7 @@ __global__ __launch_bounds__(256, 1) void loss_dz_kernel(Product p, LossRows row
                         typedef __bf16 V __attribute__((ext_vector_type(WB)));
                         V o;
 #pragma unroll
-                        for (int j = 0; j < WB; ++j) o[j] = (bf16)t.acc[i][j][r];
+                        for (int j = 0; j < WB; ++j) o[j] = term_of(t.acc[i][j][r], term == terms - 1);
                         *reinterpret_cast<V*>(dzt + (a0 + 4 * i + r) * terms * out.tokens) = o;
                     }
         if constexpr (SPLIT)
@@ -283,7 +283,7 @@ __global__ __launch_bounds__(256, 1) void loss_dz_kernel(Product p, LossRows row
 #pragma unroll
                 for (int i = 0; i < WA; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) t.acc[i][j][r] -= (float)(bf16)t.acc[i][j][r];
+                    for (int r = 0; r < 4; ++r) t.acc[i][j][r] -= (float)term_of(t.acc[i][j][r], false);
     }
 }
 

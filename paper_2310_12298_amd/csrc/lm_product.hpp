@@ -6,6 +6,8 @@
 #include "lm_common.hpp"
 #include "lm_loss_gemm.hpp"
 
+#include <math.h>
+
 #include <algorithm>
 
 namespace jorge_lm {
@@ -33,6 +35,13 @@ struct CopyJobs {
     Copies job[kCopyJobs];
 };
 
+// The next term of a split value, of which the terms before it have been subtracted. One that is infinite, or would be
+// rounded to that, is its last term alone: the last term meets only the first one of the other operand, whose sign is the
+// element's, while an infinite first term would meet the others' zeros and signs and make a NaN.
+__device__ __forceinline__ bf16 term_of(float f, bool last) {
+    const bf16 o = (bf16)f;
+    return last || __builtin_fabsf((float)o) < INFINITY ? o : (bf16)0.0f;
+}
 template <int TERMS>
 __device__ __forceinline__ void store_terms(bf16* dst, int64_t plane, float (&f)[8]) {
 #pragma unroll
@@ -40,7 +49,7 @@ __device__ __forceinline__ void store_terms(bf16* dst, int64_t plane, float (&f)
         bf16x8 o;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            o[e] = (bf16)f[e];
+            o[e] = term_of(f[e], t == TERMS - 1);
             f[e] -= (float)o[e];
         }
         *reinterpret_cast<bf16x8*>(dst + t * plane) = o;

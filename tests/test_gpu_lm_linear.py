@@ -15,6 +15,7 @@ from paper_2310_12298_amd import lm  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 F32, BF16 = torch.float32, torch.bfloat16
+INF = float("inf")
 SLOPE, BEND, OWN = 1.13, 0.8, 16
 SIZES = [(1, 1, 1), (1, 33, 17), (3, 64, 128), (16, 100, 40), (17, 256, 65), (33, 515, 130), (64, 129, 96),
          (65, 64, 64), (70, 7, 300), (130, 1, 2), (200, 1023, 255), (257, 512, 513), (1025, 96, 320)]
@@ -404,3 +405,45 @@ def test_gelu_in_fp32_keeps_its_relative_precision(tokens):
     within(lm.gated_linear_forward(x, one, one, "gelu")[:, 0], zz * zz * Phi, zz * zz * Phi, 21, "gated gelu")
     dx = lm.linear_backward(torch.ones_like(x), x, one, None, "gelu", need_weight=False)[0]
     within(dx[:, 0], Phi + zz * phi, Phi + zz.abs() * phi, 20, "gelu'")
+
+
+def test_infinities_in_fp32_products_of_many_tokens():
+    """An infinite element, or one that counts as such, makes infinities of the signs that the formula gives, and leaves
+    all else as it is: as it does where few tokens are multiplied in fp32."""
+    g = torch.Generator().manual_seed(6)
+    n, d, f = 90, 40, 72
+    x, w, u, dy = (rand(g, *s, d=F32) for s in ((n, d), (f, d), (f, d), (n, f)))
+    clean = lm.linear_forward(x, w)
+    few = [lm.linear_forward(x[:5], w), lm.linear_backward(dy, x, w)]
+    for big in (INF, -INF, 3.4e38):
+        for which in (x, w):
+            a, b = x.clone(), w.clone()
+            (a if which is x else b)[3, 7] = big
+            y, want = lm.linear_forward(a, b), a.double() @ b.double().t()
+            at = torch.zeros(n, f, dtype=torch.bool, device="cuda")
+            at[(3,) if which is x else (slice(None), 3)] = True
+            want = torch.sign(want) * INF
+            assert torch.equal(y[at].double(), want[at]) and torch.equal(y[~at], clean[~at])
+            if abs(big) == INF:
+                y = lm.linear_forward(a[:5], b)
+                assert torch.equal(y[at[:5]].double(), want[:5][at[:5]]) and torch.equal(y[~at[:5]], few[0][~at[:5]])
+        G = dy.clone()
+        G[11, 5] = big
+        dx, dw, _ = lm.linear_backward(G, x, w)
+        assert torch.equal(dx[11], torch.sign(w[5]) * big * INF) and torch.equal(dw[5], torch.sign(x[11]) * big * INF)
+        for got, ref, row in ((dx, few[1][0], 11), (dw, few[1][1], 5)):
+            keep = torch.arange(got.shape[0], device="cuda") != row
+            assert torch.equal(got[keep], ref[keep])
+    # With an activation: dz is split from the registers that formed it. u and g of the row are above 0 there.
+    G, v = dy.clone(), x[11].sign() * w[5].abs() + 0.5 * x[11]
+    w[5], u[5] = v, v
+    ref = [lm.linear_backward(dy, x, w, None, "relu"), lm.gated_linear_backward(dy, x, w, u, "relu")]
+    G[11, 5] = INF
+    got = [lm.linear_backward(G, x, w, None, "relu"), lm.gated_linear_backward(G, x, w, u, "relu")]
+    for a, b, rows in zip(got, ref, ((11, 5, None), (11, 5, 5))):
+        for t, s, row in zip(a, b, rows):
+            if t is not None:
+                want = torch.sign(x[11] if row == 5 else w[5]) * INF
+                assert torch.equal(t[row], want)
+                keep = torch.arange(t.shape[0], device="cuda") != row
+                assert torch.equal(t[keep], s[keep])

@@ -141,3 +141,17 @@ def test_autograd_forms_only_the_gradients_that_are_asked_for():
         want = want or [x.grad, y.grad]
         for g, ref, asked in ((x.grad, want[0], a), (y.grad, want[1], b)):
             assert torch.equal(g, ref) if asked else g is None
+
+
+def test_an_infinite_weight_in_fp32_takes_its_word_from_rows_where_the_logit_is_minus_infinity():
+    """As a weight so large that the word's probability is 0 there does: to the bit."""
+    h, w, t = inputs(90, 72, 300, F32)
+    t[t == 3] = 4
+    rows = h[:, 5] < 0
+    lost = []
+    for big in (1e30, 3.4e38, float("inf")):
+        w[3, 5] = big
+        lost.append([x[rows] for x in lm.cross_entropy_forward(h, w, t, label_smoothing=0.0)[:2]])
+    assert bool(torch.isfinite(lost[0][1]).all()) and int(rows.sum()) > 20
+    for other in lost[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(lost[0], other))
