@@ -176,7 +176,8 @@ jorge_status jorge_cross_entropy_backward(const jorge_loss_shape* shape, const f
  * instead of the 1.7e-3 of its own rounding. fp32: up to JORGE_LINEAR_FEW_TOKENS forward are multiplied in fp32; the
  * other products are formed from three-term bfloat16 splits as the Jorge step's are (jorge.h): values above 3.39e38
  * count as infinite, and a product of two infinities or a sum beyond fp32's range may be NaN. Their sums over more than
- * 1024 terms are formed in up to eight ranges, of which the workspace holds up to 1 GiB. */
+ * 1024 terms (2048 where z is formed again) are formed in up to eight ranges, of which a call's workspace holds up to
+ * 1 GiB at a time. */
 #define JORGE_ACT_NONE    0
 #define JORGE_ACT_RELU    1
 #define JORGE_ACT_GELU    2

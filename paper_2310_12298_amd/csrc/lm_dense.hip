@@ -788,7 +788,7 @@ bool weights_readable(const jorge_linear_shape& s, int mats, const void* weight,
 
 // fp32: the fewest ranges of a sum over K, a power of two. The accumulator's roundings leave an error that grows with the
 // root of K, 7e-7 of the sum at 2048 and 1.4e-6 at 8192; ranges of 1024 stay at 5e-7. Eight at most, and no more than
-// 1 GiB of them, as each is kept in 32 bits (`sums` of them to a range; 0: in registers).
+// 1 GiB of them, as each is kept in 32 bits (`sums` of them to a range, with the padding of its rows; 0: in registers).
 int64_t ranges_for(int64_t k, int64_t sums) {
     int64_t r = 1;
     while (r < 8 && r * 1024 < k && 2 * r * sums * 4 <= int64_t(1) << 30) r *= 2;
@@ -811,7 +811,7 @@ Plan plan_of(const jorge_linear_shape& s, int mats, const Wanted& want, bool dir
     p.turn = p.terms == 1;
     p.rows_w = mats * (p.turn ? p.kf : s.outs);
     const auto least = [&](int64_t k, int64_t sums) { return p.terms == 1 ? 1 : ranges_for(k, sums); };
-    const int64_t sums_z = mats * s.outs * s.tokens;
+    const int64_t sums_z = mats * round_up(s.outs, 4) * s.tokens, wide = round_up(s.cols, 4);
     p.z = shape_of(mats * s.outs, s.tokens, p.kd, p.products, !want.backward, want.backward ? 1 : least(p.kd, sums_z));
     p.chunks = 1;
     if (want.backward && least(p.kd, 0) > 2) {
@@ -834,8 +834,8 @@ Plan plan_of(const jorge_linear_shape& s, int mats, const Wanted& want, bool dir
     // A pair's tile of 64 x 64 holds 32 columns of each, which padding to 64 would leave without a tile.
     if (mats == 2 && p.z.blocks == 2) p.z.blocks = 4;
     if (want.backward) {
-        p.dx = shape_of(s.cols, s.tokens, mats * p.kf, p.products, true, least(mats * p.kf, s.cols * s.tokens));
-        p.dw = shape_of(s.cols, p.rows_w, p.kn, p.products, true, least(p.kn, s.cols * p.rows_w));
+        p.dx = shape_of(s.cols, s.tokens, mats * p.kf, p.products, true, least(mats * p.kf, wide * s.tokens));
+        p.dw = shape_of(s.cols, p.rows_w, p.kn, p.products, true, least(p.kn, wide * p.rows_w));
     }
     return p;
 }
@@ -844,7 +844,7 @@ struct Work {
     bf16 *x, *w, *u;          // K-contiguous copies
     bf16 *xt, *wt;            // transposes; wt: of both matrices side by side
     bf16 *dz, *dzt;
-    float *z, *dx, *dw;       // slices
+    float *z, *dx, *dw;       // slices; the three of a backward pass, each used up before the next, in one place
     float* bias;
     int64_t bytes, ldz, ldc;
 };
@@ -868,13 +868,17 @@ Work carve(void* base, const jorge_linear_shape& s, const Plan& p, const Wanted&
         if (!p.few && p.z.ranges > 1) w.z = c.take<float>(p.z.ranges * s.tokens * w.ldz);
     } else {
         const bool dz = want.dx || (p.turn && want.dw);
-        if (p.cut && z) w.z = c.take<float>(p.z.ranges * s.tokens * w.ldz);
+        const int64_t slices_z = p.cut && z ? p.z.ranges * s.tokens * w.ldz : 0;
+        const int64_t slices_dx = want.dx && p.dx.ranges > 1 ? p.dx.ranges * s.tokens * w.ldc : 0;
+        const int64_t slices_dw = want.dw && p.dw.ranges > 1 ? p.dw.ranges * p.rows_w * w.ldc : 0;
         if (want.dw && !p.turn) w.xt = c.take<bf16>(p.terms * s.cols * p.kn);
         if (want.dx && !p.turn) w.wt = c.take<bf16>(p.terms * s.cols * p.mats * p.kf);
         if (dz && (p.dz || !p.direct_dy)) w.dz = c.take<bf16>(p.terms * s.tokens * p.mats * p.kf);
         if (want.dw && !p.turn) w.dzt = c.take<bf16>(p.terms * p.mats * s.outs * p.kn);
-        if (want.dx && p.dx.ranges > 1) w.dx = c.take<float>(p.dx.ranges * s.tokens * w.ldc);
-        if (want.dw && p.dw.ranges > 1) w.dw = c.take<float>(p.dw.ranges * p.rows_w * w.ldc);
+        float* const slices = c.take<float>(std::max({slices_z, slices_dx, slices_dw}));
+        if (slices_z) w.z = slices;
+        if (slices_dx) w.dx = slices;
+        if (slices_dw) w.dw = slices;
         if (want.db) w.bias = c.take<float>(bias_parts(s, p) * s.outs);
     }
     w.bytes = c.used;

@@ -107,6 +107,21 @@ def test_linear_workspaces(lib):  # noqa: F811
     assert size(1, 1, tokens=8192, cols=2048, outs=8192, act=3) < most
 
 
+@pytest.mark.parametrize("gated,act", [(0, 0), (0, 3), (1, 3)])
+@pytest.mark.parametrize("tokens,cols,outs", [(8192, 8192, 8192), (1515, 7854, 230), (1950000, 17, 8200),
+                                              (130, 4001, 70), (4096, 2048, 1 << 17)])
+def test_ranges_of_fp32_sums_take_at_most_a_gibibyte(lib, tokens, cols, outs, gated, act):  # noqa: F811
+    """Beside the copies of three bfloat16 terms an element, of rows padded to 64, and dbias's parts."""
+    n = I64()
+    s = linear_shape(tokens=tokens, cols=cols, outs=outs, dtype=0, act=act)
+    assert lib.jorge_linear_workspace(ctypes.byref(s), gated, 1, ctypes.byref(n)) == 0
+    mats, (kd, kf, kn) = 1 + gated, (-(-v // 64) * 64 for v in (cols, outs, tokens))
+    again = tokens * kd + mats * outs * kd if gated or act else 0       # for z, formed again
+    terms = again + cols * kn + cols * mats * kf + tokens * mats * kf + mats * outs * kn
+    parts = 0 if gated else (tokens // (32 if act else 128) + 2) * outs
+    assert n.value <= 6 * terms + 4 * parts + (1 << 30) + (1 << 13)
+
+
 def attention_shape(batch=2, q=5, kv=9, heads=4, kv_heads=2, dim=16, dtype=1, scale=0.25, causal=0, window=0, ql=None,
                     kl=None, qp=A, kp=A, vp=A, token=256, head=16):
     at = (token * 16, token, head)
