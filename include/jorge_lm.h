@@ -203,8 +203,20 @@ typedef struct jorge_linear_shape {
 } jorge_linear_shape;
 
 /* Bytes of workspace of the forward (backward = 0) or backward pass of the linear (gated = 0) or gated linear layer
- * (host pointers); 0 where none is needed. */
+ * (host pointers), of any addresses and with all gradients; 0 where none is needed. */
 jorge_status jorge_linear_workspace(const jorge_linear_shape* shape, int32_t gated, int32_t backward, int64_t* bytes);
+
+/* The gradients that a call of the backward pass asks for (DWEIGHT: of both weights of the gated linear layer). */
+#define JORGE_LINEAR_DX      1
+#define JORGE_LINEAR_DWEIGHT 2
+#define JORGE_LINEAR_DBIAS   4
+
+/* Bytes of workspace of one call, of the linear (up NULL) or gated linear layer, forward (dy NULL) or backward with the
+ * gradients `wanted`: at most what jorge_linear_workspace tells. A call needs no copies of bfloat16 operands whose rows
+ * and strides are whole multiples of 64 (rows) and 8 (strides) elements, at 16-byte alignment (gate and up: of one
+ * stride). The pointers are not followed. */
+jorge_status jorge_linear_call_workspace(const jorge_linear_shape* shape, const void* dy, const void* x,
+                                         const void* weight, const void* up, int32_t wanted, int64_t* bytes);
 
 /* shape: host. bias: outs elements, residual: tokens x outs; each may be NULL. y may be residual (with ldy = ldr). */
 jorge_status jorge_linear_forward(const jorge_linear_shape* shape, const void* x, const void* weight, const void* bias,

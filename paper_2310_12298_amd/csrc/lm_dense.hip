@@ -884,7 +884,14 @@ Work carve(void* base, const jorge_linear_shape& s, const Plan& p, const Wanted&
     w.bytes = c.used;
     return w;
 }
-// What serves in place depends on addresses: room for every copy is asked for.
+// The plan of a call: what lies in whole pieces of 16 bytes is read in place. dy null: forward.
+Plan plan_of(const jorge_linear_shape& s, const Wanted& want, const void* dy, const void* x, const void* weight,
+             const void* up) {
+    const int mats = up ? 2 : 1;
+    return plan_of(s, mats, want, readable(s.dtype, s.cols, x, s.ldx), weights_readable(s, mats, weight, up),
+                   dy && readable(s.dtype, s.outs, dy, s.ldy));
+}
+// Of any addresses and all gradients.
 int64_t workspace_of(const jorge_linear_shape& s, int mats, bool backward) {
     const Wanted want{backward, backward, backward, backward && mats == 1};
     return carve(nullptr, s, plan_of(s, mats, want, false, false, false), want).bytes;
@@ -1072,9 +1079,7 @@ jorge_status check(const jorge_linear_shape* s, bool gated) {
     }
     return JORGE_OK;
 }
-jorge_status check_workspace(const jorge_linear_shape& s, int mats, bool backward, const void* workspace,
-                             int64_t bytes) {
-    const int64_t need = workspace_of(s, mats, backward);
+jorge_status check_workspace(int64_t need, const void* workspace, int64_t bytes) {
     if (need == 0) return JORGE_OK;
     if (!workspace || !aligned(workspace, kAlign)) return bad("linear: a workspace aligned to 256 bytes is needed");
     if (bytes < need) return bad("linear: the workspace is too small");
@@ -1090,11 +1095,10 @@ jorge_status run_forward(const jorge_linear_shape& s, int mats, const void* x, c
         !aligned(bias, dtype_bytes(s.bias_dtype)))
         return bad("linear: a pointer is not aligned to its element");
     if (residual && (s.ldr < s.outs)) return bad("linear: a row stride is below its columns");
-    const jorge_status st = check_workspace(s, mats, false, workspace, bytes);
-    if (st != JORGE_OK) return st;
     const Wanted want{false, false, false, false};
-    const bool direct_w = weights_readable(s, mats, weight, up);
-    const Plan p = plan_of(s, mats, want, readable(s.dtype, s.cols, x, s.ldx), direct_w, false);
+    const Plan p = plan_of(s, want, nullptr, x, weight, up);
+    const jorge_status st = check_workspace(carve(nullptr, s, p, want).bytes, workspace, bytes);
+    if (st != JORGE_OK) return st;
     const Work w = carve(workspace, s, p, want);
     const hipStream_t q = reinterpret_cast<hipStream_t>(stream);
     const Bias b{bias, s.bias_dtype == JORGE_BF16};
@@ -1139,13 +1143,11 @@ jorge_status run_backward(const jorge_linear_shape& s, int mats, const void* dy,
     if (!dy || !x || !weight || (mats == 2 && !up)) return bad("linear: dy, x and the weights are needed");
     if (!aligned(dy, e) || !aligned(x, e) || !aligned(weight, e) || !aligned(up, e))
         return bad("linear: a pointer is not aligned to its element");
-    const jorge_status st = check_workspace(s, mats, true, workspace, bytes);
-    if (st != JORGE_OK) return st;
     const Wanted want{true, g.dx != nullptr, g.dweight != nullptr, g.dbias != nullptr};
     if (!want.dx && !want.dw && !want.db) return JORGE_OK;
-    const bool direct_w = weights_readable(s, mats, weight, up);
-    const Plan p = plan_of(s, mats, want, readable(s.dtype, s.cols, x, s.ldx), direct_w,
-                           readable(s.dtype, s.outs, dy, s.ldy));
+    const Plan p = plan_of(s, want, dy, x, weight, up);
+    const jorge_status st = check_workspace(carve(nullptr, s, p, want).bytes, workspace, bytes);
+    if (st != JORGE_OK) return st;
     const Work w = carve(workspace, s, p, want);
     const Bias b{bias, s.bias_dtype == JORGE_BF16};
     if (s.dtype == JORGE_F32)
@@ -1167,6 +1169,18 @@ jorge_status jorge_linear_workspace(const jorge_linear_shape* shape, int32_t gat
     const jorge_status st = check(shape, gated != 0);
     if (st != JORGE_OK) return st;
     *bytes = shape->tokens ? workspace_of(*shape, gated ? 2 : 1, backward != 0) : 0;
+    return JORGE_OK;
+}
+
+jorge_status jorge_linear_call_workspace(const jorge_linear_shape* shape, const void* dy, const void* x,
+                                         const void* weight, const void* up, int32_t wanted, int64_t* bytes) {
+    if (!bytes) return bad("linear: bytes is needed");
+    const jorge_status st = check(shape, up != nullptr);
+    if (st != JORGE_OK) return st;
+    const Wanted want{dy != nullptr, dy && (wanted & JORGE_LINEAR_DX), dy && (wanted & JORGE_LINEAR_DWEIGHT),
+                      dy && !up && (wanted & JORGE_LINEAR_DBIAS)};
+    const bool any = !dy || want.dx || want.dw || want.db;
+    *bytes = shape->tokens && any ? carve(nullptr, *shape, plan_of(*shape, want, dy, x, weight, up), want).bytes : 0;
     return JORGE_OK;
 }
 

@@ -76,6 +76,7 @@ _SIGNATURES = {
     "jorge_cross_entropy_forward": (_I32, [_PS, _P, _P, _P, _P, _P, _P, _P, _I64, _P]),
     "jorge_cross_entropy_backward": (_I32, [_PS, _P, _I32, _P, _P, _P, _P, _P, _P, _P, _P, _I64, _P]),
     "jorge_linear_workspace": (_I32, [_PL, _I32, _I32, ctypes.POINTER(_I64)]),
+    "jorge_linear_call_workspace": (_I32, [_PL, _P, _P, _P, _P, _I32, ctypes.POINTER(_I64)]),
     "jorge_linear_forward": (_I32, [_PL, _P, _P, _P, _P, _P, _P, _I64, _P]),
     "jorge_linear_backward": (_I32, [_PL, _P, _P, _P, _P, _P, _I64, _P, _I64, _P, _P, _I64, _P]),
     "jorge_gated_linear_forward": (_I32, [_PL, _P, _P, _P, _P, _P, _I64, _P]),
@@ -392,6 +393,7 @@ def linear_cross_entropy(hidden, weight, targets, ignore_index=-100, label_smoot
 # ---------------------------------------------------------------- linear layers
 LINEAR_MAX_STRIDE = 1 << 22                   # JORGE_LINEAR_MAX_STRIDE
 LINEAR_FEW_TOKENS = 64                        # JORGE_LINEAR_FEW_TOKENS
+LINEAR_DX, LINEAR_DWEIGHT, LINEAR_DBIAS = 1, 2, 4  # JORGE_LINEAR_DX ...
 
 
 def _rows(t, what):
@@ -425,9 +427,12 @@ def _linear_shape(m, w, u, ldy, ldr, bias, activation):
                        0 if bias is None else DTYPES[bias.dtype], activation, 0)
 
 
-def _linear_workspace(lib, shape, gated, backward):
+def _linear_workspace(lib, shape, dy, x, weight, up=None, need_x=False, need_weight=False, need_bias=False):
+    """What a call needs; dy is None forward."""
     n = _I64(0)
-    _check(lib, lib.jorge_linear_workspace(ctypes.byref(shape), gated, backward, ctypes.byref(n)))
+    _check(lib, lib.jorge_linear_call_workspace(ctypes.byref(shape), _ptr(dy), x.data_ptr(), weight.data_ptr(), _ptr(up),
+                                                LINEAR_DX * bool(need_x) + LINEAR_DWEIGHT * bool(need_weight) +
+                                                LINEAR_DBIAS * bool(need_bias), ctypes.byref(n)))
     return _workspace(n.value), n.value
 
 
@@ -447,7 +452,7 @@ def linear_forward(x, weight, bias=None, activation=None, residual=None):
         r = _rows(residual, "residual")
     y = x.new_empty(shape_y)
     shape = _linear_shape(m, w, w, outs, outs if r is None else _ld(r), b, act)
-    ws, n = (None, 0) if shape.tokens <= LINEAR_FEW_TOKENS else _linear_workspace(lib, shape, 0, 0)
+    ws, n = (None, 0) if shape.tokens <= LINEAR_FEW_TOKENS else _linear_workspace(lib, shape, None, m, w)
     _check(lib, lib.jorge_linear_forward(ctypes.byref(shape), m.data_ptr(), w.data_ptr(), _ptr(b), _ptr(r),
                                          y.data_ptr(), _ptr(ws), n, _stream(x)))
     return y
@@ -468,7 +473,7 @@ def linear_backward(dy, x, weight, bias=None, activation=None, need_x=True, need
     dw = torch.empty((outs, cols), dtype=x.dtype, device=x.device) if need_weight else None
     db = torch.empty(outs, dtype=b.dtype, device=x.device) if need_bias and b is not None else None
     shape = _linear_shape(m, w, w, _ld(d), outs, b, act)
-    ws, n = _linear_workspace(lib, shape, 0, 1)
+    ws, n = _linear_workspace(lib, shape, d, m, w, None, need_x, need_weight, db is not None)
     _check(lib, lib.jorge_linear_backward(ctypes.byref(shape), d.data_ptr(), m.data_ptr(), w.data_ptr(), _ptr(b),
                                           _ptr(dx), cols, _ptr(dw), cols, _ptr(db), _ptr(ws), n, _stream(x)))
     return dx, dw, db
@@ -502,7 +507,7 @@ def gated_linear_forward(x, gate, up, activation="silu"):
     m, (g, u) = _weights(x, [(gate, "gate"), (up, "up")])
     y = x.new_empty(x.shape[:-1] + (g.shape[0],))
     shape = _linear_shape(m, g, u, g.shape[0], g.shape[0], None, act)
-    ws, n = (None, 0) if shape.tokens <= LINEAR_FEW_TOKENS else _linear_workspace(lib, shape, 1, 0)
+    ws, n = (None, 0) if shape.tokens <= LINEAR_FEW_TOKENS else _linear_workspace(lib, shape, None, m, g, u)
     _check(lib, lib.jorge_gated_linear_forward(ctypes.byref(shape), m.data_ptr(), g.data_ptr(), u.data_ptr(),
                                                y.data_ptr(), _ptr(ws), n, _stream(x)))
     return y
@@ -520,7 +525,7 @@ def gated_linear_backward(dy, x, gate, up, activation="silu", need_x=True, need_
     dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if need_x else None
     dg, du = (torch.empty((outs, cols), dtype=x.dtype, device=x.device) if need_weights else None for _ in range(2))
     shape = _linear_shape(m, g, u, _ld(d), outs, None, act)
-    ws, n = _linear_workspace(lib, shape, 1, 1)
+    ws, n = _linear_workspace(lib, shape, d, m, g, u, need_x, need_weights)
     _check(lib, lib.jorge_gated_linear_backward(ctypes.byref(shape), d.data_ptr(), m.data_ptr(), g.data_ptr(),
                                                 u.data_ptr(), _ptr(dx), cols, _ptr(dg), _ptr(du), cols, _ptr(ws), n,
                                                 _stream(x)))

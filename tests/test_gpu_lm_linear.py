@@ -447,3 +447,26 @@ def test_infinities_in_fp32_products_of_many_tokens():
                 assert torch.equal(t[row], want)
                 keep = torch.arange(t.shape[0], device="cuda") != row
                 assert torch.equal(t[keep], s[keep])
+
+
+def test_memory_that_a_call_takes_beside_its_results():
+    """None where bfloat16 operands are read as they lie and every product has a tile for each CU, so that no sum is cut; a
+    frozen weight's gradient costs nothing in fp32 either."""
+    g = torch.Generator(device="cuda").manual_seed(1)
+
+    def beside(call):
+        call()
+        torch.cuda.synchronize()
+        torch.cuda.reset_peak_memory_stats()
+        before = torch.cuda.memory_allocated()
+        out = call()
+        after = torch.cuda.memory_allocated()
+        torch.cuda.synchronize()
+        return torch.cuda.max_memory_allocated() - after, sum(t is not None for t in out), after - before
+    x, w, dy = (torch.randn(s, generator=g, device="cuda").to(BF16) for s in ((8192, 8192), (2048, 8192), (8192, 2048)))
+    assert beside(lambda: (lm.linear_forward(x, w),))[0] == 0
+    assert beside(lambda: lm.linear_backward(dy, x, w))[0] == 0
+    x, w, dy = x.float(), w.float(), dy.float()
+    every, dx = beside(lambda: lm.linear_backward(dy, x, w)), beside(lambda: lm.linear_backward(dy, x, w, need_weight=False))
+    assert every[1] == 2 and dx[1] == 1
+    assert every[0] - dx[0] > 6 * 8192 * (8192 + 2048) - 4 * 2048 * 8192

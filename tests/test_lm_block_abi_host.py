@@ -122,6 +122,89 @@ def test_ranges_of_fp32_sums_take_at_most_a_gibibyte(lib, tokens, cols, outs, ga
     assert n.value <= 6 * terms + 4 * parts + (1 << 30) + (1 << 13)
 
 
+def call_workspace(lib, dy=None, x=A, w=A, u=None, wanted=0, **kw):  # noqa: F811
+    n = I64()
+    assert lib.jorge_linear_call_workspace(ctypes.byref(linear_shape(**kw)), P(dy), P(x), P(w), P(u), wanted,
+                                           ctypes.byref(n)) == 0
+    return n.value
+
+
+def test_a_calls_workspace_has_room_for_what_the_call_uses(lib):  # noqa: F811
+    for name in ("DX", "DWEIGHT", "DBIAS"):
+        assert getattr(lm, "LINEAR_" + name) == defined("JORGE_LINEAR_" + name)
+    n = I64()
+    assert lib.jorge_linear_call_workspace(None, None, P(A), P(A), None, 0, ctypes.byref(n)) == INVALID
+    assert lib.jorge_linear_call_workspace(ctypes.byref(linear_shape()), None, P(A), P(A), None, 0, None) == INVALID
+    for kw, status, why in SHAPES:
+        refused(lib, lib.jorge_linear_call_workspace(ctypes.byref(linear_shape(**kw)), None, P(A), P(A), None, 0,
+                                                     ctypes.byref(n)), status, why)
+    plain = dict(tokens=8192, cols=8192, outs=2048)
+    # bfloat16 operands that can be read as they lie need nothing without an activation, and dz with one.
+    assert call_workspace(lib, **plain) == call_workspace(lib, A, wanted=3, **plain) == 0
+    assert call_workspace(lib, A, wanted=3, act=3, **plain) == 2 * 8192 * 2048
+    assert call_workspace(lib, A, u=A, wanted=3, act=3, **plain) == 2 * 8192 * 2 * 2048
+    # One that cannot be is copied.
+    assert call_workspace(lib, x=A + 8, **plain) == 2 * 8192 * 8192
+    assert call_workspace(lib, w=A + 8, **plain) == 2 * 2048 * 8192
+    assert call_workspace(lib, u=A + 8, **plain) == 2 * 2 * 2048 * 8192
+    assert call_workspace(lib, A + 8, wanted=3, **plain) == 2 * 8192 * 2048
+    assert call_workspace(lib, ldx=8193, **plain) == 2 * 8192 * 8192
+    # Gradients that are not asked for take none, and in fp32 none of their copies.
+    assert call_workspace(lib, A, **plain) == call_workspace(lib, tokens=0) == call_workspace(lib, A, wanted=7, tokens=0) == 0
+    plain["dtype"] = 0
+    every = call_workspace(lib, A, wanted=3, act=3, **plain)
+    for wanted in (1, 2, 4):
+        assert 0 < call_workspace(lib, A, wanted=wanted, act=3, **plain) < every
+    dw = 6 * 8192 * (8192 + 2048)                                     # x and dz across their rows
+    assert every - call_workspace(lib, A, wanted=1, act=3, **plain) >= dw
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("tokens,cols,outs", [(1, 96, 40), (64, 64, 64), (65, 64, 192), (300, 200, 130), (2048, 4096, 64),
+                                              (515, 512, 1000), (8192, 2048, 8192), (182, 5702, 6326)])
+def test_a_calls_workspace_is_no_more_than_any_calls(lib, tokens, cols, outs, dtype):  # noqa: F811
+    n = I64()
+    for act in (0, 3):
+        kw = dict(tokens=tokens, cols=cols, outs=outs, dtype=dtype, act=act)
+        s = linear_shape(**kw)
+        for u in (None, A, A + 4):
+            most = []
+            for back in (0, 1):
+                assert lib.jorge_linear_workspace(ctypes.byref(s), int(u is not None), back, ctypes.byref(n)) == 0
+                most.append(n.value)
+            for at in (A, A + 4):
+                assert call_workspace(lib, x=at, w=at, u=u, **kw) <= most[0]
+                for wanted in range(8):
+                    assert call_workspace(lib, at, A, at, u, wanted, **kw) <= most[1]
+
+
+@NO_GPU
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_a_calls_workspace_is_what_the_call_takes(lib, dtype):  # noqa: F811
+    """With it the launches are reached, with less the call is refused."""
+    for tokens, cols, outs, act in ((515, 512, 1024, 0), (300, 200, 130, 3), (130, 4001, 70, 3), (2048, 4096, 64, 2)):
+        kw = dict(tokens=tokens, cols=cols, outs=outs, dtype=dtype, act=act)
+        s = linear_shape(**kw)
+
+        def tried(need, call):
+            if need:
+                refused(lib, call(need - 256), INVALID, "too small")
+            assert call(need) == HIP_ERROR
+        for at in (A, A + 4):
+            tried(call_workspace(lib, x=at, **kw), lambda size: lib.jorge_linear_forward(
+                ctypes.byref(s), P(at), P(A), P(A), P(A), P(A), P(A), size, None))
+            tried(call_workspace(lib, x=at, u=A, **kw), lambda size: lib.jorge_gated_linear_forward(
+                ctypes.byref(s), P(at), P(A), P(A), P(A), P(A), size, None))
+            for wanted in range(1, 8):
+                dx, dw, db = (P(A) if wanted & bit else None for bit in (1, 2, 4))
+                tried(call_workspace(lib, A, at, wanted=wanted, **kw), lambda size: lib.jorge_linear_backward(
+                    ctypes.byref(s), P(A), P(at), P(A), P(A), dx, cols, dw, cols, db, P(A), size, None))
+                if wanted < 4:
+                    tried(call_workspace(lib, A, at, u=A, wanted=wanted, **kw),
+                          lambda size: lib.jorge_gated_linear_backward(ctypes.byref(s), P(A), P(at), P(A), P(A), dx, cols,
+                                                                       dw, dw, cols, P(A), size, None))
+
+
 def attention_shape(batch=2, q=5, kv=9, heads=4, kv_heads=2, dim=16, dtype=1, scale=0.25, causal=0, window=0, ql=None,
                     kl=None, qp=A, kp=A, vp=A, token=256, head=16):
     at = (token * 16, token, head)
