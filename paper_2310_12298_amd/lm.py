@@ -571,6 +571,12 @@ def _heads(t, what, like=None):
     return t, (t.data_ptr(), batch_s, token_s if tokens > 1 else 0, head_s if heads > 1 else 0)
 
 
+def _result_heads(t):
+    """Heads of a result; the token stride of a single token does not matter, and may be more than the call takes."""
+    batch, token, head, _ = t.stride()
+    return Heads(t.data_ptr(), batch, token if t.shape[1] > 1 else 0, head)
+
+
 def _lengths(t, batch, what):
     if t is None:
         return None
@@ -609,7 +615,7 @@ def attention_forward(q, k, v, scale=None, causal=False, window=None, q_lengths=
     ws = _workspace(n.value)
     out = q.new_empty(q.shape)
     lse = q.new_empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32)
-    to = Heads(out.data_ptr(), *out.stride()[:3])
+    to = _result_heads(out)
     _check(lib, lib.jorge_attention_forward(ctypes.byref(shape), ctypes.byref(to), lse.data_ptr(), _ptr(ws), n.value,
                                             _stream(q)))
     return out, lse
@@ -629,7 +635,7 @@ def attention_backward(dout, q, k, v, out, lse, scale=None, causal=False, window
     ws = _workspace(n.value)
     grads = [torch.empty(t.shape, dtype=t.dtype, device=t.device) if need else None
              for t, need in ((q, need_q), (k, need_kv), (v, need_kv))]
-    to = [None if t is None else ctypes.byref(Heads(t.data_ptr(), *t.stride()[:3])) for t in grads]
+    to = [None if t is None else ctypes.byref(_result_heads(t)) for t in grads]
     _check(lib, lib.jorge_attention_backward(ctypes.byref(shape), ctypes.byref(hd), ctypes.byref(ho), lse.data_ptr(),
                                              *to, _ptr(ws), n.value, _stream(q)))
     return tuple(grads)

@@ -397,3 +397,16 @@ def test_many_sequences_over_long_caches_of_shared_heads():
         want = plain(q[n:n + 1], k[n:n + 1], v[n:n + 1], causal=True, kl=kl[n:n + 1])
         within(lse[n:n + 1], want["lse"], want["lse_off"] / U32, 1, "lse")
         within(out[n:n + 1], want["out"], want["out_off"] / U32, 1, "out")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_token_of_more_heads_than_a_token_stride_may_hold(dtype):
+    """One token has no stride: 33000 heads of 128 are 4 224 000 elements apart from nothing."""
+    q, k, v, dout = inputs(2, 1, 9, 33000, 1, 128, dtype)
+    assert q.stride(1) > lm.ATTENTION_MAX_STRIDE
+    out, lse = lm.attention_forward(q, k, v)
+    grads = lm.attention_backward(dout, q, k, v, out, lse)
+    few = [t[:, :, :64] for t in (q, dout)]
+    part, part_lse = lm.attention_forward(few[0], k, v)
+    assert torch.equal(lse[:, :64], part_lse) and torch.equal(out[:, :, :64], part)
+    assert torch.equal(grads[0][:, :, :64], lm.attention_backward(few[1], few[0], k, v, part, part_lse)[0])
