@@ -6,8 +6,6 @@
 #include "lm_common.hpp"
 #include "lm_loss_gemm.hpp"
 
-#include <math.h>
-
 #include <algorithm>
 
 namespace jorge_lm {
@@ -39,8 +37,7 @@ struct CopyJobs {
 // rounded to that, is its last term alone: the last term meets only the first one of the other operand, whose sign is the
 // element's, while an infinite first term would meet the others' zeros and signs and make a NaN.
 __device__ __forceinline__ bf16 term_of(float f, bool last) {
-    const bf16 o = (bf16)f;
-    return last || __builtin_fabsf((float)o) < INFINITY ? o : (bf16)0.0f;
+    return (bf16)(last || __builtin_fabsf(f) < 0x1.ffp127f ? f : 0.0f);  // from there on bfloat16 rounds to infinity
 }
 template <int TERMS>
 __device__ __forceinline__ void store_terms(bf16* dst, int64_t plane, float (&f)[8]) {
