@@ -256,7 +256,8 @@ jorge_status jorge_gated_linear_backward(const jorge_linear_shape* shape, const 
  * dk and dv summed over the heads that share them. bfloat16: p and ds are rounded to bfloat16 for their products, all
  * else is fp32 (a gradient then errs by some 2.4e-3 of its size instead of the 1.7e-3 of its own rounding); where rows
  * see few keys, delta is the sum of p (do v^T), as o's rounding would not average out in it. fp32 is multiplied in
- * fp32. */
+ * fp32, and summed over 32 rows at a time before the long sum. A p below 2^-126 (forward: of
+ * the row's largest one) may count as 0. */
 
 /* Largest dim, tokens, token stride, and rows: batch * heads * q_tokens of q, batch * kv_heads * kv_tokens of k. */
 #define JORGE_ATTENTION_MAX_DIM    128

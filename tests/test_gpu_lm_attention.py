@@ -6,6 +6,8 @@ the exponential; a sum over n terms adds n roundings of the terms' magnitudes. b
 each, and delta is formed from the rounded o. A probability below 2^-126, the smallest normal number, counts as zero
 (exp2 gives no subnormal ones): that is off by less than 2^-126, whatever the rest.
 """
+import math
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -410,3 +412,42 @@ def test_a_token_of_more_heads_than_a_token_stride_may_hold(dtype):
     part, part_lse = lm.attention_forward(few[0], k, v)
     assert torch.equal(lse[:, :64], part_lse) and torch.equal(out[:, :, :64], part)
     assert torch.equal(grads[0][:, :, :64], lm.attention_backward(few[1], few[0], k, v, part, part_lse)[0])
+
+
+def test_long_sums_in_fp32_keep_their_precision():
+    """A sum over n rows is formed tile by tile of 32: n / 32 roundings of the running sum, which grows with the root of
+    the rows so far, make an error of at most 2^-24 sqrt(n / 64) of it. Backward a probability exp(z - lse) has the
+    rounding of lse and that of lse log2(e) in it, 2^-24 lse each, and lse is at most log(keys) + 1 here. What a tile's own
+    products, the scores and the exponentials add does not depend on n: e, measured where n is 256, and a tenth more.
+    One by one the products would make 2^-24 sqrt(n / 4)."""
+    def errors(nq, nk, hk, group):
+        q, k, v, dout = inputs(1, nq, nk, hk * group, hk, 64, F32)
+        out, lse = lm.attention_forward(q, k, v)
+        got = [t[0].transpose(0, 1) for t in (out, *lm.attention_backward(dout, q, k, v, out, lse))]
+        q, k, v, dout = (t[0].transpose(0, 1) for t in (q, k, v, dout))
+        far, size = [0.0] * 4, [0.0] * 4
+        for n in range(hk):
+            K, V = k[n].double(), v[n].double()
+            dk, dv = torch.zeros_like(K), torch.zeros_like(V)
+            for m in range(n * group, (n + 1) * group):
+                Q, G = q[m].double(), dout[m].double()
+                p = torch.softmax(Q @ K.t() / 8, 1)
+                o = p @ V
+                ds = p * (G @ V.t() - (G * o).sum(1, keepdim=True)) / 8
+                dk += ds.t() @ Q
+                dv += p.t() @ G
+                for i, want in ((0, o), (1, ds @ K)):
+                    far[i] += float((got[i][m].double() - want).square().sum())
+                    size[i] += float(want.square().sum())
+            for i, want in ((2, dk), (3, dv)):
+                far[i] += float((got[i][n].double() - want).square().sum())
+                size[i] += float(want.square().sum())
+        return [(a / b) ** 0.5 for a, b in zip(far, size)]
+    e = [1.1 * x for x in errors(256, 256, 1, 4)]
+    # Enough workgroups that neither axis is cut into ranges: of keys for out and dq, of queries for dk and dv.
+    for nq, nk, hk, group, names in ((1024, 16384, 1, 64, ("out", "dq")), (4096, 1024, 64, 4, ("dk", "dv"))):
+        every, lse = ("out", "dq", "dk", "dv"), 2 * (math.log(nk) + 1)
+        for name, x, base in zip(every, errors(nq, nk, hk, group), e):
+            n = nk if name in ("out", "dq") else nq * group
+            room = (base ** 2 + U32 ** 2 * (n / 64 + (0 if name == "out" else lse) ** 2)) ** 0.5
+            assert name not in names or x < room, f"{name} of {n} rows: {x:.2e}, room {room:.2e}"
