@@ -18,9 +18,10 @@
 // change results.
 //
 // Bound by the matrix cores and the exponentials between their products in training. 4 sequences of 4096, 16 heads of
-// 128, causal, bfloat16: forward 361 us (762 TFLOP/s over what is not masked; matrix cores busy 46%), dq 465 us (887;
-// 56%), dk and dv 756 us (727; 39%: one wave to a SIMD has nothing to cover its own softmax with). No bank conflicts in
-// any of them. A single token over 32 caches is bound by reading k and v: 159 us for 0.8 GB, 5.1 TB/s.
+// 128, causal, bfloat16: forward 375 us (734 TFLOP/s over what is not masked; matrix cores busy 46%), dq 477 us (864;
+// 56%), dk and dv 778 us (706; 39%: one wave to a SIMD has nothing to cover its own softmax with). No bank conflicts in
+// any of them. A single token over 32 caches is bound by reading k and v: 158 us for 0.8 GB, 5.1 TB/s. Times that are
+// set against each other below are of one session; sessions differ by up to 10%.
 //
 // Queries whose heads share a key head are rows of one sequence of own rows, (token, head) by (token, head), so that a
 // tile of k and v is read once for all of them.
@@ -31,7 +32,8 @@
 // loads.
 //
 // bfloat16: P and dS are rounded to bfloat16 for `cols`, as the matrix instructions take them; scores, statistics and
-// sums are fp32. fp32 runs on the fp32 MFMAs throughout.
+// sums are fp32. fp32 runs on the fp32 MFMAs throughout, and sums a tile before the long sum. exp2 gives no subnormal
+// numbers: a probability below 2^-126 of the row's reference (forward) or of 1 (backward) is 0.
 #include "lm_common.hpp"
 
 #include <math.h>
@@ -801,7 +803,7 @@ struct Gradient {
 // saves reading the gradient twice, or (no o) is there from attention_delta_kernel. o's rounding to bfloat16 puts an
 // error into delta that is an average over the keys that a row sees; where a workgroup's rows see few (kFewTiles), delta
 // is the sum of p dp instead, formed in a pass of its own: without it dq errs by 3.8e-3 of its size where rows see 2
-// keys, by 2.6e-3 at 96 and 2.4e-3 at 264, with it by 2.4e-3.
+// keys and by 2.6e-3 at 96, with it by 2.3e-3 to 2.4e-3, as it does with more keys.
 constexpr int kFewTiles = 4;
 struct RowStats {
     Heads o;
